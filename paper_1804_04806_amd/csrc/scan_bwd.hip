@@ -1,0 +1,367 @@
+// Selective state space scan, Backward: scan_bwd_kernel and the joins of its partial sums.
+//
+// With x the decayed gradient of the state that a token receives from its successor, dyp = dy SiLU(z):
+//   dh_t = dyp_t Cm_t + x_{t+1},  x_t = exp(d_t A) dh_t,  x behind the last token = dstate_out,
+//   dCm_t = sum over channels dyp_t h_t,  dBm_t = sum over channels dh_t d_t u_t,
+//   dd_t = sum_n x_t h_{t-1} A + u_t sum_n dh_t Bm_t,  dA = sum_t x_t h_{t-1} d_t,
+//   du_t = d_t sum_n dh_t Bm_t + skip dyp_t,  dz_t = dy_t (sum_n Cm_t h_t + skip u_t) SiLU'(z_t).
+#include <algorithm>
+
+#include "scan_common.hpp"
+
+namespace ucd {
+namespace {
+using namespace seq;
+
+// a = {a of the lower half of the wave, b of the lower half}, b = {a of the upper half, b of the upper half}
+__device__ __forceinline__ void swap_halves(float &a, float &b)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, a), __builtin_bit_cast(unsigned, b), false, false);
+    const unsigned lo = r[0], hi = r[1];      // bit_cast of a vector's element takes its first
+    a = __builtin_bit_cast(float, lo);
+    b = __builtin_bit_cast(float, hi);
+}
+
+// the same of odd and even rows of 16 lanes
+__device__ __forceinline__ void swap_rows(float &a, float &b)
+{
+    const auto r = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(unsigned, a), __builtin_bit_cast(unsigned, b), false, false);
+    const unsigned lo = r[0], hi = r[1];      // bit_cast of a vector's element takes its first
+    a = __builtin_bit_cast(float, lo);
+    b = __builtin_bit_cast(float, hi);
+}
+
+constexpr int kRor8 = 0x128, kRor4 = 0x124;
+
+// Sums of two tokens' dBm and dCm over the wave's channels: v[token][kind][state], channels are the lane bits from LPC up.  Each exchange of halves
+// adds up two values at once; r[state] is then token (lane bit 5), kind (lane bit 4), in every lane of the row with that state quarter.
+template <int LPC>
+__device__ __forceinline__ void sum_channels(float (&v)[2][2][4], float (&r)[4])
+{
+    float w[2][4];
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            swap_halves(v[0][k][j], v[1][k][j]);
+            w[k][j] = v[0][k][j] + v[1][k][j];
+        }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        swap_rows(w[0][j], w[1][j]);
+        r[j] = w[0][j] + w[1][j];
+        if (LPC < 16) r[j] += dpp<kRor8>(r[j]);
+        if (LPC < 8) r[j] += dpp<kRor4>(r[j]);
+        if (LPC < 4) r[j] += dpp<kXor2>(r[j]);
+        if (LPC < 2) r[j] += dpp<kXor1>(r[j]);
+    }
+}
+
+// One segment of a sequence from its last token to its first, 4 x 64 / LPC channels per workgroup.  STATE_ONLY: from zero, the gradient of the state
+// before the segment alone.
+template <class T, int LPC, bool WIDE, bool STATE_ONLY>
+__global__ __launch_bounds__(64 * kWaves, 2) void scan_bwd_kernel(ScanParams p, long units)
+{
+    typedef ScanWave<LPC> W;
+    constexpr int BC = 2 * kTile * W::NP;
+    __shared__ alignas(16) float2 lds_step[kWaves][kTile * W::CW];      // d_t, d_t u_t
+    __shared__ alignas(16) float lds_dy[kWaves][kTile * W::CW];         // dyp_t
+    __shared__ alignas(16) float lds_bc[kWaves][BC];
+    __shared__ alignas(16) float lds_out[kWaves][STATE_ONLY ? 1 : 3 * kTile * W::CW];   // sums over the states: dh Bm, x h A, Cm h
+    __shared__ alignas(16) float lds_sum[STATE_ONLY ? 1 : 2][STATE_ONLY ? 1 : kWaves][STATE_ONLY ? 1 : BC];
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    float2 *step = lds_step[wave];
+    float *dys = lds_dy[wave], *bm = lds_bc[wave], *cm = bm + kTile * W::NP;
+    float *gs = lds_out[wave], *es = gs + kTile * W::CW, *ys = es + kTile * W::CW;
+    const ucd_scan_t &d = p.d;
+    const bool gate = p.in.z != nullptr;
+    const int low = lane % 16 / LPC;       // the channel bits of a lane within its row
+
+    for (long unit = blockIdx.x; unit < units; unit += gridDim.x) {
+        const ScanPlace<LPC> at(p, unit);
+        if (STATE_ONLY && at.seg == 0) continue;
+        const int n = scan_length(p, at.b);
+        const int tile0 = at.seg * p.seg_tiles, tile1 = min(p.tiles, tile0 + p.seg_tiles);
+        const long ch = at.c0 + at.c;
+        const int ch0 = lane % W::LR * W::VE;
+        const bool mine = at.c < at.have;
+
+        float A2[4], x[4], dA[4] = {};
+        load_states(A2, p.in.A + ch * d.N + at.n0, at.haven, p.wide_states);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) A2[j] *= kLog2e;
+        auto seg_at = [&](int s) { return (((long)at.b * p.segs + s) * d.D + ch) * d.N + at.n0; };
+        const long state_at = ((long)at.b * d.D + ch) * d.N + at.n0;
+        load_states(x, p.dstate_out + state_at, p.dstate_out && (at.seg == p.segs - 1 || !STATE_ONLY) ? at.haven : 0, p.wide_states);
+        if (!STATE_ONLY)
+            for (int s = p.segs - 1; s > at.seg; --s) {
+                float end[4];
+                load_states(end, p.seg_state + seg_at(s), at.haven, p.wide_states);
+                // the last segment began with dstate_out
+                if (s == p.segs - 1) { x[0] = end[0]; x[1] = end[1]; x[2] = end[2]; x[3] = end[3]; }
+                else join_segment(x, A2, mine ? p.seg_step[((long)at.b * p.segs + s) * d.D + ch] : 0.f, end);
+            }
+        float bias[W::VE], skip[W::VE], dskip[W::VE] = {}, dbias[W::VE] = {}, steps = 0.f;
+#pragma unroll
+        for (int i = 0; i < W::VE; ++i) {
+            const bool have = ch0 + i < at.have;
+            bias[i] = have && p.in.dt_bias ? p.in.dt_bias[at.c0 + ch0 + i] : 0.f;
+            skip[i] = have && p.in.skip ? p.in.skip[at.c0 + ch0 + i] : 0.f;
+        }
+
+        TileRows<T, LPC> u, dt, z, dy;
+        TileStates<T, LPC, WIDE> bc;
+        float first[4];
+        auto load = [&](int tile) {
+            const int t0 = tile * kTile;
+            if (t0 >= n) return;
+            u.template load<WIDE>(p.in.u, d.u_b, d.u_l, at, t0, n);
+            dt.template load<WIDE>(p.in.dt, d.dt_b, d.dt_l, at, t0, n);
+            dy.template load<WIDE>(p.dy, d.y_b, d.y_l, at, t0, n);
+            if (gate) z.template load<WIDE>(p.in.z, d.z_b, d.z_l, at, t0, n);
+            bc.load(p, at, t0, n);
+            if (!STATE_ONLY) load_states(first, p.saved + (((long)at.b * p.tiles + tile) * d.D + ch) * d.N + at.n0, at.haven, p.wide_states);
+        };
+        if (tile1 > tile0) load(tile1 - 1);
+        for (int tile = tile1 - 1; tile >= tile0; --tile) {
+            const int t0 = tile * kTile;
+            float ut[W::P][W::VE], st[W::P][W::VE], rate[W::P][W::VE], dyp[W::P][W::VE], dzt[W::P][W::VE];
+            if (t0 < n) {
+                bc.stage(bm);
+#pragma unroll
+                for (int i = 0; i < W::P; ++i) {
+                    const int t = i * W::TP + lane / W::LR;
+#pragma unroll
+                    for (int e = 0; e < W::VE; ++e) {
+                        ut[i][e] = to_f(u.r[i].v[e]);
+                        float s = to_f(dt.r[i].v[e]) + bias[e];
+                        rate[i][e] = 1.f;
+                        if (d.softplus) s = softplus(s, &rate[i][e]);
+                        if (t0 + t >= n) s = 0.f;
+                        st[i][e] = s;
+                        float g = to_f(dy.r[i].v[e]);
+                        if (gate) {
+                            const float v = to_f(z.r[i].v[e]), sg = sigmoid(v);
+                            dzt[i][e] = g * sg * fmaf(v, 1.f - sg, 1.f);
+                            g *= v * sg;
+                        }
+                        dyp[i][e] = g;
+                        step[t * W::CW + ch0 + e] = make_float2(s, s * ut[i][e]);
+                        dys[t * W::CW + ch0 + e] = g;
+                    }
+                }
+                float h[kTile + 1][4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) h[0][j] = first[j];
+                if (tile > tile0) load(tile - 1);
+                wave_lds_order();
+                if (STATE_ONLY) {
+#pragma unroll
+                    for (int t = kTile - 1; t >= 0; --t) {
+                        const float s = step[t * W::CW + at.c].x, g = dys[t * W::CW + at.c];
+                        const float4 c = *reinterpret_cast<const float4 *>(cm + t * W::NP + at.n0);
+                        const float cs[4] = {c.x, c.y, c.z, c.w};
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) x[j] = exp2_fast(s * A2[j]) * fmaf(g, cs[j], x[j]);
+                        steps += s;
+                    }
+                } else {
+                    float a[kTile][4];
+#pragma unroll
+                    for (int t = 0; t < kTile; ++t) {
+                        const float2 s = step[t * W::CW + at.c];
+                        const float4 b = *reinterpret_cast<const float4 *>(bm + t * W::NP + at.n0);
+                        const float bs[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            a[t][j] = exp2_fast(s.x * A2[j]);
+                            h[t + 1][j] = fmaf(a[t][j], h[t][j], s.y * bs[j]);
+                        }
+                    }
+                    float *sums = lds_sum[tile & 1][wave];
+                    float gk = 0.f, ek = 0.f, yk = 0.f, v[2][2][4];
+#pragma unroll
+                    for (int t = kTile - 1; t >= 0; --t) {
+                        const float2 s = step[t * W::CW + at.c];
+                        const float g = dys[t * W::CW + at.c];
+                        const float4 b = *reinterpret_cast<const float4 *>(bm + t * W::NP + at.n0);
+                        const float4 c = *reinterpret_cast<const float4 *>(cm + t * W::NP + at.n0);
+                        const float bs[4] = {b.x, b.y, b.z, b.w}, cs[4] = {c.x, c.y, c.z, c.w};
+                        float gt = 0.f, et = 0.f, yt = 0.f;
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const float dh = fmaf(g, cs[j], x[j]);
+                            v[t % 2][0][j] = dh * s.y;
+                            v[t % 2][1][j] = g * h[t + 1][j];
+                            gt = fmaf(dh, bs[j], gt);
+                            yt = fmaf(cs[j], h[t + 1][j], yt);
+                            x[j] = a[t][j] * dh;
+                            const float w = x[j] * h[t][j];
+                            et = fmaf(w, A2[j], et);
+                            dA[j] = fmaf(w, s.x, dA[j]);
+                        }
+                        gt = sum_lanes<LPC>(gt);
+                        et = sum_lanes<LPC>(et);
+                        if (gate) yt = sum_lanes<LPC>(yt);
+                        const bool keep = LPC == 1 || at.q == t % LPC;
+                        gk = keep ? gt : gk;
+                        ek = keep ? et : ek;
+                        yk = keep ? yt : yk;
+                        if (t % LPC == 0) {
+                            const int o = (t + at.q) * W::CW + at.c;
+                            gs[o] = gk;
+                            es[o] = ek;
+                            if (gate) ys[o] = yk;
+                        }
+                        if (t % 2 == 0) {
+                            float r[4];
+                            sum_channels<LPC>(v, r);
+                            float *o = sums + ((t + lane / 32) * 2 + lane / 16 % 2) * W::NP + at.n0;
+                            if (LPC == 16) *reinterpret_cast<float4 *>(o) = make_float4(r[0], r[1], r[2], r[3]);
+                            else if (LPC == 8) *reinterpret_cast<float2 *>(o + 2 * low) = low == 0 ? make_float2(r[0], r[1]) : make_float2(r[2], r[3]);
+                            else if (low < 4) o[low] = low < 2 ? (low == 0 ? r[0] : r[1]) : (low == 2 ? r[2] : r[3]);
+                        }
+                    }
+                }
+                wave_lds_order();
+            } else if (tile > tile0) {
+                load(tile - 1);
+            }
+            if (!STATE_ONLY) {
+#pragma unroll
+                for (int i = 0; i < W::P; ++i) {
+                    const int t = i * W::TP + lane / W::LR, have = t0 + t < d.L ? at.have - ch0 : 0;
+                    Pack<T, W::VE> du, ddt, dz;
+#pragma unroll
+                    for (int e = 0; e < W::VE; ++e) {
+                        float a = 0.f, b = 0.f, c = 0.f;
+                        if (t0 + t < n) {
+                            const int o = t * W::CW + ch0 + e;
+                            const float g = gs[o];
+                            a = fmaf(g, st[i][e], skip[e] * dyp[i][e]);
+                            b = fmaf(es[o], kLn2, g * ut[i][e]) * rate[i][e];
+                            if (gate) c = dzt[i][e] * fmaf(skip[e], ut[i][e], ys[o]);
+                            dskip[e] = fmaf(dyp[i][e], ut[i][e], dskip[e]);
+                            dbias[e] += b;
+                        }
+                        du.v[e] = from_f<T>(a);
+                        ddt.v[e] = from_f<T>(b);
+                        dz.v[e] = from_f<T>(c);
+                    }
+                    const long row = t0 + t;
+                    store_pack<WIDE, T, W::VE>((T *)p.g.u + at.b * d.u_b + row * d.u_l + at.c0 + ch0, du, have);
+                    store_pack<WIDE, T, W::VE>((T *)p.g.dt + at.b * d.dt_b + row * d.dt_l + at.c0 + ch0, ddt, have);
+                    if (gate) store_pack<WIDE, T, W::VE>((T *)p.g.z + at.b * d.z_b + row * d.z_l + at.c0 + ch0, dz, have);
+                }
+                wave_lds_order();
+                if (t0 < n) {
+                    // the waves' sums, in their order; the other of the two buffers is written meanwhile
+                    __syncthreads();
+                    float *o = p.part_bc + ((((long)at.b * p.tiles + tile) * d.G + at.g) * p.blocks + unit % p.blocks) * BC;
+                    for (int i = threadIdx.x; i < BC; i += 64 * kWaves) {
+                        float v = lds_sum[tile & 1][0][i];
+#pragma unroll
+                        for (int w = 1; w < kWaves; ++w) v += lds_sum[tile & 1][w][i];
+                        o[i] = v;
+                    }
+                }
+            }
+        }
+        if (STATE_ONLY) {
+            store_states(p.seg_state + seg_at(at.seg), x, at.haven, p.wide_states);
+            if (at.q == 0 && mine) p.seg_step[((long)at.b * p.segs + at.seg) * d.D + ch] = steps;
+        } else {
+            if (p.g.state && at.seg == 0) store_states(p.g.state + state_at, x, at.haven, p.wide_states);
+            float *o = p.part_w + (((long)at.b * p.segs + at.seg) * d.D) * (d.N + 2);
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (j < at.haven) o[ch * (d.N + 2) + at.n0 + j] = dA[j];
+            // over the lanes that load other tokens of the same channels
+#pragma unroll
+            for (int e = 0; e < W::VE; ++e) {
+                for (int k = W::LR; k < 64; k *= 2) {
+                    dskip[e] += __shfl_xor(dskip[e], k);
+                    dbias[e] += __shfl_xor(dbias[e], k);
+                }
+                if (lane < W::LR && ch0 + e < at.have) {
+                    float *w = o + (at.c0 + ch0 + e) * (long)(d.N + 2) + d.N;
+                    w[0] = dskip[e];
+                    w[1] = dbias[e];
+                }
+            }
+            __syncthreads();      // lds_sum is written again by the next unit
+        }
+    }
+}
+
+// dBm and dCm: one element of either per thread, over the workgroups of a group's channels.
+template <class T>
+__global__ __launch_bounds__(256) void scan_join_bc_kernel(ScanParams p, int np, long total)
+{
+    const ucd_scan_t &d = p.d;
+    for (long i = blockIdx.x * 256l + threadIdx.x; i < total; i += gridDim.x * 256l) {
+        const int k = (int)(i % np), kind = (int)(i / np % 2);
+        const long row = i / np / 2;
+        const int g = (int)(row % d.G), t = (int)(row / d.G % d.L), b = (int)(row / d.G / d.L);
+        if (k >= d.N) continue;
+        float v = 0.f;
+        if (t < scan_length(p, b)) {
+            const float *o = p.part_bc + ((((long)b * p.tiles + t / kTile) * d.G + g) * p.blocks) * (2l * kTile * np) + (t % kTile * 2 + kind) * np + k;
+            for (int s = 0; s < p.blocks; ++s) v += o[s * (2l * kTile * np)];
+        }
+        T *out = kind ? (T *)p.g.Cm + b * d.Cm_b + (long)t * d.Cm_l : (T *)p.g.Bm + b * d.Bm_b + (long)t * d.Bm_l;
+        out[(long)g * d.N + k] = from_f<T>(v);
+    }
+}
+
+// dA, dskip and ddt_bias: one element per thread, over sequences and segments.
+__global__ __launch_bounds__(256) void scan_join_weights_kernel(ScanParams p)
+{
+    const ucd_scan_t &d = p.d;
+    const long i = blockIdx.x * 256l + threadIdx.x, row = (long)d.D * (d.N + 2);
+    if (i >= row) return;
+    const int k = (int)(i % (d.N + 2));
+    const long c = i / (d.N + 2);
+    float v = 0.f;
+    for (long s = 0; s < (long)d.B * p.segs; ++s) v += p.part_w[s * row + i];
+    float *out = k < d.N ? p.g.A + c * d.N + k : k == d.N ? (p.in.skip ? p.g.skip + c : nullptr) : p.in.dt_bias ? p.g.dt_bias + c : nullptr;
+    if (out) *out = v + (p.add ? *out : 0.f);
+}
+
+unsigned grid_of(long units) { return (unsigned)std::min(units, 1l << 22); }
+
+template <class T, int LPC, bool WIDE>
+hipError_t launch(const ScanParams &p, hipStream_t s)
+{
+    const ucd_scan_t &d = p.d;
+    const long units = (long)d.B * p.segs * d.G * p.blocks;
+    if (p.segs > 1) scan_bwd_kernel<T, LPC, WIDE, true><<<grid_of(units), 64 * kWaves, 0, s>>>(p, units);
+    if (units > 0) scan_bwd_kernel<T, LPC, WIDE, false><<<grid_of(units), 64 * kWaves, 0, s>>>(p, units);
+    const long elements = (long)d.B * d.L * d.G * 2 * ScanWave<LPC>::NP;
+    if (elements > 0) scan_join_bc_kernel<T><<<grid_of((elements + 255) / 256), 256, 0, s>>>(p, ScanWave<LPC>::NP, elements);
+    scan_join_weights_kernel<<<(unsigned)(((long)d.D * (d.N + 2) + 255) / 256), 256, 0, s>>>(p);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t scan_bwd(const ucd_scan_t &d, const ucd_scan_in_t &in, const void *dy, const float *dstate_out, const float *saved,
+                    const ucd_scan_grad_t &g, bool add, void *ws, hipStream_t s)
+{
+    ScanParams p{};
+    scan_params(d, in, UCD_SEQ_BWD, ws, p);
+    p.dy = dy;
+    p.dstate_out = dstate_out;
+    p.saved = const_cast<float *>(saved);
+    p.g = g;
+    p.add = add;
+    p.wide_states = p.wide_states && ((uintptr_t)dstate_out & 15) == 0 && ((uintptr_t)g.state & 15) == 0;
+    const bool wide = scan_wide(d, in, dy, &g);
+    return scan_by_lanes(d, [&](auto lanes) {
+        constexpr int LPC = decltype(lanes)::value;
+        if (d.dtype == 1) return wide ? launch<bf16_t, LPC, true>(p, s) : launch<bf16_t, LPC, false>(p, s);
+        return wide ? launch<float, LPC, true>(p, s) : launch<float, LPC, false>(p, s);
+    });
+}
+
+}  // namespace ucd

@@ -1,0 +1,183 @@
+// Selective state space scan, Forward: scan_fwd_kernel.
+#include <algorithm>
+#include <type_traits>
+
+#include "scan_common.hpp"
+
+namespace ucd {
+namespace {
+using namespace seq;
+
+// One segment of a sequence, 4 x 64 / LPC channels per workgroup.  STATE_ONLY: from zero, without outputs; leaves the segment's end state
+// and the sum of its steps, from which a second launch without STATE_ONLY finds its segments' first states.
+template <class T, int LPC, bool WIDE, bool STATE_ONLY>
+__global__ __launch_bounds__(64 * kWaves) void scan_fwd_kernel(ScanParams p, long units)
+{
+    typedef ScanWave<LPC> W;
+    __shared__ alignas(16) float2 lds_step[kWaves][kTile * W::CW];      // d_t, d_t u_t
+    __shared__ alignas(16) float lds_bc[kWaves][2 * kTile * W::NP];
+    __shared__ alignas(16) float lds_y[kWaves][STATE_ONLY ? 1 : kTile * W::CW];
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    float2 *step = lds_step[wave];
+    float *bm = lds_bc[wave], *cm = bm + kTile * W::NP, *ys = lds_y[wave];
+    const ucd_scan_t &d = p.d;
+
+    for (long unit = blockIdx.x; unit < units; unit += gridDim.x) {
+        const ScanPlace<LPC> at(p, unit);
+        if (at.have == 0 || (STATE_ONLY && at.seg == p.segs - 1)) continue;     // nobody needs the last segment's end
+        const int slot = p.in.slots ? p.in.slots[at.b] : at.b;
+        const bool idle = p.in.slots && (slot < 0 || slot >= d.n_slots);
+        const int n = idle ? 0 : scan_length(p, at.b);
+        const int tile0 = at.seg * p.seg_tiles, tile1 = min(p.tiles, tile0 + p.seg_tiles);
+        const long ch = at.c0 + at.c;
+        const int ch0 = lane % W::LR * W::VE;      // the channels that the lane loads
+
+        float A2[4], h[4];
+        load_states(A2, p.in.A + ch * d.N + at.n0, at.haven, p.wide_states);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) A2[j] *= kLog2e;
+        const long state_at = ((long)slot * d.D + ch) * d.N + at.n0;
+        auto seg_at = [&](int s) { return (((long)at.b * p.segs + s) * d.D + ch) * d.N + at.n0; };
+        if (STATE_ONLY || p.segs == 1) {
+            load_states(h, p.state_in + state_at, p.state_in && !idle && at.seg == 0 ? at.haven : 0, p.wide_states);
+            // state_out may be state_in: the second launch takes the first state from here
+            if (STATE_ONLY && at.seg == 0) store_states(p.seg_state + seg_at(0), h, at.haven, p.wide_states);
+            if (STATE_ONLY) h[0] = h[1] = h[2] = h[3] = 0.f;
+        } else {
+            load_states(h, p.seg_state + seg_at(0), at.haven, p.wide_states);
+            for (int s = 0; s < at.seg; ++s) {
+                float end[4];
+                load_states(end, p.seg_state + seg_at(s + 1), at.haven, p.wide_states);
+                join_segment(h, A2, at.c < at.have ? p.seg_step[((long)at.b * p.segs + s) * d.D + ch] : 0.f, end);
+            }
+        }
+        float bias[W::VE], skip[W::VE], steps = 0.f;
+#pragma unroll
+        for (int i = 0; i < W::VE; ++i) {
+            const bool have = ch0 + i < at.have;
+            bias[i] = have && p.in.dt_bias ? p.in.dt_bias[at.c0 + ch0 + i] : 0.f;
+            skip[i] = have && p.in.skip ? p.in.skip[at.c0 + ch0 + i] : 0.f;
+        }
+
+        TileRows<T, LPC> u, dt, z;
+        TileStates<T, LPC, WIDE> bc;
+        const bool gate = p.in.z != nullptr;
+        auto load = [&](int tile) {
+            const int t0 = tile * kTile;
+            if (t0 >= n) return;
+            u.template load<WIDE>(p.in.u, d.u_b, d.u_l, at, t0, n);
+            dt.template load<WIDE>(p.in.dt, d.dt_b, d.dt_l, at, t0, n);
+            if (!STATE_ONLY && gate) z.template load<WIDE>(p.in.z, d.z_b, d.z_l, at, t0, n);
+            bc.load(p, at, t0, n);
+        };
+        load(tile0);
+        for (int tile = tile0; tile < tile1; ++tile) {
+            const int t0 = tile * kTile;
+            float ut[W::P][W::VE], zt[W::P][W::VE];
+            if (t0 < n) {
+                bc.stage(bm);
+#pragma unroll
+                for (int i = 0; i < W::P; ++i) {
+                    const int t = i * W::TP + lane / W::LR;
+#pragma unroll
+                    for (int e = 0; e < W::VE; ++e) {
+                        ut[i][e] = to_f(u.r[i].v[e]);
+                        float s = to_f(dt.r[i].v[e]) + bias[e];
+                        if (d.softplus) s = softplus(s);
+                        if (t0 + t >= n) s = 0.f;     // padding: the state stays
+                        step[t * W::CW + ch0 + e] = make_float2(s, s * ut[i][e]);
+                        if (!STATE_ONLY && gate) {
+                            const float v = to_f(z.r[i].v[e]);
+                            zt[i][e] = v * sigmoid(v);
+                        }
+                    }
+                }
+                if (tile + 1 < tile1) load(tile + 1);
+                wave_lds_order();
+                if (!STATE_ONLY && p.saved) store_states(p.saved + (((long)at.b * p.tiles + tile) * d.D + ch) * d.N + at.n0, h, at.haven, p.wide_states);
+                float kept = 0.f;
+#pragma unroll
+                for (int t = 0; t < kTile; ++t) {
+                    const float2 s = step[t * W::CW + at.c];
+                    const float4 b = *reinterpret_cast<const float4 *>(bm + t * W::NP + at.n0);
+                    const float bs[4] = {b.x, b.y, b.z, b.w};
+                    if (STATE_ONLY) {
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) h[j] = fmaf(exp2_fast(s.x * A2[j]), h[j], s.y * bs[j]);
+                        steps += s.x;
+                    } else {
+                        const float4 c = *reinterpret_cast<const float4 *>(cm + t * W::NP + at.n0);
+                        const float cs[4] = {c.x, c.y, c.z, c.w};
+                        float y = 0.f;
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            h[j] = fmaf(exp2_fast(s.x * A2[j]), h[j], s.y * bs[j]);
+                            y = fmaf(h[j], cs[j], y);
+                        }
+                        y = sum_lanes<LPC>(y);
+                        kept = LPC == 1 || at.q == t % LPC ? y : kept;      // each lane of a channel keeps one token in LPC
+                        if (t % LPC == LPC - 1) ys[(t - LPC + 1 + at.q) * W::CW + at.c] = kept;
+                    }
+                }
+                wave_lds_order();
+            }
+            if (!STATE_ONLY) {
+#pragma unroll
+                for (int i = 0; i < W::P; ++i) {
+                    const int t = i * W::TP + lane / W::LR;
+                    Pack<T, W::VE> out;
+#pragma unroll
+                    for (int e = 0; e < W::VE; ++e) {
+                        float y = 0.f;
+                        if (t0 + t < n) {
+                            y = fmaf(skip[e], ut[i][e], ys[t * W::CW + ch0 + e]);
+                            if (gate) y *= zt[i][e];
+                        }
+                        out.v[e] = from_f<T>(y);
+                    }
+                    store_pack<WIDE, T, W::VE>((T *)p.y + at.b * d.y_b + (long)(t0 + t) * d.y_l + at.c0 + ch0, out, t0 + t < d.L ? at.have - ch0 : 0);
+                }
+                wave_lds_order();
+            }
+        }
+        if (STATE_ONLY) {
+            store_states(p.seg_state + seg_at(at.seg + 1), h, at.haven, p.wide_states);
+            if (at.q == 0 && at.c < at.have) p.seg_step[((long)at.b * p.segs + at.seg) * d.D + ch] = steps;
+        } else if (p.state_out && !idle && at.seg == p.segs - 1) {
+            store_states(p.state_out + state_at, h, at.haven, p.wide_states);
+        }
+    }
+}
+
+unsigned grid_of(long units) { return (unsigned)std::min(units, 1l << 22); }
+
+template <class T, int LPC, bool WIDE>
+hipError_t launch(const ScanParams &p, hipStream_t s)
+{
+    const long units = (long)p.d.B * p.segs * p.d.G * p.blocks;
+    if (p.segs > 1) scan_fwd_kernel<T, LPC, WIDE, true><<<grid_of(units), 64 * kWaves, 0, s>>>(p, units);
+    scan_fwd_kernel<T, LPC, WIDE, false><<<grid_of(units), 64 * kWaves, 0, s>>>(p, units);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t scan_fwd(const ucd_scan_t &d, const ucd_scan_in_t &in, const float *state_in, float *state_out, void *y, float *saved, void *ws,
+                    hipStream_t s)
+{
+    ScanParams p{};
+    scan_params(d, in, UCD_SEQ_FWD, ws, p);
+    p.state_in = state_in;
+    p.state_out = state_out;
+    p.y = y;
+    p.saved = saved;
+    p.wide_states = p.wide_states && ((uintptr_t)state_in & 15) == 0 && ((uintptr_t)state_out & 15) == 0;
+    const bool wide = scan_wide(d, in, y, nullptr);
+    return scan_by_lanes(d, [&](auto lanes) {
+        constexpr int LPC = decltype(lanes)::value;
+        if (d.dtype == 1) return wide ? launch<bf16_t, LPC, true>(p, s) : launch<bf16_t, LPC, false>(p, s);
+        return wide ? launch<float, LPC, true>(p, s) : launch<float, LPC, false>(p, s);
+    });
+}
+
+}  // namespace ucd

@@ -17,8 +17,91 @@ template <> __device__ __forceinline__ bf16_t from_f<bf16_t>(float v) { return (
 
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 
+// N neighbours: one load or store where WIDE says that their address is a multiple of their size, the first `have` of them otherwise.
+template <class T, int N>
+struct alignas(sizeof(T) * N) Pack {
+    T v[N];
+};
+
+template <bool WIDE, class T, int N>
+__device__ __forceinline__ Pack<T, N> load_pack(const T *p, int have)
+{
+    Pack<T, N> r;
+    if (WIDE) {
+        if (have > 0) r = *reinterpret_cast<const Pack<T, N> *>(p);
+        else
+            for (int i = 0; i < N; ++i) r.v[i] = from_f<T>(0.f);
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) r.v[i] = i < have ? p[i] : from_f<T>(0.f);
+    }
+    return r;
+}
+
+template <bool WIDE, class T, int N>
+__device__ __forceinline__ void store_pack(T *p, const Pack<T, N> &r, int have)
+{
+    if (WIDE) {
+        if (have > 0) *reinterpret_cast<Pack<T, N> *>(p) = r;
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (i < have) p[i] = r.v[i];
+    }
+}
+
+// 2^v on the transcendental unit.
+__device__ __forceinline__ float exp2_fast(float v) { return __builtin_amdgcn_exp2f(v); }
+
+// exp(v) to about an ulp: the rounding of v * log2(e), up to 2^-24 |v log2(e)| in the exponent, is put back as a factor.
+__device__ __forceinline__ float exp_full(float v)
+{
+    const float t = v * kLog2e;
+    const float lost = fmaf(v, kLog2e, -t) + v * 1.92596298e-8f;   // log2(e) is kLog2e + 1.92596298e-8
+    const float e = exp2_fast(t);
+    // an infinite v leaves a NaN in `lost`, where e is 0 or infinite
+    return fabsf(t) < 256.f ? fmaf(e * kLn2, lost, e) : e;
+}
+
 // 1 / (1 + exp(-v)).  exp(-v) overflows to infinity below -88: the quotient is then 0, as it should be.
-__device__ __forceinline__ float sigmoid(float v) { return __builtin_amdgcn_rcpf(1.f + __expf(-v)); }
+__device__ __forceinline__ float sigmoid(float v) { return __builtin_amdgcn_rcpf(1.f + exp2_fast(v * -kLog2e)); }
+
+// log(1 + exp(v)) = max(v, 0) + log1p(e), e = exp(-|v|); with w = 1 + e rounded, log1p(e) = log(w) e / (w - 1) to an ulp or two, because w - 1 is
+// exact and log(w) / (w - 1) hardly changes between 1 + e and w.  Also the function's derivative, 1 / (1 + exp(-v)).
+__device__ __forceinline__ float softplus(float v, float *derivative = nullptr)
+{
+    const float e = exp_full(-fabsf(v)), w = 1.f + e, d = w - 1.f;
+    const float l = d == 0.f ? e : __builtin_amdgcn_logf(w) * kLn2 * (e * __builtin_amdgcn_rcpf(d));
+    if (derivative) *derivative = (v >= 0.f ? 1.f : e) * __builtin_amdgcn_rcpf(w);
+    return fmaxf(v, 0.f) + l;
+}
+
+// Lane i's value from another lane of its row of 16, by the data path's own permutations.
+template <int CTRL>
+__device__ __forceinline__ float dpp(float v)
+{
+    return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), CTRL, 0xF, 0xF, true));
+}
+constexpr int kXor1 = 0xB1, kXor2 = 0x4E, kHalfMirror = 0x141, kMirror = 0x140;   // quad_perm [1,0,3,2], [2,3,0,1]; row_half_mirror; row_mirror
+
+// Sum over groups of N neighbouring lanes, N = 1, 2, 4, 8, 16, in every lane.
+template <int N>
+__device__ __forceinline__ float sum_lanes(float v)
+{
+    if (N > 1) v += dpp<kXor1>(v);
+    if (N > 2) v += dpp<kXor2>(v);
+    if (N > 4) v += dpp<kHalfMirror>(v);
+    if (N > 8) v += dpp<kMirror>(v);
+    return v;
+}
+
+// Orders a wave's own LDS accesses: the hardware runs them in program order, the compiler has to keep them so.
+__device__ __forceinline__ void wave_lds_order()
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
 
 }  // namespace seq
 }  // namespace ucd
