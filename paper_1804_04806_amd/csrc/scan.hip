@@ -71,7 +71,7 @@ size_t scan_ws_bytes(const ucd_scan_t &d, int dir)
     return n;
 }
 
-size_t scan_saved_bytes(const ucd_scan_t &d) { return (size_t)4 * d.B * ((d.L + kTile - 1) / kTile) * d.D * d.N; }
+size_t scan_saved_bytes(const ucd_scan_t &d) { return (size_t)4 * d.B * ((d.L + kTile - 1) / kTile) * (kTile / kKeep) * d.D * d.N; }
 
 hipError_t scan_step(const ucd_scan_t &d, const ucd_scan_in_t &in, float *state, void *y, hipStream_t s)
 {

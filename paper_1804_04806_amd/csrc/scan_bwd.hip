@@ -57,12 +57,32 @@ __device__ __forceinline__ void sum_channels(float (&v)[2][2][4], float (&r)[4])
     }
 }
 
+// What two tokens bring from LDS: d_t, d_t u_t and dyp_t of the lane's channel, Bm and Cm of its states.
+template <int LPC>
+struct TwoTokens {
+    float2 s[2];
+    float g[2];
+    float4 b[2], c[2];
+    __device__ __forceinline__ void load(const float2 *step, const float *dys, const float *bm, const float *cm, const ScanPlace<LPC> &at, int t, bool all)
+    {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            s[i] = step[(t + i) * ScanWave<LPC>::CW + at.c];
+            b[i] = *reinterpret_cast<const float4 *>(bm + (t + i) * ScanWave<LPC>::NP + at.n0);
+            if (!all) continue;
+            g[i] = dys[(t + i) * ScanWave<LPC>::CW + at.c];
+            c[i] = *reinterpret_cast<const float4 *>(cm + (t + i) * ScanWave<LPC>::NP + at.n0);
+        }
+    }
+};
+
 // One segment of a sequence from its last token to its first, 4 x 64 / LPC channels per workgroup.  STATE_ONLY: from zero, the gradient of the state
 // before the segment alone.
-template <class T, int LPC, bool WIDE, bool STATE_ONLY>
-__global__ __launch_bounds__(64 * kWaves, 2) void scan_bwd_kernel(ScanParams p, long units)
+template <class T, int LPC, bool WIDE, bool GATE, bool STATE_ONLY>
+__global__ __launch_bounds__(64 * kWaves, 2) void scan_bwd_kernel(ScanParams p, unsigned units)
 {
     typedef ScanWave<LPC> W;
+    typedef TwoTokens<LPC> Ahead;
     constexpr int BC = 2 * kTile * W::NP;
     __shared__ alignas(16) float2 lds_step[kWaves][kTile * W::CW];      // d_t, d_t u_t
     __shared__ alignas(16) float lds_dy[kWaves][kTile * W::CW];         // dyp_t
@@ -74,10 +94,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void scan_bwd_kernel(ScanParams p, 
     float *dys = lds_dy[wave], *bm = lds_bc[wave], *cm = bm + kTile * W::NP;
     float *gs = lds_out[wave], *es = gs + kTile * W::CW, *ys = es + kTile * W::CW;
     const ucd_scan_t &d = p.d;
-    const bool gate = p.in.z != nullptr;
     const int low = lane % 16 / LPC;       // the channel bits of a lane within its row
 
-    for (long unit = blockIdx.x; unit < units; unit += gridDim.x) {
+    for (unsigned unit = blockIdx.x; unit < units; unit += gridDim.x) {
         const ScanPlace<LPC> at(p, unit);
         if (STATE_ONLY && at.seg == 0) continue;
         const int n = scan_length(p, at.b);
@@ -111,16 +130,19 @@ __global__ __launch_bounds__(64 * kWaves, 2) void scan_bwd_kernel(ScanParams p, 
 
         TileRows<T, LPC> u, dt, z, dy;
         TileStates<T, LPC, WIDE> bc;
-        float first[4];
+        float kept[kTile / kKeep][4];
         auto load = [&](int tile) {
             const int t0 = tile * kTile;
             if (t0 >= n) return;
             u.template load<WIDE>(p.in.u, d.u_b, d.u_l, at, t0, n);
             dt.template load<WIDE>(p.in.dt, d.dt_b, d.dt_l, at, t0, n);
             dy.template load<WIDE>(p.dy, d.y_b, d.y_l, at, t0, n);
-            if (gate) z.template load<WIDE>(p.in.z, d.z_b, d.z_l, at, t0, n);
+            if (GATE) z.template load<WIDE>(p.in.z, d.z_b, d.z_l, at, t0, n);
             bc.load(p, at, t0, n);
-            if (!STATE_ONLY) load_states(first, p.saved + (((long)at.b * p.tiles + tile) * d.D + ch) * d.N + at.n0, at.haven, p.wide_states);
+            if (!STATE_ONLY)
+#pragma unroll
+                for (int i = 0; i < kTile / kKeep; ++i)
+                    load_states(kept[i], p.saved + ((((long)at.b * p.tiles + tile) * (kTile / kKeep) + i) * d.D + ch) * d.N + at.n0, at.haven, p.wide_states);
         };
         if (tile1 > tile0) load(tile1 - 1);
         for (int tile = tile1 - 1; tile >= tile0; --tile) {
@@ -140,7 +162,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void scan_bwd_kernel(ScanParams p, 
                         if (t0 + t >= n) s = 0.f;
                         st[i][e] = s;
                         float g = to_f(dy.r[i].v[e]);
-                        if (gate) {
+                        if (GATE) {
                             const float v = to_f(z.r[i].v[e]), sg = sigmoid(v);
                             dzt[i][e] = g * sg * fmaf(v, 1.f - sg, 1.f);
                             g *= v * sg;
@@ -150,9 +172,11 @@ __global__ __launch_bounds__(64 * kWaves, 2) void scan_bwd_kernel(ScanParams p, 
                         dys[t * W::CW + ch0 + e] = g;
                     }
                 }
-                float h[kTile + 1][4];
+                float before[kTile / kKeep][4];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) h[0][j] = first[j];
+                for (int i = 0; i < kTile / kKeep; ++i)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) before[i][j] = kept[i][j];
                 if (tile > tile0) load(tile - 1);
                 wave_lds_order();
                 if (STATE_ONLY) {
@@ -166,60 +190,80 @@ __global__ __launch_bounds__(64 * kWaves, 2) void scan_bwd_kernel(ScanParams p, 
                         steps += s;
                     }
                 } else {
-                    float a[kTile][4];
-#pragma unroll
-                    for (int t = 0; t < kTile; ++t) {
-                        const float2 s = step[t * W::CW + at.c];
-                        const float4 b = *reinterpret_cast<const float4 *>(bm + t * W::NP + at.n0);
-                        const float bs[4] = {b.x, b.y, b.z, b.w};
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            a[t][j] = exp2_fast(s.x * A2[j]);
-                            h[t + 1][j] = fmaf(a[t][j], h[t][j], s.y * bs[j]);
-                        }
-                    }
                     float *sums = lds_sum[tile & 1][wave];
                     float gk = 0.f, ek = 0.f, yk = 0.f, v[2][2][4];
 #pragma unroll
-                    for (int t = kTile - 1; t >= 0; --t) {
-                        const float2 s = step[t * W::CW + at.c];
-                        const float g = dys[t * W::CW + at.c];
-                        const float4 b = *reinterpret_cast<const float4 *>(bm + t * W::NP + at.n0);
-                        const float4 c = *reinterpret_cast<const float4 *>(cm + t * W::NP + at.n0);
-                        const float bs[4] = {b.x, b.y, b.z, b.w}, cs[4] = {c.x, c.y, c.z, c.w};
-                        float gt = 0.f, et = 0.f, yt = 0.f;
+                    for (int part = kTile / kKeep - 1; part >= 0; --part) {
+                        const int p0 = part * kKeep;
+                        float a[kKeep][4], h[kKeep + 1][4];
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            const float dh = fmaf(g, cs[j], x[j]);
-                            v[t % 2][0][j] = dh * s.y;
-                            v[t % 2][1][j] = g * h[t + 1][j];
-                            gt = fmaf(dh, bs[j], gt);
-                            yt = fmaf(cs[j], h[t + 1][j], yt);
-                            x[j] = a[t][j] * dh;
-                            const float w = x[j] * h[t][j];
-                            et = fmaf(w, A2[j], et);
-                            dA[j] = fmaf(w, s.x, dA[j]);
+                        for (int j = 0; j < 4; ++j) h[0][j] = before[part][j];
+                        // LDS is read two tokens ahead, as in Forward
+                        Ahead now, next;
+                        now.load(step, dys, bm, cm, at, p0, false);
+#pragma unroll
+                        for (int i = 0; i < kKeep; ++i) {
+                            if (i % 2 == 0) {
+                                if (i > 0) now = next;
+                                if (i + 2 < kKeep) next.load(step, dys, bm, cm, at, p0 + i + 2, false);
+                                else next.load(step, dys, bm, cm, at, p0 + kKeep - 2, true);
+                                __builtin_amdgcn_sched_barrier(0);
+                            }
+                            const float2 s = now.s[i % 2];
+                            const float4 b = now.b[i % 2];
+                            const float bs[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                a[i][j] = exp2_fast(s.x * A2[j]);
+                                h[i + 1][j] = fmaf(a[i][j], h[i][j], s.y * bs[j]);
+                            }
                         }
-                        gt = sum_lanes<LPC>(gt);
-                        et = sum_lanes<LPC>(et);
-                        if (gate) yt = sum_lanes<LPC>(yt);
-                        const bool keep = LPC == 1 || at.q == t % LPC;
-                        gk = keep ? gt : gk;
-                        ek = keep ? et : ek;
-                        yk = keep ? yt : yk;
-                        if (t % LPC == 0) {
-                            const int o = (t + at.q) * W::CW + at.c;
-                            gs[o] = gk;
-                            es[o] = ek;
-                            if (gate) ys[o] = yk;
-                        }
-                        if (t % 2 == 0) {
-                            float r[4];
-                            sum_channels<LPC>(v, r);
-                            float *o = sums + ((t + lane / 32) * 2 + lane / 16 % 2) * W::NP + at.n0;
-                            if (LPC == 16) *reinterpret_cast<float4 *>(o) = make_float4(r[0], r[1], r[2], r[3]);
-                            else if (LPC == 8) *reinterpret_cast<float2 *>(o + 2 * low) = low == 0 ? make_float2(r[0], r[1]) : make_float2(r[2], r[3]);
-                            else if (low < 4) o[low] = low < 2 ? (low == 0 ? r[0] : r[1]) : (low == 2 ? r[2] : r[3]);
+#pragma unroll
+                        for (int i = kKeep - 1; i >= 0; --i) {
+                            const int t = p0 + i;
+                            if (i % 2 == 1) {
+                                now = next;
+                                if (i > 1) next.load(step, dys, bm, cm, at, t - 3, true);
+                                __builtin_amdgcn_sched_barrier(0);
+                            }
+                            const float2 s = now.s[i % 2];
+                            const float g = now.g[i % 2];
+                            const float4 b = now.b[i % 2], c = now.c[i % 2];
+                            const float bs[4] = {b.x, b.y, b.z, b.w}, cs[4] = {c.x, c.y, c.z, c.w};
+                            float gt = 0.f, et = 0.f, yt = 0.f;
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                const float dh = fmaf(g, cs[j], x[j]);
+                                v[t % 2][0][j] = dh * s.y;
+                                v[t % 2][1][j] = g * h[i + 1][j];
+                                gt = fmaf(dh, bs[j], gt);
+                                if (GATE) yt = fmaf(cs[j], h[i + 1][j], yt);
+                                x[j] = a[i][j] * dh;
+                                const float w = x[j] * h[i][j];
+                                et = fmaf(w, A2[j], et);
+                                dA[j] = fmaf(w, s.x, dA[j]);
+                            }
+                            gt = sum_lanes<LPC>(gt);
+                            et = sum_lanes<LPC>(et);
+                            if (GATE) yt = sum_lanes<LPC>(yt);
+                            const bool mine_t = LPC == 1 || at.q == t % LPC;
+                            gk = mine_t ? gt : gk;
+                            ek = mine_t ? et : ek;
+                            yk = mine_t ? yt : yk;
+                            if (t % LPC == 0) {
+                                const int o = (t + at.q) * W::CW + at.c;
+                                gs[o] = gk;
+                                es[o] = ek;
+                                if (GATE) ys[o] = yk;
+                            }
+                            if (t % 2 == 0) {
+                                float r[4];
+                                sum_channels<LPC>(v, r);
+                                float *o = sums + ((t + lane / 32) * 2 + lane / 16 % 2) * W::NP + at.n0;
+                                if (LPC == 16) *reinterpret_cast<float4 *>(o) = make_float4(r[0], r[1], r[2], r[3]);
+                                else if (LPC == 8) *reinterpret_cast<float2 *>(o + 2 * low) = low == 0 ? make_float2(r[0], r[1]) : make_float2(r[2], r[3]);
+                                else if (low < 4) o[low] = low < 2 ? (low == 0 ? r[0] : r[1]) : (low == 2 ? r[2] : r[3]);
+                            }
                         }
                     }
                 }
@@ -240,7 +284,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void scan_bwd_kernel(ScanParams p, 
                             const float g = gs[o];
                             a = fmaf(g, st[i][e], skip[e] * dyp[i][e]);
                             b = fmaf(es[o], kLn2, g * ut[i][e]) * rate[i][e];
-                            if (gate) c = dzt[i][e] * fmaf(skip[e], ut[i][e], ys[o]);
+                            if (GATE) c = dzt[i][e] * fmaf(skip[e], ut[i][e], ys[o]);
                             dskip[e] = fmaf(dyp[i][e], ut[i][e], dskip[e]);
                             dbias[e] += b;
                         }
@@ -251,7 +295,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void scan_bwd_kernel(ScanParams p, 
                     const long row = t0 + t;
                     store_pack<WIDE, T, W::VE>((T *)p.g.u + at.b * d.u_b + row * d.u_l + at.c0 + ch0, du, have);
                     store_pack<WIDE, T, W::VE>((T *)p.g.dt + at.b * d.dt_b + row * d.dt_l + at.c0 + ch0, ddt, have);
-                    if (gate) store_pack<WIDE, T, W::VE>((T *)p.g.z + at.b * d.z_b + row * d.z_l + at.c0 + ch0, dz, have);
+                    if (GATE) store_pack<WIDE, T, W::VE>((T *)p.g.z + at.b * d.z_b + row * d.z_l + at.c0 + ch0, dz, have);
                 }
                 wave_lds_order();
                 if (t0 < n) {
@@ -328,17 +372,23 @@ __global__ __launch_bounds__(256) void scan_join_weights_kernel(ScanParams p)
     if (out) *out = v + (p.add ? *out : 0.f);
 }
 
-unsigned grid_of(long units) { return (unsigned)std::min(units, 1l << 22); }
+template <class T, int LPC, bool WIDE, bool GATE>
+void launch_main(const ScanParams &p, hipStream_t s)
+{
+    const unsigned units = scan_units(p), grid = std::min(units, 1u << 22);
+    if (p.segs > 1) scan_bwd_kernel<T, LPC, WIDE, GATE, true><<<grid, 64 * kWaves, 0, s>>>(p, units);
+    if (units > 0) scan_bwd_kernel<T, LPC, WIDE, GATE, false><<<grid, 64 * kWaves, 0, s>>>(p, units);
+}
 
 template <class T, int LPC, bool WIDE>
 hipError_t launch(const ScanParams &p, hipStream_t s)
 {
+    if (p.in.z) launch_main<T, LPC, WIDE, true>(p, s);
+    else launch_main<T, LPC, WIDE, false>(p, s);
     const ucd_scan_t &d = p.d;
-    const long units = (long)d.B * p.segs * d.G * p.blocks;
-    if (p.segs > 1) scan_bwd_kernel<T, LPC, WIDE, true><<<grid_of(units), 64 * kWaves, 0, s>>>(p, units);
-    if (units > 0) scan_bwd_kernel<T, LPC, WIDE, false><<<grid_of(units), 64 * kWaves, 0, s>>>(p, units);
     const long elements = (long)d.B * d.L * d.G * 2 * ScanWave<LPC>::NP;
-    if (elements > 0) scan_join_bc_kernel<T><<<grid_of((elements + 255) / 256), 256, 0, s>>>(p, ScanWave<LPC>::NP, elements);
+    if (elements > 0)
+        scan_join_bc_kernel<T><<<(unsigned)std::min((elements + 255) / 256, 1l << 22), 256, 0, s>>>(p, ScanWave<LPC>::NP, elements);
     scan_join_weights_kernel<<<(unsigned)(((long)d.D * (d.N + 2) + 255) / 256), 256, 0, s>>>(p);
     return hipGetLastError();
 }

@@ -14,6 +14,7 @@ namespace ucd {
 namespace seq {
 
 constexpr int kTile = 16;      // tokens
+constexpr int kKeep = 8;       // tokens between the states that Forward keeps for Backward
 constexpr int kWaves = 4;      // of a workgroup, on neighbouring channels
 
 template <int LPC>
@@ -28,14 +29,15 @@ struct ScanWave {
 struct ScanParams {
     ucd_scan_t d;
     ucd_scan_in_t in;
-    int per_group, blocks;       // channels of a group, and workgroups for them
+    int per_group;               // channels of a group,
+    unsigned blocks;             // and workgroups for them
     int segs, seg_tiles;         // a sequence's parts that are scanned side by side, and their length
     int tiles;                   // of a whole sequence
     bool wide_states;            // A and all states in packs of 4
     const float *state_in;
     float *state_out;
     void *y;
-    float *saved;                // [B][tiles][D][N]: states before each tile
+    float *saved;                // [B][tiles][kTile / kKeep][D][N]: states before each part of a tile
     // Forward: a sequence's first state, then the end states of its segments but the last, each from zero; Backward: the gradients of the
     // states before its segments but the first, each from zero.  And the sums of the segments' steps.
     float *seg_state, *seg_step; // [B][segs][D][N], [B][segs][D]
@@ -53,15 +55,15 @@ template <int LPC>
 struct ScanPlace {
     int b, seg, g, c0, c, q, n0;
     int have, haven;      // channels of the wave, states of the lane
-    __device__ __forceinline__ ScanPlace(const ScanParams &p, long unit)
+    __device__ __forceinline__ ScanPlace(const ScanParams &p, unsigned unit)
     {
         const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-        const int block = (int)(unit % p.blocks);
+        const int block = unit % p.blocks;
         unit /= p.blocks;
-        g = (int)(unit % p.d.G);
+        g = unit % p.d.G;
         unit /= p.d.G;
-        seg = (int)(unit % p.segs);
-        b = (int)(unit / p.segs);
+        seg = unit % p.segs;
+        b = unit / p.segs;
         const int at = (block * kWaves + wave) * ScanWave<LPC>::CW;
         have = p.per_group - at;
         have = have < 0 ? 0 : have < ScanWave<LPC>::CW ? have : ScanWave<LPC>::CW;
@@ -165,6 +167,8 @@ __device__ __forceinline__ void join_segment(float (&h)[4], const float (&A2)[4]
 bool scan_wide(const ucd_scan_t &d, const ucd_scan_in_t &in, const void *y, const ucd_scan_grad_t *g);
 void scan_params(const ucd_scan_t &d, const ucd_scan_in_t &in, int dir, void *ws, seq::ScanParams &p);
 int scan_lanes(const ucd_scan_t &d);   // LPC
+// workgroups of a launch, below 2^31 (seq_api.cpp)
+inline unsigned scan_units(const seq::ScanParams &p) { return (unsigned)p.d.B * p.segs * p.d.G * p.blocks; }
 
 // f(std::integral_constant<int, LPC>) for the descriptor's number of states
 template <class F>

@@ -8,12 +8,29 @@ namespace ucd {
 namespace {
 using namespace seq;
 
+// What two tokens bring from LDS: d_t and d_t u_t of the lane's channel, Bm and Cm of its states.
+template <int LPC, bool WITH_C>
+struct TwoTokens {
+    float2 s[2];
+    float4 b[2], c[2];
+    __device__ __forceinline__ void load(const float2 *step, const float *bm, const float *cm, const ScanPlace<LPC> &at, int t)
+    {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            s[i] = step[(t + i) * ScanWave<LPC>::CW + at.c];
+            b[i] = *reinterpret_cast<const float4 *>(bm + (t + i) * ScanWave<LPC>::NP + at.n0);
+            if (WITH_C) c[i] = *reinterpret_cast<const float4 *>(cm + (t + i) * ScanWave<LPC>::NP + at.n0);
+        }
+    }
+};
+
 // One segment of a sequence, 4 x 64 / LPC channels per workgroup.  STATE_ONLY: from zero, without outputs; leaves the segment's end state
 // and the sum of its steps, from which a second launch without STATE_ONLY finds its segments' first states.
-template <class T, int LPC, bool WIDE, bool STATE_ONLY>
-__global__ __launch_bounds__(64 * kWaves) void scan_fwd_kernel(ScanParams p, long units)
+template <class T, int LPC, bool WIDE, bool GATE, bool STATE_ONLY>
+__global__ __launch_bounds__(64 * kWaves, 2) void scan_fwd_kernel(ScanParams p, unsigned units)
 {
     typedef ScanWave<LPC> W;
+    typedef TwoTokens<LPC, !STATE_ONLY> Ahead;
     __shared__ alignas(16) float2 lds_step[kWaves][kTile * W::CW];      // d_t, d_t u_t
     __shared__ alignas(16) float lds_bc[kWaves][2 * kTile * W::NP];
     __shared__ alignas(16) float lds_y[kWaves][STATE_ONLY ? 1 : kTile * W::CW];
@@ -22,7 +39,7 @@ __global__ __launch_bounds__(64 * kWaves) void scan_fwd_kernel(ScanParams p, lon
     float *bm = lds_bc[wave], *cm = bm + kTile * W::NP, *ys = lds_y[wave];
     const ucd_scan_t &d = p.d;
 
-    for (long unit = blockIdx.x; unit < units; unit += gridDim.x) {
+    for (unsigned unit = blockIdx.x; unit < units; unit += gridDim.x) {
         const ScanPlace<LPC> at(p, unit);
         if (at.have == 0 || (STATE_ONLY && at.seg == p.segs - 1)) continue;     // nobody needs the last segment's end
         const int slot = p.in.slots ? p.in.slots[at.b] : at.b;
@@ -61,14 +78,16 @@ __global__ __launch_bounds__(64 * kWaves) void scan_fwd_kernel(ScanParams p, lon
 
         TileRows<T, LPC> u, dt, z;
         TileStates<T, LPC, WIDE> bc;
-        const bool gate = p.in.z != nullptr;
         auto load = [&](int tile) {
             const int t0 = tile * kTile;
             if (t0 >= n) return;
             u.template load<WIDE>(p.in.u, d.u_b, d.u_l, at, t0, n);
             dt.template load<WIDE>(p.in.dt, d.dt_b, d.dt_l, at, t0, n);
-            if (!STATE_ONLY && gate) z.template load<WIDE>(p.in.z, d.z_b, d.z_l, at, t0, n);
+            if (!STATE_ONLY && GATE) z.template load<WIDE>(p.in.z, d.z_b, d.z_l, at, t0, n);
             bc.load(p, at, t0, n);
+        };
+        auto keep = [&](int tile, int part) {
+            store_states(p.saved + ((((long)at.b * p.tiles + tile) * (kTile / kKeep) + part) * d.D + ch) * d.N + at.n0, h, at.haven, p.wide_states);
         };
         load(tile0);
         for (int tile = tile0; tile < tile1; ++tile) {
@@ -86,7 +105,7 @@ __global__ __launch_bounds__(64 * kWaves) void scan_fwd_kernel(ScanParams p, lon
                         if (d.softplus) s = softplus(s);
                         if (t0 + t >= n) s = 0.f;     // padding: the state stays
                         step[t * W::CW + ch0 + e] = make_float2(s, s * ut[i][e]);
-                        if (!STATE_ONLY && gate) {
+                        if (!STATE_ONLY && GATE) {
                             const float v = to_f(z.r[i].v[e]);
                             zt[i][e] = v * sigmoid(v);
                         }
@@ -94,26 +113,32 @@ __global__ __launch_bounds__(64 * kWaves) void scan_fwd_kernel(ScanParams p, lon
                 }
                 if (tile + 1 < tile1) load(tile + 1);
                 wave_lds_order();
-                if (!STATE_ONLY && p.saved) store_states(p.saved + (((long)at.b * p.tiles + tile) * d.D + ch) * d.N + at.n0, h, at.haven, p.wide_states);
+                if (!STATE_ONLY && p.saved) keep(tile, 0);
                 float kept = 0.f;
+                // two tokens' values are on their way from LDS while the two before them are computed: left to itself the compiler reads them
+                // just before their use, and a wave that has its SIMD to itself waits for each
+                Ahead now, next;
+                now.load(step, bm, cm, at, 0);
 #pragma unroll
                 for (int t = 0; t < kTile; ++t) {
-                    const float2 s = step[t * W::CW + at.c];
-                    const float4 b = *reinterpret_cast<const float4 *>(bm + t * W::NP + at.n0);
-                    const float bs[4] = {b.x, b.y, b.z, b.w};
-                    if (STATE_ONLY) {
+                    if (t % 2 == 0) {
+                        if (t > 0) now = next;
+                        if (t + 2 < kTile) next.load(step, bm, cm, at, t + 2);
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+                    const float2 s = now.s[t % 2];
+                    const float4 b = now.b[t % 2], c = now.c[t % 2];
+                    const float bs[4] = {b.x, b.y, b.z, b.w}, cs[4] = {c.x, c.y, c.z, c.w};
+                    float y = 0.f;
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) h[j] = fmaf(exp2_fast(s.x * A2[j]), h[j], s.y * bs[j]);
+                    for (int j = 0; j < 4; ++j) {
+                        h[j] = fmaf(exp2_fast(s.x * A2[j]), h[j], s.y * bs[j]);
+                        if (!STATE_ONLY) y = fmaf(h[j], cs[j], y);
+                    }
+                    if (STATE_ONLY) {
                         steps += s.x;
                     } else {
-                        const float4 c = *reinterpret_cast<const float4 *>(cm + t * W::NP + at.n0);
-                        const float cs[4] = {c.x, c.y, c.z, c.w};
-                        float y = 0.f;
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            h[j] = fmaf(exp2_fast(s.x * A2[j]), h[j], s.y * bs[j]);
-                            y = fmaf(h[j], cs[j], y);
-                        }
+                        if (p.saved && t % kKeep == kKeep - 1 && t + 1 < kTile) keep(tile, (t + 1) / kKeep);
                         y = sum_lanes<LPC>(y);
                         kept = LPC == 1 || at.q == t % LPC ? y : kept;      // each lane of a channel keeps one token in LPC
                         if (t % LPC == LPC - 1) ys[(t - LPC + 1 + at.q) * W::CW + at.c] = kept;
@@ -131,7 +156,7 @@ __global__ __launch_bounds__(64 * kWaves) void scan_fwd_kernel(ScanParams p, lon
                         float y = 0.f;
                         if (t0 + t < n) {
                             y = fmaf(skip[e], ut[i][e], ys[t * W::CW + ch0 + e]);
-                            if (gate) y *= zt[i][e];
+                            if (GATE) y *= zt[i][e];
                         }
                         out.v[e] = from_f<T>(y);
                     }
@@ -149,15 +174,19 @@ __global__ __launch_bounds__(64 * kWaves) void scan_fwd_kernel(ScanParams p, lon
     }
 }
 
-unsigned grid_of(long units) { return (unsigned)std::min(units, 1l << 22); }
+template <class T, int LPC, bool WIDE, bool GATE>
+hipError_t launch(const ScanParams &p, hipStream_t s)
+{
+    const unsigned units = scan_units(p), grid = std::min(units, 1u << 22);
+    if (p.segs > 1) scan_fwd_kernel<T, LPC, WIDE, false, true><<<grid, 64 * kWaves, 0, s>>>(p, units);
+    scan_fwd_kernel<T, LPC, WIDE, GATE, false><<<grid, 64 * kWaves, 0, s>>>(p, units);
+    return hipGetLastError();
+}
 
 template <class T, int LPC, bool WIDE>
 hipError_t launch(const ScanParams &p, hipStream_t s)
 {
-    const long units = (long)p.d.B * p.segs * p.d.G * p.blocks;
-    if (p.segs > 1) scan_fwd_kernel<T, LPC, WIDE, true><<<grid_of(units), 64 * kWaves, 0, s>>>(p, units);
-    scan_fwd_kernel<T, LPC, WIDE, false><<<grid_of(units), 64 * kWaves, 0, s>>>(p, units);
-    return hipGetLastError();
+    return p.in.z ? launch<T, LPC, WIDE, true>(p, s) : launch<T, LPC, WIDE, false>(p, s);
 }
 
 }  // namespace

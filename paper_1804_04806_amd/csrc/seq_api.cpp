@@ -99,6 +99,9 @@ bool scan_ok(const ucd_scan_t *in, ucd_scan_t &d)
 // No token at all: tensors of no elements have no address.
 bool empty(int B, int L) { return B == 0 || L == 0; }
 
+// Workgroups of the scan's launches, 16 channels each at least: their kernels count them in 32 bits.
+double scan_workgroups(const ucd_scan_t &d) { return (double)d.B * (d.D / 16 + d.G); }
+
 // A pool needs its slots and slots their pool.
 bool slots_ok(int n_slots, const int32_t *slots) { return (n_slots > 0) == (slots != nullptr); }
 
@@ -254,6 +257,7 @@ int ucd_scan_fwd(const ucd_scan_t *scan, const ucd_scan_in_t *in, const float *s
         if (!aligned(y, d.dtype) || !aligned4(state_in) || !aligned4(state_out)) return UCD_E_INVALID;
         if (saved && (rc = ws_status(scan_saved_bytes(d), saved, saved_bytes)) != UCD_OK) return rc;
         if ((rc = ws_status(scan_ws_bytes(d, UCD_SEQ_FWD), ws, ws_bytes)) != UCD_OK) return rc;
+        if (scan_workgroups(d) >= 1 << 30) return UCD_E_UNSUPPORTED;
         if (d.B == 0) return UCD_OK;
         (void)hipGetLastError();
         return hip_status(scan_fwd(d, *in, state_in, state_out, y, (float *)saved, ws, (hipStream_t)stream));
@@ -278,6 +282,7 @@ int ucd_scan_bwd(const ucd_scan_t *scan, const ucd_scan_in_t *in, const void *dy
             return UCD_E_INVALID;
         if ((rc = ws_status(scan_saved_bytes(d), saved, saved_bytes)) != UCD_OK) return rc;
         if ((rc = ws_status(scan_ws_bytes(d, UCD_SEQ_BWD), ws, ws_bytes)) != UCD_OK) return rc;
+        if (scan_workgroups(d) >= 1 << 30) return UCD_E_UNSUPPORTED;
         (void)hipGetLastError();
         return hip_status(scan_bwd(d, *in, dy, dstate_out, (const float *)saved, *grad, beta != 0.f, ws, (hipStream_t)stream));
     });
@@ -293,6 +298,7 @@ int ucd_scan_step(const ucd_scan_t *scan, const ucd_scan_in_t *in, float *state,
         const int rc = scan_inputs(d, in);
         if (rc != UCD_OK) return rc;
         if (!aligned(y, d.dtype) || !aligned4(state)) return UCD_E_INVALID;
+        if (scan_workgroups(d) >= 1 << 30) return UCD_E_UNSUPPORTED;
         if (d.B == 0) return UCD_OK;
         (void)hipGetLastError();
         return hip_status(scan_step(d, *in, state, y, (hipStream_t)stream));
