@@ -6,19 +6,18 @@
 namespace ucd {
 using namespace seq;
 
-int scan_lanes(const ucd_scan_t &d) { return d.N <= 4 ? 1 : d.N <= 8 ? 2 : d.N <= 16 ? 4 : d.N <= 32 ? 8 : 16; }
-
 static bool wide_rows(const void *p, int64_t outer, int64_t inner, size_t e)
 {
     return (uintptr_t)p % (4 * e) == 0 && outer % 4 == 0 && inner % 4 == 0;
 }
 
-bool scan_wide(const ucd_scan_t &d, const ucd_scan_in_t &in, const void *y, const ucd_scan_grad_t *g)
+bool scan_wide(const ucd_scan_t &d, const ucd_scan_in_t &in, const void *y, const float *state1, const float *state2, const ucd_scan_grad_t *g)
 {
     const size_t e = d.dtype == 1 ? 2 : 4;
     if (d.D / d.G % 4 != 0 || d.N % 4 != 0) return false;
     if (!wide_rows(in.u, d.u_b, d.u_l, e) || !wide_rows(in.dt, d.dt_b, d.dt_l, e) || !wide_rows(in.Bm, d.Bm_b, d.Bm_l, e) ||
-        !wide_rows(in.Cm, d.Cm_b, d.Cm_l, e) || !wide_rows(in.z, d.z_b, d.z_l, e) || !wide_rows(y, d.y_b, d.y_l, e))
+        !wide_rows(in.Cm, d.Cm_b, d.Cm_l, e) || !wide_rows(in.z, d.z_b, d.z_l, e) || !wide_rows(y, d.y_b, d.y_l, e) ||
+        !wide_rows(in.A, 0, 0, 4) || !wide_rows(state1, 0, 0, 4) || !wide_rows(state2, 0, 0, 4))
         return false;
     return !g || (wide_rows(g->u, 0, 0, e) && wide_rows(g->dt, 0, 0, e) && wide_rows(g->z, 0, 0, e));
 }
@@ -46,7 +45,6 @@ void scan_params(const ucd_scan_t &d, const ucd_scan_in_t &in, int dir, void *ws
     p.d = d;
     p.in = in;
     segments(d, dir, p);
-    p.wide_states = d.N % 4 == 0 && ((uintptr_t)in.A & 15) == 0;
     char *at = (char *)ws;
     if (p.segs > 1) {
         p.seg_state = (float *)at;
@@ -56,7 +54,7 @@ void scan_params(const ucd_scan_t &d, const ucd_scan_in_t &in, int dir, void *ws
     }
     if (dir == UCD_SEQ_BWD) {
         p.part_bc = (float *)at;
-        at += round16((size_t)4 * d.B * p.tiles * d.G * p.blocks * kTile * 8 * scan_lanes(d));
+        at += round16((size_t)4 * d.B * p.tiles * d.G * p.blocks * kTile * 2 * scan_states(d));
         p.part_w = (float *)at;
     }
 }
@@ -67,7 +65,7 @@ size_t scan_ws_bytes(const ucd_scan_t &d, int dir)
     segments(d, dir, p);
     size_t n = p.segs > 1 ? round16((size_t)4 * d.B * p.segs * d.D * d.N) + round16((size_t)4 * d.B * p.segs * d.D) : 0;
     if (dir == UCD_SEQ_BWD)
-        n += round16((size_t)4 * d.B * p.tiles * d.G * p.blocks * kTile * 8 * scan_lanes(d)) + (size_t)4 * d.B * p.segs * d.D * (d.N + 2);
+        n += round16((size_t)4 * d.B * p.tiles * d.G * p.blocks * kTile * 2 * scan_states(d)) + (size_t)4 * d.B * p.segs * d.D * (d.N + 2);
     return n;
 }
 

@@ -35,54 +35,53 @@ constexpr int kRor8 = 0x128, kRor4 = 0x124;
 
 // Sums of two tokens' dBm and dCm over the wave's channels: v[token][kind][state], channels are the lane bits from LPC up.  Each exchange of halves
 // adds up two values at once; r[state] is then token (lane bit 5), kind (lane bit 4), in every lane of the row with that state quarter.
-template <int LPC>
-__device__ __forceinline__ void sum_channels(float (&v)[2][2][4], float (&r)[4])
+template <class W>
+__device__ __forceinline__ void sum_channels(float (&v)[2][2][W::NPL], float (&r)[W::NPL])
 {
-    float w[2][4];
+    constexpr int LPC = W::LPC, NPL = W::NPL;
+    float w[2][NPL];
 #pragma unroll
     for (int k = 0; k < 2; ++k)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
+        for (int j = 0; j < NPL; ++j) {
             swap_halves(v[0][k][j], v[1][k][j]);
             w[k][j] = v[0][k][j] + v[1][k][j];
         }
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
+    for (int j = 0; j < NPL; ++j) {
         swap_rows(w[0][j], w[1][j]);
         r[j] = w[0][j] + w[1][j];
         if (LPC < 16) r[j] += dpp<kRor8>(r[j]);
         if (LPC < 8) r[j] += dpp<kRor4>(r[j]);
-        if (LPC < 4) r[j] += dpp<kXor2>(r[j]);
-        if (LPC < 2) r[j] += dpp<kXor1>(r[j]);
     }
 }
 
 // What two tokens bring from LDS: d_t, d_t u_t and dyp_t of the lane's channel, Bm and Cm of its states.
-template <int LPC>
+template <class W>
 struct TwoTokens {
     float2 s[2];
     float g[2];
-    float4 b[2], c[2];
-    __device__ __forceinline__ void load(const float2 *step, const float *dys, const float *bm, const float *cm, const ScanPlace<LPC> &at, int t, bool all)
+    Pack<float, W::NPL> b[2], c[2];
+    __device__ __forceinline__ void load(const float2 *step, const float *dys, const float *bm, const float *cm, const ScanPlace<W> &at, int t, bool all)
     {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            s[i] = step[(t + i) * ScanWave<LPC>::CW + at.c];
-            b[i] = *reinterpret_cast<const float4 *>(bm + (t + i) * ScanWave<LPC>::NP + at.n0);
+            s[i] = step[(t + i) * W::CW + at.c];
+            b[i] = *reinterpret_cast<const Pack<float, W::NPL> *>(bm + (t + i) * W::NP + at.n0);
             if (!all) continue;
-            g[i] = dys[(t + i) * ScanWave<LPC>::CW + at.c];
-            c[i] = *reinterpret_cast<const float4 *>(cm + (t + i) * ScanWave<LPC>::NP + at.n0);
+            g[i] = dys[(t + i) * W::CW + at.c];
+            c[i] = *reinterpret_cast<const Pack<float, W::NPL> *>(cm + (t + i) * W::NP + at.n0);
         }
     }
 };
 
 // One segment of a sequence from its last token to its first, 4 x 64 / LPC channels per workgroup.  STATE_ONLY: from zero, the gradient of the state
 // before the segment alone.
-template <class T, int LPC, bool WIDE, bool GATE, bool STATE_ONLY>
+template <class T, class W, bool WIDE, bool GATE, bool STATE_ONLY>
 __global__ __launch_bounds__(64 * kWaves, 2) void scan_bwd_kernel(ScanParams p, unsigned units)
 {
-    typedef ScanWave<LPC> W;
-    typedef TwoTokens<LPC> Ahead;
+    constexpr int LPC = W::LPC, NPL = W::NPL;
+    typedef TwoTokens<W> Ahead;
     constexpr int BC = 2 * kTile * W::NP;
     __shared__ alignas(16) float2 lds_step[kWaves][kTile * W::CW];      // d_t, d_t u_t
     __shared__ alignas(16) float lds_dy[kWaves][kTile * W::CW];         // dyp_t
@@ -97,107 +96,111 @@ __global__ __launch_bounds__(64 * kWaves, 2) void scan_bwd_kernel(ScanParams p, 
     const int low = lane % 16 / LPC;       // the channel bits of a lane within its row
 
     for (unsigned unit = blockIdx.x; unit < units; unit += gridDim.x) {
-        const ScanPlace<LPC> at(p, unit);
+        const ScanPlace<W> at(p, unit);
         if (STATE_ONLY && at.seg == 0) continue;
         const int n = scan_length(p, at.b);
         const int tile0 = at.seg * p.seg_tiles, tile1 = min(p.tiles, tile0 + p.seg_tiles);
         const long ch = at.c0 + at.c;
-        const int ch0 = lane % W::LR * W::VE;
         const bool mine = at.c < at.have;
 
-        float A2[4], x[4], dA[4] = {};
-        load_states(A2, p.in.A + ch * d.N + at.n0, at.haven, p.wide_states);
+        float A2[NPL], x[NPL], dA[NPL] = {};
+        load_states<WIDE>(A2, p.in.A + ch * d.N + at.n0, at.haven);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) A2[j] *= kLog2e;
+        for (int j = 0; j < NPL; ++j) A2[j] *= kLog2e;
         auto seg_at = [&](int s) { return (((long)at.b * p.segs + s) * d.D + ch) * d.N + at.n0; };
         const long state_at = ((long)at.b * d.D + ch) * d.N + at.n0;
-        load_states(x, p.dstate_out + state_at, p.dstate_out && (at.seg == p.segs - 1 || !STATE_ONLY) ? at.haven : 0, p.wide_states);
+        load_states<WIDE>(x, p.dstate_out + state_at, p.dstate_out && (at.seg == p.segs - 1 || !STATE_ONLY) ? at.haven : 0);
         if (!STATE_ONLY)
             for (int s = p.segs - 1; s > at.seg; --s) {
-                float end[4];
-                load_states(end, p.seg_state + seg_at(s), at.haven, p.wide_states);
+                float end[NPL];
+                load_states<WIDE>(end, p.seg_state + seg_at(s), at.haven);
                 // the last segment began with dstate_out
-                if (s == p.segs - 1) { x[0] = end[0]; x[1] = end[1]; x[2] = end[2]; x[3] = end[3]; }
-                else join_segment(x, A2, mine ? p.seg_step[((long)at.b * p.segs + s) * d.D + ch] : 0.f, end);
+                if (s == p.segs - 1) {
+#pragma unroll
+                    for (int j = 0; j < NPL; ++j) x[j] = end[j];
+                } else join_segment(x, A2, mine ? p.seg_step[((long)at.b * p.segs + s) * d.D + ch] : 0.f, end);
             }
         float bias[W::VE], skip[W::VE], dskip[W::VE] = {}, dbias[W::VE] = {}, steps = 0.f;
 #pragma unroll
         for (int i = 0; i < W::VE; ++i) {
-            const bool have = ch0 + i < at.have;
-            bias[i] = have && p.in.dt_bias ? p.in.dt_bias[at.c0 + ch0 + i] : 0.f;
-            skip[i] = have && p.in.skip ? p.in.skip[at.c0 + ch0 + i] : 0.f;
+            const bool have = at.ch0 + i < at.have;
+            bias[i] = have && p.in.dt_bias ? p.in.dt_bias[at.c0 + at.ch0 + i] : 0.f;
+            skip[i] = have && p.in.skip ? p.in.skip[at.c0 + at.ch0 + i] : 0.f;
         }
 
-        TileRows<T, LPC> u, dt, z, dy;
-        TileStates<T, LPC, WIDE> bc;
-        float kept[kTile / kKeep][4];
+        TileRows<T, W, WIDE> u, dt, z, dy;
+        TileStates<T, W, WIDE> bc;
+        float kept[kTile / kKeep][NPL];
         auto load = [&](int tile) {
             const int t0 = tile * kTile;
             if (t0 >= n) return;
-            u.template load<WIDE>(p.in.u, d.u_b, d.u_l, at, t0, n);
-            dt.template load<WIDE>(p.in.dt, d.dt_b, d.dt_l, at, t0, n);
-            dy.template load<WIDE>(p.dy, d.y_b, d.y_l, at, t0, n);
-            if (GATE) z.template load<WIDE>(p.in.z, d.z_b, d.z_l, at, t0, n);
+            u.load(p.in.u, d.u_b, d.u_l, at, t0, n);
+            dt.load(p.in.dt, d.dt_b, d.dt_l, at, t0, n);
+            dy.load(p.dy, d.y_b, d.y_l, at, t0, n);
+            if (GATE) z.load(p.in.z, d.z_b, d.z_l, at, t0, n);
             bc.load(p, at, t0, n);
             if (!STATE_ONLY)
 #pragma unroll
                 for (int i = 0; i < kTile / kKeep; ++i)
-                    load_states(kept[i], p.saved + ((((long)at.b * p.tiles + tile) * (kTile / kKeep) + i) * d.D + ch) * d.N + at.n0, at.haven, p.wide_states);
+                    load_states<WIDE>(kept[i], p.saved + ((((long)at.b * p.tiles + tile) * (kTile / kKeep) + i) * d.D + ch) * d.N + at.n0, at.haven);
         };
         if (tile1 > tile0) load(tile1 - 1);
         for (int tile = tile1 - 1; tile >= tile0; --tile) {
             const int t0 = tile * kTile;
             float ut[W::P][W::VE], st[W::P][W::VE], rate[W::P][W::VE], dyp[W::P][W::VE], dzt[W::P][W::VE];
             if (t0 < n) {
-                bc.stage(bm);
+                bc.stage(bm, d.N);
 #pragma unroll
                 for (int i = 0; i < W::P; ++i) {
-                    const int t = i * W::TP + lane / W::LR;
+                    const int t = i * W::TP + at.tok;
 #pragma unroll
                     for (int e = 0; e < W::VE; ++e) {
-                        ut[i][e] = to_f(u.r[i].v[e]);
-                        float s = to_f(dt.r[i].v[e]) + bias[e];
-                        rate[i][e] = 1.f;
-                        if (d.softplus) s = softplus(s, &rate[i][e]);
-                        if (t0 + t >= n) s = 0.f;
+                        const bool there = t0 + t < n && at.ch0 + e < at.have;
+                        ut[i][e] = u.r[i].get(e);
+                        float s = dt.r[i].get(e) + bias[e];
+                        float slope;
+                        const float soft = softplus<T>(s, &slope);
+                        s = d.softplus ? soft : s;
+                        rate[i][e] = d.softplus ? slope : 1.f;
+                        s = there ? s : 0.f;
                         st[i][e] = s;
-                        float g = to_f(dy.r[i].v[e]);
+                        float g = dy.r[i].get(e);
                         if (GATE) {
-                            const float v = to_f(z.r[i].v[e]), sg = sigmoid(v);
+                            const float v = z.r[i].get(e), sg = sigmoid(v);
                             dzt[i][e] = g * sg * fmaf(v, 1.f - sg, 1.f);
                             g *= v * sg;
                         }
+                        g = there ? g : 0.f;
                         dyp[i][e] = g;
-                        step[t * W::CW + ch0 + e] = make_float2(s, s * ut[i][e]);
-                        dys[t * W::CW + ch0 + e] = g;
+                        step[t * W::CW + at.ch0 + e] = make_float2(s, there ? s * ut[i][e] : 0.f);
+                        dys[t * W::CW + at.ch0 + e] = g;
                     }
                 }
-                float before[kTile / kKeep][4];
+                float before[kTile / kKeep][NPL];
 #pragma unroll
                 for (int i = 0; i < kTile / kKeep; ++i)
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) before[i][j] = kept[i][j];
+                    for (int j = 0; j < NPL; ++j) before[i][j] = kept[i][j];
                 if (tile > tile0) load(tile - 1);
                 wave_lds_order();
                 if (STATE_ONLY) {
 #pragma unroll
                     for (int t = kTile - 1; t >= 0; --t) {
                         const float s = step[t * W::CW + at.c].x, g = dys[t * W::CW + at.c];
-                        const float4 c = *reinterpret_cast<const float4 *>(cm + t * W::NP + at.n0);
-                        const float cs[4] = {c.x, c.y, c.z, c.w};
+                        const Pack<float, NPL> c = *reinterpret_cast<const Pack<float, W::NPL> *>(cm + t * W::NP + at.n0);
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) x[j] = exp2_fast(s * A2[j]) * fmaf(g, cs[j], x[j]);
+                        for (int j = 0; j < NPL; ++j) x[j] = exp2_fast(s * A2[j]) * fmaf(g, c.v[j], x[j]);
                         steps += s;
                     }
                 } else {
                     float *sums = lds_sum[tile & 1][wave];
-                    float gk = 0.f, ek = 0.f, yk = 0.f, v[2][2][4];
+                    float gk = 0.f, ek = 0.f, yk = 0.f, v[2][2][NPL];
 #pragma unroll
                     for (int part = kTile / kKeep - 1; part >= 0; --part) {
                         const int p0 = part * kKeep;
-                        float a[kKeep][4], h[kKeep + 1][4];
+                        float a[kKeep][NPL], h[kKeep + 1][NPL];
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) h[0][j] = before[part][j];
+                        for (int j = 0; j < NPL; ++j) h[0][j] = before[part][j];
                         // LDS is read two tokens ahead, as in Forward
                         Ahead now, next;
                         now.load(step, dys, bm, cm, at, p0, false);
@@ -210,12 +213,11 @@ __global__ __launch_bounds__(64 * kWaves, 2) void scan_bwd_kernel(ScanParams p, 
                                 __builtin_amdgcn_sched_barrier(0);
                             }
                             const float2 s = now.s[i % 2];
-                            const float4 b = now.b[i % 2];
-                            const float bs[4] = {b.x, b.y, b.z, b.w};
+                            const Pack<float, NPL> b = now.b[i % 2];
 #pragma unroll
-                            for (int j = 0; j < 4; ++j) {
+                            for (int j = 0; j < NPL; ++j) {
                                 a[i][j] = exp2_fast(s.x * A2[j]);
-                                h[i + 1][j] = fmaf(a[i][j], h[i][j], s.y * bs[j]);
+                                h[i + 1][j] = fmaf(a[i][j], h[i][j], s.y * b.v[j]);
                             }
                         }
 #pragma unroll
@@ -228,16 +230,15 @@ __global__ __launch_bounds__(64 * kWaves, 2) void scan_bwd_kernel(ScanParams p, 
                             }
                             const float2 s = now.s[i % 2];
                             const float g = now.g[i % 2];
-                            const float4 b = now.b[i % 2], c = now.c[i % 2];
-                            const float bs[4] = {b.x, b.y, b.z, b.w}, cs[4] = {c.x, c.y, c.z, c.w};
+                            const Pack<float, NPL> b = now.b[i % 2], c = now.c[i % 2];
                             float gt = 0.f, et = 0.f, yt = 0.f;
 #pragma unroll
-                            for (int j = 0; j < 4; ++j) {
-                                const float dh = fmaf(g, cs[j], x[j]);
+                            for (int j = 0; j < NPL; ++j) {
+                                const float dh = fmaf(g, c.v[j], x[j]);
                                 v[t % 2][0][j] = dh * s.y;
                                 v[t % 2][1][j] = g * h[i + 1][j];
-                                gt = fmaf(dh, bs[j], gt);
-                                if (GATE) yt = fmaf(cs[j], h[i + 1][j], yt);
+                                gt = fmaf(dh, b.v[j], gt);
+                                if (GATE) yt = fmaf(c.v[j], h[i + 1][j], yt);
                                 x[j] = a[i][j] * dh;
                                 const float w = x[j] * h[i][j];
                                 et = fmaf(w, A2[j], et);
@@ -257,12 +258,19 @@ __global__ __launch_bounds__(64 * kWaves, 2) void scan_bwd_kernel(ScanParams p, 
                                 if (GATE) ys[o] = yk;
                             }
                             if (t % 2 == 0) {
-                                float r[4];
-                                sum_channels<LPC>(v, r);
+                                float r[NPL];
+                                sum_channels<W>(v, r);
                                 float *o = sums + ((t + lane / 32) * 2 + lane / 16 % 2) * W::NP + at.n0;
-                                if (LPC == 16) *reinterpret_cast<float4 *>(o) = make_float4(r[0], r[1], r[2], r[3]);
-                                else if (LPC == 8) *reinterpret_cast<float2 *>(o + 2 * low) = low == 0 ? make_float2(r[0], r[1]) : make_float2(r[2], r[3]);
-                                else if (low < 4) o[low] = low < 2 ? (low == 0 ? r[0] : r[1]) : (low == 2 ? r[2] : r[3]);
+                                // the lanes of a row that differ in the channel share out its NPL sums
+                                constexpr int SHARES = 16 / LPC < NPL ? 16 / LPC : NPL, EACH = NPL / SHARES;
+                                Pack<float, EACH> mine_r;
+#pragma unroll
+                                for (int j = 0; j < EACH; ++j) {
+                                    mine_r.v[j] = r[j];
+#pragma unroll
+                                    for (int k = 1; k < SHARES; ++k) mine_r.v[j] = low == k ? r[k * EACH + j] : mine_r.v[j];
+                                }
+                                if (low < SHARES) *reinterpret_cast<Pack<float, EACH> *>(o + low * EACH) = mine_r;
                             }
                         }
                     }
@@ -274,34 +282,31 @@ __global__ __launch_bounds__(64 * kWaves, 2) void scan_bwd_kernel(ScanParams p, 
             if (!STATE_ONLY) {
 #pragma unroll
                 for (int i = 0; i < W::P; ++i) {
-                    const int t = i * W::TP + lane / W::LR, have = t0 + t < d.L ? at.have - ch0 : 0;
+                    const int t = i * W::TP + at.tok, o = t * W::CW + at.ch0, have = t0 + t < d.L ? at.have - at.ch0 : 0;
                     Pack<T, W::VE> du, ddt, dz;
+                    float g[W::VE], et[W::VE], yt[W::VE];
+                    lds_row(g, gs + o);
+                    lds_row(et, es + o);
+                    if (GATE) lds_row(yt, ys + o);
 #pragma unroll
                     for (int e = 0; e < W::VE; ++e) {
-                        float a = 0.f, b = 0.f, c = 0.f;
-                        if (t0 + t < n) {
-                            const int o = t * W::CW + ch0 + e;
-                            const float g = gs[o];
-                            a = fmaf(g, st[i][e], skip[e] * dyp[i][e]);
-                            b = fmaf(es[o], kLn2, g * ut[i][e]) * rate[i][e];
-                            if (GATE) c = dzt[i][e] * fmaf(skip[e], ut[i][e], ys[o]);
-                            dskip[e] = fmaf(dyp[i][e], ut[i][e], dskip[e]);
-                            dbias[e] += b;
-                        }
-                        du.v[e] = from_f<T>(a);
-                        ddt.v[e] = from_f<T>(b);
-                        dz.v[e] = from_f<T>(c);
+                        const bool there = t0 + t < n && at.ch0 + e < at.have;
+                        const float rise = fmaf(et[e], kLn2, g[e] * ut[i][e]) * rate[i][e];
+                        du.v[e] = from_f<T>(there ? fmaf(g[e], st[i][e], skip[e] * dyp[i][e]) : 0.f);
+                        ddt.v[e] = from_f<T>(there ? rise : 0.f);
+                        if (GATE) dz.v[e] = from_f<T>(there ? dzt[i][e] * fmaf(skip[e], ut[i][e], yt[e]) : 0.f);
+                        dskip[e] += there ? dyp[i][e] * ut[i][e] : 0.f;
+                        dbias[e] += there ? rise : 0.f;
                     }
-                    const long row = t0 + t;
-                    store_pack<WIDE, T, W::VE>((T *)p.g.u + at.b * d.u_b + row * d.u_l + at.c0 + ch0, du, have);
-                    store_pack<WIDE, T, W::VE>((T *)p.g.dt + at.b * d.dt_b + row * d.dt_l + at.c0 + ch0, ddt, have);
-                    if (GATE) store_pack<WIDE, T, W::VE>((T *)p.g.z + at.b * d.z_b + row * d.z_l + at.c0 + ch0, dz, have);
+                    TileRows<T, W, WIDE>::store(p.g.u, d.u_b, d.u_l, at, t0, i, du, have);
+                    TileRows<T, W, WIDE>::store(p.g.dt, d.dt_b, d.dt_l, at, t0, i, ddt, have);
+                    if (GATE) TileRows<T, W, WIDE>::store(p.g.z, d.z_b, d.z_l, at, t0, i, dz, have);
                 }
                 wave_lds_order();
                 if (t0 < n) {
                     // the waves' sums, in their order; the other of the two buffers is written meanwhile
                     __syncthreads();
-                    float *o = p.part_bc + ((((long)at.b * p.tiles + tile) * d.G + at.g) * p.blocks + unit % p.blocks) * BC;
+                    float *o = p.part_bc + ((((long)at.b * p.tiles + tile) * d.G + at.g) * p.blocks + at.block) * BC;
                     for (int i = threadIdx.x; i < BC; i += 64 * kWaves) {
                         float v = lds_sum[tile & 1][0][i];
 #pragma unroll
@@ -312,13 +317,13 @@ __global__ __launch_bounds__(64 * kWaves, 2) void scan_bwd_kernel(ScanParams p, 
             }
         }
         if (STATE_ONLY) {
-            store_states(p.seg_state + seg_at(at.seg), x, at.haven, p.wide_states);
+            store_states<WIDE>(p.seg_state + seg_at(at.seg), x, at.haven);
             if (at.q == 0 && mine) p.seg_step[((long)at.b * p.segs + at.seg) * d.D + ch] = steps;
         } else {
-            if (p.g.state && at.seg == 0) store_states(p.g.state + state_at, x, at.haven, p.wide_states);
+            if (p.g.state && at.seg == 0) store_states<WIDE>(p.g.state + state_at, x, at.haven);
             float *o = p.part_w + (((long)at.b * p.segs + at.seg) * d.D) * (d.N + 2);
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
+            for (int j = 0; j < NPL; ++j)
                 if (j < at.haven) o[ch * (d.N + 2) + at.n0 + j] = dA[j];
             // over the lanes that load other tokens of the same channels
 #pragma unroll
@@ -327,8 +332,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void scan_bwd_kernel(ScanParams p, 
                     dskip[e] += __shfl_xor(dskip[e], k);
                     dbias[e] += __shfl_xor(dbias[e], k);
                 }
-                if (lane < W::LR && ch0 + e < at.have) {
-                    float *w = o + (at.c0 + ch0 + e) * (long)(d.N + 2) + d.N;
+                if (lane < W::LR && at.ch0 + e < at.have) {
+                    float *w = o + (at.c0 + at.ch0 + e) * (long)(d.N + 2) + d.N;
                     w[0] = dskip[e];
                     w[1] = dbias[e];
                 }
@@ -372,23 +377,23 @@ __global__ __launch_bounds__(256) void scan_join_weights_kernel(ScanParams p)
     if (out) *out = v + (p.add ? *out : 0.f);
 }
 
-template <class T, int LPC, bool WIDE, bool GATE>
+template <class T, class W, bool WIDE, bool GATE>
 void launch_main(const ScanParams &p, hipStream_t s)
 {
     const unsigned units = scan_units(p), grid = std::min(units, 1u << 22);
-    if (p.segs > 1) scan_bwd_kernel<T, LPC, WIDE, GATE, true><<<grid, 64 * kWaves, 0, s>>>(p, units);
-    if (units > 0) scan_bwd_kernel<T, LPC, WIDE, GATE, false><<<grid, 64 * kWaves, 0, s>>>(p, units);
+    if (p.segs > 1) scan_bwd_kernel<T, W, WIDE, GATE, true><<<grid, 64 * kWaves, 0, s>>>(p, units);
+    if (units > 0) scan_bwd_kernel<T, W, WIDE, GATE, false><<<grid, 64 * kWaves, 0, s>>>(p, units);
 }
 
-template <class T, int LPC, bool WIDE>
+template <class T, class W, bool WIDE>
 hipError_t launch(const ScanParams &p, hipStream_t s)
 {
-    if (p.in.z) launch_main<T, LPC, WIDE, true>(p, s);
-    else launch_main<T, LPC, WIDE, false>(p, s);
+    if (p.in.z) launch_main<T, W, WIDE, true>(p, s);
+    else launch_main<T, W, WIDE, false>(p, s);
     const ucd_scan_t &d = p.d;
-    const long elements = (long)d.B * d.L * d.G * 2 * ScanWave<LPC>::NP;
+    const long elements = (long)d.B * d.L * d.G * 2 * W::NP;
     if (elements > 0)
-        scan_join_bc_kernel<T><<<(unsigned)std::min((elements + 255) / 256, 1l << 22), 256, 0, s>>>(p, ScanWave<LPC>::NP, elements);
+        scan_join_bc_kernel<T><<<(unsigned)std::min((elements + 255) / 256, 1l << 22), 256, 0, s>>>(p, W::NP, elements);
     scan_join_weights_kernel<<<(unsigned)(((long)d.D * (d.N + 2) + 255) / 256), 256, 0, s>>>(p);
     return hipGetLastError();
 }
@@ -405,12 +410,11 @@ hipError_t scan_bwd(const ucd_scan_t &d, const ucd_scan_in_t &in, const void *dy
     p.saved = const_cast<float *>(saved);
     p.g = g;
     p.add = add;
-    p.wide_states = p.wide_states && ((uintptr_t)dstate_out & 15) == 0 && ((uintptr_t)g.state & 15) == 0;
-    const bool wide = scan_wide(d, in, dy, &g);
-    return scan_by_lanes(d, [&](auto lanes) {
-        constexpr int LPC = decltype(lanes)::value;
-        if (d.dtype == 1) return wide ? launch<bf16_t, LPC, true>(p, s) : launch<bf16_t, LPC, false>(p, s);
-        return wide ? launch<float, LPC, true>(p, s) : launch<float, LPC, false>(p, s);
+    const bool wide = scan_wide(d, in, dy, dstate_out, g.state, &g);
+    return scan_by_states(d, [&](auto wave) {
+        typedef decltype(wave) W;
+        if (d.dtype == 1) return wide ? launch<bf16_t, W, true>(p, s) : launch<bf16_t, W, false>(p, s);
+        return wide ? launch<float, W, true>(p, s) : launch<float, W, false>(p, s);
     });
 }
 

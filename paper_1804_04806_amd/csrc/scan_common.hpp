@@ -1,6 +1,6 @@
 // What the scan's kernels share: how a wave is laid out over channels and states, and how it stages a tile of tokens.
 //
-// A lane holds 4 neighbouring states of one channel; LPC neighbouring lanes hold a channel's N <= 4 LPC states, a wave 64 / LPC
+// A lane holds NPL neighbouring states of one channel; LPC neighbouring lanes hold a channel's N <= LPC NPL states, a wave 64 / LPC
 // neighbouring channels, which share Bm and Cm (they are of one group).  Waves walk over tiles of 16 tokens by themselves: what
 // all states of a channel have in common (the step, its activation, the gate) is computed once per channel and token by the
 // lane that loads it, and handed to the others through the wave's own part of LDS.  No workgroup barriers.
@@ -17,9 +17,9 @@ constexpr int kTile = 16;      // tokens
 constexpr int kKeep = 8;       // tokens between the states that Forward keeps for Backward
 constexpr int kWaves = 4;      // of a workgroup, on neighbouring channels
 
-template <int LPC>
+template <int LPC_, int NPL_>
 struct ScanWave {
-    static constexpr int CW = 64 / LPC, NP = 4 * LPC;        // channels, states
+    static constexpr int LPC = LPC_, NPL = NPL_, CW = 64 / LPC, NP = NPL * LPC;        // channels, states
     static constexpr int EPL = kTile * CW / 64;              // a tile's elements per lane,
     static constexpr int VE = EPL < 4 ? EPL : 4, P = EPL / VE;   // in P packs of VE neighbours
     static constexpr int LR = CW / VE, TP = 64 / LR;         // lanes to a token, tokens to a pack of all lanes
@@ -33,7 +33,6 @@ struct ScanParams {
     unsigned blocks;             // and workgroups for them
     int segs, seg_tiles;         // a sequence's parts that are scanned side by side, and their length
     int tiles;                   // of a whole sequence
-    bool wide_states;            // A and all states in packs of 4
     const float *state_in;
     float *state_out;
     void *y;
@@ -51,28 +50,33 @@ struct ScanParams {
 };
 
 // The unit of a workgroup, its waves' channels and its lanes' states.
-template <int LPC>
+template <class W>
 struct ScanPlace {
-    int b, seg, g, c0, c, q, n0;
-    int have, haven;      // channels of the wave, states of the lane
+    int b, seg, g, block;        // of the workgroup,
+    int first, c0, have;         // its first channel, the wave's and how many of them there are
+    int c, q, n0, haven;         // the lane's channel within the wave, states from n0 on and how many of them there are
+    int tok, ch0;                // what the lane loads: token (of a pack of all lanes) and first channel within the wave
     __device__ __forceinline__ ScanPlace(const ScanParams &p, unsigned unit)
     {
         const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-        const int block = unit % p.blocks;
+        block = unit % p.blocks;
         unit /= p.blocks;
         g = unit % p.d.G;
         unit /= p.d.G;
         seg = unit % p.segs;
         b = unit / p.segs;
-        const int at = (block * kWaves + wave) * ScanWave<LPC>::CW;
+        first = g * p.per_group + block * kWaves * W::CW;
+        const int at = (block * kWaves + wave) * W::CW;
         have = p.per_group - at;
-        have = have < 0 ? 0 : have < ScanWave<LPC>::CW ? have : ScanWave<LPC>::CW;
-        c0 = g * p.per_group + at;
-        q = lane % LPC;
-        c = lane / LPC;
-        n0 = 4 * q;
+        have = have < 0 ? 0 : have < W::CW ? have : W::CW;
+        c0 = first + wave * W::CW;
+        q = lane % W::LPC;
+        c = lane / W::LPC;
+        n0 = W::NPL * q;
         haven = c < have ? p.d.N - n0 : 0;
-        haven = haven < 0 ? 0 : haven < 4 ? haven : 4;
+        haven = haven < 0 ? 0 : haven < W::NPL ? haven : W::NPL;
+        tok = lane / W::LR;
+        ch0 = lane % W::LR * W::VE;
     }
 };
 
@@ -83,104 +87,161 @@ __device__ __forceinline__ int scan_length(const ScanParams &p, int b)
     return n < 0 ? 0 : n < p.d.L ? n : p.d.L;
 }
 
-// 4 states (or a channel's 4 coefficients) of the lane
-__device__ __forceinline__ void load_states(float (&h)[4], const float *at, int haven, bool wide)
+// The lane's states, or coefficients of a channel's states.
+template <bool WIDE, int N>
+__device__ __forceinline__ void load_states(float (&h)[N], const float *at, int haven)
 {
-    const Pack<float, 4> r = wide ? load_pack<true, float, 4>(at, haven) : load_pack<false, float, 4>(at, haven);
+    const Pack<float, N> r = load_pack<WIDE, float, N>(at, haven);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) h[j] = r.v[j];
+    for (int j = 0; j < N; ++j) h[j] = r.v[j];
 }
 
-__device__ __forceinline__ void store_states(float *at, const float (&h)[4], int haven, bool wide)
+template <bool WIDE, int N>
+__device__ __forceinline__ void store_states(float *at, const float (&h)[N], int haven)
 {
-    Pack<float, 4> r;
+    Pack<float, N> r;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) r.v[j] = h[j];
-    if (wide) store_pack<true, float, 4>(at, r, haven);
-    else store_pack<false, float, 4>(at, r, haven);
+    for (int j = 0; j < N; ++j) r.v[j] = h[j];
+    store_pack<WIDE, float, N>(at, r, haven);
 }
 
-// A tile's values of a (B, L, D) tensor as they come from memory: pack i of a lane is token i * TP + lane / LR, channels (lane % LR) * VE on.
-template <class T, int LPC>
-struct TileRows {
-    typedef ScanWave<LPC> W;
-    Pack<T, W::VE> r[W::P];
+// N elements as they come from memory, in words (WIDE: one load, all of them; otherwise a word each, the first `have` of them): a lane's prefetched
+// values stay as they are until they are used.  As elements of 16 bits the compiler takes them apart, and waits for them, right behind the load.
+template <class T, int N, bool WIDE>
+struct Raw {
+    static constexpr bool PACKED = WIDE && N * sizeof(T) % 4 == 0;
+    static constexpr int WORDS = PACKED ? N * (int)sizeof(T) / 4 : N;
+    uint32_t w[WORDS];
 
-    template <bool WIDE>
-    __device__ __forceinline__ void load(const void *base, long sb, long sl, const ScanPlace<LPC> &at, int t0, int n)
+    __device__ __forceinline__ void load(const char *base, uint32_t offset, int have)
     {
-        const int lane = threadIdx.x % 64, ch = lane % W::LR * W::VE;
+        if (PACKED) {
+            typedef Pack<uint32_t, WORDS> Words;
+            const Words r = *reinterpret_cast<const Words *>(base + offset);
 #pragma unroll
-        for (int i = 0; i < W::P; ++i) {
-            const int t = t0 + i * W::TP + lane / W::LR;
-            const T *p = (const T *)base + at.b * sb + (long)t * sl + at.c0 + ch;
-            r[i] = load_pack<WIDE, T, W::VE>(p, t < n ? at.have - ch : 0);
+            for (int i = 0; i < WORDS; ++i) w[i] = r.v[i];
+        } else {
+#pragma unroll
+            for (int i = 0; i < WORDS; ++i) {
+                w[i] = 0;
+                if (!WIDE && i >= have) continue;
+                if (sizeof(T) == 4) w[i] = *reinterpret_cast<const uint32_t *>(base + offset + 4 * i);
+                else w[i] = *reinterpret_cast<const uint16_t *>(base + offset + 2 * i);
+            }
         }
+    }
+    __device__ __forceinline__ float get(int i) const
+    {
+        if (sizeof(T) == 4) return __builtin_bit_cast(float, w[i]);
+        if (!PACKED) return __builtin_bit_cast(float, w[i % WORDS] << 16);
+        return __builtin_bit_cast(float, i % 2 ? w[i / 2 % WORDS] & 0xFFFF0000u : w[i / 2 % WORDS] << 16);
     }
 };
 
-// The same of Bm and Cm: the tile's 16 rows of NP states of one, then of the other; in packs of 4 or one by one.
-template <class T, int LPC, bool WIDE>
+// A tile's values of a (B, L, D) tensor: pack i of a lane is token i * TP + lane / LR, channels (lane % LR) * VE on.  Tokens behind the sequence's last
+// repeat it and channels that are not there repeat the workgroup's first: their values are masked where they are used.
+template <class T, class W, bool WIDE>
+struct TileRows {
+    Raw<T, W::VE, WIDE> r[W::P];
+
+    // the element's place from the workgroup's first channel of the tile's first token; below 2^32 bytes (seq_api.cpp bounds the strides)
+    static __device__ __forceinline__ uint32_t offset(const ScanPlace<W> &at, int i, long sl, int last)
+    {
+        const int t = min(at.tok + i * W::TP, last), c = at.ch0 < at.have ? at.c0 - at.first + at.ch0 : 0;
+        return ((uint32_t)t * (uint32_t)sl + (uint32_t)c) * (uint32_t)sizeof(T);
+    }
+    static __device__ __forceinline__ const char *row(const void *base, long sb, long sl, const ScanPlace<W> &at, int t0)
+    {
+        return (const char *)base + (at.b * sb + t0 * sl + at.first) * (long)sizeof(T);
+    }
+    __device__ __forceinline__ void load(const void *base, long sb, long sl, const ScanPlace<W> &at, int t0, int n)
+    {
+#pragma unroll
+        for (int i = 0; i < W::P; ++i) r[i].load(row(base, sb, sl, at, t0), offset(at, i, sl, n - 1 - t0), at.have - at.ch0);
+    }
+    // pack i of an output; have: of its elements, 0 for a token that is not there
+    static __device__ __forceinline__ void store(void *base, long sb, long sl, const ScanPlace<W> &at, int t0, int i, const Pack<T, W::VE> &v, int have)
+    {
+        store_pack<WIDE, T, W::VE>((T *)(const_cast<char *>(row(base, sb, sl, at, t0)) + offset(at, i, sl, kTile)), v, have);
+    }
+};
+
+// The same of Bm and Cm: the tile's 16 rows of NP states of one, then of the other; in packs of 4 or one by one.  States that are not there are 0.
+template <class T, class W, bool WIDE>
 struct TileStates {
-    typedef ScanWave<LPC> W;
-    static constexpr int V = WIDE ? 4 : 1, P = (W::BE + V - 1) / V;
-    Pack<T, V> r[P];
+    static constexpr int V = WIDE ? 4 : 1, P = (W::BE + V - 1) / V, ROWS = kTile * W::NP;
+    Raw<T, V, WIDE> r[P];
 
     static __device__ __forceinline__ int index(int i) { return (i * 64 + (int)threadIdx.x % 64) * V; }
 
-    __device__ __forceinline__ void load(const ScanParams &p, const ScanPlace<LPC> &at, int t0, int n)
+    __device__ __forceinline__ void load(const ScanParams &p, const ScanPlace<W> &at, int t0, int n)
     {
+        const char *bm = (const char *)p.in.Bm + (at.b * p.d.Bm_b + t0 * p.d.Bm_l + (long)at.g * p.d.N) * (long)sizeof(T);
+        const char *cm = (const char *)p.in.Cm + (at.b * p.d.Cm_b + t0 * p.d.Cm_l + (long)at.g * p.d.N) * (long)sizeof(T);
 #pragma unroll
         for (int i = 0; i < P; ++i) {
-            const int e = index(i), k = e % W::NP, t = t0 + e / W::NP % kTile;
-            const bool second = e >= kTile * W::NP;
-            const int have = t < n && k < p.d.N && e < 2 * kTile * W::NP ? V : 0;
-            const T *base = second ? (const T *)p.in.Cm + at.b * p.d.Cm_b + (long)t * p.d.Cm_l : (const T *)p.in.Bm + at.b * p.d.Bm_b + (long)t * p.d.Bm_l;
-            r[i] = load_pack<WIDE, T, V>(base + (long)at.g * p.d.N + k, have);
+            const int e = index(i), k = e % W::NP, t = min(e / W::NP % kTile, n - 1 - t0);
+            const bool there = k < p.d.N;
+            // a pack of all lanes is of one tensor, but for the single one of few states
+            const bool whole = ROWS % (64 * V) == 0, second = whole ? i * 64 * V >= ROWS : e >= ROWS;
+            const uint32_t offset = ((uint32_t)t * (uint32_t)(second ? p.d.Cm_l : p.d.Bm_l) + (there ? (uint32_t)k : 0u)) * (uint32_t)sizeof(T);
+            if (whole) r[i].load(second ? cm : bm, offset, V);
+            else if (second) r[i].load(cm, offset, V);
+            else r[i].load(bm, offset, V);
         }
     }
 
     // into LDS: Bm's rows, then Cm's
-    __device__ __forceinline__ void stage(float *lds)
+    __device__ __forceinline__ void stage(float *lds, int states)
     {
 #pragma unroll
         for (int i = 0; i < P; ++i) {
             const int e = index(i);
             Pack<float, V> f;
 #pragma unroll
-            for (int j = 0; j < V; ++j) f.v[j] = to_f(r[i].v[j]);
-            if (2 * kTile * W::NP % (64 * V) == 0 || e < 2 * kTile * W::NP) *reinterpret_cast<Pack<float, V> *>(lds + e) = f;
+            for (int j = 0; j < V; ++j) f.v[j] = e % W::NP < states ? r[i].get(j) : 0.f;
+            if (2 * ROWS % (64 * V) == 0 || e < 2 * ROWS) *reinterpret_cast<Pack<float, V> *>(lds + e) = f;
         }
     }
 };
 
+// VE neighbours of a tile's row in LDS
+template <int N>
+__device__ __forceinline__ void lds_row(float (&v)[N], const float *at)
+{
+    const Pack<float, N> r = *reinterpret_cast<const Pack<float, N> *>(at);
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = r.v[i];
+}
+
 // The decay of a lane's states over a whole segment, whose steps add up to `step`, and its own end state on top.
-__device__ __forceinline__ void join_segment(float (&h)[4], const float (&A2)[4], float step, const float (&end)[4])
+template <int N>
+__device__ __forceinline__ void join_segment(float (&h)[N], const float (&A2)[N], float step, const float (&end)[N])
 {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) h[j] = fmaf(exp2_fast(step * A2[j]), h[j], end[j]);
+    for (int j = 0; j < N; ++j) h[j] = fmaf(exp2_fast(step * A2[j]), h[j], end[j]);
 }
 
 }  // namespace seq
 
-// Whether rows can be read in packs of 4 (a pack of one row is inside a group, and so of Bm and Cm).
-bool scan_wide(const ucd_scan_t &d, const ucd_scan_in_t &in, const void *y, const ucd_scan_grad_t *g);
+// Whether rows and states can be read in packs of 4 (a pack of a row lies inside a group, and so one of Bm and Cm).
+bool scan_wide(const ucd_scan_t &d, const ucd_scan_in_t &in, const void *y, const float *state1, const float *state2, const ucd_scan_grad_t *g);
 void scan_params(const ucd_scan_t &d, const ucd_scan_in_t &in, int dir, void *ws, seq::ScanParams &p);
-int scan_lanes(const ucd_scan_t &d);   // LPC
 // workgroups of a launch, below 2^31 (seq_api.cpp)
 inline unsigned scan_units(const seq::ScanParams &p) { return (unsigned)p.d.B * p.segs * p.d.G * p.blocks; }
 
-// f(std::integral_constant<int, LPC>) for the descriptor's number of states
+// f(ScanWave<LPC, NPL>()) for the descriptor's number of states
 template <class F>
-hipError_t scan_by_lanes(const ucd_scan_t &d, F f)
+hipError_t scan_by_states(const ucd_scan_t &d, F f)
 {
-    switch (scan_lanes(d)) {
-    case 1: return f(std::integral_constant<int, 1>());
-    case 2: return f(std::integral_constant<int, 2>());
-    case 4: return f(std::integral_constant<int, 4>());
-    case 8: return f(std::integral_constant<int, 8>());
-    default: return f(std::integral_constant<int, 16>());
-    }
+    using seq::ScanWave;
+    if (d.N <= 4) return f(ScanWave<4, 1>());
+    if (d.N <= 8) return f(ScanWave<4, 2>());
+    if (d.N <= 16) return f(ScanWave<4, 4>());
+    if (d.N <= 32) return f(ScanWave<8, 4>());
+    return f(ScanWave<16, 4>());
 }
+inline int scan_lanes(const ucd_scan_t &d) { return d.N <= 16 ? 4 : d.N <= 32 ? 8 : 16; }
+inline int scan_states(const ucd_scan_t &d) { return d.N <= 4 ? 4 : d.N <= 8 ? 8 : 4 * scan_lanes(d); }   // NP
 
 }  // namespace ucd

@@ -12,7 +12,7 @@ using namespace ucd;
 
 namespace {
 
-constexpr int64_t kMaxStride = int64_t(1) << 40;
+constexpr int64_t kMaxStride = int64_t(1) << 40, kMaxInner = int64_t(1) << 25;   // a tile of 16 tokens and more in 32-bit offsets of bytes
 constexpr int64_t kMaxElements = int64_t(1) << 40;
 
 template <class F>
@@ -40,7 +40,7 @@ bool fill_strides(int64_t &outer, int64_t &inner, int64_t n_outer, int64_t n_inn
 {
     if (inner == 0) inner = width;
     if (outer == 0) outer = inner * (n_inner > 1 ? n_inner : 1);
-    if (outer < 0 || inner < 0 || outer > kMaxStride || inner > kMaxStride) return false;
+    if (outer < 0 || inner < 0 || outer > kMaxStride || inner > kMaxInner) return false;
     if (n_inner > 1 && inner < width) return false;
     if (n_outer > 1 && outer < width) return false;
     if (n_inner > 1 && n_outer > 1) {

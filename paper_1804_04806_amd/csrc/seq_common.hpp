@@ -67,10 +67,12 @@ __device__ __forceinline__ float exp_full(float v)
 __device__ __forceinline__ float sigmoid(float v) { return __builtin_amdgcn_rcpf(1.f + exp2_fast(v * -kLog2e)); }
 
 // log(1 + exp(v)) = max(v, 0) + log1p(e), e = exp(-|v|); with w = 1 + e rounded, log1p(e) = log(w) e / (w - 1) to an ulp or two, because w - 1 is
-// exact and log(w) / (w - 1) hardly changes between 1 + e and w.  Also the function's derivative, 1 / (1 + exp(-v)).
+// exact and log(w) / (w - 1) hardly changes between 1 + e and w.  Also the function's derivative, 1 / (1 + exp(-v)).  For values that were rounded
+// to 8 bits exp(-|v|) without its correction: |v log2(e)| 2^-24 off.
+template <class T>
 __device__ __forceinline__ float softplus(float v, float *derivative = nullptr)
 {
-    const float e = exp_full(-fabsf(v)), w = 1.f + e, d = w - 1.f;
+    const float e = sizeof(T) == 4 ? exp_full(-fabsf(v)) : exp2_fast(-fabsf(v) * kLog2e), w = 1.f + e, d = w - 1.f;
     const float l = d == 0.f ? e : __builtin_amdgcn_logf(w) * kLn2 * (e * __builtin_amdgcn_rcpf(d));
     if (derivative) *derivative = (v >= 0.f ? 1.f : e) * __builtin_amdgcn_rcpf(w);
     return fmaxf(v, 0.f) + l;
