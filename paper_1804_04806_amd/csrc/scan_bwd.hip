@@ -121,60 +121,83 @@ __global__ __launch_bounds__(64 * kWaves, 2) void scan_bwd_kernel(ScanParams p, 
                 } else join_segment(x, A2, mine ? p.seg_step[((long)at.b * p.segs + s) * d.D + ch] : 0.f, end);
             }
         float bias[W::VE], skip[W::VE], dskip[W::VE] = {}, dbias[W::VE] = {}, steps = 0.f;
+        bool channel[W::VE];
 #pragma unroll
         for (int i = 0; i < W::VE; ++i) {
-            const bool have = at.ch0 + i < at.have;
-            bias[i] = have && p.in.dt_bias ? p.in.dt_bias[at.c0 + at.ch0 + i] : 0.f;
-            skip[i] = have && p.in.skip ? p.in.skip[at.c0 + at.ch0 + i] : 0.f;
+            channel[i] = at.ch0 + i < at.have;
+            bias[i] = channel[i] && p.in.dt_bias ? p.in.dt_bias[at.c0 + at.ch0 + i] : 0.f;
+            skip[i] = channel[i] && p.in.skip ? p.in.skip[at.c0 + at.ch0 + i] : 0.f;
         }
 
-        TileRows<T, W, WIDE> u, dt, z, dy;
+        const long t_last = (long)(tile1 - 1) * kTile, e = sizeof(T);      // of the last tile
+        const char *u_at = row_base<T>(p.in.u, d.u_b, d.u_l, at, t_last), *dt_at = row_base<T>(p.in.dt, d.dt_b, d.dt_l, at, t_last);
+        const char *z_at = row_base<T>(p.in.z, d.z_b, d.z_l, at, t_last), *dy_at = row_base<T>(p.dy, d.y_b, d.y_l, at, t_last);
+        const char *bm_at = bc_base<T>(p.in.Bm, d.Bm_b, d.Bm_l, at, t_last, d.N), *cm_at = bc_base<T>(p.in.Cm, d.Cm_b, d.Cm_l, at, t_last, d.N);
+        char *du_at = const_cast<char *>(row_base<T>(p.g.u, d.u_b, d.u_l, at, t_last)), *ddt_at = const_cast<char *>(row_base<T>(p.g.dt, d.dt_b, d.dt_l, at, t_last));
+        char *dz_at = const_cast<char *>(row_base<T>(p.g.z, d.z_b, d.z_l, at, t_last));
+        const float *saved_at = p.saved + (((long)at.b * p.tiles + tile1 - 1) * (kTile / kKeep) * d.D + at.first) * d.N;
+        const uint32_t state_off = (uint32_t)(at.c0 - at.first + at.c) * d.N + at.n0;
+        const uint32_t du_off = row_offset<T>(at, d.u_l, kTile), ddt_off = row_offset<T>(at, d.dt_l, kTile), dz_off = row_offset<T>(at, d.z_l, kTile);
+        Raw<T, W::VE, WIDE> u, dt, z, dy;
         TileStates<T, W, WIDE> bc;
         float kept[kTile / kKeep][NPL];
-        auto load = [&](int tile) {
-            const int t0 = tile * kTile;
-            if (t0 >= n) return;
-            u.load(p.in.u, d.u_b, d.u_l, at, t0, n);
-            dt.load(p.in.dt, d.dt_b, d.dt_l, at, t0, n);
-            dy.load(p.dy, d.y_b, d.y_l, at, t0, n);
-            if (GATE) z.load(p.in.z, d.z_b, d.z_l, at, t0, n);
-            bc.load(p, at, t0, n);
-            if (!STATE_ONLY)
+        uint32_t u_off, dt_off, z_off, dy_off;
+        auto place = [&](int last) {
+            u_off = row_offset<T>(at, d.u_l, last);
+            dt_off = row_offset<T>(at, d.dt_l, last);
+            dy_off = row_offset<T>(at, d.y_l, last);
+            if (GATE) z_off = row_offset<T>(at, d.z_l, last);
+            bc.place(p, last);
+        };
+        place(kTile);
+        auto load = [&](int tile) {      // and on to the tile before it
+            const int left = n - tile * kTile;
+            if (left > 0) {
+                if (left < kTile) place(left - 1);
+                u.load(u_at, u_off, at.have - at.ch0);
+                dt.load(dt_at, dt_off, at.have - at.ch0);
+                dy.load(dy_at, dy_off, at.have - at.ch0);
+                if (GATE) z.load(z_at, z_off, at.have - at.ch0);
+                bc.load(bm_at, cm_at);
+                if (!STATE_ONLY)
 #pragma unroll
-                for (int i = 0; i < kTile / kKeep; ++i)
-                    load_states<WIDE>(kept[i], p.saved + ((((long)at.b * p.tiles + tile) * (kTile / kKeep) + i) * d.D + ch) * d.N + at.n0, at.haven);
+                    for (int i = 0; i < kTile / kKeep; ++i) load_states<WIDE>(kept[i], saved_at + i * (long)d.D * d.N + state_off, at.haven);
+                if (left < kTile) place(kTile);
+            }
+            u_at -= kTile * e * d.u_l;
+            dt_at -= kTile * e * d.dt_l;
+            dy_at -= kTile * e * d.y_l;
+            if (GATE) z_at -= kTile * e * d.z_l;
+            bm_at -= kTile * e * d.Bm_l;
+            cm_at -= kTile * e * d.Cm_l;
+            saved_at -= (kTile / kKeep) * (long)d.D * d.N;
         };
         if (tile1 > tile0) load(tile1 - 1);
         for (int tile = tile1 - 1; tile >= tile0; --tile) {
-            const int t0 = tile * kTile;
-            float ut[W::P][W::VE], st[W::P][W::VE], rate[W::P][W::VE], dyp[W::P][W::VE], dzt[W::P][W::VE];
-            if (t0 < n) {
+            const int left = n - tile * kTile;
+            float ut[W::VE], st[W::VE], rate[W::VE], dyp[W::VE], dzt[W::VE];
+            if (left > 0) {
                 bc.stage(bm, d.N);
 #pragma unroll
-                for (int i = 0; i < W::P; ++i) {
-                    const int t = i * W::TP + at.tok;
-#pragma unroll
-                    for (int e = 0; e < W::VE; ++e) {
-                        const bool there = t0 + t < n && at.ch0 + e < at.have;
-                        ut[i][e] = u.r[i].get(e);
-                        float s = dt.r[i].get(e) + bias[e];
-                        float slope;
-                        const float soft = softplus<T>(s, &slope);
-                        s = d.softplus ? soft : s;
-                        rate[i][e] = d.softplus ? slope : 1.f;
-                        s = there ? s : 0.f;
-                        st[i][e] = s;
-                        float g = dy.r[i].get(e);
-                        if (GATE) {
-                            const float v = z.r[i].get(e), sg = sigmoid(v);
-                            dzt[i][e] = g * sg * fmaf(v, 1.f - sg, 1.f);
-                            g *= v * sg;
-                        }
-                        g = there ? g : 0.f;
-                        dyp[i][e] = g;
-                        step[t * W::CW + at.ch0 + e] = make_float2(s, there ? s * ut[i][e] : 0.f);
-                        dys[t * W::CW + at.ch0 + e] = g;
+                for (int i = 0; i < W::VE; ++i) {
+                    const bool there = at.tok < left && channel[i];
+                    ut[i] = u.get(i);
+                    float s = dt.get(i) + bias[i], slope;
+                    const float soft = softplus<T>(s, &slope);
+                    s = d.softplus ? soft : s;
+                    rate[i] = d.softplus ? slope : 1.f;
+                    s = there ? s : 0.f;
+                    st[i] = s;
+                    float g = dy.get(i);
+                    if (GATE) {
+                        const float v = z.get(i), sg = sigmoid(v);
+                        dzt[i] = g * sg * fmaf(v, 1.f - sg, 1.f);
+                        g *= v * sg;
                     }
+                    g = there ? g : 0.f;
+                    dyp[i] = g;
+                    step[at.tok * W::CW + at.ch0 + i] = make_float2(s, there ? s * ut[i] : 0.f);
+                    dys[at.tok * W::CW + at.ch0 + i] = g;
                 }
                 float before[kTile / kKeep][NPL];
 #pragma unroll
@@ -280,30 +303,30 @@ __global__ __launch_bounds__(64 * kWaves, 2) void scan_bwd_kernel(ScanParams p, 
                 load(tile - 1);
             }
             if (!STATE_ONLY) {
+                const int o = at.tok * W::CW + at.ch0, have = at.tok < d.L - tile * kTile ? at.have - at.ch0 : 0;
+                Pack<T, W::VE> du, ddt, dz;
+                float g[W::VE], et[W::VE], yt[W::VE];
+                lds_row(g, gs + o);
+                lds_row(et, es + o);
+                if (GATE) lds_row(yt, ys + o);
 #pragma unroll
-                for (int i = 0; i < W::P; ++i) {
-                    const int t = i * W::TP + at.tok, o = t * W::CW + at.ch0, have = t0 + t < d.L ? at.have - at.ch0 : 0;
-                    Pack<T, W::VE> du, ddt, dz;
-                    float g[W::VE], et[W::VE], yt[W::VE];
-                    lds_row(g, gs + o);
-                    lds_row(et, es + o);
-                    if (GATE) lds_row(yt, ys + o);
-#pragma unroll
-                    for (int e = 0; e < W::VE; ++e) {
-                        const bool there = t0 + t < n && at.ch0 + e < at.have;
-                        const float rise = fmaf(et[e], kLn2, g[e] * ut[i][e]) * rate[i][e];
-                        du.v[e] = from_f<T>(there ? fmaf(g[e], st[i][e], skip[e] * dyp[i][e]) : 0.f);
-                        ddt.v[e] = from_f<T>(there ? rise : 0.f);
-                        if (GATE) dz.v[e] = from_f<T>(there ? dzt[i][e] * fmaf(skip[e], ut[i][e], yt[e]) : 0.f);
-                        dskip[e] += there ? dyp[i][e] * ut[i][e] : 0.f;
-                        dbias[e] += there ? rise : 0.f;
-                    }
-                    TileRows<T, W, WIDE>::store(p.g.u, d.u_b, d.u_l, at, t0, i, du, have);
-                    TileRows<T, W, WIDE>::store(p.g.dt, d.dt_b, d.dt_l, at, t0, i, ddt, have);
-                    if (GATE) TileRows<T, W, WIDE>::store(p.g.z, d.z_b, d.z_l, at, t0, i, dz, have);
+                for (int i = 0; i < W::VE; ++i) {
+                    const bool there = at.tok < left && channel[i];
+                    const float rise = fmaf(et[i], kLn2, g[i] * ut[i]) * rate[i];
+                    du.v[i] = from_f<T>(there ? fmaf(g[i], st[i], skip[i] * dyp[i]) : 0.f);
+                    ddt.v[i] = from_f<T>(there ? rise : 0.f);
+                    if (GATE) dz.v[i] = from_f<T>(there ? dzt[i] * fmaf(skip[i], ut[i], yt[i]) : 0.f);
+                    dskip[i] += there ? dyp[i] * ut[i] : 0.f;
+                    dbias[i] += there ? rise : 0.f;
                 }
+                store_row<T, W, WIDE>(du_at, du_off, du, have);
+                store_row<T, W, WIDE>(ddt_at, ddt_off, ddt, have);
+                if (GATE) store_row<T, W, WIDE>(dz_at, dz_off, dz, have);
+                du_at -= kTile * e * d.u_l;
+                ddt_at -= kTile * e * d.dt_l;
+                if (GATE) dz_at -= kTile * e * d.z_l;
                 wave_lds_order();
-                if (t0 < n) {
+                if (left > 0) {
                     // the waves' sums, in their order; the other of the two buffers is written meanwhile
                     __syncthreads();
                     float *o = p.part_bc + ((((long)at.b * p.tiles + tile) * d.G + at.g) * p.blocks + at.block) * BC;

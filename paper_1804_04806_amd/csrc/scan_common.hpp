@@ -20,9 +20,8 @@ constexpr int kWaves = 4;      // of a workgroup, on neighbouring channels
 template <int LPC_, int NPL_>
 struct ScanWave {
     static constexpr int LPC = LPC_, NPL = NPL_, CW = 64 / LPC, NP = NPL * LPC;        // channels, states
-    static constexpr int EPL = kTile * CW / 64;              // a tile's elements per lane,
-    static constexpr int VE = EPL < 4 ? EPL : 4, P = EPL / VE;   // in P packs of VE neighbours
-    static constexpr int LR = CW / VE, TP = 64 / LR;         // lanes to a token, tokens to a pack of all lanes
+    static constexpr int VE = kTile * CW / 64;               // a tile's elements per lane, neighbours of one token
+    static constexpr int LR = CW / VE;                       // lanes to a token
     static constexpr int BE = 2 * kTile * NP / 64;           // a tile's elements of Bm and Cm per lane
 };
 
@@ -138,56 +137,61 @@ struct Raw {
     }
 };
 
-// A tile's values of a (B, L, D) tensor: pack i of a lane is token i * TP + lane / LR, channels (lane % LR) * VE on.  Tokens behind the sequence's last
-// repeat it and channels that are not there repeat the workgroup's first: their values are masked where they are used.
+// Tokens behind the sequence's last repeat it and channels that are not there repeat the workgroup's first: what is loaded of them is masked where it
+// is used.  Offsets of a tile's elements from its first token and the workgroup's first channel are below 2^32 bytes (seq_api.cpp bounds the strides).
+template <class T, class W>
+__device__ __forceinline__ uint32_t row_offset(const ScanPlace<W> &at, long sl, int last)
+{
+    const int c = at.ch0 < at.have ? at.c0 - at.first + at.ch0 : 0;
+    return ((uint32_t)min(at.tok, last) * (uint32_t)sl + (uint32_t)c) * (uint32_t)sizeof(T);
+}
+
+// The tile's first element for a workgroup: of u, dt, z, y and of Bm, Cm.  Uniform: an address is this pointer, which a tile moves on by scalar
+// arithmetic, and a lane's offset, which stays.
+template <class T, class W>
+__device__ __forceinline__ const char *row_base(const void *base, long sb, long sl, const ScanPlace<W> &at, long t0)
+{
+    return (const char *)base + (at.b * sb + t0 * sl + at.first) * (long)sizeof(T);
+}
+template <class T, class W>
+__device__ __forceinline__ const char *bc_base(const void *base, long sb, long sl, const ScanPlace<W> &at, long t0, int N)
+{
+    return (const char *)base + (at.b * sb + t0 * sl + (long)at.g * N) * (long)sizeof(T);
+}
+
 template <class T, class W, bool WIDE>
-struct TileRows {
-    Raw<T, W::VE, WIDE> r[W::P];
+__device__ __forceinline__ void store_row(char *base, uint32_t offset, const Pack<T, W::VE> &v, int have)
+{
+    store_pack<WIDE, T, W::VE>(reinterpret_cast<T *>(base + offset), v, have);
+}
 
-    // the element's place from the workgroup's first channel of the tile's first token; below 2^32 bytes (seq_api.cpp bounds the strides)
-    static __device__ __forceinline__ uint32_t offset(const ScanPlace<W> &at, int i, long sl, int last)
-    {
-        const int t = min(at.tok + i * W::TP, last), c = at.ch0 < at.have ? at.c0 - at.first + at.ch0 : 0;
-        return ((uint32_t)t * (uint32_t)sl + (uint32_t)c) * (uint32_t)sizeof(T);
-    }
-    static __device__ __forceinline__ const char *row(const void *base, long sb, long sl, const ScanPlace<W> &at, int t0)
-    {
-        return (const char *)base + (at.b * sb + t0 * sl + at.first) * (long)sizeof(T);
-    }
-    __device__ __forceinline__ void load(const void *base, long sb, long sl, const ScanPlace<W> &at, int t0, int n)
-    {
-#pragma unroll
-        for (int i = 0; i < W::P; ++i) r[i].load(row(base, sb, sl, at, t0), offset(at, i, sl, n - 1 - t0), at.have - at.ch0);
-    }
-    // pack i of an output; have: of its elements, 0 for a token that is not there
-    static __device__ __forceinline__ void store(void *base, long sb, long sl, const ScanPlace<W> &at, int t0, int i, const Pack<T, W::VE> &v, int have)
-    {
-        store_pack<WIDE, T, W::VE>((T *)(const_cast<char *>(row(base, sb, sl, at, t0)) + offset(at, i, sl, kTile)), v, have);
-    }
-};
-
-// The same of Bm and Cm: the tile's 16 rows of NP states of one, then of the other; in packs of 4 or one by one.  States that are not there are 0.
+// A tile's Bm and Cm, 16 rows of NP states of one, then of the other; in packs of 4 or one by one.  States that are not there are 0.
 template <class T, class W, bool WIDE>
 struct TileStates {
     static constexpr int V = WIDE ? 4 : 1, P = (W::BE + V - 1) / V, ROWS = kTile * W::NP;
+    static constexpr bool WHOLE = ROWS % (64 * V) == 0;      // a pack of all lanes is of one tensor
     Raw<T, V, WIDE> r[P];
+    uint32_t offset[P];
 
     static __device__ __forceinline__ int index(int i) { return (i * 64 + (int)threadIdx.x % 64) * V; }
+    static __device__ __forceinline__ bool second(int i) { return WHOLE ? i * 64 * V >= ROWS : index(i) >= ROWS; }
 
-    __device__ __forceinline__ void load(const ScanParams &p, const ScanPlace<W> &at, int t0, int n)
+    __device__ __forceinline__ void place(const ScanParams &p, int last)
     {
-        const char *bm = (const char *)p.in.Bm + (at.b * p.d.Bm_b + t0 * p.d.Bm_l + (long)at.g * p.d.N) * (long)sizeof(T);
-        const char *cm = (const char *)p.in.Cm + (at.b * p.d.Cm_b + t0 * p.d.Cm_l + (long)at.g * p.d.N) * (long)sizeof(T);
 #pragma unroll
         for (int i = 0; i < P; ++i) {
-            const int e = index(i), k = e % W::NP, t = min(e / W::NP % kTile, n - 1 - t0);
-            const bool there = k < p.d.N;
-            // a pack of all lanes is of one tensor, but for the single one of few states
-            const bool whole = ROWS % (64 * V) == 0, second = whole ? i * 64 * V >= ROWS : e >= ROWS;
-            const uint32_t offset = ((uint32_t)t * (uint32_t)(second ? p.d.Cm_l : p.d.Bm_l) + (there ? (uint32_t)k : 0u)) * (uint32_t)sizeof(T);
-            if (whole) r[i].load(second ? cm : bm, offset, V);
-            else if (second) r[i].load(cm, offset, V);
-            else r[i].load(bm, offset, V);
+            const int e = index(i), k = e % W::NP, t = min(e / W::NP % kTile, last);
+            offset[i] = ((uint32_t)t * (uint32_t)(second(i) ? p.d.Cm_l : p.d.Bm_l) + (k < p.d.N ? (uint32_t)k : 0u)) * (uint32_t)sizeof(T);
+        }
+    }
+
+    __device__ __forceinline__ void load(const char *bm, const char *cm)
+    {
+#pragma unroll
+        for (int i = 0; i < P; ++i) {
+            if (WHOLE) r[i].load(second(i) ? cm : bm, offset[i], V);
+            else if (second(i)) r[i].load(cm, offset[i], V);
+            else r[i].load(bm, offset[i], V);
         }
     }
 
@@ -199,7 +203,7 @@ struct TileStates {
             const int e = index(i);
             Pack<float, V> f;
 #pragma unroll
-            for (int j = 0; j < V; ++j) f.v[j] = e % W::NP < states ? r[i].get(j) : 0.f;
+            for (int j = 0; j < V; ++j) f.v[j] = W::NP == V || e % W::NP < states ? r[i].get(j) : 0.f;
             if (2 * ROWS % (64 * V) == 0 || e < 2 * ROWS) *reinterpret_cast<Pack<float, V> *>(lds + e) = f;
         }
     }

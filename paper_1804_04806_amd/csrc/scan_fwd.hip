@@ -79,48 +79,67 @@ __global__ __launch_bounds__(64 * kWaves, 2) void scan_fwd_kernel(ScanParams p, 
             skip[i] = have && p.in.skip ? p.in.skip[at.c0 + at.ch0 + i] : 0.f;
         }
 
-        TileRows<T, W, WIDE> u, dt, z;
+        const long t_first = (long)tile0 * kTile, e = sizeof(T);
+        const char *u_at = row_base<T>(p.in.u, d.u_b, d.u_l, at, t_first), *dt_at = row_base<T>(p.in.dt, d.dt_b, d.dt_l, at, t_first);
+        const char *z_at = row_base<T>(p.in.z, d.z_b, d.z_l, at, t_first);
+        const char *bm_at = bc_base<T>(p.in.Bm, d.Bm_b, d.Bm_l, at, t_first, d.N), *cm_at = bc_base<T>(p.in.Cm, d.Cm_b, d.Cm_l, at, t_first, d.N);
+        char *y_at = const_cast<char *>(row_base<T>(p.y, d.y_b, d.y_l, at, t_first));
+        float *saved_at = p.saved + (((long)at.b * p.tiles + tile0) * (kTile / kKeep) * d.D + at.first) * d.N;
+        const uint32_t state_off = (uint32_t)(at.c0 - at.first + at.c) * d.N + at.n0, y_off = row_offset<T>(at, d.y_l, kTile);
+        Raw<T, W::VE, WIDE> u, dt, z;
         TileStates<T, W, WIDE> bc;
-        auto load = [&](int tile) {
-            const int t0 = tile * kTile;
-            if (t0 >= n) return;
-            u.load(p.in.u, d.u_b, d.u_l, at, t0, n);
-            dt.load(p.in.dt, d.dt_b, d.dt_l, at, t0, n);
-            if (!STATE_ONLY && GATE) z.load(p.in.z, d.z_b, d.z_l, at, t0, n);
-            bc.load(p, at, t0, n);
+        uint32_t u_off, dt_off, z_off;
+        auto place = [&](int last) {
+            u_off = row_offset<T>(at, d.u_l, last);
+            dt_off = row_offset<T>(at, d.dt_l, last);
+            if (GATE) z_off = row_offset<T>(at, d.z_l, last);
+            bc.place(p, last);
         };
-        auto keep = [&](int tile, int part) {
-            store_states<WIDE>(p.saved + ((((long)at.b * p.tiles + tile) * (kTile / kKeep) + part) * d.D + ch) * d.N + at.n0, h, at.haven);
+        place(kTile);
+        auto load = [&](int tile) {      // and on to the next tile
+            const int left = n - tile * kTile;
+            if (left <= 0) return;
+            if (left < kTile) place(left - 1);
+            u.load(u_at, u_off, at.have - at.ch0);
+            dt.load(dt_at, dt_off, at.have - at.ch0);
+            if (GATE) z.load(z_at, z_off, at.have - at.ch0);
+            bc.load(bm_at, cm_at);
+            u_at += kTile * e * d.u_l;
+            dt_at += kTile * e * d.dt_l;
+            if (GATE) z_at += kTile * e * d.z_l;
+            bm_at += kTile * e * d.Bm_l;
+            cm_at += kTile * e * d.Cm_l;
         };
         load(tile0);
         for (int tile = tile0; tile < tile1; ++tile) {
-            const int t0 = tile * kTile;
-            float ut[W::P][W::VE], zt[W::P][W::VE];
-            if (t0 < n) {
+            const int left = n - tile * kTile;
+            const bool there = at.tok < left;
+            float ut[W::VE], zt[W::VE];
+            if (left > 0) {
                 bc.stage(bm, d.N);
 #pragma unroll
-                for (int i = 0; i < W::P; ++i) {
-                    const int t = i * W::TP + at.tok;
-#pragma unroll
-                    for (int e = 0; e < W::VE; ++e) {
-                        ut[i][e] = u.r[i].get(e);
-                        float s = dt.r[i].get(e) + bias[e];
-                        const float soft = softplus<T>(s);
-                        s = d.softplus ? soft : s;
-                        s = t0 + t < n ? s : 0.f;     // padding: the state stays
-                        step[t * W::CW + at.ch0 + e] = make_float2(s, t0 + t < n ? s * ut[i][e] : 0.f);
-                        if (!STATE_ONLY && GATE) {
-                            const float v = z.r[i].get(e);
-                            zt[i][e] = v * sigmoid(v);
-                        }
+                for (int i = 0; i < W::VE; ++i) {
+                    ut[i] = u.get(i);
+                    float s = dt.get(i) + bias[i];
+                    const float soft = softplus<T>(s);
+                    s = d.softplus ? soft : s;
+                    s = there ? s : 0.f;     // padding: the state stays
+                    step[at.tok * W::CW + at.ch0 + i] = make_float2(s, there ? s * ut[i] : 0.f);
+                    if (GATE) {
+                        const float v = z.get(i);
+                        zt[i] = v * sigmoid(v);
                     }
                 }
                 if (tile + 1 < tile1) load(tile + 1);
                 wave_lds_order();
-                if (!STATE_ONLY && p.saved) keep(tile, 0);
+                auto keep = [&]() {
+                    store_states<WIDE>(saved_at + state_off, h, at.haven);
+                    saved_at += (long)d.D * d.N;
+                };
+                if (!STATE_ONLY && p.saved) keep();
                 float kept = 0.f;
-                // two tokens' values are on their way from LDS while the two before them are computed: left to itself the compiler reads them
-                // just before their use, and a wave that has its SIMD to itself waits for each
+                // the next tokens' values are on their way from LDS while these are computed: left to itself the compiler reads them just
+                // before their use, and a wave that has its SIMD to itself waits for each
                 Ahead now, next;
                 now.load(step, bm, cm, at, 0);
 #pragma unroll
@@ -141,29 +160,26 @@ __global__ __launch_bounds__(64 * kWaves, 2) void scan_fwd_kernel(ScanParams p, 
                     if (STATE_ONLY) {
                         steps += s.x;
                     } else {
-                        if (p.saved && t % kKeep == kKeep - 1 && t + 1 < kTile) keep(tile, (t + 1) / kKeep);
+                        if (p.saved && t % kKeep == kKeep - 1 && t + 1 < kTile) keep();
                         y = sum_lanes<LPC>(y);
-                        kept = LPC == 1 || at.q == t % LPC ? y : kept;      // each lane of a channel keeps one token in LPC
+                        kept = at.q == t % LPC ? y : kept;      // each lane of a channel keeps one token in LPC
                         if (t % LPC == LPC - 1) ys[(t - LPC + 1 + at.q) * W::CW + at.c] = kept;
                     }
                 }
                 wave_lds_order();
             }
             if (!STATE_ONLY) {
+                Pack<T, W::VE> out;
+                float yt[W::VE];
+                lds_row(yt, ys + at.tok * W::CW + at.ch0);
 #pragma unroll
-                for (int i = 0; i < W::P; ++i) {
-                    const int t = i * W::TP + at.tok;
-                    Pack<T, W::VE> out;
-                    float yt[W::VE];
-                    lds_row(yt, ys + t * W::CW + at.ch0);
-#pragma unroll
-                    for (int e = 0; e < W::VE; ++e) {
-                        float y = fmaf(skip[e], ut[i][e], yt[e]);
-                        if (GATE) y *= zt[i][e];
-                        out.v[e] = from_f<T>(t0 + t < n ? y : 0.f);
-                    }
-                    TileRows<T, W, WIDE>::store(p.y, d.y_b, d.y_l, at, t0, i, out, t0 + t < d.L ? at.have - at.ch0 : 0);
+                for (int i = 0; i < W::VE; ++i) {
+                    float y = fmaf(skip[i], ut[i], yt[i]);
+                    if (GATE) y *= zt[i];
+                    out.v[i] = from_f<T>(there ? y : 0.f);
                 }
+                store_row<T, W, WIDE>(y_at, y_off, out, at.tok < d.L - tile * kTile ? at.have - at.ch0 : 0);
+                y_at += kTile * e * d.y_l;
                 wave_lds_order();
             }
         }
