@@ -104,39 +104,6 @@ __device__ __forceinline__ void store_states(float *at, const float (&h)[N], int
     store_pack<WIDE, float, N>(at, r, haven);
 }
 
-// N elements as they come from memory, in words (WIDE: one load, all of them; otherwise a word each, the first `have` of them): a lane's prefetched
-// values stay as they are until they are used.  As elements of 16 bits the compiler takes them apart, and waits for them, right behind the load.
-template <class T, int N, bool WIDE>
-struct Raw {
-    static constexpr bool PACKED = WIDE && N * sizeof(T) % 4 == 0;
-    static constexpr int WORDS = PACKED ? N * (int)sizeof(T) / 4 : N;
-    uint32_t w[WORDS];
-
-    __device__ __forceinline__ void load(const char *base, uint32_t offset, int have)
-    {
-        if (PACKED) {
-            typedef Pack<uint32_t, WORDS> Words;
-            const Words r = *reinterpret_cast<const Words *>(base + offset);
-#pragma unroll
-            for (int i = 0; i < WORDS; ++i) w[i] = r.v[i];
-        } else {
-#pragma unroll
-            for (int i = 0; i < WORDS; ++i) {
-                w[i] = 0;
-                if (!WIDE && i >= have) continue;
-                if (sizeof(T) == 4) w[i] = *reinterpret_cast<const uint32_t *>(base + offset + 4 * i);
-                else w[i] = *reinterpret_cast<const uint16_t *>(base + offset + 2 * i);
-            }
-        }
-    }
-    __device__ __forceinline__ float get(int i) const
-    {
-        if (sizeof(T) == 4) return __builtin_bit_cast(float, w[i]);
-        if (!PACKED) return __builtin_bit_cast(float, w[i % WORDS] << 16);
-        return __builtin_bit_cast(float, i % 2 ? w[i / 2 % WORDS] & 0xFFFF0000u : w[i / 2 % WORDS] << 16);
-    }
-};
-
 // Tokens behind the sequence's last repeat it and channels that are not there repeat the workgroup's first: what is loaded of them is masked where it
 // is used.  Offsets of a tile's elements from its first token and the workgroup's first channel are below 2^32 bytes (seq_api.cpp bounds the strides).
 template <class T, class W>

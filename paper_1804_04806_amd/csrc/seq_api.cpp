@@ -96,6 +96,13 @@ bool scan_ok(const ucd_scan_t *in, ucd_scan_t &d)
            fill_strides(d.Bm_b, d.Bm_l, d.B, d.L, GN) && fill_strides(d.Cm_b, d.Cm_l, d.B, d.L, GN);
 }
 
+// Workgroups of the convolution's launches, 32 channels by 4 runs of 8 tokens each at least: their kernels count them, and runs, in 32 bits.
+bool conv_countable(const ucd_causal_conv_t &d)
+{
+    const double runs = (double)d.B * (d.L / 8 + 1);
+    return runs < 1u << 31 && (d.D / 32 + 1.) * (runs / 4 + 1) < 1u << 31;
+}
+
 // No token at all: tensors of no elements have no address.
 bool empty(int B, int L) { return B == 0 || L == 0; }
 
@@ -179,6 +186,7 @@ int ucd_causal_conv_fwd(const ucd_causal_conv_t *conv, const void *x, const void
         if (!aligned(x, d.dtype) || !aligned(w, d.dtype) || !aligned(y, d.dtype) || !aligned(state_in, d.dtype) ||
             !aligned(state_out, d.dtype) || !aligned4(bias) || !aligned4(lengths) || !aligned4(slots))
             return UCD_E_INVALID;
+        if (!conv_countable(d)) return UCD_E_UNSUPPORTED;
         if (d.B == 0) return UCD_OK;
         CausalConvArgs a{};
         a.x = x; a.w = w; a.bias = bias; a.lengths = lengths; a.slots = slots;
@@ -203,6 +211,7 @@ int ucd_causal_conv_bwd(const ucd_causal_conv_t *conv, const void *x, const void
             return UCD_E_INVALID;
         const int rc = ws_status(causal_conv_ws_bytes(d), ws, ws_bytes);
         if (rc != UCD_OK) return rc;
+        if (!conv_countable(d)) return UCD_E_UNSUPPORTED;
         CausalConvArgs a{};
         a.x = x; a.w = w; a.bias = bias; a.lengths = lengths; a.state_in = state_in; a.dy = dy; a.dstate_out = dstate_out;
         a.dx = dx; a.dw = dw; a.dbias = dbias; a.dstate_in = dstate_in;
@@ -222,6 +231,7 @@ int ucd_causal_conv_step(const ucd_causal_conv_t *conv, const void *x, const voi
         if (!aligned(x, d.dtype) || !aligned(w, d.dtype) || !aligned(y, d.dtype) || !aligned(state, d.dtype) || !aligned4(bias) ||
             !aligned4(slots))
             return UCD_E_INVALID;
+        if (!conv_countable(d)) return UCD_E_UNSUPPORTED;
         if (d.B == 0) return UCD_OK;
         CausalConvArgs a{};
         a.x = x; a.w = w; a.bias = bias; a.slots = slots; a.state_in = state; a.state_out = state; a.y = y;

@@ -50,6 +50,39 @@ __device__ __forceinline__ void store_pack(T *p, const Pack<T, N> &r, int have)
     }
 }
 
+// N elements as they come from memory, in words (WIDE: one load, all of them; otherwise a word each, the first `have` of them): a lane's prefetched
+// values stay as they are until they are used.  As elements of 16 bits the compiler takes them apart, and waits for them, right behind the load.
+template <class T, int N, bool WIDE>
+struct Raw {
+    static constexpr bool PACKED = WIDE && N * sizeof(T) % 4 == 0;
+    static constexpr int WORDS = PACKED ? N * (int)sizeof(T) / 4 : N;
+    uint32_t w[WORDS];
+
+    __device__ __forceinline__ void load(const char *base, uint32_t offset, int have)
+    {
+        if (PACKED) {
+            typedef Pack<uint32_t, WORDS> Words;
+            const Words r = *reinterpret_cast<const Words *>(base + offset);
+#pragma unroll
+            for (int i = 0; i < WORDS; ++i) w[i] = r.v[i];
+        } else {
+#pragma unroll
+            for (int i = 0; i < WORDS; ++i) {
+                w[i] = 0;
+                if (!WIDE && i >= have) continue;
+                if (sizeof(T) == 4) w[i] = *reinterpret_cast<const uint32_t *>(base + offset + 4 * i);
+                else w[i] = *reinterpret_cast<const uint16_t *>(base + offset + 2 * i);
+            }
+        }
+    }
+    __device__ __forceinline__ float get(int i) const
+    {
+        if (sizeof(T) == 4) return __builtin_bit_cast(float, w[i]);
+        if (!PACKED) return __builtin_bit_cast(float, w[i % WORDS] << 16);
+        return __builtin_bit_cast(float, i % 2 ? w[i / 2 % WORDS] & 0xFFFF0000u : w[i / 2 % WORDS] << 16);
+    }
+};
+
 // 2^v on the transcendental unit.
 __device__ __forceinline__ float exp2_fast(float v) { return __builtin_amdgcn_exp2f(v); }
 
@@ -94,6 +127,27 @@ __device__ __forceinline__ float sum_lanes(float v)
     if (N > 2) v += dpp<kXor2>(v);
     if (N > 4) v += dpp<kHalfMirror>(v);
     if (N > 8) v += dpp<kMirror>(v);
+    return v;
+}
+
+// Joins of partial sums: workgroups of 64 columns by 16 groups of rows.  The sum over `rows` rows of a column, rows of one group apart by 16, then
+// over the groups in their order; valid in the threads of the first group.
+constexpr int kJoinColumns = 64, kJoinThreads = 1024;
+
+__device__ __forceinline__ float join_rows(const float *part, long rows, long row_length, long column)
+{
+    constexpr int GROUPS = kJoinThreads / kJoinColumns;
+    __shared__ float lds[GROUPS][kJoinColumns];
+    const int x = threadIdx.x % kJoinColumns, group = threadIdx.x / kJoinColumns;
+    float v = 0.f;
+    if (column < row_length)
+#pragma unroll 8
+        for (long r = group; r < rows; r += GROUPS) v += part[r * row_length + column];
+    lds[group][x] = v;
+    __syncthreads();
+    v = lds[0][x];
+#pragma unroll
+    for (int g = 1; g < GROUPS; ++g) v += lds[g][x];
     return v;
 }
 
