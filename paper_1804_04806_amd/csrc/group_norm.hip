@@ -1,4 +1,14 @@
 // Group norm with an activation, channels last: Forward and Backward.
+//
+// Forward reads x and writes y, Backward reads x and dy and writes dx: memory bounds both, and what counts is to read each of them once.  So a group's
+// elements stay in registers between the sums and what is made of them, wherever a workgroup can hold them:
+//   rows   single positions with groups of up to a few packs per lane: a group to 1 to 64 neighbouring lanes, samples one after the other;
+//   slabs  a sample's positions by a strip of neighbouring groups, some hundred bytes of a row, in the registers of one workgroup;
+//   parts  what fits neither: a first kernel leaves sums of parts of a group, the second joins them and reads its part again.
+// Sums of Forward are means and squares around them (two passes over registers), joined as such: no difference of large numbers is taken.
+// The gradients of gamma and beta are sums over positions, which threads keep per channel while they walk, and a join over the workgroups.
+#include <algorithm>
+
 #include "seq.h"
 #include "seq_common.hpp"
 
@@ -6,148 +16,735 @@ namespace ucd {
 namespace {
 using namespace seq;
 
-// Sum over a workgroup of 256 threads, in every thread.
-__device__ float block_sum(float v, float *lds)
+constexpr int kSlabR = 8, kRowsR = 4;       // packs per thread at most
+constexpr int kMaxThreads = 1024;
+
+struct NormParams {
+    ucd_group_norm_t d;
+    const void *x, *dy;
+    const float *gamma, *beta;
+    const float *stats_in;
+    void *y, *dx;
+    float *stats;
+    float *part;                 // Backward: [part_rows][2][C], sums of dgamma and dbeta
+    float *sums;                 // parts: [N][chunks][G * cs][2]: Forward mean and squares around it, Backward the two sums of dx
+    float *dgamma, *dbeta;
+    bool add;
+    int cg, pgl, packs;          // channels of a group, packs of a group and of all
+    int part_rows;               // rows of workgroups that share out the samples
+    // rows
+    int lanes, gx, ry, columns;  // lanes to a group; groups and samples of a workgroup; workgroups for all groups
+    // slabs, parts
+    int px, py, strips;          // packs of a strip, positions of a pass; strips of a row
+    int gps, cs;                 // groups of a strip, or strips of a group
+    int chunk, chunks;           // positions of a part, parts of a sample's positions
+};
+
+template <class T, int VE>
+__device__ __forceinline__ void load_f(float (&v)[VE], const Raw<T, VE, true> &r)
 {
-    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
-    __syncthreads();
-    if (threadIdx.x % 64 == 0) lds[threadIdx.x / 64] = v;
-    __syncthreads();
-    return lds[0] + lds[1] + lds[2] + lds[3];
+#pragma unroll
+    for (int i = 0; i < VE; ++i) v[i] = r.get(i);
 }
 
-// One sample's group per workgroup: mean, variance around it, outputs.
-template <class T>
-__global__ __launch_bounds__(256) void norm_fwd_kernel(ucd_group_norm_t d, const T *x, const float *gamma, const float *beta,
-                                                       T *y, float *stats)
+template <int VE>
+__device__ __forceinline__ void load_weights(float (&v)[VE], const float *at)
 {
-    __shared__ float lds[4];
-    const int cg = d.C / d.G;
-    const long m = (long)d.S * cg, units = (long)d.N * d.G;
-    for (long unit = blockIdx.x; unit < units; unit += gridDim.x) {
-        const long n = unit / d.G;
-        const int c0 = (int)(unit % d.G) * cg;
-        const T *xs = x + n * d.x_n + c0;
-        float sum = 0.f;
-        for (long i = threadIdx.x; i < m; i += 256) sum += to_f(xs[i / cg * d.x_s + i % cg]);
-        const float mean = block_sum(sum, lds) / m;
-        float sq = 0.f;
-        for (long i = threadIdx.x; i < m; i += 256) {
-            const float v = to_f(xs[i / cg * d.x_s + i % cg]) - mean;
-            sq += v * v;
+#pragma unroll
+    for (int i = 0; i < VE; ++i) v[i] = at[i];
+}
+
+// y of one pack
+template <class T, int VE>
+__device__ __forceinline__ Pack<T, VE> norm_pack(const Raw<T, VE, true> &r, float mean, float rstd, const float (&gamma)[VE], const float (&beta)[VE], int act)
+{
+    Pack<T, VE> out;
+#pragma unroll
+    for (int i = 0; i < VE; ++i) {
+        float u = fmaf((r.get(i) - mean) * rstd, gamma[i], beta[i]);
+        if (act == UCD_ACT_SILU) u *= sigmoid(u);
+        out.v[i] = from_f<T>(u);
+    }
+    return out;
+}
+
+// xhat and du = dy act'(u) of one element
+__device__ __forceinline__ float norm_du(float xhat, float dy, float gamma, float beta, int act)
+{
+    if (act != UCD_ACT_SILU) return dy;
+    const float u = fmaf(xhat, gamma, beta), s = sigmoid(u);
+    return dy * s * fmaf(u, 1.f - s, 1.f);
+}
+
+template <class T, int VE>
+__device__ __forceinline__ Pack<T, VE> dx_pack(const Raw<T, VE, true> &x, const Raw<T, VE, true> &dy, float mean, float rstd, float m1, float m2,
+                                               const float (&gamma)[VE], const float (&beta)[VE], int act)
+{
+    Pack<T, VE> out;
+#pragma unroll
+    for (int i = 0; i < VE; ++i) {
+        const float xhat = (x.get(i) - mean) * rstd, g = norm_du(xhat, dy.get(i), gamma[i], beta[i], act) * gamma[i];
+        out.v[i] = from_f<T>(rstd * (g - m1 - xhat * m2));
+    }
+    return out;
+}
+
+__device__ __forceinline__ float sum_group(float v, int lanes)
+{
+    for (int o = lanes >> 1; o > 0; o >>= 1) v += __shfl_xor(v, o);
+    return v;
+}
+
+// ---- rows ----------------------------------------------------------------------------------------------------------------------------------------
+
+// A lane's group and its R packs of it.
+template <int VE, int R>
+struct RowPlace {
+    int lane, g, row;
+    bool active, have[R];
+    __device__ __forceinline__ RowPlace(const NormParams &p)
+    {
+        const int group = threadIdx.x / p.lanes;
+        lane = threadIdx.x % p.lanes;
+        g = blockIdx.x % p.columns * p.gx + group % p.gx;
+        row = group / p.gx;
+        active = row < p.ry && g < p.d.G;
+#pragma unroll
+        for (int i = 0; i < R; ++i) have[i] = active && lane + i * p.lanes < p.pgl;
+    }
+    __device__ __forceinline__ int channel(const NormParams &p, int i) const { return g * p.cg + (lane + i * p.lanes) * VE; }
+};
+
+template <class T, int VE, int R>
+__global__ __launch_bounds__(256) void norm_rows_fwd_kernel(NormParams p)
+{
+    const RowPlace<VE, R> at(p);
+    if (!at.active) return;      // with all lanes of its group
+    float gamma[R][VE], beta[R][VE];
+#pragma unroll
+    for (int i = 0; i < R; ++i)
+        if (at.have[i]) {
+            load_weights<VE>(gamma[i], p.gamma + at.channel(p, i));
+            load_weights<VE>(beta[i], p.beta + at.channel(p, i));
         }
-        const float rstd = 1.f / sqrtf(block_sum(sq, lds) / m + d.eps);
-        if (stats && threadIdx.x == 0) {
-            stats[unit] = mean;
-            stats[units + unit] = rstd;
-        }
-        for (long i = threadIdx.x; i < m; i += 256) {
-            const int c = (int)(i % cg);
-            float u = (to_f(xs[i / cg * d.x_s + c]) - mean) * rstd * gamma[c0 + c] + beta[c0 + c];
-            if (d.act == UCD_ACT_SILU) u *= sigmoid(u);
-            y[n * d.y_n + i / cg * d.y_s + c0 + c] = from_f<T>(u);
+    const int step = p.part_rows * p.ry;
+    Raw<T, VE, true> next[R], r[R];
+    auto load = [&](int n) {
+#pragma unroll
+        for (int i = 0; i < R; ++i)
+            if (at.have[i]) next[i].load((const char *)((const T *)p.x + n * p.d.x_n + at.channel(p, i)), 0, VE);
+    };
+    int n = blockIdx.x / p.columns * p.ry + at.row;
+    if (n < p.d.N) load(n);
+    for (; n < p.d.N; n += step) {
+#pragma unroll
+        for (int i = 0; i < R; ++i) r[i] = next[i];
+        if (step < p.d.N - n) load(n + step);
+        float sum = 0.f, sq = 0.f;
+#pragma unroll
+        for (int i = 0; i < R; ++i)
+#pragma unroll
+            for (int e = 0; e < VE; ++e) sum += at.have[i] ? r[i].get(e) : 0.f;
+        const float mean = sum_group(sum, p.lanes) / p.cg;
+#pragma unroll
+        for (int i = 0; i < R; ++i)
+#pragma unroll
+            for (int e = 0; e < VE; ++e) {
+                const float v = r[i].get(e) - mean;
+                sq += at.have[i] ? v * v : 0.f;
+            }
+        const float rstd = 1.f / sqrtf(sum_group(sq, p.lanes) / p.cg + p.d.eps);
+#pragma unroll
+        for (int i = 0; i < R; ++i)
+            if (at.have[i])
+                *reinterpret_cast<Pack<T, VE> *>((T *)p.y + n * p.d.y_n + at.channel(p, i)) = norm_pack<T, VE>(r[i], mean, rstd, gamma[i], beta[i], p.d.act);
+        if (p.stats && at.lane == 0) {
+            p.stats[(long)n * p.d.G + at.g] = mean;
+            p.stats[((long)p.d.N + n) * p.d.G + at.g] = rstd;
         }
     }
 }
 
-__device__ float act_grad(const ucd_group_norm_t &d, float u)
+template <class T, int VE, int R>
+__global__ __launch_bounds__(256) void norm_rows_bwd_kernel(NormParams p)
 {
-    if (d.act != UCD_ACT_SILU) return 1.f;
-    const float s = sigmoid(u);
-    return s * (1.f + u * (1.f - s));
+    __shared__ float lds[256];
+    const RowPlace<VE, R> at(p);
+    float gamma[R][VE], beta[R][VE], dg[R][VE] = {}, db[R][VE] = {};
+    const int step = p.part_rows * p.ry, part_row = blockIdx.x / p.columns;
+    if (at.active) {
+#pragma unroll
+        for (int i = 0; i < R; ++i)
+            if (at.have[i]) {
+                load_weights<VE>(gamma[i], p.gamma + at.channel(p, i));
+                load_weights<VE>(beta[i], p.beta + at.channel(p, i));
+            }
+        Raw<T, VE, true> xn[R], gn[R], x[R], dy[R];
+        float next_mean = 0.f, next_rstd = 0.f;
+        auto load = [&](int n) {
+#pragma unroll
+            for (int i = 0; i < R; ++i)
+                if (at.have[i]) {
+                    xn[i].load((const char *)((const T *)p.x + n * p.d.x_n + at.channel(p, i)), 0, VE);
+                    gn[i].load((const char *)((const T *)p.dy + n * p.d.y_n + at.channel(p, i)), 0, VE);
+                }
+            next_mean = p.stats_in[(long)n * p.d.G + at.g];
+            next_rstd = p.stats_in[((long)p.d.N + n) * p.d.G + at.g];
+        };
+        int n = part_row * p.ry + at.row;
+        if (n < p.d.N) load(n);
+        for (; n < p.d.N; n += step) {
+#pragma unroll
+            for (int i = 0; i < R; ++i) {
+                x[i] = xn[i];
+                dy[i] = gn[i];
+            }
+            const float mean = next_mean, rstd = next_rstd;
+            if (step < p.d.N - n) load(n + step);
+            float s1 = 0.f, s2 = 0.f;
+#pragma unroll
+            for (int i = 0; i < R; ++i) {
+                if (!at.have[i]) continue;
+#pragma unroll
+                for (int e = 0; e < VE; ++e) {
+                    const float xhat = (x[i].get(e) - mean) * rstd, du = norm_du(xhat, dy[i].get(e), gamma[i][e], beta[i][e], p.d.act);
+                    db[i][e] += du;
+                    dg[i][e] = fmaf(du, xhat, dg[i][e]);
+                    s1 = fmaf(du, gamma[i][e], s1);
+                    s2 = fmaf(du * gamma[i][e], xhat, s2);
+                }
+            }
+            s1 = sum_group(s1, p.lanes) / p.cg;
+            s2 = sum_group(s2, p.lanes) / p.cg;
+#pragma unroll
+            for (int i = 0; i < R; ++i)
+                if (at.have[i])
+                    *reinterpret_cast<Pack<T, VE> *>((T *)p.dx + n * p.d.x_n + at.channel(p, i)) =
+                        dx_pack<T, VE>(x[i], dy[i], mean, rstd, s1, s2, gamma[i], beta[i], p.d.act);
+        }
+    }
+    // over the samples side by side in the workgroup, in their order
+    const int apart = p.gx * p.lanes;
+#pragma unroll
+    for (int i = 0; i < R; ++i)
+#pragma unroll
+        for (int e = 0; e < VE; ++e)
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                float v = k ? db[i][e] : dg[i][e];
+                if (p.ry > 1) {
+                    __syncthreads();
+                    lds[threadIdx.x] = v;
+                    __syncthreads();
+                    if (at.row == 0)
+                        for (int r = 1; r < p.ry; ++r) v += lds[threadIdx.x + r * apart];
+                }
+                if (at.have[i] && at.row == 0) p.part[((long)part_row * 2 + k) * p.d.C + at.channel(p, i) + e] = v;
+            }
 }
 
-template <class T>
-__global__ __launch_bounds__(256) void norm_bwd_kernel(ucd_group_norm_t d, const T *x, const float *gamma, const float *beta,
-                                                       const float *stats, const T *dy, T *dx)
-{
-    __shared__ float lds[4];
-    const int cg = d.C / d.G;
-    const long m = (long)d.S * cg, units = (long)d.N * d.G;
-    for (long unit = blockIdx.x; unit < units; unit += gridDim.x) {
-        const long n = unit / d.G;
-        const int c0 = (int)(unit % d.G) * cg;
-        const T *xs = x + n * d.x_n + c0;
-        const T *dys = dy + n * d.y_n + c0;
-        const float mean = stats[unit], rstd = stats[units + unit];
-        float s1 = 0.f, s2 = 0.f;
-        for (long i = threadIdx.x; i < m; i += 256) {
-            const int c = (int)(i % cg);
-            const float xhat = (to_f(xs[i / cg * d.x_s + c]) - mean) * rstd;
-            const float g = gamma[c0 + c] * to_f(dys[i / cg * d.y_s + c]) * act_grad(d, xhat * gamma[c0 + c] + beta[c0 + c]);
-            s1 += g;
-            s2 += g * xhat;
+// ---- slabs and parts -----------------------------------------------------------------------------------------------------------------------------
+
+// A thread's pack of a strip and its positions.
+template <int VE>
+struct SlabPlace {
+    int strip, local, g, c0, ty;     // local: the group within the strip
+    bool active;
+    __device__ __forceinline__ SlabPlace(const NormParams &p, int strip_) : strip(strip_)
+    {
+        const int tx = threadIdx.x % p.px;
+        ty = threadIdx.x / p.px;
+        active = ty < p.py;
+        int pack;
+        if (p.cs > 1) {
+            const int k = strip % p.cs * p.px + tx;
+            g = strip / p.cs;
+            local = 0;
+            pack = g * p.pgl + k;
+            active = active && k < p.pgl;
+        } else {
+            pack = strip * p.px + tx;
+            local = tx / p.pgl;
+            g = strip * p.gps + local;
+            active = active && pack < p.packs;
         }
-        s1 = block_sum(s1, lds) / m;
-        s2 = block_sum(s2, lds) / m;
-        for (long i = threadIdx.x; i < m; i += 256) {
-            const int c = (int)(i % cg);
-            const float xhat = (to_f(xs[i / cg * d.x_s + c]) - mean) * rstd;
-            const float g = gamma[c0 + c] * to_f(dys[i / cg * d.y_s + c]) * act_grad(d, xhat * gamma[c0 + c] + beta[c0 + c]);
-            dx[n * d.x_n + i / cg * d.x_s + c0 + c] = from_f<T>(rstd * (g - s1 - xhat * s2));
+        c0 = pack * VE;
+    }
+};
+
+// Sums over a workgroup's threads of one group, for each of its groups; in every thread that of its own.
+__device__ __forceinline__ float2 sum_slab(const NormParams &p, float a, float b, bool active, int local)
+{
+    __shared__ float2 lds[kMaxThreads], res[kMaxThreads];
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, waves = blockDim.x / 64;
+    lds[threadIdx.x] = active ? make_float2(a, b) : make_float2(0.f, 0.f);
+    __syncthreads();
+    const int groups = p.cs > 1 ? 1 : p.gps, width = p.cs > 1 ? p.px : p.pgl, count = width * p.py;
+    for (int j = wave; j < groups; j += waves) {
+        float2 v = make_float2(0.f, 0.f);
+        for (int i = lane; i < count; i += 64) {
+            const float2 w = lds[i / width * p.px + j * width + i % width];
+            v.x += w.x;
+            v.y += w.y;
+        }
+        for (int o = 32; o > 0; o >>= 1) {
+            v.x += __shfl_xor(v.x, o);
+            v.y += __shfl_xor(v.y, o);
+        }
+        if (lane == 0) res[j] = v;
+    }
+    __syncthreads();
+    return res[active ? local : 0];
+}
+
+template <class T, int VE, int R>
+struct Slab {
+    Raw<T, VE, true> r[R];
+    // The words as they are: floats made of them before are made again behind this, instead of being kept beside them from one pass to the next.
+    __device__ __forceinline__ void fresh()
+    {
+#pragma unroll
+        for (int i = 0; i < R; ++i)
+#pragma unroll
+            for (int k = 0; k < Raw<T, VE, true>::WORDS; ++k) asm volatile("" : "+v"(r[i].w[k]));
+    }
+    __device__ __forceinline__ void load(const void *base, long sn, long ss, const NormParams &p, const SlabPlace<VE> &at, int n, int s0, int count)
+    {
+        const T *from = (const T *)base + n * sn + at.c0;
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+            const int s = at.ty + i * p.py;
+            if (at.active && s < count) r[i].load((const char *)(from + (long)(s0 + s) * ss), 0, VE);
+        }
+    }
+};
+
+// A part's mean and the squares around it, in every thread of its group.
+template <class T, int VE, int R>
+__device__ __forceinline__ float2 slab_moments(const NormParams &p, Slab<T, VE, R> &x, const SlabPlace<VE> &at, int count, float elements)
+{
+    float sum = 0.f, sq = 0.f;
+#pragma unroll
+    for (int i = 0; i < R; ++i)
+        if (at.ty + i * p.py < count)
+#pragma unroll
+            for (int e = 0; e < VE; ++e) sum += x.r[i].get(e);
+    const float mean = sum_slab(p, sum, 0.f, at.active, at.local).x / elements;
+    x.fresh();
+#pragma unroll
+    for (int i = 0; i < R; ++i)
+        if (at.ty + i * p.py < count)
+#pragma unroll
+            for (int e = 0; e < VE; ++e) {
+                const float v = x.r[i].get(e) - mean;
+                sq = fmaf(v, v, sq);
+            }
+    x.fresh();
+    return make_float2(mean, sum_slab(p, sq, 0.f, at.active, at.local).x);
+}
+
+template <class T, int VE, int R>
+__device__ __forceinline__ void slab_store_y(const NormParams &p, const Slab<T, VE, R> &x, const SlabPlace<VE> &at, int n, int s0, int count, float mean,
+                                             float rstd, const float (&gamma)[VE], const float (&beta)[VE])
+{
+    T *y = (T *)p.y + n * p.d.y_n + at.c0;
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        const int s = at.ty + i * p.py;
+        if (at.active && s < count) *reinterpret_cast<Pack<T, VE> *>(y + (long)(s0 + s) * p.d.y_s) = norm_pack<T, VE>(x.r[i], mean, rstd, gamma, beta, p.d.act);
+    }
+}
+
+// The first thread of each group of a workgroup.
+template <int VE>
+__device__ __forceinline__ bool leads(const NormParams &p, const SlabPlace<VE> &at)
+{
+    return at.active && at.ty == 0 && (p.cs > 1 ? threadIdx.x == 0 : threadIdx.x % p.px == at.local * p.pgl);
+}
+
+template <class T, int VE, int R>
+__global__ __launch_bounds__(kMaxThreads) void norm_slab_fwd_kernel(NormParams p)
+{
+    const SlabPlace<VE> at(p, blockIdx.x % p.strips);
+    float gamma[VE] = {}, beta[VE] = {};
+    if (at.active) {
+        load_weights<VE>(gamma, p.gamma + at.c0);
+        load_weights<VE>(beta, p.beta + at.c0);
+    }
+    const float elements = (float)p.d.S * p.cg;
+    for (int n = blockIdx.x / p.strips; n < p.d.N; n += p.part_rows) {
+        Slab<T, VE, R> x;
+        x.load(p.x, p.d.x_n, p.d.x_s, p, at, n, 0, p.d.S);
+        const float2 m = slab_moments<T, VE, R>(p, x, at, p.d.S, elements);
+        const float rstd = 1.f / sqrtf(m.y / elements + p.d.eps);
+        slab_store_y<T, VE, R>(p, x, at, n, 0, p.d.S, m.x, rstd, gamma, beta);
+        if (p.stats && leads<VE>(p, at)) {
+            p.stats[(long)n * p.d.G + at.g] = m.x;
+            p.stats[((long)p.d.N + n) * p.d.G + at.g] = rstd;
         }
     }
 }
 
-// One channel per workgroup.
-template <class T>
-__global__ __launch_bounds__(256) void norm_weights_kernel(ucd_group_norm_t d, const T *x, const float *gamma, const float *beta,
-                                                           const float *stats, const T *dy, float *dgamma, float *dbeta, bool add)
+// The two sums of dx over a part of a sample, and per-channel sums on top of dg, db.
+template <class T, int VE, int R>
+__device__ __forceinline__ float2 slab_grads(const NormParams &p, Slab<T, VE, R> &x, Slab<T, VE, R> &dy, const SlabPlace<VE> &at, int count,
+                                             float mean, float rstd, const float (&gamma)[VE], const float (&beta)[VE], float (&dg)[VE], float (&db)[VE])
 {
-    __shared__ float lds[4];
-    const int c = blockIdx.x, g = c / (d.C / d.G);
-    const long rows = (long)d.N * d.S, units = (long)d.N * d.G;
     float s1 = 0.f, s2 = 0.f;
-    for (long i = threadIdx.x; i < rows; i += 256) {
-        const long n = i / d.S, s = i % d.S;
-        const float xhat = (to_f(x[n * d.x_n + s * d.x_s + c]) - stats[n * d.G + g]) * stats[units + n * d.G + g];
-        const float du = to_f(dy[n * d.y_n + s * d.y_s + c]) * act_grad(d, xhat * gamma[c] + beta[c]);
-        s1 += du;
-        s2 += du * xhat;
-    }
-    s1 = block_sum(s1, lds);
-    s2 = block_sum(s2, lds);
-    if (threadIdx.x == 0) {
-        dbeta[c] = s1 + (add ? dbeta[c] : 0.f);
-        dgamma[c] = s2 + (add ? dgamma[c] : 0.f);
+    if (at.active)
+#pragma unroll
+        for (int i = 0; i < R; ++i)
+            if (at.ty + i * p.py < count)
+#pragma unroll
+                for (int e = 0; e < VE; ++e) {
+                    const float xhat = (x.r[i].get(e) - mean) * rstd, du = norm_du(xhat, dy.r[i].get(e), gamma[e], beta[e], p.d.act);
+                    db[e] += du;
+                    dg[e] = fmaf(du, xhat, dg[e]);
+                    s1 = fmaf(du, gamma[e], s1);
+                    s2 = fmaf(du * gamma[e], xhat, s2);
+                }
+    x.fresh();
+    dy.fresh();
+    return sum_slab(p, s1, s2, at.active, at.local);
+}
+
+template <class T, int VE, int R>
+__device__ __forceinline__ void slab_store_dx(const NormParams &p, const Slab<T, VE, R> &x, const Slab<T, VE, R> &dy, const SlabPlace<VE> &at, int n, int s0,
+                                              int count, float mean, float rstd, float m1, float m2, const float (&gamma)[VE], const float (&beta)[VE])
+{
+    T *dx = (T *)p.dx + n * p.d.x_n + at.c0;
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        const int s = at.ty + i * p.py;
+        if (at.active && s < count)
+            *reinterpret_cast<Pack<T, VE> *>(dx + (long)(s0 + s) * p.d.x_s) = dx_pack<T, VE>(x.r[i], dy.r[i], mean, rstd, m1, m2, gamma, beta, p.d.act);
     }
 }
 
-unsigned blocks_of(long units) { return (unsigned)(units < (1 << 20) ? units : (1 << 20)); }
+// A row of the partial sums of dgamma and dbeta: over the threads of a channel, in a fixed order; within a wave first, where its lanes hold whole rows of
+// the strip.
+template <int VE>
+__device__ __forceinline__ void slab_store_part(const NormParams &p, const SlabPlace<VE> &at, long part_row, float (&dg)[VE], float (&db)[VE])
+{
+    __shared__ float2 lds[VE][kMaxThreads];
+    const bool in_wave = 64 % p.px == 0;
+    if (in_wave)
+#pragma unroll
+        for (int e = 0; e < VE; ++e)
+            for (int o = p.px; o < 64; o *= 2) {
+                dg[e] += __shfl_xor(dg[e], o);
+                db[e] += __shfl_xor(db[e], o);
+            }
+    const int lane = threadIdx.x % 64, slot = in_wave ? (int)threadIdx.x / 64 * p.px + lane : (int)threadIdx.x;
+    if (!in_wave || lane < p.px)
+#pragma unroll
+        for (int e = 0; e < VE; ++e) lds[e][slot] = make_float2(dg[e], db[e]);
+    __syncthreads();
+    const int rows = in_wave ? (int)blockDim.x / 64 : p.py, first = p.cs > 1 ? at.strip / p.cs * p.pgl + at.strip % p.cs * p.px : at.strip * p.px;
+    const int end = p.cs > 1 ? (at.strip / p.cs + 1) * p.pgl : p.packs;
+    for (int i = threadIdx.x; i < p.px * VE; i += blockDim.x) {
+        const int pack = i / VE, e = i % VE;
+        if (first + pack >= end) continue;
+        float2 v = lds[e][pack];
+        for (int r = 1; r < rows; ++r) {
+            const float2 w = lds[e][r * p.px + pack];
+            v.x += w.x;
+            v.y += w.y;
+        }
+        const long c = (long)(first + pack) * VE + e;
+        p.part[part_row * 2 * p.d.C + c] = v.x;
+        p.part[(part_row * 2 + 1) * p.d.C + c] = v.y;
+    }
+    __syncthreads();
+}
+
+template <class T, int VE, int R>
+__global__ __launch_bounds__(kMaxThreads) void norm_slab_bwd_kernel(NormParams p)
+{
+    const SlabPlace<VE> at(p, blockIdx.x % p.strips);
+    float gamma[VE] = {}, beta[VE] = {}, dg[VE] = {}, db[VE] = {};
+    if (at.active) {
+        load_weights<VE>(gamma, p.gamma + at.c0);
+        load_weights<VE>(beta, p.beta + at.c0);
+    }
+    const float elements = (float)p.d.S * p.cg;
+    const int part_row = blockIdx.x / p.strips;
+    for (int n = part_row; n < p.d.N; n += p.part_rows) {
+        Slab<T, VE, R> x, dy;
+        x.load(p.x, p.d.x_n, p.d.x_s, p, at, n, 0, p.d.S);
+        dy.load(p.dy, p.d.y_n, p.d.y_s, p, at, n, 0, p.d.S);
+        const float mean = at.active ? p.stats_in[(long)n * p.d.G + at.g] : 0.f, rstd = at.active ? p.stats_in[((long)p.d.N + n) * p.d.G + at.g] : 0.f;
+        const float2 s = slab_grads<T, VE, R>(p, x, dy, at, p.d.S, mean, rstd, gamma, beta, dg, db);
+        slab_store_dx<T, VE, R>(p, x, dy, at, n, 0, p.d.S, mean, rstd, s.x / elements, s.y / elements, gamma, beta);
+    }
+    slab_store_part<VE>(p, at, part_row, dg, db);
+}
+
+// Parts, first kernel: moments, or the sums of dx and those of dgamma and dbeta, of one part.
+template <class T, int VE, int R, bool BACKWARD>
+__global__ __launch_bounds__(kMaxThreads) void norm_part_kernel(NormParams p, unsigned units)
+{
+    for (unsigned unit = blockIdx.x; unit < units; unit += gridDim.x) {
+        const SlabPlace<VE> at(p, unit % p.strips);
+        const unsigned row = unit / p.strips;                       // sample and chunk
+        const int n = row / p.chunks, s0 = row % p.chunks * p.chunk, count = min(p.chunk, p.d.S - s0);
+        Slab<T, VE, R> x, dy;
+        x.load(p.x, p.d.x_n, p.d.x_s, p, at, n, s0, count);
+        float2 out;
+        if (BACKWARD) {
+            dy.load(p.dy, p.d.y_n, p.d.y_s, p, at, n, s0, count);
+            float gamma[VE] = {}, beta[VE] = {}, dg[VE] = {}, db[VE] = {}, mean = 0.f, rstd = 0.f;
+            if (at.active) {
+                load_weights<VE>(gamma, p.gamma + at.c0);
+                load_weights<VE>(beta, p.beta + at.c0);
+                mean = p.stats_in[(long)n * p.d.G + at.g];
+                rstd = p.stats_in[((long)p.d.N + n) * p.d.G + at.g];
+            }
+            out = slab_grads<T, VE, R>(p, x, dy, at, count, mean, rstd, gamma, beta, dg, db);
+            slab_store_part<VE>(p, at, row, dg, db);
+        } else {
+            const int width = p.cs > 1 ? min(p.px, p.pgl - (int)(unit % p.strips) % p.cs * p.px) : p.pgl;
+            out = slab_moments<T, VE, R>(p, x, at, count, (float)count * width * VE);
+        }
+        if (leads<VE>(p, at)) {
+            float *to = p.sums + 2 * ((long)row * p.d.G * p.cs + (p.cs > 1 ? at.strip : at.g));
+            to[0] = out.x;
+            to[1] = out.y;
+        }
+        __syncthreads();
+    }
+}
+
+// The parts of a group joined, by one wave: Forward the mean of the means, weighted by their elements, and all squares around it.
+template <int VE, bool BACKWARD>
+__device__ __forceinline__ float2 join_parts(const NormParams &p, int n, int g)
+{
+    const int lane = threadIdx.x % 64, parts = p.chunks * p.cs;
+    auto at = [&](int i) { return p.sums + 2 * (((long)n * p.chunks + i / p.cs) * p.d.G * p.cs + (long)g * p.cs + i % p.cs); };
+    auto elements = [&](int i) {
+        const int width = p.cs > 1 ? min(p.px, p.pgl - i % p.cs * p.px) : p.pgl;
+        return (float)min(p.chunk, p.d.S - i / p.cs * p.chunk) * width * VE;
+    };
+    const float all = (float)p.d.S * p.cg;
+    float2 v = make_float2(0.f, 0.f);
+    for (int i = lane; i < parts; i += 64) {
+        const float *s = at(i);
+        v.x += BACKWARD ? s[0] : s[0] * (elements(i) / all);
+        v.y += BACKWARD ? s[1] : 0.f;
+    }
+    for (int o = 32; o > 0; o >>= 1) {
+        v.x += __shfl_xor(v.x, o);
+        v.y += __shfl_xor(v.y, o);
+    }
+    if (BACKWARD) return make_float2(v.x / all, v.y / all);
+    for (int i = lane; i < parts; i += 64) {
+        const float *s = at(i), off = s[0] - v.x;
+        v.y += s[1] + off * off * elements(i);
+    }
+    for (int o = 32; o > 0; o >>= 1) v.y += __shfl_xor(v.y, o);
+    return make_float2(v.x, 1.f / sqrtf(v.y / all + p.d.eps));
+}
+
+// Parts, second kernel: y or dx of one part.
+template <class T, int VE, int R, bool BACKWARD>
+__global__ __launch_bounds__(kMaxThreads) void norm_apply_kernel(NormParams p, unsigned units)
+{
+    __shared__ float2 lds[kMaxThreads];
+    const int wave = threadIdx.x / 64, waves = blockDim.x / 64;
+    for (unsigned unit = blockIdx.x; unit < units; unit += gridDim.x) {
+        const SlabPlace<VE> at(p, unit % p.strips);
+        const unsigned row = unit / p.strips;
+        const int n = row / p.chunks, s0 = row % p.chunks * p.chunk, count = min(p.chunk, p.d.S - s0);
+        Slab<T, VE, R> x, dy;
+        x.load(p.x, p.d.x_n, p.d.x_s, p, at, n, s0, count);
+        if (BACKWARD) dy.load(p.dy, p.d.y_n, p.d.y_s, p, at, n, s0, count);
+        const int g0 = p.cs > 1 ? at.strip / p.cs : at.strip * p.gps, groups = p.cs > 1 ? 1 : min(p.gps, p.d.G - g0);
+        for (int j = wave; j < groups; j += waves) {
+            const float2 v = join_parts<VE, BACKWARD>(p, n, g0 + j);
+            if (threadIdx.x % 64 == 0) lds[j] = v;
+        }
+        __syncthreads();
+        const float2 m = lds[at.active ? at.local : 0];
+        if (at.active) {
+            float gamma[VE], beta[VE];
+            load_weights<VE>(gamma, p.gamma + at.c0);
+            load_weights<VE>(beta, p.beta + at.c0);
+            if (BACKWARD) {
+                const float mean = p.stats_in[(long)n * p.d.G + at.g], rstd = p.stats_in[((long)p.d.N + n) * p.d.G + at.g];
+                slab_store_dx<T, VE, R>(p, x, dy, at, n, s0, count, mean, rstd, m.x, m.y, gamma, beta);
+            } else {
+                slab_store_y<T, VE, R>(p, x, at, n, s0, count, m.x, m.y, gamma, beta);
+                if (p.stats && s0 == 0 && leads<VE>(p, at) && (p.cs == 1 || at.strip % p.cs == 0)) {
+                    p.stats[(long)n * p.d.G + at.g] = m.x;
+                    p.stats[((long)p.d.N + n) * p.d.G + at.g] = m.y;
+                }
+            }
+        }
+        __syncthreads();
+    }
+}
+
+__global__ __launch_bounds__(kJoinThreads) void norm_join_kernel(NormParams p)
+{
+    const long i = blockIdx.x * (long)kJoinColumns + threadIdx.x % kJoinColumns, row = 2l * p.d.C;
+    const float v = join_rows(p.part, p.part_rows, row, i);
+    if (i >= row || threadIdx.x >= kJoinColumns) return;
+    float *out = i < p.d.C ? p.dgamma + i : p.dbeta + (i - p.d.C);
+    *out = v + (p.add ? *out : 0.f);
+}
+
+// ---- which way, and how it is divided ------------------------------------------------------------------------------------------------------------
+
+enum Way { ROWS, SLABS, PARTS };
+
+int ceil_div(long a, long b) { return (int)((a + b - 1) / b); }
+
+// With packs of VE.
+Way divide(const ucd_group_norm_t &d, int VE, int dir, NormParams &p, int &threads, int &R)
+{
+    const int e = d.dtype == 1 ? 2 : 4;
+    p.d = d;
+    p.cg = d.C / d.G;
+    p.pgl = p.cg / VE;
+    p.packs = d.C / VE;
+    if (d.S == 1 && p.pgl <= 64 * kRowsR) {
+        R = p.pgl <= 64 ? 1 : kRowsR;
+        p.lanes = 1;
+        while (p.lanes * R < p.pgl) p.lanes *= 2;
+        threads = 256;
+        const int groups = 256 / p.lanes;
+        p.gx = std::min(d.G, groups);
+        p.ry = std::min(groups / p.gx, d.N);
+        p.columns = ceil_div(d.G, p.gx);
+        p.part_rows = std::max(1, std::min(ceil_div(d.N, p.ry), 2048 / p.columns));
+        return ROWS;
+    }
+    // a strip is as many groups as make 128 bytes of a row; or a workgroup's part of a group
+    p.cs = ceil_div(p.pgl, kMaxThreads);
+    p.gps = p.cs > 1 ? 1 : std::min({d.G, std::max(1, ceil_div(128, p.cg * e)), kMaxThreads / p.pgl});
+    p.px = p.cs > 1 ? kMaxThreads : p.gps * p.pgl;
+    p.strips = p.cs > 1 ? d.G * p.cs : ceil_div(d.G, p.gps);
+    const long packs = (long)d.S * p.px;
+    if (p.cs == 1 && packs <= (long)kMaxThreads / p.px * p.px * kSlabR) {
+        // few packs to a thread while there are threads
+        threads = 64;
+        while (threads < kMaxThreads && (threads < p.px || (long)ceil_div(d.S, threads / p.px) > (packs <= 4096 ? 2 : kSlabR))) threads *= 2;
+        R = ceil_div(d.S, threads / p.px) <= 2 ? 2 : kSlabR;
+        p.py = threads / p.px;
+        p.part_rows = std::max(1, std::min(d.N, 4096 / p.strips));
+        return SLABS;
+    }
+    threads = kMaxThreads;
+    R = kSlabR;
+    p.py = threads / p.px;
+    p.chunk = std::min(d.S, p.py * R);
+    p.chunks = ceil_div(d.S, p.chunk);
+    p.part_rows = d.N * p.chunks;
+    return PARTS;
+}
+
+size_t ws_bytes(const ucd_group_norm_t &d, int VE, int dir)
+{
+    NormParams p{};
+    int threads, R;
+    const Way way = divide(d, VE, dir, p, threads, R);
+    size_t n = dir == UCD_SEQ_BWD ? (size_t)8 * p.part_rows * d.C : 0;
+    if (way == PARTS) n += (size_t)8 * d.N * p.chunks * d.G * p.cs;
+    return n;
+}
+
+// packs that all tensors' rows and groups consist of
+int pack_of(const ucd_group_norm_t &d, const void *a, const void *b, const void *c)
+{
+    const int e = d.dtype == 1 ? 2 : 4;
+    for (int ve = 16 / e; ve > 1; ve /= 2) {
+        const uintptr_t bytes = ve * e, at = (uintptr_t)a | (uintptr_t)b | (uintptr_t)c;
+        if (d.C / d.G % ve == 0 && at % bytes == 0 && d.x_n % ve == 0 && d.x_s % ve == 0 && d.y_n % ve == 0 && d.y_s % ve == 0) return ve;
+    }
+    return 1;
+}
+
+template <class T, int VE, int R>
+void run(NormParams &p, Way way, int threads, bool backward, hipStream_t s)
+{
+    if (way == PARTS) {
+        const unsigned units = (unsigned)p.strips * p.part_rows, grid = std::min(units, 1u << 21);
+        if (backward) {
+            norm_part_kernel<T, VE, kSlabR, true><<<grid, threads, 0, s>>>(p, units);
+            norm_apply_kernel<T, VE, kSlabR, true><<<grid, threads, 0, s>>>(p, units);
+        } else {
+            norm_part_kernel<T, VE, kSlabR, false><<<grid, threads, 0, s>>>(p, units);
+            norm_apply_kernel<T, VE, kSlabR, false><<<grid, threads, 0, s>>>(p, units);
+        }
+    } else if (way == SLABS) {
+        if (backward) norm_slab_bwd_kernel<T, VE, R == 1 ? 2 : kSlabR><<<p.strips * p.part_rows, threads, 0, s>>>(p);
+        else norm_slab_fwd_kernel<T, VE, R == 1 ? 2 : kSlabR><<<p.strips * p.part_rows, threads, 0, s>>>(p);
+    } else {
+        if (backward) norm_rows_bwd_kernel<T, VE, R><<<p.columns * p.part_rows, threads, 0, s>>>(p);
+        else norm_rows_fwd_kernel<T, VE, R><<<p.columns * p.part_rows, threads, 0, s>>>(p);
+    }
+}
+
+template <class T, int VE>
+hipError_t launch(NormParams &p, int dir, bool backward, void *ws, hipStream_t s)
+{
+    const ucd_group_norm_t d = p.d;
+    int threads, R;
+    const Way way = divide(d, VE, dir, p, threads, R);
+    char *at = (char *)ws;
+    if (backward) {
+        p.part = (float *)at;
+        at += (size_t)8 * p.part_rows * d.C;
+    }
+    p.sums = (float *)at;
+    if (R <= 2) run<T, VE, 1>(p, way, threads, backward, s);
+    else run<T, VE, kRowsR>(p, way, threads, backward, s);
+    if (backward) norm_join_kernel<<<ceil_div(2l * d.C, kJoinColumns), kJoinThreads, 0, s>>>(p);
+    return hipGetLastError();
+}
+
+hipError_t dispatch(NormParams &p, int pack, int dir, void *ws, hipStream_t s)
+{
+    const bool backward = dir == UCD_SEQ_BWD;
+    if (p.d.dtype == 1) {
+        if (pack == 8) return launch<bf16_t, 8>(p, dir, backward, ws, s);
+        if (pack == 4) return launch<bf16_t, 4>(p, dir, backward, ws, s);
+        if (pack == 2) return launch<bf16_t, 2>(p, dir, backward, ws, s);
+        return launch<bf16_t, 1>(p, dir, backward, ws, s);
+    }
+    if (pack == 4) return launch<float, 4>(p, dir, backward, ws, s);
+    if (pack == 2) return launch<float, 2>(p, dir, backward, ws, s);
+    return launch<float, 1>(p, dir, backward, ws, s);
+}
 
 }  // namespace
 
-size_t group_norm_ws_bytes(const ucd_group_norm_t &, int) { return 0; }
-
-template <class T>
-static hipError_t fwd(const ucd_group_norm_t &d, const void *x, const float *gamma, const float *beta_w, void *y, float *stats,
-                      hipStream_t s)
+size_t group_norm_ws_bytes(const ucd_group_norm_t &d, int dir)
 {
-    norm_fwd_kernel<T><<<blocks_of((long)d.N * d.G), 256, 0, s>>>(d, (const T *)x, gamma, beta_w, (T *)y, stats);
-    return hipGetLastError();
-}
-
-template <class T>
-static hipError_t bwd(const ucd_group_norm_t &d, const void *x, const float *gamma, const float *beta_w, const float *stats,
-                      const void *dy, void *dx, float *dgamma, float *dbeta, bool add, hipStream_t s)
-{
-    norm_bwd_kernel<T><<<blocks_of((long)d.N * d.G), 256, 0, s>>>(d, (const T *)x, gamma, beta_w, stats, (const T *)dy, (T *)dx);
-    norm_weights_kernel<T><<<d.C, 256, 0, s>>>(d, (const T *)x, gamma, beta_w, stats, (const T *)dy, dgamma, dbeta, add);
-    return hipGetLastError();
+    // whichever packs the tensors' alignment allows
+    size_t most = 0;
+    for (int ve = d.dtype == 1 ? 8 : 4; ve >= 1; ve /= 2)
+        if (d.C / d.G % ve == 0) most = std::max(most, ws_bytes(d, ve, dir));
+    return most;
 }
 
 hipError_t group_norm_fwd(const ucd_group_norm_t &d, const void *x, const float *gamma, const float *beta_w, void *y,
-                          float *stats, void *, hipStream_t s)
+                          float *stats, void *ws, hipStream_t s)
 {
-    return d.dtype == 1 ? fwd<bf16_t>(d, x, gamma, beta_w, y, stats, s) : fwd<float>(d, x, gamma, beta_w, y, stats, s);
+    NormParams p{};
+    p.d = d;
+    p.x = x; p.gamma = gamma; p.beta = beta_w; p.y = y; p.stats = stats;
+    return dispatch(p, pack_of(d, x, y, nullptr), UCD_SEQ_FWD, ws, s);
 }
 
 hipError_t group_norm_bwd(const ucd_group_norm_t &d, const void *x, const float *gamma, const float *beta_w,
-                          const float *stats, const void *dy, void *dx, float *dgamma, float *dbeta, bool add, void *,
+                          const float *stats, const void *dy, void *dx, float *dgamma, float *dbeta, bool add, void *ws,
                           hipStream_t s)
 {
-    return d.dtype == 1 ? bwd<bf16_t>(d, x, gamma, beta_w, stats, dy, dx, dgamma, dbeta, add, s)
-                        : bwd<float>(d, x, gamma, beta_w, stats, dy, dx, dgamma, dbeta, add, s);
+    NormParams p{};
+    p.d = d;
+    p.x = x; p.gamma = gamma; p.beta = beta_w; p.stats_in = stats; p.dy = dy; p.dx = dx; p.dgamma = dgamma; p.dbeta = dbeta; p.add = add;
+    return dispatch(p, pack_of(d, x, dy, dx), UCD_SEQ_BWD, ws, s);
 }
 
 }  // namespace ucd
