@@ -13,26 +13,6 @@ namespace ucd {
 namespace {
 using namespace seq;
 
-// a = {a of the lower half of the wave, b of the lower half}, b = {a of the upper half, b of the upper half}
-__device__ __forceinline__ void swap_halves(float &a, float &b)
-{
-    const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, a), __builtin_bit_cast(unsigned, b), false, false);
-    const unsigned lo = r[0], hi = r[1];      // bit_cast of a vector's element takes its first
-    a = __builtin_bit_cast(float, lo);
-    b = __builtin_bit_cast(float, hi);
-}
-
-// the same of odd and even rows of 16 lanes
-__device__ __forceinline__ void swap_rows(float &a, float &b)
-{
-    const auto r = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(unsigned, a), __builtin_bit_cast(unsigned, b), false, false);
-    const unsigned lo = r[0], hi = r[1];      // bit_cast of a vector's element takes its first
-    a = __builtin_bit_cast(float, lo);
-    b = __builtin_bit_cast(float, hi);
-}
-
-constexpr int kRor8 = 0x128, kRor4 = 0x124;
-
 // Sums of two tokens' dBm and dCm over the wave's channels: v[token][kind][state], channels are the lane bits from LPC up.  Each exchange of halves
 // adds up two values at once; r[state] is then token (lane bit 5), kind (lane bit 4), in every lane of the row with that state quarter.
 template <class W>

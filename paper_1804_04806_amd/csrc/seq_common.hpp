@@ -118,6 +118,7 @@ __device__ __forceinline__ float dpp(float v)
     return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), CTRL, 0xF, 0xF, true));
 }
 constexpr int kXor1 = 0xB1, kXor2 = 0x4E, kHalfMirror = 0x141, kMirror = 0x140;   // quad_perm [1,0,3,2], [2,3,0,1]; row_half_mirror; row_mirror
+constexpr int kRor8 = 0x128, kRor4 = 0x124;                                       // row_ror
 
 // Sum over groups of N neighbouring lanes, N = 1, 2, 4, 8, 16, in every lane.
 template <int N>
@@ -127,6 +128,64 @@ __device__ __forceinline__ float sum_lanes(float v)
     if (N > 2) v += dpp<kXor2>(v);
     if (N > 4) v += dpp<kHalfMirror>(v);
     if (N > 8) v += dpp<kMirror>(v);
+    return v;
+}
+
+// a = {a of the lower half of the wave, b of the lower half}, b = {a of the upper half, b of the upper half}
+__device__ __forceinline__ void swap_halves(float &a, float &b)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, a), __builtin_bit_cast(unsigned, b), false, false);
+    const unsigned lo = r[0], hi = r[1];      // bit_cast of a vector's element takes its first
+    a = __builtin_bit_cast(float, lo);
+    b = __builtin_bit_cast(float, hi);
+}
+
+// the same of odd and even rows of 16 lanes
+__device__ __forceinline__ void swap_rows(float &a, float &b)
+{
+    const auto r = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(unsigned, a), __builtin_bit_cast(unsigned, b), false, false);
+    const unsigned lo = r[0], hi = r[1];      // bit_cast of a vector's element takes its first
+    a = __builtin_bit_cast(float, lo);
+    b = __builtin_bit_cast(float, hi);
+}
+
+// Sum over groups of `lanes` neighbouring lanes, a power of two up to the wave, in every lane.  All lanes of a wave take part.
+__device__ __forceinline__ float sum_group(float v, int lanes)
+{
+    if (lanes > 1) v += dpp<kXor1>(v);
+    if (lanes > 2) v += dpp<kXor2>(v);
+    if (lanes > 4) v += dpp<kHalfMirror>(v);
+    if (lanes > 8) v += dpp<kMirror>(v);
+    if (lanes > 16) {
+        float w = v;
+        swap_rows(v, w);
+        v += w;
+    }
+    if (lanes > 32) {
+        float w = v;
+        swap_halves(v, w);
+        v += w;
+    }
+    return v;
+}
+
+// Sum over the lanes that differ in the bits from `from` (a power of two) up, in every lane.
+__device__ __forceinline__ float sum_apart(float v, int from)
+{
+    if (from <= 32) {
+        float w = v;
+        swap_halves(v, w);
+        v += w;
+    }
+    if (from <= 16) {
+        float w = v;
+        swap_rows(v, w);
+        v += w;
+    }
+    if (from <= 8) v += dpp<kRor8>(v);
+    if (from <= 4) v += dpp<kRor4>(v);
+    if (from <= 2) v += dpp<kXor2>(v);
+    if (from <= 1) v += dpp<kXor1>(v);
     return v;
 }
 
