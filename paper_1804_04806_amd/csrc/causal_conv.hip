@@ -176,6 +176,40 @@ __global__ __launch_bounds__(256) void conv_fwd_kernel(ConvParams p, unsigned un
     }
 }
 
+// One token: a thread to VE channels of a sequence, few of them, so that single sequences fill some hundred workgroups too; all loads but the state's
+// place are under way at once.
+template <class T, int VE, int K, bool SILU>
+__global__ __launch_bounds__(256) void conv_step_kernel(ConvParams p)
+{
+    const unsigned pack = blockIdx.x * 256u + threadIdx.x;
+    if (pack >= p.packs) return;
+    const int c0 = (int)pack * VE;
+    float w[K][VE], bias[VE];
+    load_weights<T, VE, K>(w, bias, p, c0);
+    for (int b = blockIdx.y; b < p.d.B; b += gridDim.y) {
+        float x[VE], out[VE] = {};
+        load_channels<T, VE>(x, (const T *)p.a.x + b * p.d.x_b + c0);
+        const int slot = p.a.slots ? p.a.slots[b] : b;
+        if (!p.a.slots || (slot >= 0 && slot < p.d.n_slots)) {
+            T *state = (T *)p.a.state_out + (long)slot * (K - 1) * p.d.D + c0;
+            float before[K][VE];
+#pragma unroll
+            for (int k = 0; k < K - 1; ++k) load_channels<T, VE>(before[k], state + (long)k * p.d.D);
+#pragma unroll
+            for (int i = 0; i < VE; ++i) {
+                before[K - 1][i] = x[i];
+                float u = bias[i];
+#pragma unroll
+                for (int k = 0; k < K; ++k) u = fmaf(w[k][i], before[k][i], u);
+                out[i] = SILU ? u * sigmoid(u) : u;
+            }
+#pragma unroll
+            for (int k = 0; k < K - 1; ++k) store_channels<T, VE>(state + (long)k * p.d.D, before[k + 1]);
+        }
+        store_channels<T, VE>((T *)p.a.y + b * p.d.y_b + c0, out);
+    }
+}
+
 // dx, the gradient of the state before the first token, and sums of dw and dbias over the workgroup's runs.
 // At token t: du_t = dy_t act'(u_t), and dx of token t - K + 1, the last that du_t reaches, is complete.
 template <class T, int VE, int K, bool SILU>
@@ -319,7 +353,8 @@ bool whole_packs(const ucd_causal_conv_t &d, const CausalConvArgs &a, int ve)
 // Packs: Forward 16 bytes.  Backward keeps four times as much of a channel in registers (its window of tokens and gradients, filter and their sums):
 // two bf16 channels to a thread leave four waves to a SIMD, 47.7 us where four take 48.5 and eight, two waves to a SIMD, 69 (8 x 2048 x 2048);
 // of single sequences of 512 tokens, 4096 channels, 11.8, 13.0 and 15.8.
-constexpr int kFwdPack[2] = {4, 8}, kBwdPack[2] = {4, 2};
+constexpr int kFwdPack[2] = {4, 8}, kBwdPack[2] = {4, 2}, kStepPack[2] = {2, 2};
+enum Form { FORWARD, BACKWARD, STEP };
 
 // Runs are as long as leaves two waves to a SIMD, 8 to 32 tokens.
 template <int VE>
@@ -347,6 +382,13 @@ hipError_t run_fwd(const ConvParams &p, hipStream_t s)
 }
 
 template <class T, int VE, int K, bool SILU>
+hipError_t run_step(const ConvParams &p, hipStream_t s)
+{
+    conv_step_kernel<T, VE, K, SILU><<<dim3((p.packs + 255) / 256, (unsigned)std::min(p.d.B, 65535)), 256, 0, s>>>(p);
+    return hipGetLastError();
+}
+
+template <class T, int VE, int K, bool SILU>
 hipError_t run_bwd(const ConvParams &p, hipStream_t s)
 {
     conv_bwd_kernel<T, VE, K, SILU><<<p.blocks_x * p.part_rows, 256, 0, s>>>(p);
@@ -354,14 +396,16 @@ hipError_t run_bwd(const ConvParams &p, hipStream_t s)
     return hipGetLastError();
 }
 
-template <class T, int VE, int K, bool BACKWARD>
+template <class T, int VE, int K, Form FORM>
 hipError_t by_act(const ConvParams &p, hipStream_t s)
 {
-    if constexpr (BACKWARD) return p.d.act == UCD_ACT_SILU ? run_bwd<T, VE, K, true>(p, s) : run_bwd<T, VE, K, false>(p, s);
-    else return p.d.act == UCD_ACT_SILU ? run_fwd<T, VE, K, true>(p, s) : run_fwd<T, VE, K, false>(p, s);
+    const bool silu = p.d.act == UCD_ACT_SILU;
+    if constexpr (FORM == BACKWARD) return silu ? run_bwd<T, VE, K, true>(p, s) : run_bwd<T, VE, K, false>(p, s);
+    else if constexpr (FORM == STEP) return silu ? run_step<T, VE, K, true>(p, s) : run_step<T, VE, K, false>(p, s);
+    else return silu ? run_fwd<T, VE, K, true>(p, s) : run_fwd<T, VE, K, false>(p, s);
 }
 
-template <class T, int VE, bool BACKWARD>
+template <class T, int VE, Form FORM>
 hipError_t by_taps(const ucd_causal_conv_t &d, const CausalConvArgs &a, bool add, void *ws, hipStream_t s)
 {
     ConvParams p{};
@@ -370,24 +414,24 @@ hipError_t by_taps(const ucd_causal_conv_t &d, const CausalConvArgs &a, bool add
     p.part = (float *)ws;
     p.add = add;
     switch (d.K) {
-    case 1: return by_act<T, VE, 1, BACKWARD>(p, s);
-    case 2: return by_act<T, VE, 2, BACKWARD>(p, s);
-    case 3: return by_act<T, VE, 3, BACKWARD>(p, s);
-    case 4: return by_act<T, VE, 4, BACKWARD>(p, s);
-    case 5: return by_act<T, VE, 5, BACKWARD>(p, s);
-    case 6: return by_act<T, VE, 6, BACKWARD>(p, s);
-    case 7: return by_act<T, VE, 7, BACKWARD>(p, s);
-    default: return by_act<T, VE, 8, BACKWARD>(p, s);
+    case 1: return by_act<T, VE, 1, FORM>(p, s);
+    case 2: return by_act<T, VE, 2, FORM>(p, s);
+    case 3: return by_act<T, VE, 3, FORM>(p, s);
+    case 4: return by_act<T, VE, 4, FORM>(p, s);
+    case 5: return by_act<T, VE, 5, FORM>(p, s);
+    case 6: return by_act<T, VE, 6, FORM>(p, s);
+    case 7: return by_act<T, VE, 7, FORM>(p, s);
+    default: return by_act<T, VE, 8, FORM>(p, s);
     }
 }
 
-template <bool BACKWARD>
+template <Form FORM>
 hipError_t dispatch(const ucd_causal_conv_t &d, const CausalConvArgs &a, bool add, void *ws, hipStream_t s)
 {
-    constexpr const int *packs = BACKWARD ? kBwdPack : kFwdPack;
+    constexpr const int *packs = FORM == BACKWARD ? kBwdPack : FORM == STEP ? kStepPack : kFwdPack;
     const bool whole = whole_packs(d, a, packs[d.dtype]);
-    if (d.dtype == 1) return whole ? by_taps<bf16_t, packs[1], BACKWARD>(d, a, add, ws, s) : by_taps<bf16_t, 1, BACKWARD>(d, a, add, ws, s);
-    return whole ? by_taps<float, packs[0], BACKWARD>(d, a, add, ws, s) : by_taps<float, 1, BACKWARD>(d, a, add, ws, s);
+    if (d.dtype == 1) return whole ? by_taps<bf16_t, packs[1], FORM>(d, a, add, ws, s) : by_taps<bf16_t, 1, FORM>(d, a, add, ws, s);
+    return whole ? by_taps<float, packs[0], FORM>(d, a, add, ws, s) : by_taps<float, 1, FORM>(d, a, add, ws, s);
 }
 
 }  // namespace
@@ -402,13 +446,13 @@ size_t causal_conv_ws_bytes(const ucd_causal_conv_t &d)
     return (size_t)4 * std::max(single.part_rows, packs.part_rows) * (d.K + 1) * d.D;
 }
 
-hipError_t causal_conv_fwd(const ucd_causal_conv_t &d, const CausalConvArgs &a, hipStream_t s) { return dispatch<false>(d, a, false, nullptr, s); }
+hipError_t causal_conv_fwd(const ucd_causal_conv_t &d, const CausalConvArgs &a, hipStream_t s) { return dispatch<FORWARD>(d, a, false, nullptr, s); }
 
 hipError_t causal_conv_bwd(const ucd_causal_conv_t &d, const CausalConvArgs &a, bool add, void *ws, hipStream_t s)
 {
-    return dispatch<true>(d, a, add, ws, s);
+    return dispatch<BACKWARD>(d, a, add, ws, s);
 }
 
-hipError_t causal_conv_step(const ucd_causal_conv_t &d, const CausalConvArgs &a, hipStream_t s) { return causal_conv_fwd(d, a, s); }
+hipError_t causal_conv_step(const ucd_causal_conv_t &d, const CausalConvArgs &a, hipStream_t s) { return dispatch<STEP>(d, a, false, nullptr, s); }
 
 }  // namespace ucd
