@@ -1,0 +1,156 @@
+"""The sequence operators together: a block's outputs and gradients against the same block in plain torch in 64 bits, its
+decoding against whole sequences, and a captured decoding step."""
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+
+def plain_block(block, x):
+    """Block.forward from elementary operations in x's type."""
+    import torch
+    p = {k: v.to(x.dtype).detach().cpu().requires_grad_() for k, v in block.named_parameters()}
+
+    def norm(v, gamma, beta, groups):
+        v = v.reshape(v.shape[:2] + (groups, -1))
+        v = (v - v.mean(-1, keepdim=True)) / torch.sqrt(v.var(-1, correction=0, keepdim=True) + 1e-5)
+        return v.flatten(2) * gamma + beta
+    u, z = (norm(x, p["gamma"], p["beta"], 1) @ p["w_in"]).split(block.inner, -1)
+    pad = torch.nn.functional.pad(u, (0, 0, block.taps - 1, 0))
+    c = torch.nn.functional.silu(p["conv_b"] + sum(pad[:, k:k + x.shape[1]] * p["conv_w"][:, k] for k in range(block.taps)))
+    dt, bm, cm = (c @ p["w_x"]).split([block.rank, block.states, block.states], -1)
+    delta, a = torch.nn.functional.softplus(dt @ p["w_dt"] + p["dt_bias"]), -torch.exp(p["log_a"])
+    h, y = 0, []
+    for t in range(x.shape[1]):
+        h = torch.exp(delta[:, t, :, None] * a) * h + (delta[:, t] * c[:, t])[..., None] * bm[:, t, None]
+        y.append((h * cm[:, t, None]).sum(-1) + p["skip"] * c[:, t])
+    y = torch.stack(y, 1) * torch.nn.functional.silu(z)
+    return x + norm(y, p["head_gamma"], p["head_beta"], block.heads) @ p["w_out"], p
+
+
+@pytest.mark.parametrize("B, L, width, inner, states", [(2, 37, 24, 40, 16), (3, 5, 16, 36, 7), (1, 150, 32, 64, 32)])
+def test_block_gradients(B, L, width, inner, states):
+    """fp32 against 64 bits: relative 1e-4 in the 2-norm, ten operators deep, each within 1e-5 (library products too)."""
+    import torch
+    from paper_1804_04806_amd.sequence_block import Block
+    torch.manual_seed(1)
+    block = Block(width, inner, states=states)
+    x = torch.randn(B, L, width, device="cuda", requires_grad=True)
+    dy = torch.randn(B, L, width, device="cuda")
+    y = block(x)
+    y.backward(dy)
+    xr = x.detach().double().cpu().requires_grad_()
+    ref, p = plain_block(block, xr)
+    ref.backward(dy.double().cpu())
+
+    def close(a, b, what):
+        a, b = a.detach().double().cpu(), b.detach()
+        assert float((a - b).norm()) <= 1e-4 * float(b.norm()), (what, float((a - b).norm() / b.norm()))
+    close(y, ref, "y")
+    close(x.grad, xr.grad, "x")
+    for name, v in block.named_parameters():
+        close(v.grad, p[name].grad, name)
+
+
+def test_training_and_decoding():
+    """The loss falls, and prompts followed by single tokens give what whole sequences give (fp32: sums in another order)."""
+    import torch
+    from paper_1804_04806_amd.sequence_block import decode, train
+    blocks, losses = train(steps=40)
+    assert np.mean(losses[-5:]) < 0.8 * np.mean(losses[:5]), losses
+    x = torch.randn(4, 40, 64, device="cuda")
+    with torch.no_grad():
+        whole = x
+        for block in blocks:
+            whole = block(whole)
+    prompts = [30, 1, 17, 8]
+    out = decode(blocks, x, prompts)
+    assert len(out) == 10
+    for i, got in enumerate(out):
+        for b, n in enumerate(prompts):
+            assert float((got[b] - whole[b, n + i]).abs().max()) <= 1e-3 * float(whole.abs().max())
+
+
+def test_decoding_step_in_a_graph():
+    """A captured step of three operators, replayed between eager work: every replay moves the states on as the eager calls do."""
+    import torch
+    from paper_1804_04806_amd import seq
+    B, D, N, K, pool = 6, 96, 16, 4, 9
+    g = torch.Generator(device="cuda")
+    g.manual_seed(3)
+
+    def rand(*shape):
+        return torch.randn(shape, device="cuda", generator=g)
+    x, w, dt, bm, cm, z = rand(B, 1, D), rand(D, K), rand(B, 1, D), rand(B, 1, 1, N), rand(B, 1, 1, N), rand(B, 1, D)
+    a, gamma, beta = -torch.rand(D, N, device="cuda", generator=g), rand(D), rand(D)
+    slots = torch.tensor([3, 1, 8, 0, 5, 7], dtype=torch.int32, device="cuda")
+    conv, scan = seq.causal_conv(B, 1, D, K, act=seq.ACT_SILU, n_slots=pool), seq.scan(B, 1, D, N, n_slots=pool)
+    norm = seq.group_norm(B, 1, D, 4)
+    start = (rand(pool, K - 1, D), rand(pool, D, N))
+
+    def make():
+        return {"states": [t.clone() for t in start], "c": torch.empty_like(x), "y": torch.empty_like(x), "out": torch.empty_like(x)}
+
+    def step(s):
+        seq.ucd_causal_conv_step(conv, x, w, None, s["states"][0], s["c"], slots=slots)
+        seq.ucd_scan_step(scan, s["c"], dt, a, bm, cm, s["states"][1], s["y"], z=z, slots=slots)
+        seq.ucd_group_norm_fwd(norm, s["y"], gamma, beta, s["out"])
+    eager, captured = make(), make()
+    graph = torch.cuda.CUDAGraph()
+    step(make())
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        step(captured)
+    for i in range(4):
+        x.copy_(rand(B, 1, D))
+        step(eager)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(eager["out"], captured["out"]), i
+        assert all(torch.equal(p, q) for p, q in zip(eager["states"], captured["states"])), i
+
+
+def test_training_step_in_a_graph():
+    """Forward and Backward of the three operators captured, replayed on new inputs between eager work."""
+    import torch
+    from paper_1804_04806_amd import seq
+    B, L, D, N, K = 2, 600, 64, 16, 4
+    g = torch.Generator(device="cuda")
+    g.manual_seed(4)
+
+    def rand(*shape):
+        return torch.randn(shape, device="cuda", generator=g)
+    x, w, dt, bm, cm, dy = rand(B, L, D), rand(D, K), rand(B, L, D), rand(B, L, 1, N), rand(B, L, 1, N), rand(B, L, D)
+    a, gamma, beta = -torch.rand(D, N, device="cuda", generator=g), rand(D), rand(D)
+    conv, scan, norm = seq.causal_conv(B, L, D, K, act=seq.ACT_SILU), seq.scan(B, L, D, N), seq.group_norm(B, L, D, 8, act=seq.ACT_SILU)
+    need = max([seq.ucd_causal_conv_workspace_size(conv)] + [f(d, k) for f, d in ((seq.ucd_scan_workspace_size, scan), (
+        seq.ucd_group_norm_workspace_size, norm)) for k in (seq.FWD, seq.BWD)])
+
+    def make():
+        s = {k: torch.empty(B, L, D, device="cuda") for k in ("c", "y", "out", "dyy", "dc", "dx", "ddt")}
+        s.update(ws=torch.empty(need, dtype=torch.uint8, device="cuda"), stats=torch.empty(2, B, 8, device="cuda"),
+                 saved=torch.empty(seq.ucd_scan_saved_size(scan), dtype=torch.uint8, device="cuda"), dg=torch.empty(D, device="cuda"),
+                 db=torch.empty(D, device="cuda"), dA=torch.empty_like(a), dB=torch.empty_like(bm), dC=torch.empty_like(cm),
+                 dw=torch.empty_like(w))
+        return s
+
+    def step(s):
+        seq.ucd_causal_conv_fwd(conv, x, w, None, s["c"])
+        seq.ucd_scan_fwd(scan, s["c"], dt, a, bm, cm, s["y"], saved=s["saved"], ws=s["ws"])
+        seq.ucd_group_norm_fwd(norm, s["y"], gamma, beta, s["out"], s["stats"], ws=s["ws"])
+        seq.ucd_group_norm_bwd(norm, s["y"], gamma, beta, s["stats"], dy, s["dyy"], s["dg"], s["db"], ws=s["ws"])
+        seq.ucd_scan_bwd(scan, s["c"], dt, a, bm, cm, s["dyy"], s["saved"], s["dc"], s["ddt"], s["dA"], s["dB"], s["dC"], ws=s["ws"])
+        seq.ucd_causal_conv_bwd(conv, x, w, None, s["dc"], s["dx"], s["dw"], None, ws=s["ws"])
+    eager, captured = make(), make()
+    step(captured)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(captured)
+    for i in range(4):
+        x.copy_(rand(B, L, D))
+        step(eager)
+        graph.replay()
+        torch.cuda.synchronize()
+        for k in ("out", "dx", "ddt", "dA", "dB", "dC", "dw", "dg", "db"):
+            assert torch.equal(eager[k], captured[k]), (i, k)
