@@ -255,6 +255,18 @@ __global__ __launch_bounds__(kRowsBwdThreads) void norm_rows_bwd_kernel(NormPara
 
 // ---- slabs and parts -----------------------------------------------------------------------------------------------------------------------------
 
+// Workgroups are dealt to the chip's 8 XCDs in turn, each of which has an L2 of its own: the strips of a sample, whose rows meet inside cache lines, go to
+// the same one.  The grid is whole rounds of 8 samples (or rows of samples); false for those that there are not.
+constexpr unsigned kXcds = 8;
+
+__device__ __forceinline__ bool strip_of(unsigned block, int strips, int rows, int &strip, int &row)
+{
+    const unsigned k = block / kXcds;
+    strip = (int)(k % (unsigned)strips);
+    row = (int)(k / (unsigned)strips * kXcds + block % kXcds);
+    return row < rows;
+}
+
 // A thread's pack of a strip and its positions.
 template <int VE>
 struct SlabPlace {
@@ -410,8 +422,10 @@ __device__ __forceinline__ bool leads(const NormParams &p, const SlabPlace<VE> &
 template <bool SILU, class T, int VE, int R>
 __global__ __launch_bounds__(kMaxThreads, (slab_waves<T, VE, R>())) void norm_slab_fwd_kernel(NormParams p)
 {
-    const SlabPlace<VE> at(p, blockIdx.x % p.strips);
-    for (int n = blockIdx.x / p.strips; n < p.d.N; n += p.part_rows) {
+    int strip, first;
+    if (!strip_of(blockIdx.x, p.strips, p.part_rows, strip, first)) return;
+    const SlabPlace<VE> at(p, strip);
+    for (int n = first; n < p.d.N; n += p.part_rows) {
         Slab<T, VE, R> x;
         x.load(p.x, p.d.x_n, p.d.x_s, p, at, n, 0, p.d.S);
         const float2 m = slab_moments<T, VE, R>(p, x, at, p.d.S, p.share);
@@ -502,13 +516,14 @@ __device__ __forceinline__ void slab_store_part(const NormParams &p, const SlabP
 template <bool SILU, class T, int VE, int R>
 __global__ __launch_bounds__(kMaxThreads) void norm_slab_bwd_kernel(NormParams p)
 {
-    const SlabPlace<VE> at(p, blockIdx.x % p.strips);
+    int strip, part_row;
+    if (!strip_of(blockIdx.x, p.strips, p.part_rows, strip, part_row)) return;
+    const SlabPlace<VE> at(p, strip);
     float gamma[VE] = {}, beta[VE] = {}, dg[VE] = {}, db[VE] = {};
     if (at.active) {
         load_weights<VE>(gamma, p.gamma + at.c0);
         load_weights<VE>(beta, p.beta + at.c0);
     }
-    const int part_row = blockIdx.x / p.strips;
     for (int n = part_row; n < p.d.N; n += p.part_rows) {
         Slab<T, VE, R> x, dy;
         x.load(p.x, p.d.x_n, p.d.x_s, p, at, n, 0, p.d.S);
@@ -525,8 +540,9 @@ template <bool SILU, class T, int VE, int R, bool BACKWARD>
 __global__ __launch_bounds__(kMaxThreads, BACKWARD || VE * sizeof(T) == 16 ? 4 : 8) void norm_part_kernel(NormParams p, unsigned units)
 {
     for (unsigned unit = blockIdx.x; unit < units; unit += gridDim.x) {
-        const SlabPlace<VE> at(p, unit % p.strips);
-        const unsigned row = unit / p.strips;                       // sample and chunk
+        int strip, row;                                             // row: sample and chunk
+        if (!strip_of(unit, p.strips, p.part_rows, strip, row)) continue;
+        const SlabPlace<VE> at(p, strip);
         const int n = row / p.chunks, s0 = row % p.chunks * p.chunk, count = min(p.chunk, p.d.S - s0);
         Slab<T, VE, R> x, dy;
         x.load(p.x, p.d.x_n, p.d.x_s, p, at, n, s0, count);
@@ -543,7 +559,7 @@ __global__ __launch_bounds__(kMaxThreads, BACKWARD || VE * sizeof(T) == 16 ? 4 :
             out = slab_grads<SILU, T, VE, R>(p, x, dy, at, mean, rstd, gamma, beta, dg, db);
             slab_store_part<VE>(p, at, row, dg, db);
         } else {
-            const int width = p.cs > 1 ? min(p.px, p.pgl - (int)(unit % p.strips) % p.cs * p.px) : p.pgl;
+            const int width = p.cs > 1 ? min(p.px, p.pgl - strip % p.cs * p.px) : p.pgl;
             out = slab_moments<T, VE, R>(p, x, at, count, 1.f / ((float)count * width * VE));
         }
         if (leads<VE>(p, at)) {
@@ -589,8 +605,9 @@ __global__ __launch_bounds__(kMaxThreads, BACKWARD || VE * sizeof(T) == 16 ? 4 :
     __shared__ float2 lds[kMaxThreads];
     const int wave = threadIdx.x / 64, waves = blockDim.x / 64;
     for (unsigned unit = blockIdx.x; unit < units; unit += gridDim.x) {
-        const SlabPlace<VE> at(p, unit % p.strips);
-        const unsigned row = unit / p.strips;
+        int strip, row;
+        if (!strip_of(unit, p.strips, p.part_rows, strip, row)) continue;
+        const SlabPlace<VE> at(p, strip);
         const int n = row / p.chunks, s0 = row % p.chunks * p.chunk, count = min(p.chunk, p.d.S - s0);
         Slab<T, VE, R> x, dy;
         x.load(p.x, p.d.x_n, p.d.x_s, p, at, n, s0, count);
@@ -632,6 +649,7 @@ __global__ __launch_bounds__(kJoinThreads) void norm_join_kernel(NormParams p)
 
 // ---- which way, and how it is divided ------------------------------------------------------------------------------------------------------------
 
+constexpr int kStripBytes = 128, kWidenPacks = 1024;
 enum Way { ROWS, SLABS, PARTS };
 
 int ceil_div(long a, long b) { return (int)((a + b - 1) / b); }
@@ -658,16 +676,18 @@ Way divide(const ucd_group_norm_t &d, int VE, bool backward, NormParams &p, int 
         p.part_rows = std::max(1, std::min(ceil_div(d.N, p.ry), (backward ? kRowsBwdGroups : 2048) / p.columns));
         return ROWS;
     }
-    // a strip is as many groups as make 128 bytes of a row, fewer down to 64 bytes where their slab would not fit; or a workgroup's part of a group
+    // a strip is as many groups as make 128 bytes of a row, fewer down to 32 bytes where their slab would not fit, more where
+    // it would be a few waves' work; or a workgroup's part of a group
     const int most = slab_packs(d.dtype, VE, false), few = slab_packs(d.dtype, VE, true);
     p.cs = ceil_div(p.pgl, kMaxThreads);
-    p.gps = p.cs > 1 ? 1 : std::min({d.G, std::max(1, ceil_div(128, p.cg * e)), kMaxThreads / p.pgl});
+    p.gps = p.cs > 1 ? 1 : std::min({d.G, std::max(1, ceil_div(kStripBytes, p.cg * e)), kMaxThreads / p.pgl});
     auto fits = [&](int groups) { return (long)ceil_div(d.S, kMaxThreads / (groups * p.pgl)) <= most; };
     if (p.cs == 1 && !fits(p.gps)) {
         int groups = p.gps;
         while (groups > 1 && !fits(groups)) --groups;
-        if (fits(groups) && (groups * p.cg * e >= 64 || groups == d.G)) p.gps = groups;
+        if (fits(groups) && (groups * p.cg * e >= 32 || groups == d.G)) p.gps = groups;
     }
+    while (p.cs == 1 && (long)d.S * p.gps * p.pgl < kWidenPacks && 2 * p.gps <= d.G && 2 * p.gps * p.pgl <= 64) p.gps *= 2;
     p.px = p.cs > 1 ? kMaxThreads : p.gps * p.pgl;
     p.strips = p.cs > 1 ? d.G * p.cs : ceil_div(d.G, p.gps);
     auto power = [](int n) { return (n & (n - 1)) == 0; };
@@ -716,6 +736,8 @@ int pack_of(const ucd_group_norm_t &d, int dir, const void *a, const void *b, co
     return 1;
 }
 
+unsigned strip_units(const NormParams &p) { return (unsigned)p.strips * ((p.part_rows + kXcds - 1) / kXcds * kXcds); }
+
 template <bool SILU, class T, int VE, bool BACKWARD>
 hipError_t launch(NormParams &p, void *ws, hipStream_t s)
 {
@@ -730,11 +752,11 @@ hipError_t launch(NormParams &p, void *ws, hipStream_t s)
     p.sums = (float *)at;
     constexpr int MOST = slab_packs<T, VE>(false), FEW = slab_packs<T, VE>(true);
     if (way == PARTS) {
-        const unsigned units = (unsigned)p.strips * p.part_rows, grid = std::min(units, 1u << 21);
+        const unsigned units = strip_units(p), grid = std::min(units, 1u << 21);
         norm_part_kernel<SILU, T, VE, MOST, BACKWARD><<<grid, threads, 0, s>>>(p, units);
         norm_apply_kernel<SILU, T, VE, MOST, BACKWARD><<<grid, threads, 0, s>>>(p, units);
     } else if (way == SLABS) {
-        const unsigned grid = (unsigned)p.strips * p.part_rows;
+        const unsigned grid = strip_units(p);
         if constexpr (BACKWARD) {
             if (R == FEW) norm_slab_bwd_kernel<SILU, T, VE, FEW><<<grid, threads, 0, s>>>(p);
             else norm_slab_bwd_kernel<SILU, T, VE, MOST><<<grid, threads, 0, s>>>(p);
