@@ -152,15 +152,18 @@ __global__ __launch_bounds__(64 * kWaves, 2) void scan_bwd_kernel(ScanParams p, 
             cm_at -= kTile * e * d.Cm_l;
             saved_at -= (kTile / kKeep) * (long)d.D * d.N;
         };
+        // FULL: all tokens, channels and states of the segment are there, as is the rule (see Forward).
+        auto walk = [&](auto whole) {
+        constexpr bool FULL = decltype(whole)::value;
         if (tile1 > tile0) load(tile1 - 1);
         for (int tile = tile1 - 1; tile >= tile0; --tile) {
             const int left = n - tile * kTile;
             float ut[W::VE], st[W::VE], rate[W::VE], dyp[W::VE], dzt[W::VE];
-            if (left > 0) {
-                bc.stage(bm, d.N);
+            if (FULL || left > 0) {
+                bc.template stage<FULL>(bm, d.N);
 #pragma unroll
                 for (int i = 0; i < W::VE; ++i) {
-                    const bool there = at.tok < left && channel[i];
+                    const bool there = FULL || (at.tok < left && channel[i]);
                     ut[i] = u.get(i);
                     float s = dt.get(i) + bias[i], slope;
                     const float soft = softplus<T>(s, &slope);
@@ -291,7 +294,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void scan_bwd_kernel(ScanParams p, 
                 if (GATE) lds_row(yt, ys + o);
 #pragma unroll
                 for (int i = 0; i < W::VE; ++i) {
-                    const bool there = at.tok < left && channel[i];
+                    const bool there = FULL || (at.tok < left && channel[i]);
                     const float rise = fmaf(et[i], kLn2, g[i] * ut[i]) * rate[i];
                     du.v[i] = from_f<T>(there ? fmaf(g[i], st[i], skip[i] * dyp[i]) : 0.f);
                     ddt.v[i] = from_f<T>(there ? rise : 0.f);
@@ -299,18 +302,22 @@ __global__ __launch_bounds__(64 * kWaves, 2) void scan_bwd_kernel(ScanParams p, 
                     dskip[i] += there ? dyp[i] * ut[i] : 0.f;
                     dbias[i] += there ? rise : 0.f;
                 }
-                store_row<T, W, WIDE>(du_at, du_off, du, have);
-                store_row<T, W, WIDE>(ddt_at, ddt_off, ddt, have);
-                if (GATE) store_row<T, W, WIDE>(dz_at, dz_off, dz, have);
+                store_row<T, W, WIDE, FULL>(du_at, du_off, du, have);
+                store_row<T, W, WIDE, FULL>(ddt_at, ddt_off, ddt, have);
+                if (GATE) store_row<T, W, WIDE, FULL>(dz_at, dz_off, dz, have);
                 du_at -= kTile * e * d.u_l;
                 ddt_at -= kTile * e * d.dt_l;
                 if (GATE) dz_at -= kTile * e * d.z_l;
                 wave_lds_order();
-                if (left > 0) {
+                if (FULL || left > 0) {
                     // the waves' sums, in their order; the other of the two buffers is written meanwhile
-                    __syncthreads();
+                    lds_barrier();
                     float *o = p.part_bc + ((((long)at.b * p.tiles + tile) * d.G + at.g) * p.blocks + at.block) * BC;
-                    for (int i = threadIdx.x; i < BC; i += 64 * kWaves) {
+                    constexpr int EACH = (BC + 64 * kWaves - 1) / (64 * kWaves);
+#pragma unroll
+                    for (int k = 0; k < EACH; ++k) {
+                        const int i = (int)threadIdx.x + k * 64 * kWaves;
+                        if (BC % (64 * kWaves) != 0 && i >= BC) continue;
                         float v = lds_sum[tile & 1][0][i];
 #pragma unroll
                         for (int w = 1; w < kWaves; ++w) v += lds_sum[tile & 1][w][i];
@@ -319,6 +326,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void scan_bwd_kernel(ScanParams p, 
                 }
             }
         }
+        };
+        if (WIDE && n >= tile1 * kTile && at.have == W::CW && d.N == W::NP) walk(std::integral_constant<bool, WIDE>());
+        else walk(std::false_type());
         if (STATE_ONLY) {
             store_states<WIDE>(p.seg_state + seg_at(at.seg), x, at.haven);
             if (at.q == 0 && mine) p.seg_step[((long)at.b * p.segs + at.seg) * d.D + ch] = steps;
@@ -341,7 +351,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void scan_bwd_kernel(ScanParams p, 
                     w[1] = dbias[e];
                 }
             }
-            __syncthreads();      // lds_sum is written again by the next unit
+            lds_barrier();      // lds_sum is written again by the next unit
         }
     }
 }

@@ -95,13 +95,14 @@ __device__ __forceinline__ void load_states(float (&h)[N], const float *at, int 
     for (int j = 0; j < N; ++j) h[j] = r.v[j];
 }
 
-template <bool WIDE, int N>
+template <bool WIDE, bool FULL = false, int N>
 __device__ __forceinline__ void store_states(float *at, const float (&h)[N], int haven)
 {
     Pack<float, N> r;
 #pragma unroll
     for (int j = 0; j < N; ++j) r.v[j] = h[j];
-    store_pack<WIDE, float, N>(at, r, haven);
+    if (WIDE && FULL) *reinterpret_cast<Pack<float, N> *>(at) = r;
+    else store_pack<WIDE, float, N>(at, r, haven);
 }
 
 // Tokens behind the sequence's last repeat it and channels that are not there repeat the workgroup's first: what is loaded of them is masked where it
@@ -126,10 +127,11 @@ __device__ __forceinline__ const char *bc_base(const void *base, long sb, long s
     return (const char *)base + (at.b * sb + t0 * sl + (long)at.g * N) * (long)sizeof(T);
 }
 
-template <class T, class W, bool WIDE>
+template <class T, class W, bool WIDE, bool FULL = false>
 __device__ __forceinline__ void store_row(char *base, uint32_t offset, const Pack<T, W::VE> &v, int have)
 {
-    store_pack<WIDE, T, W::VE>(reinterpret_cast<T *>(base + offset), v, have);
+    if (WIDE && FULL) *reinterpret_cast<Pack<T, W::VE> *>(base + offset) = v;
+    else store_pack<WIDE, T, W::VE>(reinterpret_cast<T *>(base + offset), v, have);
 }
 
 // A tile's Bm and Cm, 16 rows of NP states of one, then of the other; in packs of 4 or one by one.  States that are not there are 0.
@@ -162,7 +164,8 @@ struct TileStates {
         }
     }
 
-    // into LDS: Bm's rows, then Cm's
+    // into LDS: Bm's rows, then Cm's; FULL: all NP states are there
+    template <bool FULL = false>
     __device__ __forceinline__ void stage(float *lds, int states)
     {
 #pragma unroll
@@ -170,7 +173,7 @@ struct TileStates {
             const int e = index(i);
             Pack<float, V> f;
 #pragma unroll
-            for (int j = 0; j < V; ++j) f.v[j] = W::NP == V || e % W::NP < states ? r[i].get(j) : 0.f;
+            for (int j = 0; j < V; ++j) f.v[j] = FULL || W::NP == V || e % W::NP < states ? r[i].get(j) : 0.f;
             if (2 * ROWS % (64 * V) == 0 || e < 2 * ROWS) *reinterpret_cast<Pack<float, V> *>(lds + e) = f;
         }
     }

@@ -110,79 +110,89 @@ __global__ __launch_bounds__(64 * kWaves, 2) void scan_fwd_kernel(ScanParams p, 
             bm_at += kTile * e * d.Bm_l;
             cm_at += kTile * e * d.Cm_l;
         };
-        load(tile0);
-        for (int tile = tile0; tile < tile1; ++tile) {
-            const int left = n - tile * kTile;
-            const bool there = at.tok < left;
-            float ut[W::VE], zt[W::VE];
-            if (left > 0) {
-                bc.stage(bm, d.N);
+        // FULL: all tokens, channels and states of the segment are there, as is the rule.  Without masks and without branches around the stores, behind
+        // which the loads' arrival could only be told by waiting for the stores too.  SAVE: states are kept for Backward.
+        auto walk = [&](auto full, auto save) {
+            constexpr bool FULL = decltype(full)::value, SAVE = decltype(save)::value;
+            load(tile0);
+            for (int tile = tile0; tile < tile1; ++tile) {
+                const int left = n - tile * kTile;
+                const bool there = FULL || at.tok < left;
+                float ut[W::VE], zt[W::VE];
+                if (FULL || left > 0) {
+                    bc.template stage<FULL>(bm, d.N);
 #pragma unroll
-                for (int i = 0; i < W::VE; ++i) {
-                    ut[i] = u.get(i);
-                    float s = dt.get(i) + bias[i];
-                    const float soft = softplus<T>(s);
-                    s = d.softplus ? soft : s;
-                    s = there ? s : 0.f;     // padding: the state stays
-                    step[at.tok * W::CW + at.ch0 + i] = make_float2(s, there ? s * ut[i] : 0.f);
-                    if (GATE) {
-                        const float v = z.get(i);
-                        zt[i] = v * sigmoid(v);
+                    for (int i = 0; i < W::VE; ++i) {
+                        ut[i] = u.get(i);
+                        float s = dt.get(i) + bias[i];
+                        const float soft = softplus<T>(s);
+                        s = d.softplus ? soft : s;
+                        s = there ? s : 0.f;     // padding: the state stays
+                        step[at.tok * W::CW + at.ch0 + i] = make_float2(s, there ? s * ut[i] : 0.f);
+                        if (GATE) {
+                            const float v = z.get(i);
+                            zt[i] = v * sigmoid(v);
+                        }
                     }
+                    if (tile + 1 < tile1) load(tile + 1);
+                    wave_lds_order();
+                    auto keep = [&]() {
+                        store_states<WIDE, FULL>(saved_at + state_off, h, at.haven);
+                        saved_at += (long)d.D * d.N;
+                    };
+                    if (SAVE) keep();
+                    float kept = 0.f;
+                    // the next tokens' values are on their way from LDS while these are computed: left to itself the compiler reads them just
+                    // before their use, and a wave that has its SIMD to itself waits for each
+                    Ahead now, next;
+                    now.load(step, bm, cm, at, 0);
+#pragma unroll
+                    for (int t = 0; t < kTile; ++t) {
+                        if (t % kAhead == 0) {
+                            if (t > 0) now = next;
+                            if (t + kAhead < kTile) next.load(step, bm, cm, at, t + kAhead);
+                            __builtin_amdgcn_sched_barrier(0);
+                        }
+                        const float2 s = now.s[t % kAhead];
+                        const Pack<float, NPL> b = now.b[t % kAhead], c = now.c[t % kAhead];
+                        float y = 0.f;
+#pragma unroll
+                        for (int j = 0; j < NPL; ++j) {
+                            h[j] = fmaf(exp2_fast(s.x * A2[j]), h[j], s.y * b.v[j]);
+                            if (!STATE_ONLY) y = fmaf(h[j], c.v[j], y);
+                        }
+                        if (STATE_ONLY) {
+                            steps += s.x;
+                        } else {
+                            if (SAVE && t % kKeep == kKeep - 1 && t + 1 < kTile) keep();
+                            y = sum_lanes<LPC>(y);
+                            kept = at.q == t % LPC ? y : kept;      // each lane of a channel keeps one token in LPC
+                            if (t % LPC == LPC - 1) ys[(t - LPC + 1 + at.q) * W::CW + at.c] = kept;
+                        }
+                    }
+                    wave_lds_order();
                 }
-                if (tile + 1 < tile1) load(tile + 1);
-                wave_lds_order();
-                auto keep = [&]() {
-                    store_states<WIDE>(saved_at + state_off, h, at.haven);
-                    saved_at += (long)d.D * d.N;
-                };
-                if (!STATE_ONLY && p.saved) keep();
-                float kept = 0.f;
-                // the next tokens' values are on their way from LDS while these are computed: left to itself the compiler reads them just
-                // before their use, and a wave that has its SIMD to itself waits for each
-                Ahead now, next;
-                now.load(step, bm, cm, at, 0);
+                if (!STATE_ONLY) {
+                    Pack<T, W::VE> out;
+                    float yt[W::VE];
+                    lds_row(yt, ys + at.tok * W::CW + at.ch0);
 #pragma unroll
-                for (int t = 0; t < kTile; ++t) {
-                    if (t % kAhead == 0) {
-                        if (t > 0) now = next;
-                        if (t + kAhead < kTile) next.load(step, bm, cm, at, t + kAhead);
-                        __builtin_amdgcn_sched_barrier(0);
+                    for (int i = 0; i < W::VE; ++i) {
+                        float y = fmaf(skip[i], ut[i], yt[i]);
+                        if (GATE) y *= zt[i];
+                        out.v[i] = from_f<T>(there ? y : 0.f);
                     }
-                    const float2 s = now.s[t % kAhead];
-                    const Pack<float, NPL> b = now.b[t % kAhead], c = now.c[t % kAhead];
-                    float y = 0.f;
-#pragma unroll
-                    for (int j = 0; j < NPL; ++j) {
-                        h[j] = fmaf(exp2_fast(s.x * A2[j]), h[j], s.y * b.v[j]);
-                        if (!STATE_ONLY) y = fmaf(h[j], c.v[j], y);
-                    }
-                    if (STATE_ONLY) {
-                        steps += s.x;
-                    } else {
-                        if (p.saved && t % kKeep == kKeep - 1 && t + 1 < kTile) keep();
-                        y = sum_lanes<LPC>(y);
-                        kept = at.q == t % LPC ? y : kept;      // each lane of a channel keeps one token in LPC
-                        if (t % LPC == LPC - 1) ys[(t - LPC + 1 + at.q) * W::CW + at.c] = kept;
-                    }
+                    store_row<T, W, WIDE, FULL>(y_at, y_off, out, at.tok < d.L - tile * kTile ? at.have - at.ch0 : 0);
+                    y_at += kTile * e * d.y_l;
+                    wave_lds_order();
                 }
-                wave_lds_order();
             }
-            if (!STATE_ONLY) {
-                Pack<T, W::VE> out;
-                float yt[W::VE];
-                lds_row(yt, ys + at.tok * W::CW + at.ch0);
-#pragma unroll
-                for (int i = 0; i < W::VE; ++i) {
-                    float y = fmaf(skip[i], ut[i], yt[i]);
-                    if (GATE) y *= zt[i];
-                    out.v[i] = from_f<T>(there ? y : 0.f);
-                }
-                store_row<T, W, WIDE>(y_at, y_off, out, at.tok < d.L - tile * kTile ? at.have - at.ch0 : 0);
-                y_at += kTile * e * d.y_l;
-                wave_lds_order();
-            }
-        }
+        };
+        const bool full = WIDE && n >= tile1 * kTile && at.have == W::CW && d.N == W::NP, save = !STATE_ONLY && p.saved;
+        if (full && save) walk(std::integral_constant<bool, WIDE>(), std::integral_constant<bool, !STATE_ONLY>());
+        else if (full) walk(std::integral_constant<bool, WIDE>(), std::false_type());
+        else if (save) walk(std::false_type(), std::integral_constant<bool, !STATE_ONLY>());
+        else walk(std::false_type(), std::false_type());
         if (STATE_ONLY) {
             store_states<WIDE>(p.seg_state + seg_at(at.seg + 1), h, at.haven);
             if (at.q == 0 && at.c < at.have) p.seg_step[((long)at.b * p.segs + at.seg) * d.D + ch] = steps;
