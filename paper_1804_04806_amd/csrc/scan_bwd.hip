@@ -200,7 +200,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void scan_bwd_kernel(ScanParams p, 
                     }
                 } else {
                     float *sums = lds_sum[tile & 1][wave];
-                    float gk = 0.f, ek = 0.f, yk = 0.f, v[2][2][NPL];
+                    LaneSums<LPC> g_sums, e_sums, y_sums;
+                    float v[2][2][NPL];
 #pragma unroll
                     for (int part = kTile / kKeep - 1; part >= 0; --part) {
                         const int p0 = part * kKeep;
@@ -250,18 +251,14 @@ __global__ __launch_bounds__(64 * kWaves, 2) void scan_bwd_kernel(ScanParams p, 
                                 et = fmaf(w, A2[j], et);
                                 dA[j] = fmaf(w, s.x, dA[j]);
                             }
-                            gt = sum_lanes<LPC>(gt);
-                            et = sum_lanes<LPC>(et);
-                            if (GATE) yt = sum_lanes<LPC>(yt);
-                            const bool mine_t = LPC == 1 || at.q == t % LPC;
-                            gk = mine_t ? gt : gk;
-                            ek = mine_t ? et : ek;
-                            yk = mine_t ? yt : yk;
+                            g_sums.add(t, gt, at.q);
+                            e_sums.add(t, et, at.q);
+                            if (GATE) y_sums.add(t, yt, at.q);
                             if (t % LPC == 0) {
                                 const int o = (t + at.q) * W::CW + at.c;
-                                gs[o] = gk;
-                                es[o] = ek;
-                                if (GATE) ys[o] = yk;
+                                gs[o] = g_sums.get(at.q);
+                                es[o] = e_sums.get(at.q);
+                                if (GATE) ys[o] = y_sums.get(at.q);
                             }
                             if (t % 2 == 0) {
                                 float r[NPL];
@@ -356,23 +353,32 @@ __global__ __launch_bounds__(64 * kWaves, 2) void scan_bwd_kernel(ScanParams p, 
     }
 }
 
-// dBm and dCm: one element of either per thread, over the workgroups of a group's channels.
+// dBm and dCm: four neighbouring elements of either per thread, over the workgroups of a group's channels.
 template <class T>
 __global__ __launch_bounds__(256) void scan_join_bc_kernel(ScanParams p, int np, long total)
 {
     const ucd_scan_t &d = p.d;
     for (long i = blockIdx.x * 256l + threadIdx.x; i < total; i += gridDim.x * 256l) {
-        const int k = (int)(i % np), kind = (int)(i / np % 2);
-        const long row = i / np / 2;
+        const int k = (int)(i % (np / 4)) * 4, kind = (int)(i / (np / 4) % 2);
+        const long row = i / (np / 4) / 2;
         const int g = (int)(row % d.G), t = (int)(row / d.G % d.L), b = (int)(row / d.G / d.L);
-        if (k >= d.N) continue;
-        float v = 0.f;
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
         if (t < scan_length(p, b)) {
             const float *o = p.part_bc + ((((long)b * p.tiles + t / kTile) * d.G + g) * p.blocks) * (2l * kTile * np) + (t % kTile * 2 + kind) * np + k;
-            for (int s = 0; s < p.blocks; ++s) v += o[s * (2l * kTile * np)];
+#pragma unroll 8
+            for (unsigned s = 0; s < p.blocks; ++s) {
+                const float4 w = *reinterpret_cast<const float4 *>(o + s * (2l * kTile * np));
+                v.x += w.x;
+                v.y += w.y;
+                v.z += w.z;
+                v.w += w.w;
+            }
         }
-        T *out = kind ? (T *)p.g.Cm + b * d.Cm_b + (long)t * d.Cm_l : (T *)p.g.Bm + b * d.Bm_b + (long)t * d.Bm_l;
-        out[(long)g * d.N + k] = from_f<T>(v);
+        T *out = (kind ? (T *)p.g.Cm + b * d.Cm_b + (long)t * d.Cm_l : (T *)p.g.Bm + b * d.Bm_b + (long)t * d.Bm_l) + (long)g * d.N + k;
+        const float f[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (k + j < d.N) out[j] = from_f<T>(f[j]);
     }
 }
 
@@ -403,7 +409,7 @@ hipError_t launch(const ScanParams &p, hipStream_t s)
     if (p.in.z) launch_main<T, W, WIDE, true>(p, s);
     else launch_main<T, W, WIDE, false>(p, s);
     const ucd_scan_t &d = p.d;
-    const long elements = (long)d.B * d.L * d.G * 2 * W::NP;
+    const long elements = (long)d.B * d.L * d.G * 2 * W::NP / 4;
     if (elements > 0)
         scan_join_bc_kernel<T><<<(unsigned)std::min((elements + 255) / 256, 1l << 22), 256, 0, s>>>(p, W::NP, elements);
     scan_join_weights_kernel<<<(unsigned)(((long)d.D * (d.N + 2) + kJoinColumns - 1) / kJoinColumns), kJoinThreads, 0, s>>>(p);

@@ -141,7 +141,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void scan_fwd_kernel(ScanParams p, 
                         saved_at += (long)d.D * d.N;
                     };
                     if (SAVE) keep();
-                    float kept = 0.f;
+                    LaneSums<LPC> sums;
                     // the next tokens' values are on their way from LDS while these are computed: left to itself the compiler reads them just
                     // before their use, and a wave that has its SIMD to itself waits for each
                     Ahead now, next;
@@ -165,9 +165,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void scan_fwd_kernel(ScanParams p, 
                             steps += s.x;
                         } else {
                             if (SAVE && t % kKeep == kKeep - 1 && t + 1 < kTile) keep();
-                            y = sum_lanes<LPC>(y);
-                            kept = at.q == t % LPC ? y : kept;      // each lane of a channel keeps one token in LPC
-                            if (t % LPC == LPC - 1) ys[(t - LPC + 1 + at.q) * W::CW + at.c] = kept;
+                            sums.add(t, y, at.q);
+                            if (t % LPC == LPC - 1) ys[(t - LPC + 1 + at.q) * W::CW + at.c] = sums.get(at.q);
                         }
                     }
                     wave_lds_order();

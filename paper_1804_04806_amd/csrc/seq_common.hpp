@@ -131,6 +131,30 @@ __device__ __forceinline__ float sum_lanes(float v)
     return v;
 }
 
+// The sums over LPC neighbouring lanes of values that come token by token (up or down); after LPC of them, of which t is the last and first the lowest,
+// lane q of each group has that of token first + q.
+template <int LPC>
+struct LaneSums {
+    float v[4], kept = 0.f;
+    __device__ __forceinline__ void add(int t, float value, int q)
+    {
+        if (LPC == 4) {
+            v[t % 4] = value;
+            return;
+        }
+        value = sum_lanes<LPC>(value);
+        kept = q == t % LPC ? value : kept;
+    }
+    __device__ __forceinline__ float get(int q) const
+    {
+        if (LPC != 4) return kept;
+        // pairs of lanes share out pairs of tokens, then pairs of pairs: 9 instructions where sums in every lane and a choice are 12
+        const bool odd = q & 1, high = q & 2;
+        const float low = (odd ? v[1] : v[0]) + dpp<kXor1>(odd ? v[0] : v[1]), top = (odd ? v[3] : v[2]) + dpp<kXor1>(odd ? v[2] : v[3]);
+        return (high ? top : low) + dpp<kXor2>(high ? low : top);
+    }
+};
+
 // a = {a of the lower half of the wave, b of the lower half}, b = {a of the upper half, b of the upper half}
 __device__ __forceinline__ void swap_halves(float &a, float &b)
 {
