@@ -22,6 +22,7 @@ bool scan_wide(const ucd_scan_t &d, const ucd_scan_in_t &in, const void *y, cons
     return !g || (wide_rows(g->u, 0, 0, e) && wide_rows(g->dt, 0, 0, e) && wide_rows(g->z, 0, 0, e));
 }
 
+// The library's own buffers of states have NP of them to a channel, so that they are read in packs whatever N is.
 // Segments: a launch is waves of 64 / lanes channels that walk over all tokens, and 1024 of them give every SIMD one.  With fewer, sequences are cut
 // into segments that are scanned side by side, after a first launch over the states alone, which costs two thirds of the second; so much that four
 // waves to a SIMD (Forward; Backward's registers leave room for two) are then worth it, down to segments of four tiles.  Times per token, channel and
@@ -52,7 +53,7 @@ void scan_params(const ucd_scan_t &d, const ucd_scan_in_t &in, int dir, void *ws
     char *at = (char *)ws;
     if (p.segs > 1) {
         p.seg_state = (float *)at;
-        at += round16((size_t)4 * d.B * p.segs * d.D * d.N);
+        at += round16((size_t)4 * d.B * p.segs * d.D * scan_states(d));
         p.seg_step = (float *)at;
         at += round16((size_t)4 * d.B * p.segs * d.D);
     }
@@ -67,12 +68,12 @@ size_t scan_ws_bytes(const ucd_scan_t &d, int dir)
 {
     ScanParams p{};
     segments(d, dir, p);
-    size_t n = p.segs > 1 ? round16((size_t)4 * d.B * p.segs * d.D * d.N) + round16((size_t)4 * d.B * p.segs * d.D) : 0;
+    size_t n = p.segs > 1 ? round16((size_t)4 * d.B * p.segs * d.D * scan_states(d)) + round16((size_t)4 * d.B * p.segs * d.D) : 0;
     if (dir == UCD_SEQ_BWD)
         n += round16((size_t)4 * d.B * p.tiles * d.G * p.blocks * kTile * 2 * scan_states(d)) + (size_t)4 * d.B * p.segs * d.D * (d.N + 2);
     return n;
 }
 
-size_t scan_saved_bytes(const ucd_scan_t &d) { return (size_t)4 * d.B * ((d.L + kTile - 1) / kTile) * (kTile / kKeep) * d.D * d.N; }
+size_t scan_saved_bytes(const ucd_scan_t &d) { return (size_t)4 * d.B * ((d.L + kTile - 1) / kTile) * (kTile / kKeep) * d.D * scan_states(d); }
 
 }  // namespace ucd

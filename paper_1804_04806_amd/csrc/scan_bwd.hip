@@ -87,13 +87,13 @@ __global__ __launch_bounds__(64 * kWaves, 2) void scan_bwd_kernel(ScanParams p, 
         load_states<WIDE>(A2, p.in.A + ch * d.N + at.n0, at.haven);
 #pragma unroll
         for (int j = 0; j < NPL; ++j) A2[j] *= kLog2e;
-        auto seg_at = [&](int s) { return (((long)at.b * p.segs + s) * d.D + ch) * d.N + at.n0; };
+        auto seg_at = [&](int s) { return (((long)at.b * p.segs + s) * d.D + ch) * W::NP + at.n0; };
         const long state_at = ((long)at.b * d.D + ch) * d.N + at.n0;
         load_states<WIDE>(x, p.dstate_out + state_at, p.dstate_out && (at.seg == p.segs - 1 || !STATE_ONLY) ? at.haven : 0);
         if (!STATE_ONLY)
             for (int s = p.segs - 1; s > at.seg; --s) {
                 float end[NPL];
-                load_states<WIDE>(end, p.seg_state + seg_at(s), at.haven);
+                load_own(end, p.seg_state + seg_at(s), mine);
                 // the last segment began with dstate_out
                 if (s == p.segs - 1) {
 #pragma unroll
@@ -115,8 +115,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void scan_bwd_kernel(ScanParams p, 
         const char *bm_at = bc_base<T>(p.in.Bm, d.Bm_b, d.Bm_l, at, t_last, d.N), *cm_at = bc_base<T>(p.in.Cm, d.Cm_b, d.Cm_l, at, t_last, d.N);
         char *du_at = const_cast<char *>(row_base<T>(p.g.u, d.u_b, d.u_l, at, t_last)), *ddt_at = const_cast<char *>(row_base<T>(p.g.dt, d.dt_b, d.dt_l, at, t_last));
         char *dz_at = const_cast<char *>(row_base<T>(p.g.z, d.z_b, d.z_l, at, t_last));
-        const float *saved_at = p.saved + (((long)at.b * p.tiles + tile1 - 1) * (kTile / kKeep) * d.D + at.first) * d.N;
-        const uint32_t state_off = (uint32_t)(at.c0 - at.first + at.c) * d.N + at.n0;
+        const float *saved_at = p.saved + (((long)at.b * p.tiles + tile1 - 1) * (kTile / kKeep) * d.D + at.first) * W::NP;
+        const uint32_t state_off = (uint32_t)(at.c0 - at.first + at.c) * W::NP + at.n0;
         const uint32_t du_off = row_offset<T>(at, d.u_l, kTile), ddt_off = row_offset<T>(at, d.dt_l, kTile), dz_off = row_offset<T>(at, d.z_l, kTile);
         Raw<T, W::VE, WIDE> u, dt, z, dy;
         TileStates<T, W, WIDE> bc;
@@ -141,7 +141,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void scan_bwd_kernel(ScanParams p, 
                 bc.load(bm_at, cm_at);
                 if (!STATE_ONLY)
 #pragma unroll
-                    for (int i = 0; i < kTile / kKeep; ++i) load_states<WIDE>(kept[i], saved_at + i * (long)d.D * d.N + state_off, at.haven);
+                    for (int i = 0; i < kTile / kKeep; ++i) load_own(kept[i], saved_at + i * (long)d.D * W::NP + state_off, mine);
                 if (left < kTile) place(kTile);
             }
             u_at -= kTile * e * d.u_l;
@@ -150,9 +150,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void scan_bwd_kernel(ScanParams p, 
             if (GATE) z_at -= kTile * e * d.z_l;
             bm_at -= kTile * e * d.Bm_l;
             cm_at -= kTile * e * d.Cm_l;
-            saved_at -= (kTile / kKeep) * (long)d.D * d.N;
+            saved_at -= (kTile / kKeep) * (long)d.D * W::NP;
         };
-        // FULL: all tokens, channels and states of the segment are there, as is the rule (see Forward).
+        // FULL: all tokens and channels of the segment are there, and in packs all states, as is the rule (see Forward).
         auto walk = [&](auto whole) {
         constexpr bool FULL = decltype(whole)::value;
         if (tile1 > tile0) load(tile1 - 1);
@@ -160,7 +160,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void scan_bwd_kernel(ScanParams p, 
             const int left = n - tile * kTile;
             float ut[W::VE], st[W::VE], rate[W::VE], dyp[W::VE], dzt[W::VE];
             if (FULL || left > 0) {
-                bc.template stage<FULL>(bm, d.N);
+                bc.template stage<FULL && WIDE>(bm, d.N);
 #pragma unroll
                 for (int i = 0; i < W::VE; ++i) {
                     const bool there = FULL || (at.tok < left && channel[i]);
@@ -324,10 +324,10 @@ __global__ __launch_bounds__(64 * kWaves, 2) void scan_bwd_kernel(ScanParams p, 
             }
         }
         };
-        if (WIDE && n >= tile1 * kTile && at.have == W::CW && d.N == W::NP) walk(std::integral_constant<bool, WIDE>());
+        if (n >= tile1 * kTile && at.have == W::CW && (!WIDE || d.N == W::NP)) walk(std::true_type());
         else walk(std::false_type());
         if (STATE_ONLY) {
-            store_states<WIDE>(p.seg_state + seg_at(at.seg), x, at.haven);
+            store_own(p.seg_state + seg_at(at.seg), x, mine);
             if (at.q == 0 && mine) p.seg_step[((long)at.b * p.segs + at.seg) * d.D + ch] = steps;
         } else {
             if (p.g.state && at.seg == 0) store_states<WIDE>(p.g.state + state_at, x, at.haven);

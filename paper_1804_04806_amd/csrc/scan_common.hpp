@@ -35,10 +35,10 @@ struct ScanParams {
     const float *state_in;
     float *state_out;
     void *y;
-    float *saved;                // [B][tiles][kTile / kKeep][D][N]: states before each part of a tile
+    float *saved;                // [B][tiles][kTile / kKeep][D][NP]: states before each part of a tile
     // Forward: a sequence's first state, then the end states of its segments but the last, each from zero; Backward: the gradients of the
     // states before its segments but the first, each from zero.  And the sums of the segments' steps.
-    float *seg_state, *seg_step; // [B][segs][D][N], [B][segs][D]
+    float *seg_state, *seg_step; // [B][segs][D][NP], [B][segs][D]
     // Backward
     const void *dy;
     const float *dstate_out;
@@ -95,14 +95,25 @@ __device__ __forceinline__ void load_states(float (&h)[N], const float *at, int 
     for (int j = 0; j < N; ++j) h[j] = r.v[j];
 }
 
-template <bool WIDE, bool FULL = false, int N>
+template <bool WIDE, int N>
 __device__ __forceinline__ void store_states(float *at, const float (&h)[N], int haven)
 {
     Pack<float, N> r;
 #pragma unroll
     for (int j = 0; j < N; ++j) r.v[j] = h[j];
-    if (WIDE && FULL) *reinterpret_cast<Pack<float, N> *>(at) = r;
-    else store_pack<WIDE, float, N>(at, r, haven);
+    store_pack<WIDE, float, N>(at, r, haven);
+}
+
+// The same in the library's own buffers, whose channels have NP states: always a whole pack.
+template <int N>
+__device__ __forceinline__ void load_own(float (&h)[N], const float *at, bool there)
+{
+    load_states<true, N>(h, at, there);
+}
+template <int N>
+__device__ __forceinline__ void store_own(float *at, const float (&h)[N], bool there)
+{
+    store_states<true, N>(at, h, there);
 }
 
 // Tokens behind the sequence's last repeat it and channels that are not there repeat the workgroup's first: what is loaded of them is masked where it
@@ -130,7 +141,7 @@ __device__ __forceinline__ const char *bc_base(const void *base, long sb, long s
 template <class T, class W, bool WIDE, bool FULL = false>
 __device__ __forceinline__ void store_row(char *base, uint32_t offset, const Pack<T, W::VE> &v, int have)
 {
-    if (WIDE && FULL) *reinterpret_cast<Pack<T, W::VE> *>(base + offset) = v;
+    if (FULL) store_pack<WIDE, T, W::VE>(reinterpret_cast<T *>(base + offset), v, W::VE);
     else store_pack<WIDE, T, W::VE>(reinterpret_cast<T *>(base + offset), v, have);
 }
 
@@ -164,8 +175,8 @@ struct TileStates {
         }
     }
 
-    // into LDS: Bm's rows, then Cm's; FULL: all NP states are there
-    template <bool FULL = false>
+    // into LDS: Bm's rows, then Cm's; ALL: all NP states are there
+    template <bool ALL>
     __device__ __forceinline__ void stage(float *lds, int states)
     {
 #pragma unroll
@@ -173,7 +184,7 @@ struct TileStates {
             const int e = index(i);
             Pack<float, V> f;
 #pragma unroll
-            for (int j = 0; j < V; ++j) f.v[j] = FULL || W::NP == V || e % W::NP < states ? r[i].get(j) : 0.f;
+            for (int j = 0; j < V; ++j) f.v[j] = ALL || e % W::NP < states ? r[i].get(j) : 0.f;
             if (2 * ROWS % (64 * V) == 0 || e < 2 * ROWS) *reinterpret_cast<Pack<float, V> *>(lds + e) = f;
         }
     }

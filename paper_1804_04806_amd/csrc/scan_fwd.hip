@@ -55,20 +55,21 @@ __global__ __launch_bounds__(64 * kWaves, 2) void scan_fwd_kernel(ScanParams p, 
 #pragma unroll
         for (int j = 0; j < NPL; ++j) A2[j] *= kLog2e;
         const long state_at = ((long)slot * d.D + ch) * d.N + at.n0;
-        auto seg_at = [&](int s) { return (((long)at.b * p.segs + s) * d.D + ch) * d.N + at.n0; };
+        auto seg_at = [&](int s) { return (((long)at.b * p.segs + s) * d.D + ch) * W::NP + at.n0; };
+        const bool mine = at.c < at.have;
         if (STATE_ONLY || p.segs == 1) {
             load_states<WIDE>(h, p.state_in + state_at, p.state_in && !idle && at.seg == 0 ? at.haven : 0);
             // state_out may be state_in: the second launch takes the first state from here
-            if (STATE_ONLY && at.seg == 0) store_states<WIDE>(p.seg_state + seg_at(0), h, at.haven);
+            if (STATE_ONLY && at.seg == 0) store_own(p.seg_state + seg_at(0), h, mine);
             if (STATE_ONLY)
 #pragma unroll
                 for (int j = 0; j < NPL; ++j) h[j] = 0.f;
         } else {
-            load_states<WIDE>(h, p.seg_state + seg_at(0), at.haven);
+            load_own(h, p.seg_state + seg_at(0), mine);
             for (int s = 0; s < at.seg; ++s) {
                 float end[NPL];
-                load_states<WIDE>(end, p.seg_state + seg_at(s + 1), at.haven);
-                join_segment(h, A2, at.c < at.have ? p.seg_step[((long)at.b * p.segs + s) * d.D + ch] : 0.f, end);
+                load_own(end, p.seg_state + seg_at(s + 1), mine);
+                join_segment(h, A2, mine ? p.seg_step[((long)at.b * p.segs + s) * d.D + ch] : 0.f, end);
             }
         }
         float bias[W::VE], skip[W::VE], steps = 0.f;
@@ -84,8 +85,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void scan_fwd_kernel(ScanParams p, 
         const char *z_at = row_base<T>(p.in.z, d.z_b, d.z_l, at, t_first);
         const char *bm_at = bc_base<T>(p.in.Bm, d.Bm_b, d.Bm_l, at, t_first, d.N), *cm_at = bc_base<T>(p.in.Cm, d.Cm_b, d.Cm_l, at, t_first, d.N);
         char *y_at = const_cast<char *>(row_base<T>(p.y, d.y_b, d.y_l, at, t_first));
-        float *saved_at = p.saved + (((long)at.b * p.tiles + tile0) * (kTile / kKeep) * d.D + at.first) * d.N;
-        const uint32_t state_off = (uint32_t)(at.c0 - at.first + at.c) * d.N + at.n0, y_off = row_offset<T>(at, d.y_l, kTile);
+        float *saved_at = p.saved + (((long)at.b * p.tiles + tile0) * (kTile / kKeep) * d.D + at.first) * W::NP;
+        const uint32_t state_off = (uint32_t)(at.c0 - at.first + at.c) * W::NP + at.n0, y_off = row_offset<T>(at, d.y_l, kTile);
         Raw<T, W::VE, WIDE> u, dt, z;
         TileStates<T, W, WIDE> bc;
         uint32_t u_off, dt_off, z_off;
@@ -110,7 +111,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void scan_fwd_kernel(ScanParams p, 
             bm_at += kTile * e * d.Bm_l;
             cm_at += kTile * e * d.Cm_l;
         };
-        // FULL: all tokens, channels and states of the segment are there, as is the rule.  Without masks and without branches around the stores, behind
+        // FULL: all tokens and channels of the segment are there, and in packs all states, as is the rule.  Without masks and without branches around the stores, behind
         // which the loads' arrival could only be told by waiting for the stores too.  SAVE: states are kept for Backward.
         auto walk = [&](auto full, auto save) {
             constexpr bool FULL = decltype(full)::value, SAVE = decltype(save)::value;
@@ -120,7 +121,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void scan_fwd_kernel(ScanParams p, 
                 const bool there = FULL || at.tok < left;
                 float ut[W::VE], zt[W::VE];
                 if (FULL || left > 0) {
-                    bc.template stage<FULL>(bm, d.N);
+                    bc.template stage<FULL && WIDE>(bm, d.N);
 #pragma unroll
                     for (int i = 0; i < W::VE; ++i) {
                         ut[i] = u.get(i);
@@ -137,8 +138,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void scan_fwd_kernel(ScanParams p, 
                     if (tile + 1 < tile1) load(tile + 1);
                     wave_lds_order();
                     auto keep = [&]() {
-                        store_states<WIDE, FULL>(saved_at + state_off, h, at.haven);
-                        saved_at += (long)d.D * d.N;
+                        store_own(saved_at + state_off, h, FULL || mine);
+                        saved_at += (long)d.D * W::NP;
                     };
                     if (SAVE) keep();
                     LaneSums<LPC> sums;
@@ -187,14 +188,15 @@ __global__ __launch_bounds__(64 * kWaves, 2) void scan_fwd_kernel(ScanParams p, 
                 }
             }
         };
-        const bool full = WIDE && n >= tile1 * kTile && at.have == W::CW && d.N == W::NP, save = !STATE_ONLY && p.saved;
-        if (full && save) walk(std::integral_constant<bool, WIDE>(), std::integral_constant<bool, !STATE_ONLY>());
-        else if (full) walk(std::integral_constant<bool, WIDE>(), std::false_type());
-        else if (save) walk(std::false_type(), std::integral_constant<bool, !STATE_ONLY>());
+        const bool full = n >= tile1 * kTile && at.have == W::CW && (!WIDE || d.N == W::NP), save = !STATE_ONLY && p.saved;
+        typedef std::integral_constant<bool, !STATE_ONLY> Save;
+        if (full && save) walk(std::true_type(), Save());
+        else if (full) walk(std::true_type(), std::false_type());
+        else if (save) walk(std::false_type(), Save());
         else walk(std::false_type(), std::false_type());
         if (STATE_ONLY) {
-            store_states<WIDE>(p.seg_state + seg_at(at.seg + 1), h, at.haven);
-            if (at.q == 0 && at.c < at.have) p.seg_step[((long)at.b * p.segs + at.seg) * d.D + ch] = steps;
+            store_own(p.seg_state + seg_at(at.seg + 1), h, mine);
+            if (at.q == 0 && mine) p.seg_step[((long)at.b * p.segs + at.seg) * d.D + ch] = steps;
         } else if (p.state_out && !idle && at.seg == p.segs - 1) {
             store_states<WIDE>(p.state_out + state_at, h, at.haven);
         }

@@ -50,7 +50,7 @@ __device__ __forceinline__ void store_pack(T *p, const Pack<T, N> &r, int have)
     }
 }
 
-// N elements as they come from memory, in words (WIDE: one load, all of them; otherwise a word each, the first `have` of them): a lane's prefetched
+// N elements as they come from memory, in words (WIDE: one load; otherwise a word each, the last of `have` of them again behind it): a lane's prefetched
 // values stay as they are until they are used.  As elements of 16 bits the compiler takes them apart, and waits for them, right behind the load.
 template <class T, int N, bool WIDE>
 struct Raw {
@@ -68,10 +68,9 @@ struct Raw {
         } else {
 #pragma unroll
             for (int i = 0; i < WORDS; ++i) {
-                w[i] = 0;
-                if (!WIDE && i >= have) continue;
-                if (sizeof(T) == 4) w[i] = *reinterpret_cast<const uint32_t *>(base + offset + 4 * i);
-                else w[i] = *reinterpret_cast<const uint16_t *>(base + offset + 2 * i);
+                const uint32_t at = offset + (uint32_t)sizeof(T) * (WIDE ? i : max(0, min(i, have - 1)));
+                if (sizeof(T) == 4) w[i] = *reinterpret_cast<const uint32_t *>(base + at);
+                else w[i] = *reinterpret_cast<const uint16_t *>(base + at);
             }
         }
     }
