@@ -6,22 +6,6 @@
 namespace ucd {
 using namespace seq;
 
-static bool wide_rows(const void *p, int64_t outer, int64_t inner, size_t e)
-{
-    return (uintptr_t)p % (4 * e) == 0 && outer % 4 == 0 && inner % 4 == 0;
-}
-
-bool scan_wide(const ucd_scan_t &d, const ucd_scan_in_t &in, const void *y, const float *state1, const float *state2, const ucd_scan_grad_t *g)
-{
-    const size_t e = d.dtype == 1 ? 2 : 4;
-    if (d.D / d.G % 4 != 0 || d.N % 4 != 0) return false;
-    if (!wide_rows(in.u, d.u_b, d.u_l, e) || !wide_rows(in.dt, d.dt_b, d.dt_l, e) || !wide_rows(in.Bm, d.Bm_b, d.Bm_l, e) ||
-        !wide_rows(in.Cm, d.Cm_b, d.Cm_l, e) || !wide_rows(in.z, d.z_b, d.z_l, e) || !wide_rows(y, d.y_b, d.y_l, e) ||
-        !wide_rows(in.A, 0, 0, 4) || !wide_rows(state1, 0, 0, 4) || !wide_rows(state2, 0, 0, 4))
-        return false;
-    return !g || (wide_rows(g->u, 0, 0, e) && wide_rows(g->dt, 0, 0, e) && wide_rows(g->z, 0, 0, e));
-}
-
 // The library's own buffers of states have NP of them to a channel, so that they are read in packs whatever N is.
 // Segments: a launch is waves of 64 / lanes channels that walk over all tokens, and 1024 of them give every SIMD one.  With fewer, sequences are cut
 // into segments that are scanned side by side, after a first launch over the states alone, which costs two thirds of the second; so much that four

@@ -76,7 +76,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void scan_bwd_kernel(ScanParams p, 
     const int low = lane % 16 / LPC;       // the channel bits of a lane within its row
 
     for (unsigned unit = blockIdx.x; unit < units; unit += gridDim.x) {
-        const ScanPlace<W> at(p, unit);
+        const ScanPlace<W> at(p, unit, WIDE);
         if (STATE_ONLY && at.seg == 0) continue;
         const int n = scan_length(p, at.b);
         const int tile0 = at.seg * p.seg_tiles, tile1 = min(p.tiles, tile0 + p.seg_tiles);
@@ -84,12 +84,12 @@ __global__ __launch_bounds__(64 * kWaves, 2) void scan_bwd_kernel(ScanParams p, 
         const bool mine = at.c < at.have;
 
         float A2[NPL], x[NPL], dA[NPL] = {};
-        load_states<WIDE>(A2, p.in.A + ch * d.N + at.n0, at.haven);
+        load_states(A2, p.in.A + ch * d.N + at.n0, at.haven);
 #pragma unroll
         for (int j = 0; j < NPL; ++j) A2[j] *= kLog2e;
         auto seg_at = [&](int s) { return (((long)at.b * p.segs + s) * d.D + ch) * W::NP + at.n0; };
         const long state_at = ((long)at.b * d.D + ch) * d.N + at.n0;
-        load_states<WIDE>(x, p.dstate_out + state_at, p.dstate_out && (at.seg == p.segs - 1 || !STATE_ONLY) ? at.haven : 0);
+        load_states(x, p.dstate_out + state_at, p.dstate_out && (at.seg == p.segs - 1 || !STATE_ONLY) ? at.haven : 0);
         if (!STATE_ONLY)
             for (int s = p.segs - 1; s > at.seg; --s) {
                 float end[NPL];
@@ -101,12 +101,10 @@ __global__ __launch_bounds__(64 * kWaves, 2) void scan_bwd_kernel(ScanParams p, 
                 } else join_segment(x, A2, mine ? p.seg_step[((long)at.b * p.segs + s) * d.D + ch] : 0.f, end);
             }
         float bias[W::VE], skip[W::VE], dskip[W::VE] = {}, dbias[W::VE] = {}, steps = 0.f;
-        bool channel[W::VE];
 #pragma unroll
         for (int i = 0; i < W::VE; ++i) {
-            channel[i] = at.ch0 + i < at.have;
-            bias[i] = channel[i] && p.in.dt_bias ? p.in.dt_bias[at.c0 + at.ch0 + i] : 0.f;
-            skip[i] = channel[i] && p.in.skip ? p.in.skip[at.c0 + at.ch0 + i] : 0.f;
+            bias[i] = at.channel[i] && p.in.dt_bias ? p.in.dt_bias[at.c0 + at.ch0 + i] : 0.f;
+            skip[i] = at.channel[i] && p.in.skip ? p.in.skip[at.c0 + at.ch0 + i] : 0.f;
         }
 
         const long t_last = (long)(tile1 - 1) * kTile, e = sizeof(T);      // of the last tile
@@ -119,7 +117,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void scan_bwd_kernel(ScanParams p, 
         const uint32_t state_off = (uint32_t)(at.c0 - at.first + at.c) * W::NP + at.n0;
         const uint32_t du_off = row_offset<T>(at, d.u_l, kTile), ddt_off = row_offset<T>(at, d.dt_l, kTile), dz_off = row_offset<T>(at, d.z_l, kTile);
         Raw<T, W::VE, WIDE> u, dt, z, dy;
-        TileStates<T, W, WIDE> bc;
+        TileStates<T, W> bc;
+        bc.clear(bm, d.N);
         float kept[kTile / kKeep][NPL];
         uint32_t u_off, dt_off, z_off, dy_off;
         auto place = [&](int last) {
@@ -152,7 +151,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void scan_bwd_kernel(ScanParams p, 
             cm_at -= kTile * e * d.Cm_l;
             saved_at -= (kTile / kKeep) * (long)d.D * W::NP;
         };
-        // FULL: all tokens and channels of the segment are there, and in packs all states, as is the rule (see Forward).
+        // FULL: all tokens and channels of the segment are there, as is the rule (see Forward).
         auto walk = [&](auto whole) {
         constexpr bool FULL = decltype(whole)::value;
         if (tile1 > tile0) load(tile1 - 1);
@@ -160,10 +159,10 @@ __global__ __launch_bounds__(64 * kWaves, 2) void scan_bwd_kernel(ScanParams p, 
             const int left = n - tile * kTile;
             float ut[W::VE], st[W::VE], rate[W::VE], dyp[W::VE], dzt[W::VE];
             if (FULL || left > 0) {
-                bc.template stage<FULL && WIDE>(bm, d.N);
+                bc.stage(bm, d.N);
 #pragma unroll
                 for (int i = 0; i < W::VE; ++i) {
-                    const bool there = FULL || (at.tok < left && channel[i]);
+                    const bool there = FULL || (at.tok < left && at.channel[i]);
                     ut[i] = u.get(i);
                     float s = dt.get(i) + bias[i], slope;
                     const float soft = softplus<T>(s, &slope);
@@ -179,8 +178,10 @@ __global__ __launch_bounds__(64 * kWaves, 2) void scan_bwd_kernel(ScanParams p, 
                     }
                     g = there ? g : 0.f;
                     dyp[i] = g;
-                    step[at.tok * W::CW + at.ch0 + i] = make_float2(s, there ? s * ut[i] : 0.f);
-                    dys[at.tok * W::CW + at.ch0 + i] = g;
+                    if (FULL || at.channel[i]) {
+                        step[at.tok * W::CW + at.ch0 + i] = make_float2(s, there ? s * ut[i] : 0.f);
+                        dys[at.tok * W::CW + at.ch0 + i] = g;
+                    }
                 }
                 float before[kTile / kKeep][NPL];
 #pragma unroll
@@ -283,15 +284,15 @@ __global__ __launch_bounds__(64 * kWaves, 2) void scan_bwd_kernel(ScanParams p, 
                 load(tile - 1);
             }
             if (!STATE_ONLY) {
-                const int o = at.tok * W::CW + at.ch0, have = at.tok < d.L - tile * kTile ? at.have - at.ch0 : 0;
+                const bool token = at.tok < d.L - tile * kTile;
                 Pack<T, W::VE> du, ddt, dz;
                 float g[W::VE], et[W::VE], yt[W::VE];
-                lds_row(g, gs + o);
-                lds_row(et, es + o);
-                if (GATE) lds_row(yt, ys + o);
+                lds_row<W, FULL>(g, gs, at);
+                lds_row<W, FULL>(et, es, at);
+                if (GATE) lds_row<W, FULL>(yt, ys, at);
 #pragma unroll
                 for (int i = 0; i < W::VE; ++i) {
-                    const bool there = FULL || (at.tok < left && channel[i]);
+                    const bool there = FULL || (at.tok < left && at.channel[i]);
                     const float rise = fmaf(et[i], kLn2, g[i] * ut[i]) * rate[i];
                     du.v[i] = from_f<T>(there ? fmaf(g[i], st[i], skip[i] * dyp[i]) : 0.f);
                     ddt.v[i] = from_f<T>(there ? rise : 0.f);
@@ -299,9 +300,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void scan_bwd_kernel(ScanParams p, 
                     dskip[i] += there ? dyp[i] * ut[i] : 0.f;
                     dbias[i] += there ? rise : 0.f;
                 }
-                store_row<T, W, WIDE, FULL>(du_at, du_off, du, have);
-                store_row<T, W, WIDE, FULL>(ddt_at, ddt_off, ddt, have);
-                if (GATE) store_row<T, W, WIDE, FULL>(dz_at, dz_off, dz, have);
+                store_row<T, W, WIDE, FULL>(du_at, du_off, du, at, token);
+                store_row<T, W, WIDE, FULL>(ddt_at, ddt_off, ddt, at, token);
+                if (GATE) store_row<T, W, WIDE, FULL>(dz_at, dz_off, dz, at, token);
                 du_at -= kTile * e * d.u_l;
                 ddt_at -= kTile * e * d.dt_l;
                 if (GATE) dz_at -= kTile * e * d.z_l;
@@ -324,13 +325,22 @@ __global__ __launch_bounds__(64 * kWaves, 2) void scan_bwd_kernel(ScanParams p, 
             }
         }
         };
-        if (n >= tile1 * kTile && at.have == W::CW && (!WIDE || d.N == W::NP)) walk(std::true_type());
-        else walk(std::false_type());
+        if (n >= tile1 * kTile && at.have == W::CW) {
+            walk(std::integral_constant<bool, WIDE>());
+        } else {
+            // channels that are not there add zeros to the sums
+#pragma unroll
+            for (int i = 0; i < W::VE; ++i) {
+                step[lane + i * 64] = make_float2(0.f, 0.f);
+                dys[lane + i * 64] = 0.f;
+            }
+            walk(std::false_type());
+        }
         if (STATE_ONLY) {
             store_own(p.seg_state + seg_at(at.seg), x, mine);
             if (at.q == 0 && mine) p.seg_step[((long)at.b * p.segs + at.seg) * d.D + ch] = steps;
         } else {
-            if (p.g.state && at.seg == 0) store_states<WIDE>(p.g.state + state_at, x, at.haven);
+            if (p.g.state && at.seg == 0) store_states(p.g.state + state_at, x, at.haven);
             float *o = p.part_w + (((long)at.b * p.segs + at.seg) * d.D) * (d.N + 2);
 #pragma unroll
             for (int j = 0; j < NPL; ++j)
@@ -342,7 +352,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void scan_bwd_kernel(ScanParams p, 
                     dskip[e] += __shfl_xor(dskip[e], k);
                     dbias[e] += __shfl_xor(dbias[e], k);
                 }
-                if (lane < W::LR && at.ch0 + e < at.have) {
+                if (lane < W::LR && at.channel[e]) {
                     float *w = o + (at.c0 + at.ch0 + e) * (long)(d.N + 2) + d.N;
                     w[0] = dskip[e];
                     w[1] = dbias[e];
@@ -428,7 +438,7 @@ hipError_t scan_bwd(const ucd_scan_t &d, const ucd_scan_in_t &in, const void *dy
     p.saved = const_cast<float *>(saved);
     p.g = g;
     p.add = add;
-    const bool wide = scan_wide(d, in, dy, dstate_out, g.state, &g);
+    const bool wide = scan_wide(d);
     return scan_by_states(d, [&](auto wave) {
         typedef decltype(wave) W;
         if (d.dtype == 1) return wide ? launch<bf16_t, W, true>(p, s) : launch<bf16_t, W, false>(p, s);

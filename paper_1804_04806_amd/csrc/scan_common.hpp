@@ -53,9 +53,13 @@ template <class W>
 struct ScanPlace {
     int b, seg, g, block;        // of the workgroup,
     int first, c0, have;         // its first channel, the wave's and how many of them there are
+    int base;                    // no pack of a row begins before this channel
     int c, q, n0, haven;         // the lane's channel within the wave, states from n0 on and how many of them there are
-    int tok, ch0;                // what the lane loads: token (of a pack of all lanes) and first channel within the wave
-    __device__ __forceinline__ ScanPlace(const ScanParams &p, unsigned unit)
+    // What the lane loads: token (of a pack of all lanes) and first channel within the wave.  The last packs of a group are moved back to its end: they
+    // may begin in another lane's channels, and then do the same as that lane, or in another wave's, which are left alone.
+    int tok, ch0;
+    bool channel[W::VE];         // is the wave's
+    __device__ __forceinline__ ScanPlace(const ScanParams &p, unsigned unit, bool wide)
     {
         const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
         block = unit % p.blocks;
@@ -76,6 +80,14 @@ struct ScanPlace {
         haven = haven < 0 ? 0 : haven < W::NPL ? haven : W::NPL;
         tok = lane / W::LR;
         ch0 = lane % W::LR * W::VE;
+        base = first;
+        if (wide) {
+            const int end = p.per_group - at;
+            ch0 = end - W::VE < ch0 ? end - W::VE : ch0;
+            base = first < W::VE ? 0 : first - W::VE;
+        }
+#pragma unroll
+        for (int i = 0; i < W::VE; ++i) channel[i] = ch0 + i >= 0 && ch0 + i < have;
     }
 };
 
@@ -87,41 +99,47 @@ __device__ __forceinline__ int scan_length(const ScanParams &p, int b)
 }
 
 // The lane's states, or coefficients of a channel's states.
-template <bool WIDE, int N>
+template <int N>
 __device__ __forceinline__ void load_states(float (&h)[N], const float *at, int haven)
 {
-    const Pack<float, N> r = load_pack<WIDE, float, N>(at, haven);
+    const Pack<float, N> r = haven == N ? loose_load<float, N>(at) : load_pack<false, float, N>(at, haven);
 #pragma unroll
     for (int j = 0; j < N; ++j) h[j] = r.v[j];
 }
 
-template <bool WIDE, int N>
+template <int N>
 __device__ __forceinline__ void store_states(float *at, const float (&h)[N], int haven)
 {
     Pack<float, N> r;
 #pragma unroll
     for (int j = 0; j < N; ++j) r.v[j] = h[j];
-    store_pack<WIDE, float, N>(at, r, haven);
+    if (haven == N) loose_store<float, N>(at, r);
+    else store_pack<false, float, N>(at, r, haven);
 }
 
 // The same in the library's own buffers, whose channels have NP states: always a whole pack.
 template <int N>
 __device__ __forceinline__ void load_own(float (&h)[N], const float *at, bool there)
 {
-    load_states<true, N>(h, at, there);
+    const Pack<float, N> r = load_pack<true, float, N>(at, there);
+#pragma unroll
+    for (int j = 0; j < N; ++j) h[j] = r.v[j];
 }
 template <int N>
 __device__ __forceinline__ void store_own(float *at, const float (&h)[N], bool there)
 {
-    store_states<true, N>(at, h, there);
+    Pack<float, N> r;
+#pragma unroll
+    for (int j = 0; j < N; ++j) r.v[j] = h[j];
+    store_pack<true, float, N>(at, r, there);
 }
 
-// Tokens behind the sequence's last repeat it and channels that are not there repeat the workgroup's first: what is loaded of them is masked where it
-// is used.  Offsets of a tile's elements from its first token and the workgroup's first channel are below 2^32 bytes (seq_api.cpp bounds the strides).
+// Tokens behind the sequence's last repeat it and (one by one) channels that are not there repeat the workgroup's first: what is loaded of them is
+// masked where it is used.  Offsets of a tile's elements from its first token and `base` are below 2^32 bytes (seq_api.cpp bounds the strides).
 template <class T, class W>
 __device__ __forceinline__ uint32_t row_offset(const ScanPlace<W> &at, long sl, int last)
 {
-    const int c = at.ch0 < at.have ? at.c0 - at.first + at.ch0 : 0;
+    const int c = at.ch0 < at.have ? at.c0 - at.base + at.ch0 : at.first - at.base;
     return ((uint32_t)min(at.tok, last) * (uint32_t)sl + (uint32_t)c) * (uint32_t)sizeof(T);
 }
 
@@ -130,7 +148,7 @@ __device__ __forceinline__ uint32_t row_offset(const ScanPlace<W> &at, long sl, 
 template <class T, class W>
 __device__ __forceinline__ const char *row_base(const void *base, long sb, long sl, const ScanPlace<W> &at, long t0)
 {
-    return (const char *)base + (at.b * sb + t0 * sl + at.first) * (long)sizeof(T);
+    return (const char *)base + (at.b * sb + t0 * sl + at.base) * (long)sizeof(T);
 }
 template <class T, class W>
 __device__ __forceinline__ const char *bc_base(const void *base, long sb, long sl, const ScanPlace<W> &at, long t0, int N)
@@ -138,30 +156,40 @@ __device__ __forceinline__ const char *bc_base(const void *base, long sb, long s
     return (const char *)base + (at.b * sb + t0 * sl + (long)at.g * N) * (long)sizeof(T);
 }
 
-template <class T, class W, bool WIDE, bool FULL = false>
-__device__ __forceinline__ void store_row(char *base, uint32_t offset, const Pack<T, W::VE> &v, int have)
+// WIDE: rows have a pack's elements before their end (see ScanPlace); FULL: they are the wave's, as is the token.
+template <class T, class W, bool WIDE, bool FULL>
+__device__ __forceinline__ void store_row(char *base, uint32_t offset, const Pack<T, W::VE> &v, const ScanPlace<W> &at, bool token)
 {
-    if (FULL) store_pack<WIDE, T, W::VE>(reinterpret_cast<T *>(base + offset), v, W::VE);
-    else store_pack<WIDE, T, W::VE>(reinterpret_cast<T *>(base + offset), v, have);
+    T *to = reinterpret_cast<T *>(base + offset);
+    if (FULL || (WIDE && token && at.ch0 >= 0)) {
+        loose_store<T, W::VE>(to, v);
+    } else if (token) {
+#pragma unroll
+        for (int i = 0; i < W::VE; ++i)
+            if (at.channel[i]) to[i] = v.v[i];
+    }
 }
 
-// A tile's Bm and Cm, 16 rows of NP states of one, then of the other; in packs of 4 or one by one.  States that are not there are 0.
-template <class T, class W, bool WIDE>
+// A tile's Bm and Cm, 16 rows of NP states of one, then of the other, in packs of 4; a row's last pack is moved back to its end.  Up to 4 states: one by
+// one.  In LDS a row's states behind the N-th stay 0.
+template <class T, class W>
 struct TileStates {
-    static constexpr int V = WIDE ? 4 : 1, P = (W::BE + V - 1) / V, ROWS = kTile * W::NP;
+    static constexpr int V = W::NP > 4 ? 4 : 1, P = W::BE / V, ROWS = kTile * W::NP;
+    static_assert(2 * ROWS == 64 * V * P, "all lanes have a pack");
     static constexpr bool WHOLE = ROWS % (64 * V) == 0;      // a pack of all lanes is of one tensor
-    Raw<T, V, WIDE> r[P];
+    Raw<T, V, true> r[P];
     uint32_t offset[P];
 
     static __device__ __forceinline__ int index(int i) { return (i * 64 + (int)threadIdx.x % 64) * V; }
     static __device__ __forceinline__ bool second(int i) { return WHOLE ? i * 64 * V >= ROWS : index(i) >= ROWS; }
+    static __device__ __forceinline__ int state(int e, int states) { return min(e % W::NP, states - V); }
 
     __device__ __forceinline__ void place(const ScanParams &p, int last)
     {
 #pragma unroll
         for (int i = 0; i < P; ++i) {
-            const int e = index(i), k = e % W::NP, t = min(e / W::NP % kTile, last);
-            offset[i] = ((uint32_t)t * (uint32_t)(second(i) ? p.d.Cm_l : p.d.Bm_l) + (k < p.d.N ? (uint32_t)k : 0u)) * (uint32_t)sizeof(T);
+            const int e = index(i), t = min(e / W::NP % kTile, last);
+            offset[i] = ((uint32_t)t * (uint32_t)(second(i) ? p.d.Cm_l : p.d.Bm_l) + (uint32_t)state(e, p.d.N)) * (uint32_t)sizeof(T);
         }
     }
 
@@ -175,8 +203,13 @@ struct TileStates {
         }
     }
 
-    // into LDS: Bm's rows, then Cm's; ALL: all NP states are there
-    template <bool ALL>
+    // before the first tile
+    static __device__ __forceinline__ void clear(float *lds, int states)
+    {
+        if (states == W::NP) return;
+#pragma unroll
+        for (int i = 0; i < P * V; ++i) lds[i * 64 + (int)threadIdx.x % 64] = 0.f;
+    }
     __device__ __forceinline__ void stage(float *lds, int states)
     {
 #pragma unroll
@@ -184,19 +217,25 @@ struct TileStates {
             const int e = index(i);
             Pack<float, V> f;
 #pragma unroll
-            for (int j = 0; j < V; ++j) f.v[j] = ALL || e % W::NP < states ? r[i].get(j) : 0.f;
-            if (2 * ROWS % (64 * V) == 0 || e < 2 * ROWS) *reinterpret_cast<Pack<float, V> *>(lds + e) = f;
+            for (int j = 0; j < V; ++j) f.v[j] = r[i].get(j);
+            loose_store<float, V>(lds + e - e % W::NP + state(e, states), f);
         }
     }
 };
 
-// VE neighbours of a tile's row in LDS
-template <int N>
-__device__ __forceinline__ void lds_row(float (&v)[N], const float *at)
+// What a lane takes from its token's row in LDS; FULL: all of it is the wave's.
+template <class W, bool FULL>
+__device__ __forceinline__ void lds_row(float (&v)[W::VE], const float *rows, const ScanPlace<W> &at)
 {
-    const Pack<float, N> r = *reinterpret_cast<const Pack<float, N> *>(at);
+    const float *row = rows + at.tok * W::CW;
+    if (FULL) {
+        const Pack<float, W::VE> r = *reinterpret_cast<const Pack<float, W::VE> *>(row + at.ch0);
 #pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = r.v[i];
+        for (int i = 0; i < W::VE; ++i) v[i] = r.v[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < W::VE; ++i) v[i] = row[max(at.ch0 + i, 0)];
+    }
 }
 
 // The decay of a lane's states over a whole segment, whose steps add up to `step`, and its own end state on top.
@@ -209,8 +248,8 @@ __device__ __forceinline__ void join_segment(float (&h)[N], const float (&A2)[N]
 
 }  // namespace seq
 
-// Whether rows and states can be read in packs of 4 (a pack of a row lies inside a group, and so one of Bm and Cm).
-bool scan_wide(const ucd_scan_t &d, const ucd_scan_in_t &in, const void *y, const float *state1, const float *state2, const ucd_scan_grad_t *g);
+// Whether rows can be read in packs of 4.
+inline bool scan_wide(const ucd_scan_t &d) { return d.D / d.G >= 4; }
 void scan_params(const ucd_scan_t &d, const ucd_scan_in_t &in, int dir, void *ws, seq::ScanParams &p);
 // workgroups of a launch, below 2^31 (seq_api.cpp)
 inline unsigned scan_units(const seq::ScanParams &p) { return (unsigned)p.d.B * p.segs * p.d.G * p.blocks; }

@@ -42,7 +42,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void scan_fwd_kernel(ScanParams p, 
     const ucd_scan_t &d = p.d;
 
     for (unsigned unit = blockIdx.x; unit < units; unit += gridDim.x) {
-        const ScanPlace<W> at(p, unit);
+        const ScanPlace<W> at(p, unit, WIDE);
         if (at.have == 0 || (STATE_ONLY && at.seg == p.segs - 1)) continue;     // nobody needs the last segment's end
         const int slot = p.in.slots ? p.in.slots[at.b] : at.b;
         const bool idle = p.in.slots && (slot < 0 || slot >= d.n_slots);
@@ -51,14 +51,14 @@ __global__ __launch_bounds__(64 * kWaves, 2) void scan_fwd_kernel(ScanParams p, 
         const long ch = at.c0 + at.c;
 
         float A2[NPL], h[NPL];
-        load_states<WIDE>(A2, p.in.A + ch * d.N + at.n0, at.haven);
+        load_states(A2, p.in.A + ch * d.N + at.n0, at.haven);
 #pragma unroll
         for (int j = 0; j < NPL; ++j) A2[j] *= kLog2e;
         const long state_at = ((long)slot * d.D + ch) * d.N + at.n0;
         auto seg_at = [&](int s) { return (((long)at.b * p.segs + s) * d.D + ch) * W::NP + at.n0; };
         const bool mine = at.c < at.have;
         if (STATE_ONLY || p.segs == 1) {
-            load_states<WIDE>(h, p.state_in + state_at, p.state_in && !idle && at.seg == 0 ? at.haven : 0);
+            load_states(h, p.state_in + state_at, p.state_in && !idle && at.seg == 0 ? at.haven : 0);
             // state_out may be state_in: the second launch takes the first state from here
             if (STATE_ONLY && at.seg == 0) store_own(p.seg_state + seg_at(0), h, mine);
             if (STATE_ONLY)
@@ -75,7 +75,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void scan_fwd_kernel(ScanParams p, 
         float bias[W::VE], skip[W::VE], steps = 0.f;
 #pragma unroll
         for (int i = 0; i < W::VE; ++i) {
-            const bool have = at.ch0 + i < at.have;
+            const bool have = at.channel[i];
             bias[i] = have && p.in.dt_bias ? p.in.dt_bias[at.c0 + at.ch0 + i] : 0.f;
             skip[i] = have && p.in.skip ? p.in.skip[at.c0 + at.ch0 + i] : 0.f;
         }
@@ -88,7 +88,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void scan_fwd_kernel(ScanParams p, 
         float *saved_at = p.saved + (((long)at.b * p.tiles + tile0) * (kTile / kKeep) * d.D + at.first) * W::NP;
         const uint32_t state_off = (uint32_t)(at.c0 - at.first + at.c) * W::NP + at.n0, y_off = row_offset<T>(at, d.y_l, kTile);
         Raw<T, W::VE, WIDE> u, dt, z;
-        TileStates<T, W, WIDE> bc;
+        TileStates<T, W> bc;
+        bc.clear(bm, d.N);
         uint32_t u_off, dt_off, z_off;
         auto place = [&](int last) {
             u_off = row_offset<T>(at, d.u_l, last);
@@ -111,8 +112,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void scan_fwd_kernel(ScanParams p, 
             bm_at += kTile * e * d.Bm_l;
             cm_at += kTile * e * d.Cm_l;
         };
-        // FULL: all tokens and channels of the segment are there, and in packs all states, as is the rule.  Without masks and without branches around the stores, behind
-        // which the loads' arrival could only be told by waiting for the stores too.  SAVE: states are kept for Backward.
+        // FULL: all tokens and channels of the segment are there, as is the rule.  Without masks and without branches around the stores, behind which the
+        // loads' arrival could only be told by waiting for the stores too.  SAVE: states are kept for Backward.
         auto walk = [&](auto full, auto save) {
             constexpr bool FULL = decltype(full)::value, SAVE = decltype(save)::value;
             load(tile0);
@@ -121,7 +122,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void scan_fwd_kernel(ScanParams p, 
                 const bool there = FULL || at.tok < left;
                 float ut[W::VE], zt[W::VE];
                 if (FULL || left > 0) {
-                    bc.template stage<FULL && WIDE>(bm, d.N);
+                    bc.stage(bm, d.N);
 #pragma unroll
                     for (int i = 0; i < W::VE; ++i) {
                         ut[i] = u.get(i);
@@ -129,7 +130,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void scan_fwd_kernel(ScanParams p, 
                         const float soft = softplus<T>(s);
                         s = d.softplus ? soft : s;
                         s = there ? s : 0.f;     // padding: the state stays
-                        step[at.tok * W::CW + at.ch0 + i] = make_float2(s, there ? s * ut[i] : 0.f);
+                        if (FULL || at.channel[i]) step[at.tok * W::CW + at.ch0 + i] = make_float2(s, there ? s * ut[i] : 0.f);
                         if (GATE) {
                             const float v = z.get(i);
                             zt[i] = v * sigmoid(v);
@@ -175,30 +176,30 @@ __global__ __launch_bounds__(64 * kWaves, 2) void scan_fwd_kernel(ScanParams p, 
                 if (!STATE_ONLY) {
                     Pack<T, W::VE> out;
                     float yt[W::VE];
-                    lds_row(yt, ys + at.tok * W::CW + at.ch0);
+                    lds_row<W, FULL>(yt, ys, at);
 #pragma unroll
                     for (int i = 0; i < W::VE; ++i) {
                         float y = fmaf(skip[i], ut[i], yt[i]);
                         if (GATE) y *= zt[i];
                         out.v[i] = from_f<T>(there ? y : 0.f);
                     }
-                    store_row<T, W, WIDE, FULL>(y_at, y_off, out, at.tok < d.L - tile * kTile ? at.have - at.ch0 : 0);
+                    store_row<T, W, WIDE, FULL>(y_at, y_off, out, at, at.tok < d.L - tile * kTile);
                     y_at += kTile * e * d.y_l;
                     wave_lds_order();
                 }
             }
         };
-        const bool full = n >= tile1 * kTile && at.have == W::CW && (!WIDE || d.N == W::NP), save = !STATE_ONLY && p.saved;
+        const bool full = n >= tile1 * kTile && at.have == W::CW, save = !STATE_ONLY && p.saved;
         typedef std::integral_constant<bool, !STATE_ONLY> Save;
-        if (full && save) walk(std::true_type(), Save());
-        else if (full) walk(std::true_type(), std::false_type());
+        if (full && save) walk(std::integral_constant<bool, WIDE>(), Save());
+        else if (full) walk(std::integral_constant<bool, WIDE>(), std::false_type());
         else if (save) walk(std::false_type(), Save());
         else walk(std::false_type(), std::false_type());
         if (STATE_ONLY) {
             store_own(p.seg_state + seg_at(at.seg + 1), h, mine);
             if (at.q == 0 && mine) p.seg_step[((long)at.b * p.segs + at.seg) * d.D + ch] = steps;
         } else if (p.state_out && !idle && at.seg == p.segs - 1) {
-            store_states<WIDE>(p.state_out + state_at, h, at.haven);
+            store_states(p.state_out + state_at, h, at.haven);
         }
     }
 }
@@ -229,7 +230,7 @@ hipError_t scan_fwd(const ucd_scan_t &d, const ucd_scan_in_t &in, const float *s
     p.state_out = state_out;
     p.y = y;
     p.saved = saved;
-    const bool wide = scan_wide(d, in, y, state_in, state_out, nullptr);
+    const bool wide = scan_wide(d);
     return scan_by_states(d, [&](auto wave) {
         typedef decltype(wave) W;
         if (d.dtype == 1) return wide ? launch<bf16_t, W, true>(p, s) : launch<bf16_t, W, false>(p, s);

@@ -17,18 +17,33 @@ template <> __device__ __forceinline__ bf16_t from_f<bf16_t>(float v) { return (
 
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 
-// N neighbours: one load or store where WIDE says that their address is a multiple of their size, the first `have` of them otherwise.
+// N neighbours: one load or store where WIDE says that they are all there or none, the first `have` of them otherwise.  Global memory is read and
+// written in such packs from any element's address on.
 template <class T, int N>
 struct alignas(sizeof(T) * N) Pack {
     T v[N];
 };
+template <class T, int N>
+struct __attribute__((packed, aligned(sizeof(T)))) LoosePack {
+    T v[N];
+};
+template <class T, int N>
+__device__ __forceinline__ Pack<T, N> loose_load(const T *p)
+{
+    return __builtin_bit_cast(Pack<T, N>, *reinterpret_cast<const LoosePack<T, N> *>(p));
+}
+template <class T, int N>
+__device__ __forceinline__ void loose_store(T *p, const Pack<T, N> &r)
+{
+    *reinterpret_cast<LoosePack<T, N> *>(p) = __builtin_bit_cast(LoosePack<T, N>, r);
+}
 
 template <bool WIDE, class T, int N>
 __device__ __forceinline__ Pack<T, N> load_pack(const T *p, int have)
 {
     Pack<T, N> r;
     if (WIDE) {
-        if (have > 0) r = *reinterpret_cast<const Pack<T, N> *>(p);
+        if (have > 0) r = loose_load<T, N>(p);
         else
             for (int i = 0; i < N; ++i) r.v[i] = from_f<T>(0.f);
     } else {
@@ -42,7 +57,7 @@ template <bool WIDE, class T, int N>
 __device__ __forceinline__ void store_pack(T *p, const Pack<T, N> &r, int have)
 {
     if (WIDE) {
-        if (have > 0) *reinterpret_cast<Pack<T, N> *>(p) = r;
+        if (have > 0) loose_store<T, N>(p, r);
     } else {
 #pragma unroll
         for (int i = 0; i < N; ++i)
@@ -61,7 +76,9 @@ struct Raw {
     __device__ __forceinline__ void load(const char *base, uint32_t offset, int have)
     {
         if (PACKED) {
-            typedef Pack<uint32_t, WORDS> Words;
+            struct __attribute__((packed, aligned(sizeof(T)))) Words {
+                uint32_t v[WORDS];
+            };
             const Words r = *reinterpret_cast<const Words *>(base + offset);
 #pragma unroll
             for (int i = 0; i < WORDS; ++i) w[i] = r.v[i];
