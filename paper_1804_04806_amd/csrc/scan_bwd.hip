@@ -103,8 +103,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void scan_bwd_kernel(ScanParams p, 
         float bias[W::VE], skip[W::VE], dskip[W::VE] = {}, dbias[W::VE] = {}, steps = 0.f;
 #pragma unroll
         for (int i = 0; i < W::VE; ++i) {
-            bias[i] = at.channel[i] && p.in.dt_bias ? p.in.dt_bias[at.c0 + at.ch0 + i] : 0.f;
-            skip[i] = at.channel[i] && p.in.skip ? p.in.skip[at.c0 + at.ch0 + i] : 0.f;
+            bias[i] = at.channel(i) && p.in.dt_bias ? p.in.dt_bias[at.c0 + at.ch0 + i] : 0.f;
+            skip[i] = at.channel(i) && p.in.skip ? p.in.skip[at.c0 + at.ch0 + i] : 0.f;
         }
 
         const long t_last = (long)(tile1 - 1) * kTile, e = sizeof(T);      // of the last tile
@@ -115,7 +115,6 @@ __global__ __launch_bounds__(64 * kWaves, 2) void scan_bwd_kernel(ScanParams p, 
         char *dz_at = const_cast<char *>(row_base<T>(p.g.z, d.z_b, d.z_l, at, t_last));
         const float *saved_at = p.saved + (((long)at.b * p.tiles + tile1 - 1) * (kTile / kKeep) * d.D + at.first) * W::NP;
         const uint32_t state_off = (uint32_t)(at.c0 - at.first + at.c) * W::NP + at.n0;
-        const uint32_t du_off = row_offset<T>(at, d.u_l, kTile), ddt_off = row_offset<T>(at, d.dt_l, kTile), dz_off = row_offset<T>(at, d.z_l, kTile);
         Raw<T, W::VE, WIDE> u, dt, z, dy;
         TileStates<T, W> bc;
         bc.clear(bm, d.N);
@@ -129,10 +128,11 @@ __global__ __launch_bounds__(64 * kWaves, 2) void scan_bwd_kernel(ScanParams p, 
             bc.place(p, last);
         };
         place(kTile);
-        auto load = [&](int tile) {      // and on to the tile before it
+        auto load = [&](int tile, auto whole) {      // and on to the tile before it; whole: all its tokens are there
+            constexpr bool FULL = decltype(whole)::value;
             const int left = n - tile * kTile;
-            if (left > 0) {
-                if (left < kTile) place(left - 1);
+            if (FULL || left > 0) {
+                if (!FULL && left < kTile) place(left - 1);
                 u.load(u_at, u_off, at.have - at.ch0);
                 dt.load(dt_at, dt_off, at.have - at.ch0);
                 dy.load(dy_at, dy_off, at.have - at.ch0);
@@ -141,7 +141,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void scan_bwd_kernel(ScanParams p, 
                 if (!STATE_ONLY)
 #pragma unroll
                     for (int i = 0; i < kTile / kKeep; ++i) load_own(kept[i], saved_at + i * (long)d.D * W::NP + state_off, mine);
-                if (left < kTile) place(kTile);
+                if (!FULL && left < kTile) place(kTile);
             }
             u_at -= kTile * e * d.u_l;
             dt_at -= kTile * e * d.dt_l;
@@ -154,7 +154,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void scan_bwd_kernel(ScanParams p, 
         // FULL: all tokens and channels of the segment are there, as is the rule (see Forward).
         auto walk = [&](auto whole) {
         constexpr bool FULL = decltype(whole)::value;
-        if (tile1 > tile0) load(tile1 - 1);
+        if (tile1 > tile0) load(tile1 - 1, whole);
         for (int tile = tile1 - 1; tile >= tile0; --tile) {
             const int left = n - tile * kTile;
             float ut[W::VE], st[W::VE], rate[W::VE], dyp[W::VE], dzt[W::VE];
@@ -162,7 +162,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void scan_bwd_kernel(ScanParams p, 
                 bc.stage(bm, d.N);
 #pragma unroll
                 for (int i = 0; i < W::VE; ++i) {
-                    const bool there = FULL || (at.tok < left && at.channel[i]);
+                    const bool there = FULL || (at.tok < left && at.channel(i));
                     ut[i] = u.get(i);
                     float s = dt.get(i) + bias[i], slope;
                     const float soft = softplus<T>(s, &slope);
@@ -178,7 +178,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void scan_bwd_kernel(ScanParams p, 
                     }
                     g = there ? g : 0.f;
                     dyp[i] = g;
-                    if (FULL || at.channel[i]) {
+                    if (FULL || at.channel(i)) {
                         step[at.tok * W::CW + at.ch0 + i] = make_float2(s, there ? s * ut[i] : 0.f);
                         dys[at.tok * W::CW + at.ch0 + i] = g;
                     }
@@ -188,7 +188,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void scan_bwd_kernel(ScanParams p, 
                 for (int i = 0; i < kTile / kKeep; ++i)
 #pragma unroll
                     for (int j = 0; j < NPL; ++j) before[i][j] = kept[i][j];
-                if (tile > tile0) load(tile - 1);
+                if (tile > tile0) load(tile - 1, whole);
                 wave_lds_order();
                 if (STATE_ONLY) {
 #pragma unroll
@@ -281,7 +281,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void scan_bwd_kernel(ScanParams p, 
                 }
                 wave_lds_order();
             } else if (tile > tile0) {
-                load(tile - 1);
+                load(tile - 1, whole);
             }
             if (!STATE_ONLY) {
                 const bool token = at.tok < d.L - tile * kTile;
@@ -292,7 +292,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void scan_bwd_kernel(ScanParams p, 
                 if (GATE) lds_row<W, FULL>(yt, ys, at);
 #pragma unroll
                 for (int i = 0; i < W::VE; ++i) {
-                    const bool there = FULL || (at.tok < left && at.channel[i]);
+                    const bool there = FULL || (at.tok < left && at.channel(i));
                     const float rise = fmaf(et[i], kLn2, g[i] * ut[i]) * rate[i];
                     du.v[i] = from_f<T>(there ? fmaf(g[i], st[i], skip[i] * dyp[i]) : 0.f);
                     ddt.v[i] = from_f<T>(there ? rise : 0.f);
@@ -300,9 +300,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void scan_bwd_kernel(ScanParams p, 
                     dskip[i] += there ? dyp[i] * ut[i] : 0.f;
                     dbias[i] += there ? rise : 0.f;
                 }
-                store_row<T, W, WIDE, FULL>(du_at, du_off, du, at, token);
-                store_row<T, W, WIDE, FULL>(ddt_at, ddt_off, ddt, at, token);
-                if (GATE) store_row<T, W, WIDE, FULL>(dz_at, dz_off, dz, at, token);
+                store_row<T, W, WIDE, FULL>(du_at, u_off, du, at, token);
+                store_row<T, W, WIDE, FULL>(ddt_at, dt_off, ddt, at, token);
+                if (GATE) store_row<T, W, WIDE, FULL>(dz_at, z_off, dz, at, token);
                 du_at -= kTile * e * d.u_l;
                 ddt_at -= kTile * e * d.dt_l;
                 if (GATE) dz_at -= kTile * e * d.z_l;
@@ -352,7 +352,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void scan_bwd_kernel(ScanParams p, 
                     dskip[e] += __shfl_xor(dskip[e], k);
                     dbias[e] += __shfl_xor(dbias[e], k);
                 }
-                if (lane < W::LR && at.channel[e]) {
+                if (lane < W::LR && at.channel(e)) {
                     float *w = o + (at.c0 + at.ch0 + e) * (long)(d.N + 2) + d.N;
                     w[0] = dskip[e];
                     w[1] = dbias[e];

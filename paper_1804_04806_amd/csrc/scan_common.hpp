@@ -58,7 +58,7 @@ struct ScanPlace {
     // What the lane loads: token (of a pack of all lanes) and first channel within the wave.  The last packs of a group are moved back to its end: they
     // may begin in another lane's channels, and then do the same as that lane, or in another wave's, which are left alone.
     int tok, ch0;
-    bool channel[W::VE];         // is the wave's
+    __device__ __forceinline__ bool channel(int i) const { return ch0 + i >= 0 && ch0 + i < have; }     // is the wave's
     __device__ __forceinline__ ScanPlace(const ScanParams &p, unsigned unit, bool wide)
     {
         const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
@@ -86,8 +86,6 @@ struct ScanPlace {
             ch0 = end - W::VE < ch0 ? end - W::VE : ch0;
             base = first < W::VE ? 0 : first - W::VE;
         }
-#pragma unroll
-        for (int i = 0; i < W::VE; ++i) channel[i] = ch0 + i >= 0 && ch0 + i < have;
     }
 };
 
@@ -166,7 +164,7 @@ __device__ __forceinline__ void store_row(char *base, uint32_t offset, const Pac
     } else if (token) {
 #pragma unroll
         for (int i = 0; i < W::VE; ++i)
-            if (at.channel[i]) to[i] = v.v[i];
+            if (at.channel(i)) to[i] = v.v[i];
     }
 }
 

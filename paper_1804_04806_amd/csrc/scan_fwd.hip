@@ -75,7 +75,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void scan_fwd_kernel(ScanParams p, 
         float bias[W::VE], skip[W::VE], steps = 0.f;
 #pragma unroll
         for (int i = 0; i < W::VE; ++i) {
-            const bool have = at.channel[i];
+            const bool have = at.channel(i);
             bias[i] = have && p.in.dt_bias ? p.in.dt_bias[at.c0 + at.ch0 + i] : 0.f;
             skip[i] = have && p.in.skip ? p.in.skip[at.c0 + at.ch0 + i] : 0.f;
         }
@@ -98,10 +98,11 @@ __global__ __launch_bounds__(64 * kWaves, 2) void scan_fwd_kernel(ScanParams p, 
             bc.place(p, last);
         };
         place(kTile);
-        auto load = [&](int tile) {      // and on to the next tile
+        auto load = [&](int tile, auto full) {      // and on to the next tile; full: all its tokens are there
+            constexpr bool FULL = decltype(full)::value;
             const int left = n - tile * kTile;
-            if (left <= 0) return;
-            if (left < kTile) place(left - 1);
+            if (!FULL && left <= 0) return;
+            if (!FULL && left < kTile) place(left - 1);
             u.load(u_at, u_off, at.have - at.ch0);
             dt.load(dt_at, dt_off, at.have - at.ch0);
             if (GATE) z.load(z_at, z_off, at.have - at.ch0);
@@ -116,7 +117,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void scan_fwd_kernel(ScanParams p, 
         // loads' arrival could only be told by waiting for the stores too.  SAVE: states are kept for Backward.
         auto walk = [&](auto full, auto save) {
             constexpr bool FULL = decltype(full)::value, SAVE = decltype(save)::value;
-            load(tile0);
+            if (tile1 > tile0) load(tile0, full);
             for (int tile = tile0; tile < tile1; ++tile) {
                 const int left = n - tile * kTile;
                 const bool there = FULL || at.tok < left;
@@ -130,13 +131,13 @@ __global__ __launch_bounds__(64 * kWaves, 2) void scan_fwd_kernel(ScanParams p, 
                         const float soft = softplus<T>(s);
                         s = d.softplus ? soft : s;
                         s = there ? s : 0.f;     // padding: the state stays
-                        if (FULL || at.channel[i]) step[at.tok * W::CW + at.ch0 + i] = make_float2(s, there ? s * ut[i] : 0.f);
+                        if (FULL || at.channel(i)) step[at.tok * W::CW + at.ch0 + i] = make_float2(s, there ? s * ut[i] : 0.f);
                         if (GATE) {
                             const float v = z.get(i);
                             zt[i] = v * sigmoid(v);
                         }
                     }
-                    if (tile + 1 < tile1) load(tile + 1);
+                    if (tile + 1 < tile1) load(tile + 1, full);
                     wave_lds_order();
                     auto keep = [&]() {
                         store_own(saved_at + state_off, h, FULL || mine);
