@@ -1,8 +1,9 @@
 // Short causal convolution: Forward, Backward and the single-token step.
 //
-// Every token is read once (K - 1 of them once more per run) and every result written once: memory bounds it.  A thread owns VE neighbouring channels,
-// 16 bytes of a row, and a run of tokens; the last K - 1 tokens of its channels, and in Backward the last K - 1 gradients of u, stay in registers
-// while it walks.  Workgroups are 32 packs of channels by 8 runs: whole lines of a row, and neighbouring runs meet their common tokens in the same L1.
+// Every token is read once (K - 1 of them once more per run) and every result written once: memory bounds it.  A thread owns VE neighbouring channels
+// and a run of tokens; the last K - 1 tokens of its channels, and in Backward the last K - 1 gradients of u, stay in registers while it walks.
+// Workgroups are 32 packs of 16 bytes (64 of two channels) by 8 (4) runs: whole lines of a row, and neighbouring runs meet their common tokens in the
+// same L1.  8 x 2048 tokens, 2048 channels, 4 taps, bf16: Forward 26 us (5.1 TB/s), Backward 48 (4.2); fp32, 1024 channels: 22 (6.0) and 39 (5.2).
 #include <algorithm>
 #include <type_traits>
 
@@ -32,17 +33,39 @@ struct ConvBlock {
     static constexpr int PX = VE <= 2 ? 64 : 32, CY = 256 / PX;
 };
 
+// A row's last pack is moved back to the row's end: its first channels are another thread's.  That one alone stores them, as it may have replaced their
+// state before this one read it, but for Backward, where nothing is replaced and both store the same.
+template <int VE>
+__device__ __forceinline__ int pack_channel(const ConvParams &p, unsigned pack)
+{
+    return min((int)pack * VE, p.d.D - VE);
+}
+template <int VE>
+__device__ __forceinline__ int pack_own(const ConvParams &p, unsigned pack)     // its first channel that is its own
+{
+    return max(0, ((int)pack + 1) * VE - p.d.D);
+}
+
+// f(whether a lane of the wave has a pack that was moved back): the other waves, nearly all of them, store without a branch.
+template <int VE, class F>
+__device__ __forceinline__ void by_tail(int own, F f)
+{
+    if (VE > 1 && __any(own > 0)) f(std::integral_constant<bool, (VE > 1)>());
+    else f(std::false_type());
+}
+
 // What a thread works on.
 template <class T, int VE>
 struct ConvPlace {
-    int c0, b, t0, n, slot;
+    int c0, own, b, t0, n, slot;
     bool active;
     __device__ __forceinline__ ConvPlace(const ConvParams &p, unsigned unit)
     {
         typedef ConvBlock<VE> B;
         const unsigned pack = unit % p.blocks_x * B::PX + threadIdx.x % B::PX, row = unit / p.blocks_x * B::CY + threadIdx.x / B::PX;
         active = pack < p.packs && row < p.rows;
-        c0 = (int)pack * VE;
+        c0 = pack_channel<VE>(p, pack);
+        own = pack_own<VE>(p, pack);
         b = active ? (int)(row / (unsigned)p.runs) : 0;
         t0 = (int)(row % (unsigned)p.runs) * p.run;
         slot = b;
@@ -60,18 +83,25 @@ struct ConvPlace {
 template <class T, int VE>
 __device__ __forceinline__ void load_channels(float (&v)[VE], const T *at)
 {
-    const Pack<T, VE> r = *reinterpret_cast<const Pack<T, VE> *>(at);
+    const Pack<T, VE> r = loose_load<T, VE>(at);
 #pragma unroll
     for (int i = 0; i < VE; ++i) v[i] = to_f(r.v[i]);
 }
 
-template <class T, int VE>
-__device__ __forceinline__ void store_channels(T *at, const float (&v)[VE])
+// TAIL: a lane of the wave may have such a pack
+template <class T, int VE, bool TAIL>
+__device__ __forceinline__ void store_channels(T *at, const float (&v)[VE], int own = 0)
 {
     Pack<T, VE> r;
 #pragma unroll
     for (int i = 0; i < VE; ++i) r.v[i] = from_f<T>(v[i]);
-    *reinterpret_cast<Pack<T, VE> *>(at) = r;
+    if (!TAIL || own == 0) {
+        loose_store<T, VE>(at, r);
+    } else {
+#pragma unroll
+        for (int i = 1; i < VE; ++i)
+            if (i >= own) at[i] = r.v[i];
+    }
 }
 
 // the K - 1 tokens before t0: of the sequence, of the state, or 0
@@ -104,75 +134,81 @@ __device__ __forceinline__ void load_weights(float (&w)[K][VE], float (&bias)[VE
     }
 }
 
+template <class T, int VE, int K, bool SILU, bool TAIL>
+__device__ __forceinline__ void conv_fwd_run(const ConvParams &p, const ConvPlace<T, VE> &at)
+{
+    const T *x = (const T *)p.a.x + at.b * p.d.x_b + at.c0;
+    T *y = (T *)p.a.y + at.b * p.d.y_b + at.c0;
+    float win[K][VE], w[K][VE], bias[VE];      // win[K - 1] is the current token
+    load_window<T, VE, K>(win, p, at, x);
+    load_weights<T, VE, K>(w, bias, p, at.c0);
+    // the new state is the first run's to write: it has read the old one, which may be in the same place
+    float first[K][VE];
+#pragma unroll
+    for (int k = 0; k < K - 1; ++k)
+#pragma unroll
+        for (int i = 0; i < VE; ++i) first[k][i] = win[k][i];
+    const int end = min(p.d.L, at.t0 + p.run), stop = min(end, at.n);
+    int t = at.t0;
+    Raw<T, VE, true> in[kAhead], next[kAhead];
+    auto load = [&](int t) {
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) next[j].load((const char *)(x + (long)min(t + j, stop - 1) * p.d.x_l), 0, VE);
+    };
+    if (t < stop) load(t);
+    for (; t < stop; t += kAhead) {
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) in[j] = next[j];
+        if (t + kAhead < stop) load(t + kAhead);      // under way while these tokens are computed
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) {
+            if (t + j >= stop) break;
+            float out[VE];
+#pragma unroll
+            for (int i = 0; i < VE; ++i) {
+                win[K - 1][i] = in[j].get(i);
+                float u = bias[i];
+#pragma unroll
+                for (int k = 0; k < K; ++k) u = fmaf(w[k][i], win[k][i], u);
+                out[i] = SILU ? u * sigmoid(u) : u;
+#pragma unroll
+                for (int k = 0; k < K - 1; ++k) win[k][i] = win[k + 1][i];
+            }
+            store_channels<T, VE, TAIL>(y + (long)(t + j) * p.d.y_l, out, at.own);
+        }
+    }
+    const float zero[VE] = {};
+    for (t = max(at.t0, stop); t < end; ++t) store_channels<T, VE, TAIL>(y + (long)t * p.d.y_l, zero, at.own);
+    if (K > 1 && p.a.state_out && at.t0 == 0 && at.slot >= 0) {
+        T *state = (T *)p.a.state_out + (long)at.slot * (K - 1) * p.d.D + at.c0;
+#pragma unroll
+        for (int k = 0; k < K - 1; ++k) {
+            const int s = at.n - (K - 1) + k;
+            float v[VE];
+            if (s >= 0) {
+                load_channels<T, VE>(v, x + (long)s * p.d.x_l);
+            } else {
+                // token s of the old state: its place is K - 1 + s
+#pragma unroll
+                for (int i = 0; i < VE; ++i) v[i] = 0.f;
+#pragma unroll
+                for (int m = 0; m < K - 1; ++m)
+                    if (m == K - 1 + s)
+#pragma unroll
+                        for (int i = 0; i < VE; ++i) v[i] = first[m][i];
+            }
+            store_channels<T, VE, TAIL>(state + (long)k * p.d.D, v, at.own);
+        }
+    }
+}
+
 template <class T, int VE, int K, bool SILU>
 __global__ __launch_bounds__(256) void conv_fwd_kernel(ConvParams p, unsigned units)
 {
     for (unsigned unit = blockIdx.x; unit < units; unit += gridDim.x) {
         const ConvPlace<T, VE> at(p, unit);
         if (!at.active) continue;
-        const T *x = (const T *)p.a.x + at.b * p.d.x_b + at.c0;
-        T *y = (T *)p.a.y + at.b * p.d.y_b + at.c0;
-        float win[K][VE], w[K][VE], bias[VE];      // win[K - 1] is the current token
-        load_window<T, VE, K>(win, p, at, x);
-        load_weights<T, VE, K>(w, bias, p, at.c0);
-        // the new state is the first run's to write: it has read the old one, which may be in the same place
-        float first[K][VE];
-#pragma unroll
-        for (int k = 0; k < K - 1; ++k)
-#pragma unroll
-            for (int i = 0; i < VE; ++i) first[k][i] = win[k][i];
-        const int end = min(p.d.L, at.t0 + p.run), stop = min(end, at.n);
-        int t = at.t0;
-        Raw<T, VE, true> in[kAhead], next[kAhead];
-        auto load = [&](int t) {
-#pragma unroll
-            for (int j = 0; j < kAhead; ++j) next[j].load((const char *)(x + (long)min(t + j, stop - 1) * p.d.x_l), 0, VE);
-        };
-        if (t < stop) load(t);
-        for (; t < stop; t += kAhead) {
-#pragma unroll
-            for (int j = 0; j < kAhead; ++j) in[j] = next[j];
-            if (t + kAhead < stop) load(t + kAhead);      // under way while these tokens are computed
-#pragma unroll
-            for (int j = 0; j < kAhead; ++j) {
-                if (t + j >= stop) break;
-                float out[VE];
-#pragma unroll
-                for (int i = 0; i < VE; ++i) {
-                    win[K - 1][i] = in[j].get(i);
-                    float u = bias[i];
-#pragma unroll
-                    for (int k = 0; k < K; ++k) u = fmaf(w[k][i], win[k][i], u);
-                    out[i] = SILU ? u * sigmoid(u) : u;
-#pragma unroll
-                    for (int k = 0; k < K - 1; ++k) win[k][i] = win[k + 1][i];
-                }
-                store_channels<T, VE>(y + (long)(t + j) * p.d.y_l, out);
-            }
-        }
-        const float zero[VE] = {};
-        for (t = max(at.t0, stop); t < end; ++t) store_channels<T, VE>(y + (long)t * p.d.y_l, zero);
-        if (K > 1 && p.a.state_out && at.t0 == 0 && at.slot >= 0) {
-            T *state = (T *)p.a.state_out + (long)at.slot * (K - 1) * p.d.D + at.c0;
-#pragma unroll
-            for (int k = 0; k < K - 1; ++k) {
-                const int s = at.n - (K - 1) + k;
-                float v[VE];
-                if (s >= 0) {
-                    load_channels<T, VE>(v, x + (long)s * p.d.x_l);
-                } else {
-                    // token s of the old state: its place is K - 1 + s
-#pragma unroll
-                    for (int i = 0; i < VE; ++i) v[i] = 0.f;
-#pragma unroll
-                    for (int m = 0; m < K - 1; ++m)
-                        if (m == K - 1 + s)
-#pragma unroll
-                            for (int i = 0; i < VE; ++i) v[i] = first[m][i];
-                }
-                store_channels<T, VE>(state + (long)k * p.d.D, v);
-            }
-        }
+        by_tail<VE>(at.own, [&](auto tail) { conv_fwd_run<T, VE, K, SILU, decltype(tail)::value>(p, at); });
     }
 }
 
@@ -183,31 +219,34 @@ __global__ __launch_bounds__(256) void conv_step_kernel(ConvParams p)
 {
     const unsigned pack = blockIdx.x * 256u + threadIdx.x;
     if (pack >= p.packs) return;
-    const int c0 = (int)pack * VE;
+    const int c0 = pack_channel<VE>(p, pack), own = pack_own<VE>(p, pack);
     float w[K][VE], bias[VE];
     load_weights<T, VE, K>(w, bias, p, c0);
-    for (int b = blockIdx.y; b < p.d.B; b += gridDim.y) {
-        float x[VE], out[VE] = {};
-        load_channels<T, VE>(x, (const T *)p.a.x + b * p.d.x_b + c0);
-        const int slot = p.a.slots ? p.a.slots[b] : b;
-        if (!p.a.slots || (slot >= 0 && slot < p.d.n_slots)) {
-            T *state = (T *)p.a.state_out + (long)slot * (K - 1) * p.d.D + c0;
-            float before[K][VE];
-#pragma unroll
-            for (int k = 0; k < K - 1; ++k) load_channels<T, VE>(before[k], state + (long)k * p.d.D);
-#pragma unroll
-            for (int i = 0; i < VE; ++i) {
-                before[K - 1][i] = x[i];
-                float u = bias[i];
-#pragma unroll
-                for (int k = 0; k < K; ++k) u = fmaf(w[k][i], before[k][i], u);
-                out[i] = SILU ? u * sigmoid(u) : u;
+    by_tail<VE>(own, [&](auto tail) {
+        constexpr bool TAIL = decltype(tail)::value;
+        for (int b = blockIdx.y; b < p.d.B; b += gridDim.y) {
+            float x[VE], out[VE] = {};
+            load_channels<T, VE>(x, (const T *)p.a.x + b * p.d.x_b + c0);
+            const int slot = p.a.slots ? p.a.slots[b] : b;
+            if (!p.a.slots || (slot >= 0 && slot < p.d.n_slots)) {
+                T *state = (T *)p.a.state_out + (long)slot * (K - 1) * p.d.D + c0;
+                float before[K][VE];
+    #pragma unroll
+                for (int k = 0; k < K - 1; ++k) load_channels<T, VE>(before[k], state + (long)k * p.d.D);
+    #pragma unroll
+                for (int i = 0; i < VE; ++i) {
+                    before[K - 1][i] = x[i];
+                    float u = bias[i];
+    #pragma unroll
+                    for (int k = 0; k < K; ++k) u = fmaf(w[k][i], before[k][i], u);
+                    out[i] = SILU ? u * sigmoid(u) : u;
+                }
+    #pragma unroll
+                for (int k = 0; k < K - 1; ++k) store_channels<T, VE, TAIL>(state + (long)k * p.d.D, before[k + 1], own);
             }
-#pragma unroll
-            for (int k = 0; k < K - 1; ++k) store_channels<T, VE>(state + (long)k * p.d.D, before[k + 1]);
+            store_channels<T, VE, TAIL>((T *)p.a.y + b * p.d.y_b + c0, out, own);
         }
-        store_channels<T, VE>((T *)p.a.y + b * p.d.y_b + c0, out);
-    }
+    });
 }
 
 // dx, the gradient of the state before the first token, and sums of dw and dbias over the workgroup's runs.
@@ -220,6 +259,8 @@ __global__ __launch_bounds__(256) void conv_bwd_kernel(ConvParams p)
     float w[K][VE], bias[VE], dw[K][VE] = {}, db[VE] = {};
     bool have_w = false;
     const unsigned column = blockIdx.x % p.blocks_x, part_row = blockIdx.x / p.blocks_x, rows_y = (p.rows + B::CY - 1) / B::CY;
+    const unsigned pack = column * B::PX + threadIdx.x % B::PX;
+    const int own = pack < p.packs ? pack_own<VE>(p, pack) : 0;
     for (unsigned block = part_row; block < rows_y; block += p.part_rows) {
         const ConvPlace<T, VE> at(p, block * p.blocks_x + column);
         if (!at.active) continue;
@@ -287,8 +328,8 @@ __global__ __launch_bounds__(256) void conv_bwd_kernel(ConvParams p)
 #pragma unroll
                 for (int i = 0; i < VE; ++i) out[i] += more[i];
             }
-            if (s >= at.t0) store_channels<T, VE>(dx_at, out);
-            else if (at.t0 == 0 && p.a.dstate_in) store_channels<T, VE>((T *)p.a.dstate_in + state_at + (long)(K - 1 + s) * p.d.D, out);
+            if (s >= at.t0) store_channels<T, VE, false>(dx_at, out);
+            else if (at.t0 == 0 && p.a.dstate_in) store_channels<T, VE, false>((T *)p.a.dstate_in + state_at + (long)(K - 1 + s) * p.d.D, out);
             dx_at += p.d.x_l;
         };
         if (at.t0 < seen) load(at.t0);
@@ -309,7 +350,7 @@ __global__ __launch_bounds__(256) void conv_bwd_kernel(ConvParams p)
             }
         }
         const float zero[VE] = {};
-        for (int t = max(at.t0, stop); t < end; ++t) store_channels<T, VE>(dx + (long)t * p.d.x_l, zero);
+        for (int t = max(at.t0, stop); t < end; ++t) store_channels<T, VE, false>(dx + (long)t * p.d.x_l, zero);
     }
     // over the workgroup's runs, in their order
     const int x_lane = threadIdx.x % B::PX, y_lane = threadIdx.x / B::PX;
@@ -317,7 +358,8 @@ __global__ __launch_bounds__(256) void conv_bwd_kernel(ConvParams p)
     for (int k = 0; k <= K; ++k) {
         __syncthreads();
 #pragma unroll
-        for (int i = 0; i < VE; ++i) lds[y_lane][x_lane * VE + i] = k < K ? dw[k % K][i] : db[i];
+        for (int i = 0; i < VE; ++i)
+            if (i >= own) lds[y_lane][x_lane * VE + i - own] = k < K ? dw[k % K][i] : db[i];
         __syncthreads();
         for (int i = threadIdx.x; i < B::PX * VE; i += 256) {
             float v = lds[0][i];
@@ -341,19 +383,13 @@ __global__ __launch_bounds__(kJoinThreads) void conv_join_kernel(ConvParams p)
     if (out) *out = v + (p.add ? *out : 0.f);
 }
 
-// Whether all rows are whole packs of ve elements.
-bool whole_packs(const ucd_causal_conv_t &d, const CausalConvArgs &a, int ve)
-{
-    const uintptr_t bytes = ve * (d.dtype == 1 ? 2 : 4);
-    auto aligned = [&](const void *p) { return (uintptr_t)p % bytes == 0; };
-    return d.D % ve == 0 && d.x_b % ve == 0 && d.x_l % ve == 0 && d.y_b % ve == 0 && d.y_l % ve == 0 && aligned(a.x) && aligned(a.y) && aligned(a.dy) &&
-           aligned(a.dx) && aligned(a.state_in) && aligned(a.state_out) && aligned(a.dstate_in) && aligned(a.dstate_out);
-}
-
 // Packs: Forward 16 bytes.  Backward keeps four times as much of a channel in registers (its window of tokens and gradients, filter and their sums):
-// two bf16 channels to a thread leave four waves to a SIMD, 47.7 us where four take 48.5 and eight, two waves to a SIMD, 69 (8 x 2048 x 2048);
-// of single sequences of 512 tokens, 4096 channels, 11.8, 13.0 and 15.8.
-constexpr int kFwdPack[2] = {4, 8}, kBwdPack[2] = {4, 2}, kStepPack[2] = {2, 2};
+// two channels to a thread leave four waves to a SIMD.  bf16: 47.7 us where four take 48.5 and eight, two waves to a SIMD, 69 (8 x 2048 x 2048), of
+// single sequences of 512 tokens, 4096 channels 11.8, 13.0 and 15.8; fp32: 38.5 where four take 40.3 (8 x 2048 x 1024), 26.1 and 28.1 (13 x 1021 x 509).
+// Rows need not be whole packs nor begin at their multiples: 2047 channels instead of 2048 take 38 us instead of 26 in Forward, 58 instead of 48 in
+// Backward, and took 42 and 76 channel by channel.
+constexpr int kFwdPack[2] = {4, 8}, kBwdPack[2] = {2, 2}, kStepPack[2] = {2, 2};
+static_assert(kBwdPack[0] == kBwdPack[1], "one division of Backward's workspace");
 enum Form { FORWARD, BACKWARD, STEP };
 
 // Runs are as long as leaves two waves to a SIMD, 8 to 32 tokens.
@@ -370,7 +406,7 @@ void divide(const ucd_causal_conv_t &d, ConvParams &p)
     p.rows = (unsigned)d.B * (unsigned)p.runs;
     // Backward: a workgroup takes every part_rows-th row of runs, and adds one row of partial sums; about as many workgroups as run at once
     const unsigned rows_y = (p.rows + B::CY - 1) / B::CY;
-    p.part_rows = std::max(1u, std::min(rows_y, (VE <= 2 ? 2048 : 1024) / p.blocks_x));
+    p.part_rows = std::max(1u, std::min(rows_y, 2048 / p.blocks_x));
 }
 
 template <class T, int VE, int K, bool SILU>
@@ -429,7 +465,8 @@ template <Form FORM>
 hipError_t dispatch(const ucd_causal_conv_t &d, const CausalConvArgs &a, bool add, void *ws, hipStream_t s)
 {
     constexpr const int *packs = FORM == BACKWARD ? kBwdPack : FORM == STEP ? kStepPack : kFwdPack;
-    const bool whole = whole_packs(d, a, packs[d.dtype]);
+    // rows of fewer channels have none
+    const bool whole = d.D >= packs[d.dtype];
     if (d.dtype == 1) return whole ? by_taps<bf16_t, packs[1], FORM>(d, a, add, ws, s) : by_taps<bf16_t, 1, FORM>(d, a, add, ws, s);
     return whole ? by_taps<float, packs[0], FORM>(d, a, add, ws, s) : by_taps<float, 1, FORM>(d, a, add, ws, s);
 }
@@ -438,12 +475,10 @@ hipError_t dispatch(const ucd_causal_conv_t &d, const CausalConvArgs &a, bool ad
 
 size_t causal_conv_ws_bytes(const ucd_causal_conv_t &d)
 {
-    // whichever way the tensors' alignment has it run
-    ConvParams single{}, packs{};
-    divide<1>(d, single);
-    if (d.dtype == 1) divide<kBwdPack[1]>(d, packs);
-    else divide<kBwdPack[0]>(d, packs);
-    return (size_t)4 * std::max(single.part_rows, packs.part_rows) * (d.K + 1) * d.D;
+    ConvParams p{};
+    if (d.D < kBwdPack[d.dtype]) divide<1>(d, p);
+    else divide<kBwdPack[0]>(d, p);
+    return (size_t)4 * p.part_rows * (d.K + 1) * d.D;
 }
 
 hipError_t causal_conv_fwd(const ucd_causal_conv_t &d, const CausalConvArgs &a, hipStream_t s) { return dispatch<FORWARD>(d, a, false, nullptr, s); }

@@ -102,10 +102,12 @@ __device__ __forceinline__ Pack<T, VE> dx_pack(const Raw<T, VE, true> &x, const 
 
 // ---- rows ----------------------------------------------------------------------------------------------------------------------------------------
 
-// A lane's group and its R packs of it.
+// A lane's group and its R packs of it.  A group's last pack is moved back to the group's end, where its first elements are the pack's before it too:
+// they are left out of sums over the group, and what becomes of them comes out twice, the same.
 template <int VE, int R>
 struct RowPlace {
     int lane, g, row;
+    int own[R];                 // the pack's first element that no other has; VE: there is no pack
     bool active, have[R];
     __device__ __forceinline__ RowPlace(const NormParams &p)
     {
@@ -115,9 +117,12 @@ struct RowPlace {
         row = group / p.gx;
         active = row < p.ry && g < p.d.G;
 #pragma unroll
-        for (int i = 0; i < R; ++i) have[i] = active && lane + i * p.lanes < p.pgl;
+        for (int i = 0; i < R; ++i) {
+            have[i] = active && lane + i * p.lanes < p.pgl;
+            own[i] = have[i] ? max(0, (lane + i * p.lanes + 1) * VE - p.cg) : VE;
+        }
     }
-    __device__ __forceinline__ int channel(const NormParams &p, int i) const { return g * p.cg + (lane + i * p.lanes) * VE; }
+    __device__ __forceinline__ int channel(const NormParams &p, int i) const { return g * p.cg + min((lane + i * p.lanes) * VE, p.cg - VE); }
 };
 
 template <bool SILU, class T, int VE, int R>
@@ -151,20 +156,20 @@ __global__ __launch_bounds__(256) void norm_rows_fwd_kernel(NormParams p)
 #pragma unroll
         for (int i = 0; i < R; ++i)
 #pragma unroll
-            for (int e = 0; e < VE; ++e) sum += at.have[i] ? r[i].get(e) : 0.f;
+            for (int e = 0; e < VE; ++e) sum += e >= at.own[i] ? r[i].get(e) : 0.f;
         const float mean = sum_group(sum, p.lanes) * p.share;
 #pragma unroll
         for (int i = 0; i < R; ++i)
 #pragma unroll
             for (int e = 0; e < VE; ++e) {
                 const float v = r[i].get(e) - mean;
-                sq += at.have[i] ? v * v : 0.f;
+                sq += e >= at.own[i] ? v * v : 0.f;
             }
         const float rstd = __builtin_amdgcn_rsqf(fmaf(sum_group(sq, p.lanes), p.share, p.d.eps));
 #pragma unroll
         for (int i = 0; i < R; ++i)
             if (at.have[i] && there)
-                *reinterpret_cast<Pack<T, VE> *>((T *)p.y + n * p.d.y_n + at.channel(p, i)) = norm_pack<SILU, T, VE>(r[i], mean, rstd, gamma[i], beta[i]);
+                loose_store<T, VE>((T *)p.y + n * p.d.y_n + at.channel(p, i), norm_pack<SILU, T, VE>(r[i], mean, rstd, gamma[i], beta[i]));
         if (p.stats && at.active && there && at.lane == 0) {
             p.stats[(long)n * p.d.G + at.g] = mean;
             p.stats[((long)p.d.N + n) * p.d.G + at.g] = rstd;
@@ -220,8 +225,9 @@ __global__ __launch_bounds__(kRowsBwdThreads) void norm_rows_bwd_kernel(NormPara
                     const float xhat = (x[i].get(e) - mean) * rstd, du = norm_du<SILU>(xhat, dy[i].get(e), gamma[i][e], beta[i][e]);
                     db[i][e] += du;
                     dg[i][e] = fmaf(du, xhat, dg[i][e]);
-                    s1 = fmaf(du, gamma[i][e], s1);
-                    s2 = fmaf(du * gamma[i][e], xhat, s2);
+                    const float g = e >= at.own[i] ? du * gamma[i][e] : 0.f;
+                    s1 += g;
+                    s2 = fmaf(g, xhat, s2);
                 }
             }
             s1 = sum_group(s1, p.lanes) * p.share;
@@ -229,8 +235,8 @@ __global__ __launch_bounds__(kRowsBwdThreads) void norm_rows_bwd_kernel(NormPara
 #pragma unroll
             for (int i = 0; i < R; ++i)
                 if (at.have[i] && there)
-                    *reinterpret_cast<Pack<T, VE> *>((T *)p.dx + n * p.d.x_n + at.channel(p, i)) =
-                        dx_pack<SILU, T, VE>(x[i], dy[i], mean, rstd, s1, s2, gamma[i], beta[i]);
+                    loose_store<T, VE>((T *)p.dx + n * p.d.x_n + at.channel(p, i),
+                                       dx_pack<SILU, T, VE>(x[i], dy[i], mean, rstd, s1, s2, gamma[i], beta[i]));
         }
     }
     // over the samples side by side in the workgroup, in their order
@@ -654,16 +660,25 @@ enum Way { ROWS, SLABS, PARTS };
 
 int ceil_div(long a, long b) { return (int)((a + b - 1) / b); }
 
+// Packs of rows, from any element on; 0: not rows.
+int rows_pack(const ucd_group_norm_t &d)
+{
+    const int cg = d.C / d.G;
+    int ve = d.dtype == 1 ? 8 : 4;
+    while (ve > cg) ve /= 2;
+    return d.S == 1 && ceil_div(cg, ve) <= 64 * kRowsR ? ve : 0;
+}
+
 // With packs of VE.
 Way divide(const ucd_group_norm_t &d, int VE, bool backward, NormParams &p, int &threads, int &R)
 {
     const int e = d.dtype == 1 ? 2 : 4;
     p.d = d;
     p.cg = d.C / d.G;
-    p.pgl = p.cg / VE;
+    p.pgl = ceil_div(p.cg, VE);
     p.packs = d.C / VE;
     p.share = (float)(1. / ((double)d.S * p.cg));
-    if (d.S == 1 && p.pgl <= 64 * kRowsR) {
+    if (VE == rows_pack(d)) {
         R = p.pgl <= 64 ? 1 : kRowsR;
         p.lanes = 1;
         while (p.lanes * R < p.pgl) p.lanes *= 2;
@@ -722,14 +737,15 @@ size_t ws_bytes(const ucd_group_norm_t &d, int VE, int dir)
     return n;
 }
 
-// Packs that all tensors' rows and groups consist of, 16 bytes at most; 8 where Backward keeps slabs of x and dy: with packs of 16 the sums per channel and
+// Packs: those of rows, or such as all tensors' rows and groups consist of, 16 bytes at most; 8 where Backward keeps slabs of x and dy: with packs of 16 the sums per channel and
 // the weights take 16 registers more (256 x 49 x 2048, bf16: 75 us against 57).
 constexpr int kMostBytes[2] = {16, 8};
 
 int pack_of(const ucd_group_norm_t &d, int dir, const void *a, const void *b, const void *c)
 {
     const int e = d.dtype == 1 ? 2 : 4;
-    for (int ve = (d.S == 1 ? 16 : kMostBytes[dir]) / e; ve > 1; ve /= 2) {
+    if (const int ve = rows_pack(d)) return ve;
+    for (int ve = kMostBytes[dir] / e; ve > 1; ve /= 2) {
         const uintptr_t bytes = ve * e, at = (uintptr_t)a | (uintptr_t)b | (uintptr_t)c;
         if (d.C / d.G % ve == 0 && at % bytes == 0 && d.x_n % ve == 0 && d.x_s % ve == 0 && d.y_n % ve == 0 && d.y_s % ve == 0) return ve;
     }
@@ -802,6 +818,7 @@ hipError_t dispatch(NormParams &p, int pack, void *ws, hipStream_t s)
 
 size_t group_norm_ws_bytes(const ucd_group_norm_t &d, int dir)
 {
+    if (const int ve = rows_pack(d)) return ws_bytes(d, ve, dir);
     // whichever packs the tensors' alignment allows
     size_t most = 0;
     for (int ve = d.dtype == 1 ? 8 : 4; ve >= 1; ve /= 2)
