@@ -38,7 +38,7 @@ struct NormParams {
     float *sums;                 // parts: [N][chunks][G * cs][2]: Forward mean and squares around it, Backward the two sums of dx
     float *dgamma, *dbeta;
     bool add;
-    int cg, pgl, packs;          // channels of a group, packs of a group and of all
+    int cg, pgl;                 // channels and packs of a group
     float share;                 // 1 / a group's elements
     int part_rows;               // rows of workgroups that share out the samples
     // rows
@@ -273,30 +273,38 @@ __device__ __forceinline__ bool strip_of(unsigned block, int strips, int rows, i
     return row < rows;
 }
 
+// The first channel of a group's k-th pack; the last is moved back to the group's end, as in rows.
+template <int VE>
+__device__ __forceinline__ int pack_channel(const NormParams &p, int g, int k)
+{
+    return g * p.cg + min(k * VE, p.cg - VE);
+}
+
 // A thread's pack of a strip and its positions.
 template <int VE>
 struct SlabPlace {
     int strip, local, g, c0, ty;     // local: the group within the strip
+    int own;                         // as in rows; only where groups are no whole packs
     bool active;
     __device__ __forceinline__ SlabPlace(const NormParams &p, int strip_) : strip(strip_)
     {
         const int tx = threadIdx.x % p.px;
         ty = threadIdx.x / p.px;
         active = ty < p.py;
-        int pack;
+        int k;
         if (p.cs > 1) {
-            const int k = strip % p.cs * p.px + tx;
+            k = strip % p.cs * p.px + tx;
             g = strip / p.cs;
             local = 0;
-            pack = g * p.pgl + k;
             active = active && k < p.pgl;
         } else {
-            pack = strip * p.px + tx;
             local = tx / p.pgl;       // < gps
+            k = tx % p.pgl;
             g = strip * p.gps + local;
-            active = active && pack < p.packs;
+            active = active && g < p.d.G;
         }
-        c0 = pack * VE;
+        c0 = pack_channel<VE>(p, g, k);
+        own = max(0, (k + 1) * VE - p.cg);
     }
 };
 
@@ -382,14 +390,14 @@ struct Slab {
 };
 
 // A part's mean and the squares around it, in every thread of its group.
-template <class T, int VE, int R>
+template <bool TAIL, class T, int VE, int R>
 __device__ __forceinline__ float2 slab_moments(const NormParams &p, Slab<T, VE, R> &x, const SlabPlace<VE> &at, int count, float share)
 {
     float sum = 0.f, sq = 0.f;
 #pragma unroll
     for (int i = 0; i < R; ++i)
 #pragma unroll
-        for (int e = 0; e < VE; ++e) sum += x.r[i].get(e);
+        for (int e = 0; e < VE; ++e) sum += !TAIL || e >= at.own ? x.r[i].get(e) : 0.f;
     const float mean = sum_slab(p, sum, 0.f, at.active, at.local).x * share;
     x.fresh();
     int s = at.ty;
@@ -399,7 +407,7 @@ __device__ __forceinline__ float2 slab_moments(const NormParams &p, Slab<T, VE, 
         float part = 0.f;
 #pragma unroll
         for (int e = 0; e < VE; ++e) {
-            const float v = x.r[i].get(e) - mean;
+            const float v = !TAIL || e >= at.own ? x.r[i].get(e) - mean : 0.f;
             part = fmaf(v, v, part);
         }
         sq += s < count ? part : 0.f;
@@ -414,7 +422,7 @@ __device__ __forceinline__ void slab_store_y(const NormParams &p, const Slab<T, 
 {
     slab_pass<T, R>(p.y, p.d.y_n, p.d.y_s, p, at.active, at.ty, at.c0, n, s0, count, [&](int i, bool there, T *q) {
         const Pack<T, VE> out = norm_pack<SILU, T, VE>(x.r[i], mean, rstd, gamma, beta);
-        if (there) *reinterpret_cast<Pack<T, VE> *>(q) = out;
+        if (there) loose_store<T, VE>(q, out);
     });
 }
 
@@ -425,7 +433,7 @@ __device__ __forceinline__ bool leads(const NormParams &p, const SlabPlace<VE> &
     return at.active && at.ty == 0 && (p.cs > 1 ? threadIdx.x == 0 : threadIdx.x % p.px == at.local * p.pgl);
 }
 
-template <bool SILU, class T, int VE, int R>
+template <bool SILU, bool TAIL, class T, int VE, int R>
 __global__ __launch_bounds__(kMaxThreads, (slab_waves<T, VE, R>())) void norm_slab_fwd_kernel(NormParams p)
 {
     int strip, first;
@@ -434,7 +442,7 @@ __global__ __launch_bounds__(kMaxThreads, (slab_waves<T, VE, R>())) void norm_sl
     for (int n = first; n < p.d.N; n += p.part_rows) {
         Slab<T, VE, R> x;
         x.load(p.x, p.d.x_n, p.d.x_s, p, at, n, 0, p.d.S);
-        const float2 m = slab_moments<T, VE, R>(p, x, at, p.d.S, p.share);
+        const float2 m = slab_moments<TAIL, T, VE, R>(p, x, at, p.d.S, p.share);
         const float rstd = __builtin_amdgcn_rsqf(fmaf(m.y, p.share, p.d.eps));
         float gamma[VE] = {}, beta[VE] = {};
         if (at.active) {
@@ -450,7 +458,7 @@ __global__ __launch_bounds__(kMaxThreads, (slab_waves<T, VE, R>())) void norm_sl
 }
 
 // The two sums of dx over a part of a sample, and per-channel sums on top of dg, db.  (x and dy of positions that are not there are 0, and so is du.)
-template <bool SILU, class T, int VE, int R>
+template <bool SILU, bool TAIL, class T, int VE, int R>
 __device__ __forceinline__ float2 slab_grads(const NormParams &p, Slab<T, VE, R> &x, Slab<T, VE, R> &dy, const SlabPlace<VE> &at, float mean, float rstd,
                                              const float (&gamma)[VE], const float (&beta)[VE], float (&dg)[VE], float (&db)[VE])
 {
@@ -462,8 +470,9 @@ __device__ __forceinline__ float2 slab_grads(const NormParams &p, Slab<T, VE, R>
             const float xhat = (x.r[i].get(e) - mean) * rstd, du = norm_du<SILU>(xhat, dy.r[i].get(e), gamma[e], beta[e]);
             db[e] += du;
             dg[e] = fmaf(du, xhat, dg[e]);
-            s1 = fmaf(du, gamma[e], s1);
-            s2 = fmaf(du * gamma[e], xhat, s2);
+            const float weight = !TAIL || e >= at.own ? gamma[e] : 0.f;
+            s1 = fmaf(du, weight, s1);
+            s2 = fmaf(du * weight, xhat, s2);
             // now: the compiler would add up all du and du xhat behind the sums s1, s2, and keep them until then
             asm volatile("" : "+v"(db[e]), "+v"(dg[e]));
         }
@@ -479,7 +488,7 @@ __device__ __forceinline__ void slab_store_dx(const NormParams &p, const Slab<T,
 {
     slab_pass<T, R>(p.dx, p.d.x_n, p.d.x_s, p, at.active, at.ty, at.c0, n, s0, count, [&](int i, bool there, T *q) {
         const Pack<T, VE> out = dx_pack<SILU, T, VE>(x.r[i], dy.r[i], mean, rstd, m1, m2, gamma, beta);
-        if (there) *reinterpret_cast<Pack<T, VE> *>(q) = out;
+        if (there) loose_store<T, VE>(q, out);
     });
 }
 
@@ -501,25 +510,25 @@ __device__ __forceinline__ void slab_store_part(const NormParams &p, const SlabP
 #pragma unroll
         for (int e = 0; e < VE; ++e) lds[e][slot] = make_float2(dg[e], db[e]);
     __syncthreads();
-    const int rows = in_wave ? (int)blockDim.x / 64 : p.py, first = p.cs > 1 ? at.strip / p.cs * p.pgl + at.strip % p.cs * p.px : at.strip * p.px;
-    const int end = p.cs > 1 ? (at.strip / p.cs + 1) * p.pgl : p.packs;
+    const int rows = in_wave ? (int)blockDim.x / 64 : p.py;
     for (int i = threadIdx.x; i < p.px * VE; i += blockDim.x) {
         const int pack = i / VE, e = i % VE;
-        if (first + pack >= end) continue;
+        const int g = p.cs > 1 ? at.strip / p.cs : at.strip * p.gps + pack / p.pgl, k = p.cs > 1 ? at.strip % p.cs * p.px + pack : pack % p.pgl;
+        if (g >= p.d.G || k >= p.pgl) continue;
         float2 v = lds[e][pack];
         for (int r = 1; r < rows; ++r) {
             const float2 w = lds[e][r * p.px + pack];
             v.x += w.x;
             v.y += w.y;
         }
-        const long c = (long)(first + pack) * VE + e;
+        const long c = pack_channel<VE>(p, g, k) + e;
         p.part[part_row * 2 * p.d.C + c] = v.x;
         p.part[(part_row * 2 + 1) * p.d.C + c] = v.y;
     }
     __syncthreads();
 }
 
-template <bool SILU, class T, int VE, int R>
+template <bool SILU, bool TAIL, class T, int VE, int R>
 __global__ __launch_bounds__(kMaxThreads) void norm_slab_bwd_kernel(NormParams p)
 {
     int strip, part_row;
@@ -535,14 +544,21 @@ __global__ __launch_bounds__(kMaxThreads) void norm_slab_bwd_kernel(NormParams p
         x.load(p.x, p.d.x_n, p.d.x_s, p, at, n, 0, p.d.S);
         dy.load(p.dy, p.d.y_n, p.d.y_s, p, at, n, 0, p.d.S);
         const float mean = at.active ? p.stats_in[(long)n * p.d.G + at.g] : 0.f, rstd = at.active ? p.stats_in[((long)p.d.N + n) * p.d.G + at.g] : 0.f;
-        const float2 s = slab_grads<SILU, T, VE, R>(p, x, dy, at, mean, rstd, gamma, beta, dg, db);
+        const float2 s = slab_grads<SILU, TAIL, T, VE, R>(p, x, dy, at, mean, rstd, gamma, beta, dg, db);
         slab_store_dx<SILU, T, VE, R>(p, x, dy, at, n, 0, p.d.S, mean, rstd, s.x * p.share, s.y * p.share, gamma, beta);
     }
     slab_store_part<VE>(p, at, part_row, dg, db);
 }
 
+// Channels of a group's part k of p.cs.
+template <int VE>
+__device__ __forceinline__ int part_channels(const NormParams &p, int k)
+{
+    return p.cs > 1 ? min(p.px * VE, p.cg - k * p.px * VE) : p.cg;
+}
+
 // Parts, first kernel: moments, or the sums of dx and those of dgamma and dbeta, of one part.
-template <bool SILU, class T, int VE, int R, bool BACKWARD>
+template <bool SILU, bool TAIL, class T, int VE, int R, bool BACKWARD>
 __global__ __launch_bounds__(kMaxThreads, BACKWARD || VE * sizeof(T) == 16 ? 4 : 8) void norm_part_kernel(NormParams p, unsigned units)
 {
     for (unsigned unit = blockIdx.x; unit < units; unit += gridDim.x) {
@@ -562,11 +578,10 @@ __global__ __launch_bounds__(kMaxThreads, BACKWARD || VE * sizeof(T) == 16 ? 4 :
                 mean = p.stats_in[(long)n * p.d.G + at.g];
                 rstd = p.stats_in[((long)p.d.N + n) * p.d.G + at.g];
             }
-            out = slab_grads<SILU, T, VE, R>(p, x, dy, at, mean, rstd, gamma, beta, dg, db);
+            out = slab_grads<SILU, TAIL, T, VE, R>(p, x, dy, at, mean, rstd, gamma, beta, dg, db);
             slab_store_part<VE>(p, at, row, dg, db);
         } else {
-            const int width = p.cs > 1 ? min(p.px, p.pgl - strip % p.cs * p.px) : p.pgl;
-            out = slab_moments<T, VE, R>(p, x, at, count, 1.f / ((float)count * width * VE));
+            out = slab_moments<TAIL, T, VE, R>(p, x, at, count, 1.f / ((float)count * part_channels<VE>(p, strip % p.cs)));
         }
         if (leads<VE>(p, at)) {
             float *to = p.sums + 2 * ((long)row * p.d.G * p.cs + (p.cs > 1 ? at.strip : at.g));
@@ -584,8 +599,7 @@ __device__ __forceinline__ float2 join_parts(const NormParams &p, int n, int g)
     const int lane = threadIdx.x % 64, parts = p.chunks * p.cs;
     auto at = [&](int i) { return p.sums + 2 * (((long)n * p.chunks + i / p.cs) * p.d.G * p.cs + (long)g * p.cs + i % p.cs); };
     auto elements = [&](int i) {
-        const int width = p.cs > 1 ? min(p.px, p.pgl - i % p.cs * p.px) : p.pgl;
-        return (float)min(p.chunk, p.d.S - i / p.cs * p.chunk) * width * VE;
+        return (float)min(p.chunk, p.d.S - i / p.cs * p.chunk) * part_channels<VE>(p, i % p.cs);
     };
     float2 v = make_float2(0.f, 0.f);
     for (int i = lane; i < parts; i += 64) {
@@ -676,7 +690,6 @@ Way divide(const ucd_group_norm_t &d, int VE, bool backward, NormParams &p, int 
     p.d = d;
     p.cg = d.C / d.G;
     p.pgl = ceil_div(p.cg, VE);
-    p.packs = d.C / VE;
     p.share = (float)(1. / ((double)d.S * p.cg));
     if (VE == rows_pack(d)) {
         R = p.pgl <= 64 ? 1 : kRowsR;
@@ -737,24 +750,25 @@ size_t ws_bytes(const ucd_group_norm_t &d, int VE, int dir)
     return n;
 }
 
-// Packs: those of rows, or such as all tensors' rows and groups consist of, 16 bytes at most; 8 where Backward keeps slabs of x and dy: with packs of 16 the sums per channel and
-// the weights take 16 registers more (256 x 49 x 2048, bf16: 75 us against 57).
+// Packs: those of rows, or the largest up to 16 bytes that leave no more than a quarter of the packs' elements to the packs before; up to 8 bytes where
+// Backward keeps slabs of x and dy of many positions: with packs of 16 the sums per channel and the weights take 16 registers more (256 x 49 x 2048, bf16:
+// 75 us against 57).  The tensors need not be aligned to them.
 constexpr int kMostBytes[2] = {16, 8};
 
-int pack_of(const ucd_group_norm_t &d, int dir, const void *a, const void *b, const void *c)
+int pack_of(const ucd_group_norm_t &d, int dir)
 {
-    const int e = d.dtype == 1 ? 2 : 4;
     if (const int ve = rows_pack(d)) return ve;
-    for (int ve = kMostBytes[dir] / e; ve > 1; ve /= 2) {
-        const uintptr_t bytes = ve * e, at = (uintptr_t)a | (uintptr_t)b | (uintptr_t)c;
-        if (d.C / d.G % ve == 0 && at % bytes == 0 && d.x_n % ve == 0 && d.x_s % ve == 0 && d.y_n % ve == 0 && d.y_s % ve == 0) return ve;
-    }
-    return 1;
+    const int cg = d.C / d.G;
+    int ve = (d.S == 1 ? 16 : kMostBytes[dir]) / (d.dtype == 1 ? 2 : 4);
+    while (ve > 1 && 10l * ceil_div(cg, ve) * ve > 13l * cg) ve /= 2;
+    while (ve > cg) ve /= 2;
+    return ve;
 }
 
 unsigned strip_units(const NormParams &p) { return (unsigned)p.strips * ((p.part_rows + kXcds - 1) / kXcds * kXcds); }
 
-template <bool SILU, class T, int VE, bool BACKWARD>
+// TAIL: groups are no whole packs
+template <bool SILU, bool TAIL, class T, int VE, bool BACKWARD>
 hipError_t launch(NormParams &p, void *ws, hipStream_t s)
 {
     const ucd_group_norm_t d = p.d;
@@ -769,16 +783,16 @@ hipError_t launch(NormParams &p, void *ws, hipStream_t s)
     constexpr int MOST = slab_packs<T, VE>(false), FEW = slab_packs<T, VE>(true);
     if (way == PARTS) {
         const unsigned units = strip_units(p), grid = std::min(units, 1u << 21);
-        norm_part_kernel<SILU, T, VE, MOST, BACKWARD><<<grid, threads, 0, s>>>(p, units);
+        norm_part_kernel<SILU, TAIL, T, VE, MOST, BACKWARD><<<grid, threads, 0, s>>>(p, units);
         norm_apply_kernel<SILU, T, VE, MOST, BACKWARD><<<grid, threads, 0, s>>>(p, units);
     } else if (way == SLABS) {
         const unsigned grid = strip_units(p);
         if constexpr (BACKWARD) {
-            if (R == FEW) norm_slab_bwd_kernel<SILU, T, VE, FEW><<<grid, threads, 0, s>>>(p);
-            else norm_slab_bwd_kernel<SILU, T, VE, MOST><<<grid, threads, 0, s>>>(p);
+            if (R == FEW) norm_slab_bwd_kernel<SILU, TAIL, T, VE, FEW><<<grid, threads, 0, s>>>(p);
+            else norm_slab_bwd_kernel<SILU, TAIL, T, VE, MOST><<<grid, threads, 0, s>>>(p);
         } else {
-            if (R == FEW) norm_slab_fwd_kernel<SILU, T, VE, FEW><<<grid, threads, 0, s>>>(p);
-            else norm_slab_fwd_kernel<SILU, T, VE, MOST><<<grid, threads, 0, s>>>(p);
+            if (R == FEW) norm_slab_fwd_kernel<SILU, TAIL, T, VE, FEW><<<grid, threads, 0, s>>>(p);
+            else norm_slab_fwd_kernel<SILU, TAIL, T, VE, MOST><<<grid, threads, 0, s>>>(p);
         }
     } else {
         const unsigned grid = (unsigned)p.columns * p.part_rows;
@@ -797,7 +811,10 @@ hipError_t launch(NormParams &p, void *ws, hipStream_t s)
 template <class T, int VE, bool BACKWARD>
 hipError_t by_act(NormParams &p, void *ws, hipStream_t s)
 {
-    return p.d.act == UCD_ACT_SILU ? launch<true, T, VE, BACKWARD>(p, ws, s) : launch<false, T, VE, BACKWARD>(p, ws, s);
+    const bool silu = p.d.act == UCD_ACT_SILU;
+    if (VE > 1 && p.d.C / p.d.G % VE != 0)
+        return silu ? launch<true, (VE > 1), T, VE, BACKWARD>(p, ws, s) : launch<false, (VE > 1), T, VE, BACKWARD>(p, ws, s);
+    return silu ? launch<true, false, T, VE, BACKWARD>(p, ws, s) : launch<false, false, T, VE, BACKWARD>(p, ws, s);
 }
 
 template <bool BACKWARD>
@@ -818,12 +835,7 @@ hipError_t dispatch(NormParams &p, int pack, void *ws, hipStream_t s)
 
 size_t group_norm_ws_bytes(const ucd_group_norm_t &d, int dir)
 {
-    if (const int ve = rows_pack(d)) return ws_bytes(d, ve, dir);
-    // whichever packs the tensors' alignment allows
-    size_t most = 0;
-    for (int ve = d.dtype == 1 ? 8 : 4; ve >= 1; ve /= 2)
-        if (d.C / d.G % ve == 0) most = std::max(most, ws_bytes(d, ve, dir));
-    return most;
+    return ws_bytes(d, pack_of(d, dir), dir);
 }
 
 hipError_t group_norm_fwd(const ucd_group_norm_t &d, const void *x, const float *gamma, const float *beta_w, void *y,
@@ -832,7 +844,7 @@ hipError_t group_norm_fwd(const ucd_group_norm_t &d, const void *x, const float 
     NormParams p{};
     p.d = d;
     p.x = x; p.gamma = gamma; p.beta = beta_w; p.y = y; p.stats = stats;
-    return dispatch<false>(p, pack_of(d, UCD_SEQ_FWD, x, y, nullptr), ws, s);
+    return dispatch<false>(p, pack_of(d, UCD_SEQ_FWD), ws, s);
 }
 
 hipError_t group_norm_bwd(const ucd_group_norm_t &d, const void *x, const float *gamma, const float *beta_w,
@@ -842,7 +854,7 @@ hipError_t group_norm_bwd(const ucd_group_norm_t &d, const void *x, const float 
     NormParams p{};
     p.d = d;
     p.x = x; p.gamma = gamma; p.beta = beta_w; p.stats_in = stats; p.dy = dy; p.dx = dx; p.dgamma = dgamma; p.dbeta = dbeta; p.add = add;
-    return dispatch<true>(p, pack_of(d, UCD_SEQ_BWD, x, dy, dx), ws, s);
+    return dispatch<true>(p, pack_of(d, UCD_SEQ_BWD), ws, s);
 }
 
 }  // namespace ucd
