@@ -11,8 +11,7 @@
  *   - dtype 0: activations (and their gradients, filters and convolution states) fp32; dtype 1:
  *     bfloat16, rounded to nearest-even once.  Everything else is fp32: norm weights, biases, A,
  *     skip, scan states, statistics, gradients of all weights; and so is all arithmetic.
- *   - Any alignment of an element's own size is accepted; 16-byte aligned rows (base, strides and
- *     widths) are read in wide loads.
+ *   - Any alignment of an element's own size is accepted, of workspaces and saved states 16 bytes.
  *   - Outputs overlap no input and no other output, but for state_out == state_in.
  *   - Gradients of weights are beta * old + sum, beta in {0, 1}, as in ucd_conv_bwd_filter: a
  *     mini-batch may be run in parts.  beta = 0 ignores old contents.
