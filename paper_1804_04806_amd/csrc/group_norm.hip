@@ -17,6 +17,8 @@ namespace {
 using namespace seq;
 
 constexpr int kRowsR = 4;                   // packs of a group per lane at most
+// Backward of rows (8192 x 1 x 2048 in 16 groups, bf16): 25.6 us; with 256 threads in 1024 workgroups, and twice the partial sums, 32; with 512 in 2048
+// 44; with 1024 in 256 24.5, but 16.9 instead of 16.2 for 512 channels in 4 groups.
 constexpr int kRowsBwdThreads = 512, kRowsBwdGroups = 512;
 // A slab's threads at most, and packs per thread: as many as fill 32 registers of the 128 that a thread has then (and 32 of dy in Backward), or a quarter.
 constexpr int kMaxThreads = 1024;
@@ -669,7 +671,13 @@ __global__ __launch_bounds__(kJoinThreads) void norm_join_kernel(NormParams p)
 
 // ---- which way, and how it is divided ------------------------------------------------------------------------------------------------------------
 
-constexpr int kStripBytes = 128, kWidenPacks = 1024;
+// Strips of 64 bytes: 34 us instead of 35 in Forward, 61 instead of 59 in Backward (64 x 1024 x 512, bf16, 32 groups), but 30 instead of 23 and 59
+// instead of 38 where rows are no whole lines (37 x 1305 x 231, fp32, 77 groups); of 256 bytes: the same within 1 us.
+constexpr int kStripBytes = 128;
+// Slabs below 1024 packs are widened (2048 x 16 x 512, bf16, 32 groups: 20 and 37 us, 31 and 76 as they are); to 4096 where that leaves 1024 workgroups
+// (256 x 49 x 2048, 32 groups: Forward 27 us instead of 33; 256 x 196 x 1024: 56 and 100 instead of 66 and 115; but 16 x 196 x 1024, with fewer
+// workgroups: 12 and 18 instead of 8 and 14).
+constexpr int kWidenPacks = 1024, kWidenMost = 4096, kWidenGroups = 1024;
 enum Way { ROWS, SLABS, PARTS };
 
 int ceil_div(long a, long b) { return (int)((a + b - 1) / b); }
@@ -715,7 +723,11 @@ Way divide(const ucd_group_norm_t &d, int VE, bool backward, NormParams &p, int 
         while (groups > 1 && !fits(groups)) --groups;
         if (fits(groups) && (groups * p.cg * e >= 32 || groups == d.G)) p.gps = groups;
     }
-    while (p.cs == 1 && (long)d.S * p.gps * p.pgl < kWidenPacks && 2 * p.gps <= d.G && 2 * p.gps * p.pgl <= 64) p.gps *= 2;
+    auto widen = [&] {
+        const long packs = (long)d.S * p.gps * p.pgl;
+        return packs < kWidenPacks || (packs < kWidenMost && (long)d.N * ceil_div(d.G, 2 * p.gps) >= kWidenGroups);
+    };
+    while (p.cs == 1 && 2 * p.gps <= d.G && 2 * p.gps * p.pgl <= 64 && widen() && fits(2 * p.gps)) p.gps *= 2;
     p.px = p.cs > 1 ? kMaxThreads : p.gps * p.pgl;
     p.strips = p.cs > 1 ? d.G * p.cs : ceil_div(d.G, p.gps);
     auto power = [](int n) { return (n & (n - 1)) == 0; };
