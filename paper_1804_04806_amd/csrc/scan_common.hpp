@@ -3,7 +3,8 @@
 // A lane holds NPL neighbouring states of one channel; LPC neighbouring lanes hold a channel's N <= LPC NPL states, a wave 64 / LPC
 // neighbouring channels, which share Bm and Cm (they are of one group).  Waves walk over tiles of 16 tokens by themselves: what
 // all states of a channel have in common (the step, its activation, the gate) is computed once per channel and token by the
-// lane that loads it, and handed to the others through the wave's own part of LDS.  No workgroup barriers.
+// lane that loads it, and handed to the others through the wave's own part of LDS.  Workgroups meet in Backward only, once a tile, to add up
+// their waves' sums over channels.
 #pragma once
 #include <type_traits>
 
