@@ -98,8 +98,10 @@ __device__ __forceinline__ Pack<T, VE> dx_pack(const Raw<T, VE, true> &x, const 
     Pack<T, VE> out;
 #pragma unroll
     for (int i = 0; i < VE; ++i) {
+        // rounded as in the sums m1 is made of: of a group of one element nothing must be left
+#pragma clang fp contract(off)
         const float xhat = (x.get(i) - mean) * rstd, g = norm_du<SILU>(xhat, dy.get(i), gamma[i], beta[i]) * gamma[i];
-        out.v[i] = from_f<T>(rstd * (g - m1 - xhat * m2));
+        out.v[i] = from_f<T>(rstd * fmaf(-xhat, m2, g - m1));
     }
     return out;
 }

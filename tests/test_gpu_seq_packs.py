@@ -83,3 +83,12 @@ def test_scan_rows_of_no_whole_packs(shape, dtype):
 @pytest.mark.parametrize("shape", [SCANS[3], SCANS[5], (2, 64, 64, 16, 1), (1, 40, 64, 8, 2)], ids=str)
 def test_scan_rows_anywhere(shape, dtype):
     scan.run(shape, dtype, seed=13, strides=True, shift=1)
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("silu", [False, True])
+@pytest.mark.parametrize("shape", [(1, 1, 1, 1), (700, 1, 33, 33), (3, 1, 100, 100)], ids=str)
+def test_norm_of_single_elements_has_no_gradient(shape, silu, dtype):
+    """dx is a difference of equal terms: exactly 0, not what rounding them differently would leave of it."""
+    got, _ = norm.run(shape, dtype, silu, seed=15)
+    assert not got["dx"].any() and not got["dgamma"].any()
