@@ -72,6 +72,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void scan_bwd_kernel(ScanParams p, 
     __shared__ alignas(16) float lds_bc[kWaves][BC];
     __shared__ alignas(16) float lds_out[kWaves][STATE_ONLY ? 1 : 3 * kTile * W::CW];   // sums over the states: dh Bm, x h A, Cm h
     __shared__ alignas(16) float lds_sum[STATE_ONLY ? 1 : 2][STATE_ONLY ? 1 : kWaves][STATE_ONLY ? 1 : BC];
+    // the lane's dA of the tiles so far: a tile's sum first, then theirs, or thousands of tokens' roundings would add up
+    __shared__ Pack<float, NPL> lds_dA[STATE_ONLY ? 1 : kWaves][STATE_ONLY ? 1 : 64];
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
     float2 *step = lds_step[wave];
     float *dys = lds_dy[wave], *bm = lds_bc[wave], *cm = bm + kTile * W::NP;
@@ -88,6 +90,17 @@ __global__ __launch_bounds__(64 * kWaves, 2) void scan_bwd_kernel(ScanParams p, 
         const bool mine = at.c < at.have;
 
         float A2[NPL], x[NPL], dA[NPL] = {};
+        Pack<float, NPL> &all_dA = lds_dA[STATE_ONLY ? 0 : wave][STATE_ONLY ? 0 : lane];
+        auto add_dA = [&](bool first) {
+            Pack<float, NPL> sum = all_dA;
+#pragma unroll
+            for (int j = 0; j < NPL; ++j) {
+                sum.v[j] = dA[j] + (first ? 0.f : sum.v[j]);
+                dA[j] = 0.f;
+            }
+            all_dA = sum;
+        };
+        if (!STATE_ONLY) add_dA(true);
         load_states(A2, p.in.A + ch * d.N + at.n0, at.haven);
 #pragma unroll
         for (int j = 0; j < NPL; ++j) A2[j] *= kLog2e;
@@ -282,6 +295,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void scan_bwd_kernel(ScanParams p, 
                             }
                         }
                     }
+                    add_dA(false);
                 }
                 wave_lds_order();
             } else if (tile > tile0) {
@@ -348,7 +362,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void scan_bwd_kernel(ScanParams p, 
             float *o = p.part_w + (((long)at.b * p.segs + at.seg) * d.D) * (d.N + 2);
 #pragma unroll
             for (int j = 0; j < NPL; ++j)
-                if (j < at.haven) o[ch * (d.N + 2) + at.n0 + j] = dA[j];
+                if (j < at.haven) o[ch * (d.N + 2) + at.n0 + j] = all_dA.v[j];
             // over the lanes that load other tokens of the same channels
 #pragma unroll
             for (int e = 0; e < W::VE; ++e) {
