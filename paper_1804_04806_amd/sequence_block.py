@@ -34,9 +34,18 @@ def _dtype(t):
 
 
 def _rows(t):
-    """A tensor whose last extent is contiguous, and its strides of sequence and token."""
-    t = t if t.stride(-1) == 1 or t.shape[-1] == 1 else t.contiguous()
-    return t, t.stride()[:2]
+    """A tensor (B, L, ...) whose rows are dense and apart from each other, and its strides of sequence and token, 0 (the dense
+    one) where there is only one.  Copied where it is not such a tensor, as broadcast ones are not: all of their rows are one."""
+    dense, span = True, 1
+    for n, stride in zip(reversed(t.shape[2:]), reversed(t.stride()[2:])):
+        dense = dense and (n == 1 or stride == span)
+        span *= n
+    for stride, n in sorted(zip(t.stride()[:2], t.shape[:2])):
+        if n > 1:
+            dense = dense and stride >= span
+            span += stride * (n - 1)
+    t = t if dense else t.contiguous()
+    return t, tuple(stride if n > 1 else 0 for stride, n in zip(t.stride()[:2], t.shape[:2]))
 
 
 class GroupNorm(torch.autograd.Function):

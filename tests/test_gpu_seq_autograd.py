@@ -1,0 +1,101 @@
+"""The operators' autograd functions against the same formulas in plain torch, 64 bits, on the CPU: tensors that programs
+pass without making them dense first."""
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+B, L, D, N, K = 3, 21, 24, 9, 4
+
+
+def silu(v):
+    import torch
+    return v * torch.sigmoid(v)
+
+
+def plain_conv(x, w, bias):
+    import torch
+    pad = torch.nn.functional.pad(x, (0, 0, w.shape[1] - 1, 0))
+    return silu(bias + sum(pad[:, k:k + x.shape[1]] * w[:, k] for k in range(w.shape[1])))
+
+
+def plain_scan(u, dt, A, Bm, Cm, skip, z, dt_bias):
+    import torch
+    delta = torch.nn.functional.softplus(dt + dt_bias)
+    h, y = 0, []
+    for t in range(u.shape[1]):
+        h = torch.exp(delta[:, t, :, None] * A) * h + (delta[:, t] * u[:, t])[..., None] * Bm[:, t, None]
+        y.append((h * Cm[:, t, None]).sum(-1) + skip * u[:, t])
+    return torch.stack(y, 1) * silu(z)
+
+
+def plain_norm(x, gamma, beta, groups, act):
+    v = x.reshape(x.shape[:2] + (groups, -1))
+    v = (v - v.mean(-1, keepdim=True)) / (v.var(-1, correction=0, keepdim=True) + 1e-5).sqrt()
+    v = v.flatten(2) * gamma + beta
+    return silu(v) if act else v
+
+
+def compare(function, plain, leaves, view, extra=()):
+    """function(*view(leaves)) and the leaves' gradients against plain's: fp32, each sum of some dozen terms and each decay a few
+    2^-24 off, 1e-5 allowed in the 2-norm."""
+    import torch
+    torch.manual_seed(2)
+    on = {k: v.detach().cuda().requires_grad_() for k, v in leaves.items()}
+    ref = {k: v.detach().double().requires_grad_() for k, v in leaves.items()}
+    y = function(*view(on), *extra)
+    yr = plain(*view(ref), *extra)
+    dy = torch.randn(yr.shape)
+    y.backward(dy.cuda())
+    yr.backward(dy.double())
+
+    def close(a, b, what):
+        a, b = a.detach().double().cpu(), b.detach()
+        assert a.shape == b.shape and float((a - b).norm()) <= 1e-5 * float(b.norm()), (what, float((a - b).norm() / b.norm()))
+    close(y, yr, "y")
+    for k in leaves:
+        close(on[k].grad, ref[k].grad, k)
+
+
+SHAPES = {"whole": (B, L), "over sequences": (1, L), "over tokens": (B, 1), "over both": (1, 1)}
+
+
+def scan_leaves(rows):
+    """Leaves of the scan; `rows` gives the first two extents of some of them."""
+    import torch
+    torch.manual_seed(1)
+    shape = {k: rows.get(k, (B, L)) for k in ("u", "dt", "Bm", "Cm", "z")}
+    v = {k: torch.randn(*s, N if k in ("Bm", "Cm") else D) for k, s in shape.items()}
+    v.update(A=-torch.rand(D, N) * 4, skip=torch.randn(D), dt_bias=torch.randn(D) - 3)
+    return v
+
+
+ORDER = ("u", "dt", "A", "Bm", "Cm", "skip", "z", "dt_bias")
+
+
+def scan_args(v):
+    return [v[k].expand(B, L, -1) if k in ("u", "dt", "Bm", "Cm", "z") else v[k] for k in ORDER]
+
+
+@pytest.mark.parametrize("rows", ["over sequences", "over tokens", "over both"])
+@pytest.mark.parametrize("names", [("Bm", "Cm"), ("z",), ("u",), ("dt",), ("u", "dt", "Bm", "Cm", "z")], ids=str)
+def test_scan_of_broadcast_tensors(names, rows):
+    from paper_1804_04806_amd.sequence_block import Scan
+    compare(Scan.apply, plain_scan, scan_leaves({k: SHAPES[rows] for k in names}), scan_args)
+
+
+@pytest.mark.parametrize("rows", SHAPES)
+def test_conv_of_broadcast_tensors(rows):
+    import torch
+    from paper_1804_04806_amd.sequence_block import CausalConv
+    torch.manual_seed(3)
+    leaves = {"x": torch.randn(*SHAPES[rows], D), "w": torch.randn(D, K) * 0.5, "bias": torch.randn(D)}
+    compare(CausalConv.apply, plain_conv, leaves, lambda v: [v["x"].expand(B, L, -1), v["w"], v["bias"]])
+
+
+@pytest.mark.parametrize("rows", SHAPES)
+def test_norm_of_broadcast_tensors(rows):
+    import torch
+    from paper_1804_04806_amd.sequence_block import GroupNorm
+    torch.manual_seed(4)
+    leaves = {"x": torch.randn(*SHAPES[rows], D), "gamma": 1 + 0.3 * torch.randn(D), "beta": torch.randn(D)}
+    compare(GroupNorm.apply, plain_norm, leaves, lambda v: [v["x"].expand(B, L, -1), v["gamma"], v["beta"]], (4, True))

@@ -1,0 +1,49 @@
+"""What the block hands to the sequence operators, without a GPU: the strides and extents of its tensors."""
+import pytest
+import torch
+
+from paper_1804_04806_amd import sequence_block as sb
+
+B, L, N = 4, 6, 16
+
+
+def views():
+    """Tensors (B, L, N) as programs have them, by name."""
+    dense = torch.randn(B, L, N)
+    return {
+        "dense": dense,
+        "half": torch.randn(B, L, 2 * N)[:, :, :N],
+        "tokens first": torch.randn(L, B, N).transpose(0, 1),
+        "over sequences": torch.randn(1, L, N).expand(B, L, N),
+        "over tokens": torch.randn(B, 1, N).expand(B, L, N),
+        "over both": torch.randn(N).expand(B, L, N),
+        "over channels": torch.randn(B, L, 1).expand(B, L, N),
+        "channels first": torch.randn(B, N, L).transpose(1, 2),
+        "windows": torch.randn(B, L + N).unfold(1, N, 1)[:, :L],
+        "reversed nesting": torch.randn(B, L * N + 3).as_strided((B, L, N), (N + 1, N, 1)),
+        "one sequence": torch.randn(1, L, N),
+        "one token": torch.randn(B, L, N)[:, 2:3],
+        "one sequence, any stride": torch.randn(1, L, N).as_strided((1, L, N), (1, N, 1)),
+        "one token, any stride": torch.randn(B, 1, N).as_strided((B, 1, N), (N, 1, 1)),
+        "one channel": torch.randn(B, L, 3)[:, :, 1:2],
+    }
+
+
+@pytest.mark.parametrize("name", views())
+def test_rows_are_where_the_descriptor_says(name):
+    """The rows that strides describe, 0 standing for the dense one, are the tensor's values, lie inside its memory and apart
+    from each other; so do those of a gradient laid out alike."""
+    t = views()[name]
+    rows, (outer, inner) = sb._rows(t)
+    assert torch.equal(rows, t)
+    b, l, n = t.shape
+    inner = inner or n
+    outer = outer or inner * l
+    at = [i * outer + j * inner for i in range(b) for j in range(l)]
+    span = max(at) + n
+    like = torch.empty_strided(rows.shape, rows.stride())
+    for m in (rows, like):
+        assert m.storage_offset() + span <= m.untyped_storage().nbytes() // m.element_size()
+    assert torch.equal(rows.as_strided((b, l, n), (outer, inner, 1)), t)
+    at.sort()
+    assert all(q - p >= n for p, q in zip(at, at[1:]))
