@@ -48,12 +48,17 @@ def _rows(t):
     return t, tuple(stride if n > 1 else 0 for stride, n in zip(t.stride()[:2], t.shape[:2]))
 
 
+def _dense(*tensors):
+    """Tensors without strides of their own, as the operators read weights."""
+    return (None if t is None else t.contiguous() for t in tensors)
+
+
 class GroupNorm(torch.autograd.Function):
     """Group norm of single tokens: x (B, L, C)."""
 
     @staticmethod
     def forward(ctx, x, gamma, beta, groups, silu):
-        x = x.contiguous()
+        x, gamma, beta = _dense(x, gamma, beta)
         n = x.shape[0] * x.shape[1]
         desc = seq.group_norm(n, 1, x.shape[2], groups, act=int(silu), dtype=_dtype(x))
         y, stats = torch.empty_like(x), torch.empty(2, n, groups, device=x.device)
@@ -78,6 +83,7 @@ class CausalConv(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, w, bias):
         x, stride = _rows(x)
+        w, bias = _dense(w, bias)
         b, l, d = x.shape
         desc = seq.causal_conv(b, l, d, w.shape[1], act=seq.ACT_SILU, dtype=_dtype(x), x_stride=stride)
         y = torch.empty(b, l, d, dtype=x.dtype, device=x.device)
@@ -103,6 +109,7 @@ class Scan(torch.autograd.Function):
     def forward(ctx, u, dt, A, Bm, Cm, skip, z, dt_bias):
         rows = {k: _rows(t) for k, t in dict(u=u, dt=dt, Bm=Bm, Cm=Cm, z=z).items()}
         u, dt, Bm, Cm, z = (rows[k][0] for k in ("u", "dt", "Bm", "Cm", "z"))
+        A, skip, dt_bias = _dense(A, skip, dt_bias)
         b, l, d = u.shape
         desc = seq.scan(b, l, d, A.shape[1], dtype=_dtype(u), **{k + "_stride": s for k, (_, s) in rows.items()})
         y = torch.empty(b, l, d, dtype=u.dtype, device=u.device)

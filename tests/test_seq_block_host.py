@@ -47,3 +47,36 @@ def test_rows_are_where_the_descriptor_says(name):
     assert torch.equal(rows.as_strided((b, l, n), (outer, inner, 1)), t)
     at.sort()
     assert all(q - p >= n for p, q in zip(at, at[1:]))
+
+
+def weights(kind=torch.float32):
+    """Arguments of the functions, their weights as views: (function, arguments, names of the weights)."""
+    x = torch.randn(2, 3, 8, dtype=kind)
+    two = torch.randn(2, 3, 5, dtype=kind)
+    return [(sb.GroupNorm, [x, torch.randn(16)[::2], torch.randn(1).expand(8), 4, False], (1, 2)),
+            (sb.CausalConv, [x, torch.randn(4, 8, dtype=kind).t(), torch.randn(1).expand(8)], (1, 2)),
+            (sb.Scan, [x, x.clone(), torch.randn(1, 5).expand(8, 5), two, two.clone(), torch.randn(16)[::2], x.clone(),
+                       torch.randn(1).expand(8)], (2, 5, 7))]
+
+
+class Stop(Exception):
+    pass
+
+
+@pytest.mark.parametrize("i", range(3), ids=["norm", "conv", "scan"])
+def test_weights_reach_the_operators_dense(i, monkeypatch):
+    """What is passed by its address alone holds its values side by side."""
+    function, args, names = weights()[i]
+    got = []
+
+    def call(desc, *given, **more):
+        got.extend(list(given) + list(more.values()))
+        raise Stop
+    monkeypatch.setattr(sb, "_DEVICE", "cpu", raising=False)
+    for name in ("ucd_group_norm_fwd", "ucd_causal_conv_fwd", "ucd_scan_fwd"):
+        monkeypatch.setattr(sb.seq, name, call)
+    with pytest.raises(Stop):
+        function.apply(*args)
+    for n in names:
+        assert any(isinstance(t, torch.Tensor) and t.is_contiguous() and t.shape == args[n].shape and torch.equal(t, args[n])
+                   for t in got), n
