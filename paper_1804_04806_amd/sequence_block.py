@@ -29,8 +29,36 @@ def _workspace(nbytes, device):
     return _ws.get(device) if nbytes else None
 
 
+_DEVICE = "cuda"
+
+
 def _dtype(t):
-    return {torch.float32: 0, torch.bfloat16: 1}[t.dtype]
+    """The operators' number of an activation's type."""
+    if t.dtype not in (torch.float32, torch.bfloat16):
+        raise TypeError(f"activations are float32 or bfloat16, not {t.dtype}")
+    return int(t.dtype == torch.bfloat16)
+
+
+def _check(*given):
+    """The operators are given addresses alone: refuses what is not as they will read it.  Each is a name, a tensor or None,
+    its shape and its type; all are on the first one's device."""
+    given = [g for g in given if g[1] is not None]
+    for name, t, shape, kind in given:
+        if t.dtype != kind:
+            raise TypeError(f"{name} is {t.dtype} where {kind} is read")
+        if t.shape != tuple(shape):
+            raise ValueError(f"{name} is {tuple(t.shape)} where {tuple(shape)} is read")
+    device = given[0][1].device
+    for name, t, _, _ in given:
+        if t.device != device or device.type != _DEVICE:
+            raise ValueError(f"{name} is on {t.device}, {given[0][0]} on {device}: all are read on one {_DEVICE} device")
+
+
+def _tokens(name, t):
+    """The extents of an activation tensor."""
+    if t.dim() != 3:
+        raise ValueError(f"{name} is {tuple(t.shape)}, not (sequences, tokens, channels)")
+    return t.shape
 
 
 def _rows(t):
@@ -58,6 +86,9 @@ class GroupNorm(torch.autograd.Function):
 
     @staticmethod
     def forward(ctx, x, gamma, beta, groups, silu):
+        _dtype(x)
+        c = _tokens("x", x)[2:]
+        _check(("x", x, x.shape, x.dtype), ("gamma", gamma, c, torch.float32), ("beta", beta, c, torch.float32))
         x, gamma, beta = _dense(x, gamma, beta)
         n = x.shape[0] * x.shape[1]
         desc = seq.group_norm(n, 1, x.shape[2], groups, act=int(silu), dtype=_dtype(x))
@@ -78,13 +109,15 @@ class GroupNorm(torch.autograd.Function):
 
 
 class CausalConv(torch.autograd.Function):
-    """SiLU of the short causal convolution: x (B, L, D), w (D, K) of x's type."""
+    """SiLU of the short causal convolution: x (B, L, D), w (D, K) of x's type, bias (D) fp32."""
 
     @staticmethod
     def forward(ctx, x, w, bias):
+        _dtype(x)
+        b, l, d = _tokens("x", x)
+        _check(("x", x, x.shape, x.dtype), ("w", w, (d, w.shape[-1]), x.dtype), ("bias", bias, (d,), torch.float32))
         x, stride = _rows(x)
         w, bias = _dense(w, bias)
-        b, l, d = x.shape
         desc = seq.causal_conv(b, l, d, w.shape[1], act=seq.ACT_SILU, dtype=_dtype(x), x_stride=stride)
         y = torch.empty(b, l, d, dtype=x.dtype, device=x.device)
         seq.ucd_causal_conv_fwd(desc, x, w, bias, y)
@@ -103,15 +136,21 @@ class CausalConv(torch.autograd.Function):
 
 
 class Scan(torch.autograd.Function):
-    """The gated selective scan: u, dt, z (B, L, D), Bm, Cm (B, L, N)."""
+    """The gated selective scan: u, dt, z (B, L, D) and Bm, Cm (B, L, N) of one type; A (D, N), skip, dt_bias (D) fp32."""
 
     @staticmethod
     def forward(ctx, u, dt, A, Bm, Cm, skip, z, dt_bias):
+        _dtype(u)
+        b, l, d = _tokens("u", u)
+        n = A.shape[-1]
+        states = [(b, l, 1, n) if m.dim() == 4 else (b, l, n) for m in (Bm, Cm)]
+        _check(("u", u, u.shape, u.dtype), ("dt", dt, u.shape, u.dtype), ("z", z, u.shape, u.dtype), ("Bm", Bm, states[0], u.dtype),
+               ("Cm", Cm, states[1], u.dtype), ("A", A, (d, n), torch.float32), ("skip", skip, (d,), torch.float32),
+               ("dt_bias", dt_bias, (d,), torch.float32))
         rows = {k: _rows(t) for k, t in dict(u=u, dt=dt, Bm=Bm, Cm=Cm, z=z).items()}
         u, dt, Bm, Cm, z = (rows[k][0] for k in ("u", "dt", "Bm", "Cm", "z"))
         A, skip, dt_bias = _dense(A, skip, dt_bias)
-        b, l, d = u.shape
-        desc = seq.scan(b, l, d, A.shape[1], dtype=_dtype(u), **{k + "_stride": s for k, (_, s) in rows.items()})
+        desc = seq.scan(b, l, d, n, dtype=_dtype(u), **{k + "_stride": s for k, (_, s) in rows.items()})
         y = torch.empty(b, l, d, dtype=u.dtype, device=u.device)
         saved = torch.empty(seq.ucd_scan_saved_size(desc), dtype=torch.uint8, device=u.device)
         seq.ucd_scan_fwd(desc, u, dt, A, Bm, Cm, y, skip=skip, z=z, dt_bias=dt_bias, saved=saved,
@@ -134,7 +173,8 @@ class Scan(torch.autograd.Function):
 
 class Block(torch.nn.Module):
     """One block: tokens of `width`, `inner` channels with `states` states each, `heads` groups behind the scan.
-    Projections and filters are of `dtype`, everything else is fp32."""
+    Projections and filters are of `dtype`, everything else is fp32; a block that was converted to bfloat16 as a whole, and one
+    under autocast, hands the operators its weights in the types that they read."""
 
     def __init__(self, width, inner, states=16, taps=4, heads=4, rank=8, dtype=torch.float32, device="cuda"):
         super().__init__()
@@ -157,17 +197,23 @@ class Block(torch.nn.Module):
         self.log_a = plain(torch.log(torch.arange(1, states + 1, dtype=torch.float32)).repeat(inner, 1))
         self.skip = plain(torch.ones(inner))
 
+    def _norm(self, x):
+        return GroupNorm.apply(x, self.gamma.float(), self.beta.float(), 1, False)
+
+    def _heads_norm(self, y):
+        return GroupNorm.apply(y, self.head_gamma.float(), self.head_beta.float(), self.heads, False)
+
     def _split(self, c):
         dt, bm, cm = (c @ self.w_x).split([self.rank, self.states, self.states], dim=-1)
         return dt @ self.w_dt, bm, cm
 
     def forward(self, x):
-        uz = GroupNorm.apply(x, self.gamma, self.beta, 1, False) @ self.w_in
+        uz = self._norm(x) @ self.w_in
         u, z = uz.split(self.inner, dim=-1)
-        c = CausalConv.apply(u, self.conv_w, self.conv_b)
+        c = CausalConv.apply(u, self.conv_w.to(u.dtype), self.conv_b.float())
         dt, bm, cm = self._split(c)
-        y = Scan.apply(c, dt, -torch.exp(self.log_a), bm, cm, self.skip, z, self.dt_bias)
-        return x + GroupNorm.apply(y, self.head_gamma, self.head_beta, self.heads, False) @ self.w_out
+        y = Scan.apply(c, dt, -torch.exp(self.log_a.float()), bm, cm, self.skip.float(), z, self.dt_bias.float())
+        return x + self._heads_norm(y) @ self.w_out
 
     # ---- decoding ----
 
@@ -181,30 +227,38 @@ class Block(torch.nn.Module):
     def extend(self, x, pools, slots, lengths=None):
         """Outputs for the next tokens x (B, L, width) of the sequences in `slots`, whose states move on; with `lengths`
         prompts of their own lengths, padded to L.  One token takes the single-token kernels."""
-        b, l, _ = x.shape
-        kind, n = _dtype(x), pools[0].shape[0]
-        uz = GroupNorm.apply(x, self.gamma, self.beta, 1, False) @ self.w_in
+        b, l, _ = _tokens("x", x)
+        n = pools[0].shape[0]
+        uz = self._norm(x) @ self.w_in
         (u, us), (z, zs) = (_rows(t) for t in uz.split(self.inner, dim=-1))
-        c = torch.empty(b, l, self.inner, dtype=x.dtype, device=x.device)
+        kind = _dtype(u)
+        _check(("x", x, x.shape, x.dtype), ("the convolution's states", pools[0], (n, self.taps - 1, self.inner), u.dtype),
+               ("the scan's states", pools[1], (n, self.inner, self.states), torch.float32), ("slots", slots, (b,), torch.int32),
+               ("lengths", lengths, (b,), torch.int32))
+        if not (pools[0].is_contiguous() and pools[1].is_contiguous()):
+            raise ValueError("the states are replaced in place: pools have to be contiguous")
+        slots, lengths, conv_w, conv_b, skip, dt_bias = _dense(slots, lengths, self.conv_w.to(u.dtype), self.conv_b.float(),
+                                                               self.skip.float(), self.dt_bias.float())
+        c = torch.empty(b, l, self.inner, dtype=u.dtype, device=u.device)
         conv = seq.causal_conv(b, l, self.inner, self.taps, act=seq.ACT_SILU, dtype=kind, n_slots=n, x_stride=us)
         step = l == 1 and lengths is None
         if step:
-            seq.ucd_causal_conv_step(conv, u, self.conv_w, self.conv_b, pools[0], c, slots=slots)
+            seq.ucd_causal_conv_step(conv, u, conv_w, conv_b, pools[0], c, slots=slots)
         else:
-            seq.ucd_causal_conv_fwd(conv, u, self.conv_w, self.conv_b, c, lengths=lengths, slots=slots, state_in=pools[0],
+            seq.ucd_causal_conv_fwd(conv, u, conv_w, conv_b, c, lengths=lengths, slots=slots, state_in=pools[0],
                                     state_out=pools[0])
         dt, bm, cm = self._split(c)
         (dt, ds), (bm, bs), (cm, cs) = (_rows(t) for t in (dt, bm, cm))
         scan = seq.scan(b, l, self.inner, self.states, dtype=kind, n_slots=n, z_stride=zs, dt_stride=ds, Bm_stride=bs,
                         Cm_stride=cs)
-        y, a = torch.empty_like(c), -torch.exp(self.log_a)
-        more = dict(skip=self.skip, z=z, dt_bias=self.dt_bias, slots=slots)
+        y, a = torch.empty_like(c), -torch.exp(self.log_a.float().contiguous())
+        more = dict(skip=skip, z=z, dt_bias=dt_bias, slots=slots)
         if step:
             seq.ucd_scan_step(scan, c, dt, a, bm, cm, pools[1], y, **more)
         else:
             seq.ucd_scan_fwd(scan, c, dt, a, bm, cm, y, lengths=lengths, state_in=pools[1], state_out=pools[1],
                              ws=_workspace(seq.ucd_scan_workspace_size(scan, seq.FWD), x.device), **more)
-        return x + GroupNorm.apply(y, self.head_gamma, self.head_beta, self.heads, False) @ self.w_out
+        return x + self._heads_norm(y) @ self.w_out
 
 
 def train(steps=60, layers=2, width=64, inner=128, batch=16, length=96, delay=12, dtype=torch.float32, seed=0):

@@ -117,3 +117,45 @@ def test_weights_of_any_layout():
         leaves["A"] = -4 * A
         compare(Scan.apply, plain_scan, leaves,
                 lambda v: [dict(v, A=view(v["A"]), skip=v["skip"].expand(D), dt_bias=v["dt_bias"][::2])[k] for k in ORDER])
+
+
+def test_block_converted_as_a_whole():
+    """Block.to(bfloat16) is the block that was made in bfloat16 with the same weights: the same bits, gradients rounded once."""
+    import torch
+    from paper_1804_04806_amd.sequence_block import Block
+    torch.manual_seed(6)
+    made, whole = Block(32, 48, dtype=torch.bfloat16), Block(32, 48).to(torch.bfloat16)
+    made.load_state_dict(whole.state_dict())
+    assert made.gamma.dtype == torch.float32 and whole.gamma.dtype == torch.bfloat16
+    x, dy = (torch.randn(2, 40, 32, device="cuda").bfloat16() for _ in range(2))
+    out = [block(x) for block in (made, whole)]
+    assert torch.equal(*out)
+    for y in out:
+        y.backward(dy)
+    for (name, p), q in zip(made.named_parameters(), whole.parameters()):
+        assert torch.equal(p.grad.bfloat16(), q.grad) and float(q.grad.abs().max()) > 0, name
+    slots, got = torch.arange(2, dtype=torch.int32, device="cuda"), []
+    for block in (made, whole):
+        pools = block.pools(2)
+        got.append((block.extend(x[:, :39], pools, slots), block.extend(x[:, 39:], pools, slots)) + pools)
+    assert all(torch.equal(a, b) for a, b in zip(*got))
+
+
+def test_block_under_autocast():
+    """bfloat16 products around fp32 weights: about ten results between input and output that are rounded to 8 bits, 2^-8 of
+    each at most, where the block without autocast rounds none; gradients pass them twice."""
+    import torch
+    from paper_1804_04806_amd.sequence_block import Block
+    torch.manual_seed(7)
+    block = Block(32, 48)
+    x, dy = torch.randn(2, 40, 32, device="cuda"), torch.randn(2, 40, 32, device="cuda")
+    got = []
+    for on in (False, True):
+        block.zero_grad()
+        with torch.autocast("cuda", dtype=torch.bfloat16, enabled=on):
+            y = block(x)
+        y.backward(dy)
+        got.append([y.detach()] + [p.grad.clone() for p in block.parameters()])
+    for i, (a, b) in enumerate(zip(*got)):
+        assert a.dtype == b.dtype == torch.float32
+        assert float((a - b).norm()) <= (10 if i == 0 else 20) * 2.0 ** -8 * float(a.norm()), i

@@ -80,3 +80,56 @@ def test_weights_reach_the_operators_dense(i, monkeypatch):
     for n in names:
         assert any(isinstance(t, torch.Tensor) and t.is_contiguous() and t.shape == args[n].shape and torch.equal(t, args[n])
                    for t in got), n
+
+
+def test_foreign_types_and_shapes_are_refused():
+    """The operators read addresses: a tensor of another type or shape is refused before anything is launched."""
+    bf16, f64 = torch.bfloat16, torch.float64
+    for i, (function, args, names) in enumerate(weights()):
+        # weights as a module that was converted as a whole has them, tensors that are half as large as what is read
+        for n in names:
+            bad = list(args)
+            bad[n] = bad[n].to(bf16)
+            with pytest.raises(TypeError):
+                function.apply(*bad)
+            bad[n] = args[n][:-1]
+            with pytest.raises(ValueError):
+                function.apply(*bad)
+        for kind in (f64, torch.float16, torch.int32):
+            with pytest.raises(TypeError):
+                function.apply(args[0].to(kind), *args[1:])
+        # another type beside the others', as autocast leaves it
+        with pytest.raises(TypeError):
+            function.apply(*([args[0]] + [t.to(bf16) if isinstance(t, torch.Tensor) else t for t in args[1:]]))
+        with pytest.raises(ValueError):
+            function.apply(args[0][0], *args[1:])
+        # memory of the host
+        with pytest.raises(ValueError):
+            function.apply(*args)
+    function, args, _ = weights()[2]
+    for n in (1, 3, 4, 6):
+        for cut in (lambda t: t[:1], lambda t: t[:, :2], lambda t: t[:, :, :3]):
+            bad = list(args)
+            bad[n] = cut(bad[n])
+            with pytest.raises(ValueError):
+                function.apply(*bad)
+
+
+def test_states_and_places_are_checked(monkeypatch):
+    """Decoding: places and lengths are int32, states of the type and extents that the kernels move on in place."""
+    monkeypatch.setattr(sb, "_DEVICE", "cpu", raising=False)
+    for name in ("ucd_group_norm_fwd", "ucd_causal_conv_fwd", "ucd_causal_conv_step", "ucd_scan_fwd", "ucd_scan_step"):
+        monkeypatch.setattr(sb.seq, name, lambda *a, **k: None)
+    block = sb.Block(16, 24, device="cpu")
+    x, slots, lengths = torch.randn(2, 3, 16), torch.tensor([1, 0], dtype=torch.int32), torch.tensor([3, 1], dtype=torch.int32)
+    pools = block.pools(4)
+    assert block.extend(x, pools, slots, lengths).shape == x.shape
+    assert block.extend(x[:, :1], pools, slots).shape == (2, 1, 16)
+    for bad in (dict(slots=slots.long()), dict(lengths=lengths.long()), dict(pools=(pools[0].bfloat16(), pools[1])),
+                dict(pools=(pools[0], pools[1].bfloat16()))):
+        with pytest.raises(TypeError):
+            block.extend(**{**dict(x=x, pools=pools, slots=slots, lengths=lengths), **bad})
+    for bad in (dict(slots=slots[:1]), dict(lengths=lengths[:1]), dict(pools=(pools[0], pools[1][:3])), dict(pools=(pools[0][:, 1:], pools[1])),
+                dict(pools=(pools[0], torch.zeros(4, 16, 24).transpose(1, 2))), dict(x=x[0])):
+        with pytest.raises(ValueError):
+            block.extend(**{**dict(x=x, pools=pools, slots=slots, lengths=lengths), **bad})
