@@ -19,14 +19,9 @@ import torch
 
 from . import seq
 
-_ws = {}
-
-
 def _workspace(nbytes, device):
-    """The program's one workspace of a device, as large as any call needed so far; calls of one stream share it."""
-    if nbytes and (device not in _ws or _ws[device].numel() < nbytes):
-        _ws[device] = torch.empty(nbytes, dtype=torch.uint8, device=device)
-    return _ws.get(device) if nbytes else None
+    """A call's workspace, of the current stream like the call: what other streams or captured graphs hold is never shared."""
+    return torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
 
 
 _DEVICE = "cuda"

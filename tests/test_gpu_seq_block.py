@@ -154,3 +154,57 @@ def test_training_step_in_a_graph():
         torch.cuda.synchronize()
         for k in ("out", "dx", "ddt", "dA", "dB", "dC", "dw", "dg", "db"):
             assert torch.equal(eager[k], captured[k]), (i, k)
+
+
+def test_block_on_two_streams():
+    """Calls on two streams at once, whose scans are in segments and leave partial sums: each gives what it gives alone."""
+    import torch
+    from paper_1804_04806_amd.sequence_block import Block
+    torch.manual_seed(8)
+    blocks = [Block(32, 64) for _ in range(2)]
+    x = [torch.randn(2, 700, 32, device="cuda") for _ in blocks]
+
+    def step(block, x):
+        y = block(x)
+        grads = torch.autograd.grad(y, list(block.parameters()), torch.ones_like(y))
+        return [y.detach(), *grads]
+    want = [step(*pair) for pair in zip(blocks, x)]
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream() for _ in blocks], [[], []]
+    for _ in range(5):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                got[i].append(step(blocks[i], x[i]))
+    torch.cuda.synchronize()
+    for i, w in enumerate(want):
+        for g in got[i]:
+            assert all(torch.equal(a, b) for a, b in zip(w, g)), i
+
+
+def test_captured_block_and_larger_calls():
+    """A captured prompt whose scan has a workspace, replayed after eager calls that need larger ones."""
+    import torch
+    from paper_1804_04806_amd.sequence_block import Block
+    torch.manual_seed(9)
+    block = Block(32, 64)
+    slots = torch.tensor([2, 0], dtype=torch.int32, device="cuda")
+    x = torch.randn(2, 200, 32, device="cuda")
+    eager, captured = block.pools(3), block.pools(3)
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        for _ in range(2):
+            block.extend(x, block.pools(3), slots)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = block.extend(x, captured, slots)
+    for i in range(4):
+        big = torch.randn(3, 900 + 300 * i, 32, device="cuda")
+        block.extend(big, block.pools(3), torch.arange(3, dtype=torch.int32, device="cuda"))
+        junk = [torch.full((1 << 22,), float("nan"), device="cuda") for _ in range(4)]
+        x.copy_(torch.randn_like(x))
+        want = block.extend(x, eager, slots)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(bool(torch.isnan(j).all()) for j in junk)
+        assert torch.equal(out, want) and all(torch.equal(a, b) for a, b in zip(eager, captured)), i

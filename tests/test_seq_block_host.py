@@ -133,3 +133,11 @@ def test_states_and_places_are_checked(monkeypatch):
                 dict(pools=(pools[0], torch.zeros(4, 16, 24).transpose(1, 2))), dict(x=x[0])):
         with pytest.raises(ValueError):
             block.extend(**{**dict(x=x, pools=pools, slots=slots, lengths=lengths), **bad})
+
+
+def test_workspaces_are_a_calls_own():
+    """Calls on two streams may run at once, and a captured one runs again later: none has the memory of another's workspace."""
+    first, second, larger = (sb._workspace(n, torch.device("cpu")) for n in (4096, 64, 1 << 16))
+    spans = sorted((t.data_ptr(), t.data_ptr() + t.numel()) for t in (first, second, larger))
+    assert all(end <= begin for (_, end), (begin, _) in zip(spans, spans[1:]))
+    assert [t.numel() for t in (first, second, larger)] == [4096, 64, 1 << 16]
