@@ -427,8 +427,9 @@ template <class T, class W, bool WIDE, bool GATE>
 void launch_main(const ScanParams &p, hipStream_t s)
 {
     const unsigned units = scan_units(p), grid = std::min(units, 1u << 22);
+    if (units == 0) return;       // no sequences: the joins write the gradients of the weights
     if (p.segs > 1) scan_bwd_kernel<T, W, WIDE, GATE, true><<<grid, 64 * kWaves, 0, s>>>(p, units);
-    if (units > 0) scan_bwd_kernel<T, W, WIDE, GATE, false><<<grid, 64 * kWaves, 0, s>>>(p, units);
+    scan_bwd_kernel<T, W, WIDE, GATE, false><<<grid, 64 * kWaves, 0, s>>>(p, units);
 }
 
 template <class T, class W, bool WIDE>
