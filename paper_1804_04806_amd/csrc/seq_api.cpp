@@ -14,6 +14,8 @@ namespace {
 
 constexpr int64_t kMaxStride = int64_t(1) << 40, kMaxInner = int64_t(1) << 25;   // a tile of 16 tokens and more in 32-bit offsets of bytes
 constexpr int64_t kMaxElements = int64_t(1) << 40;
+// Positions, sequences and what they are divided into are counted in 32 bits, and loops over them step up to 2^20 beyond their end.
+constexpr int32_t kMaxExtent = 1 << 30;
 
 template <class F>
 int guarded(F body) noexcept
@@ -51,6 +53,7 @@ bool fill_strides(int64_t &outer, int64_t &inner, int64_t n_outer, int64_t n_inn
     return true;
 }
 
+bool extent_ok(int32_t n, int32_t least) { return n >= least && n <= kMaxExtent; }
 bool dtype_ok(int dtype) { return dtype == 0 || dtype == 1; }
 bool act_ok(int act) { return act == UCD_ACT_NONE || act == UCD_ACT_SILU; }
 bool aligned(const void *p, int dtype) { return ((uintptr_t)p & (dtype == 1 ? 1u : 3u)) == 0; }
@@ -69,7 +72,7 @@ int ws_status(size_t need, const void *ws, size_t ws_bytes)
 bool norm_ok(const ucd_group_norm_t *in, ucd_group_norm_t &d)
 {
     d = *in;
-    if (d.N < 1 || d.S < 1 || d.C < 1 || d.G < 1 || d.C % d.G != 0 || !act_ok(d.act) || !dtype_ok(d.dtype)) return false;
+    if (!extent_ok(d.N, 1) || !extent_ok(d.S, 1) || !extent_ok(d.C, 1) || d.G < 1 || d.C % d.G != 0 || !act_ok(d.act) || !dtype_ok(d.dtype)) return false;
     if (!(d.eps >= 0.f) || std::isinf(d.eps)) return false;
     if ((double)d.N * d.S * d.C > (double)kMaxElements) return false;
     return fill_strides(d.x_n, d.x_s, d.N, d.S, d.C) && fill_strides(d.y_n, d.y_s, d.N, d.S, d.C);
@@ -78,7 +81,7 @@ bool norm_ok(const ucd_group_norm_t *in, ucd_group_norm_t &d)
 bool conv_ok(const ucd_causal_conv_t *in, ucd_causal_conv_t &d)
 {
     d = *in;
-    if (d.B < 0 || d.L < 0 || d.D < 1 || d.K < 1 || d.K > 8 || !act_ok(d.act) || !dtype_ok(d.dtype) || d.n_slots < 0) return false;
+    if (!extent_ok(d.B, 0) || !extent_ok(d.L, 0) || !extent_ok(d.D, 1) || d.K < 1 || d.K > 8 || !act_ok(d.act) || !dtype_ok(d.dtype) || d.n_slots < 0) return false;
     if ((double)d.B * (d.L + 1) * d.D > (double)kMaxElements) return false;
     return fill_strides(d.x_b, d.x_l, d.B, d.L, d.D) && fill_strides(d.y_b, d.y_l, d.B, d.L, d.D);
 }
@@ -86,7 +89,7 @@ bool conv_ok(const ucd_causal_conv_t *in, ucd_causal_conv_t &d)
 bool scan_ok(const ucd_scan_t *in, ucd_scan_t &d)
 {
     d = *in;
-    if (d.B < 0 || d.L < 0 || d.D < 1 || d.N < 1 || d.N > 64 || d.G < 1 || d.D % d.G != 0 || !dtype_ok(d.dtype)) return false;
+    if (!extent_ok(d.B, 0) || !extent_ok(d.L, 0) || !extent_ok(d.D, 1) || d.N < 1 || d.N > 64 || d.G < 1 || d.D % d.G != 0 || !dtype_ok(d.dtype)) return false;
     if (d.softplus != 0 && d.softplus != 1) return false;
     if (d.n_slots < 0 || (double)d.B * (d.L + 1) * d.D > (double)kMaxElements) return false;
     const int64_t GN = (int64_t)d.G * d.N;
