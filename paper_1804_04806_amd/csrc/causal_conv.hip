@@ -375,12 +375,11 @@ __global__ __launch_bounds__(256) void conv_bwd_kernel(ConvParams p)
 __global__ __launch_bounds__(kJoinThreads) void conv_join_kernel(ConvParams p)
 {
     const int K = p.d.K;
-    const long i = blockIdx.x * (long)kJoinColumns + threadIdx.x % kJoinColumns, row = (long)(K + 1) * p.d.D;
-    const float v = join_rows(p.part, p.part_rows, row, i);
-    if (i >= row || threadIdx.x >= kJoinColumns) return;
-    const int c = (int)(i % p.d.D), k = (int)(i / p.d.D);
-    float *out = k < K ? p.a.dw + (long)c * K + k : p.a.dbias ? p.a.dbias + c : nullptr;
-    if (out) *out = v + (p.add ? *out : 0.f);
+    join_columns(p.part, p.part_rows, (long)(K + 1) * p.d.D, [&](long i, float v) {
+        const int c = (int)(i % p.d.D), k = (int)(i / p.d.D);
+        float *out = k < K ? p.a.dw + (long)c * K + k : p.a.dbias ? p.a.dbias + c : nullptr;
+        if (out) *out = v + (p.add ? *out : 0.f);
+    });
 }
 
 // Packs: Forward 16 bytes.  Backward keeps four times as much of a channel in registers (its window of tokens and gradients, filter and their sums):
@@ -428,7 +427,7 @@ template <class T, int VE, int K, bool SILU>
 hipError_t run_bwd(const ConvParams &p, hipStream_t s)
 {
     conv_bwd_kernel<T, VE, K, SILU><<<p.blocks_x * p.part_rows, 256, 0, s>>>(p);
-    conv_join_kernel<<<(unsigned)(((long)(K + 1) * p.d.D + kJoinColumns - 1) / kJoinColumns), kJoinThreads, 0, s>>>(p);
+    conv_join_kernel<<<join_grid((long)(K + 1) * p.d.D), kJoinThreads, 0, s>>>(p);
     return hipGetLastError();
 }
 

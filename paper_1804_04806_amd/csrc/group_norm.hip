@@ -49,6 +49,7 @@ struct NormParams {
     int lanes, gx, ry, columns;  // lanes to a group; groups and samples of a workgroup; workgroups for all groups
     // slabs, parts
     int px, py, strips;          // packs of a strip, positions of a pass; strips of a row
+    unsigned unit0;              // slabs: a launch's first workgroup
     int gps, cs;                 // groups of a strip, or strips of a group
     int chunk, chunks;           // positions of a part, parts of a sample's positions
     bool in_wave;                // strips and their groups are powers of two of lanes
@@ -443,7 +444,7 @@ template <bool SILU, bool TAIL, class T, int VE, int R>
 __global__ __launch_bounds__(kMaxThreads, (slab_waves<T, VE, R>())) void norm_slab_fwd_kernel(NormParams p)
 {
     int strip, first;
-    if (!strip_of(blockIdx.x, p.strips, p.part_rows, strip, first)) return;
+    if (!strip_of(p.unit0 + blockIdx.x, p.strips, p.part_rows, strip, first)) return;
     const SlabPlace<VE> at(p, strip);
     for (int n = first; n < p.d.N; n += p.part_rows) {
         Slab<T, VE, R> x;
@@ -538,7 +539,7 @@ template <bool SILU, bool TAIL, class T, int VE, int R>
 __global__ __launch_bounds__(kMaxThreads) void norm_slab_bwd_kernel(NormParams p)
 {
     int strip, part_row;
-    if (!strip_of(blockIdx.x, p.strips, p.part_rows, strip, part_row)) return;
+    if (!strip_of(p.unit0 + blockIdx.x, p.strips, p.part_rows, strip, part_row)) return;
     const SlabPlace<VE> at(p, strip);
     float gamma[VE] = {}, beta[VE] = {}, dg[VE] = {}, db[VE] = {};
     if (at.active) {
@@ -666,11 +667,10 @@ __global__ __launch_bounds__(kMaxThreads, BACKWARD || VE * sizeof(T) == 16 ? 4 :
 
 __global__ __launch_bounds__(kJoinThreads) void norm_join_kernel(NormParams p)
 {
-    const long i = blockIdx.x * (long)kJoinColumns + threadIdx.x % kJoinColumns, row = 2l * p.d.C;
-    const float v = join_rows(p.part, p.part_rows, row, i);
-    if (i >= row || threadIdx.x >= kJoinColumns) return;
-    float *out = i < p.d.C ? p.dgamma + i : p.dbeta + (i - p.d.C);
-    *out = v + (p.add ? *out : 0.f);
+    join_columns(p.part, p.part_rows, 2l * p.d.C, [&](long i, float v) {
+        float *out = i < p.d.C ? p.dgamma + i : p.dbeta + (i - p.d.C);
+        *out = v + (p.add ? *out : 0.f);
+    });
 }
 
 // ---- which way, and how it is divided ------------------------------------------------------------------------------------------------------------
@@ -798,18 +798,21 @@ hipError_t launch(NormParams &p, void *ws, hipStream_t s)
     }
     p.sums = (float *)at;
     constexpr int MOST = slab_packs<T, VE>(false), FEW = slab_packs<T, VE>(true);
+    // 2^21 workgroups of up to 1024 threads to a launch: 2^32 threads are no grid
+    const unsigned units = strip_units(p), grid = std::min(units, 1u << 21);
     if (way == PARTS) {
-        const unsigned units = strip_units(p), grid = std::min(units, 1u << 21);
         norm_part_kernel<SILU, TAIL, T, VE, MOST, BACKWARD><<<grid, threads, 0, s>>>(p, units);
         norm_apply_kernel<SILU, T, VE, MOST, BACKWARD><<<grid, threads, 0, s>>>(p, units);
     } else if (way == SLABS) {
-        const unsigned grid = strip_units(p);
-        if constexpr (BACKWARD) {
-            if (R == FEW) norm_slab_bwd_kernel<SILU, TAIL, T, VE, FEW><<<grid, threads, 0, s>>>(p);
-            else norm_slab_bwd_kernel<SILU, TAIL, T, VE, MOST><<<grid, threads, 0, s>>>(p);
-        } else {
-            if (R == FEW) norm_slab_fwd_kernel<SILU, TAIL, T, VE, FEW><<<grid, threads, 0, s>>>(p);
-            else norm_slab_fwd_kernel<SILU, TAIL, T, VE, MOST><<<grid, threads, 0, s>>>(p);
+        for (p.unit0 = 0; p.unit0 < units; p.unit0 += grid) {
+            const unsigned now = std::min(grid, units - p.unit0);
+            if constexpr (BACKWARD) {
+                if (R == FEW) norm_slab_bwd_kernel<SILU, TAIL, T, VE, FEW><<<now, threads, 0, s>>>(p);
+                else norm_slab_bwd_kernel<SILU, TAIL, T, VE, MOST><<<now, threads, 0, s>>>(p);
+            } else {
+                if (R == FEW) norm_slab_fwd_kernel<SILU, TAIL, T, VE, FEW><<<now, threads, 0, s>>>(p);
+                else norm_slab_fwd_kernel<SILU, TAIL, T, VE, MOST><<<now, threads, 0, s>>>(p);
+            }
         }
     } else {
         const unsigned grid = (unsigned)p.columns * p.part_rows;
@@ -821,7 +824,7 @@ hipError_t launch(NormParams &p, void *ws, hipStream_t s)
             else norm_rows_fwd_kernel<SILU, T, VE, kRowsR><<<grid, threads, 0, s>>>(p);
         }
     }
-    if (BACKWARD) norm_join_kernel<<<ceil_div(2l * d.C, kJoinColumns), kJoinThreads, 0, s>>>(p);
+    if (BACKWARD) norm_join_kernel<<<join_grid(2l * d.C), kJoinThreads, 0, s>>>(p);
     return hipGetLastError();
 }
 

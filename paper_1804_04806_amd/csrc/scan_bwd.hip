@@ -414,13 +414,12 @@ __global__ __launch_bounds__(256) void scan_join_bc_kernel(ScanParams p, int np,
 __global__ __launch_bounds__(kJoinThreads) void scan_join_weights_kernel(ScanParams p)
 {
     const ucd_scan_t &d = p.d;
-    const long i = blockIdx.x * (long)kJoinColumns + threadIdx.x % kJoinColumns, row = (long)d.D * (d.N + 2);
-    const float v = join_rows(p.part_w, (long)d.B * p.segs, row, i);
-    if (i >= row || threadIdx.x >= kJoinColumns) return;
-    const int k = (int)(i % (d.N + 2));
-    const long c = i / (d.N + 2);
-    float *out = k < d.N ? p.g.A + c * d.N + k : k == d.N ? (p.in.skip ? p.g.skip + c : nullptr) : p.in.dt_bias ? p.g.dt_bias + c : nullptr;
-    if (out) *out = v + (p.add ? *out : 0.f);
+    join_columns(p.part_w, (long)d.B * p.segs, (long)d.D * (d.N + 2), [&](long i, float v) {
+        const int k = (int)(i % (d.N + 2));
+        const long c = i / (d.N + 2);
+        float *out = k < d.N ? p.g.A + c * d.N + k : k == d.N ? (p.in.skip ? p.g.skip + c : nullptr) : p.in.dt_bias ? p.g.dt_bias + c : nullptr;
+        if (out) *out = v + (p.add ? *out : 0.f);
+    });
 }
 
 template <class T, class W, bool WIDE, bool GATE>
@@ -441,7 +440,7 @@ hipError_t launch(const ScanParams &p, hipStream_t s)
     const long elements = (long)d.B * d.L * d.G * 2 * W::NP / 4;
     if (elements > 0)
         scan_join_bc_kernel<T><<<(unsigned)std::min((elements + 255) / 256, 1l << 22), 256, 0, s>>>(p, W::NP, elements);
-    scan_join_weights_kernel<<<(unsigned)(((long)d.D * (d.N + 2) + kJoinColumns - 1) / kJoinColumns), kJoinThreads, 0, s>>>(p);
+    scan_join_weights_kernel<<<join_grid((long)d.D * (d.N + 2)), kJoinThreads, 0, s>>>(p);
     return hipGetLastError();
 }
 

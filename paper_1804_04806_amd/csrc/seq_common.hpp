@@ -2,6 +2,7 @@
 #pragma once
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cstdint>
 
 namespace ucd {
@@ -248,6 +249,20 @@ __device__ __forceinline__ float join_rows(const float *part, long rows, long ro
 #pragma unroll
     for (int g = 1; g < GROUPS; ++g) v += lds[g][x];
     return v;
+}
+
+// out(column, sum) for all columns.  A grid of 2^32 threads is none, so that workgroups may have several times 64 columns.
+inline unsigned join_grid(long columns) { return (unsigned)std::min((columns + kJoinColumns - 1) / kJoinColumns, 1l << 21); }
+
+template <class F>
+__device__ __forceinline__ void join_columns(const float *part, long rows, long row_length, F out)
+{
+    for (long first = blockIdx.x * (long)kJoinColumns; first < row_length; first += gridDim.x * (long)kJoinColumns) {
+        const long column = first + threadIdx.x % kJoinColumns;
+        const float v = join_rows(part, rows, row_length, column);
+        if (column < row_length && threadIdx.x < kJoinColumns) out(column, v);
+        __syncthreads();
+    }
 }
 
 // Orders a wave's own LDS accesses: the hardware runs them in program order, the compiler has to keep them so.
