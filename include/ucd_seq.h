@@ -6,9 +6,9 @@
  * codes, no allocation, no synchronisation, nothing launched by a call that fails)
  *   - Channels are the last extent and contiguous.  Every activation tensor has two strides, in
  *     elements, of its sequence (sample) and of its token (position); 0 stands for the dense one.
- *     An extent is at most 2^30, a tensor has at most 2^40 elements; rows must not overlap, a
- *     token's stride is at most 2^25 and a sequence's 2^40 (UCD_E_INVALID otherwise); a gradient
- *     has the strides of its tensor.
+ *     An extent is at most 2^30, a row 2^25 elements, a tensor 2^40; rows must not overlap, a
+ *     token's stride is at most 2^25 and a sequence's 2^40 (UCD_E_INVALID otherwise), but for
+ *     those of an extent of one, which are not taken; a gradient has the strides of its tensor.
  *   - dtype 0: activations (and their gradients, filters and convolution states) fp32; dtype 1:
  *     bfloat16, rounded to nearest-even once.  Everything else is fp32: norm weights, biases, A,
  *     skip, scan states, statistics, gradients of all weights; and so is all arithmetic.

@@ -37,12 +37,15 @@ int hip_status(hipError_t e)
     return UCD_E_HIP;
 }
 
-// Fills in dense strides; false where rows of `width` elements would overlap.
+// Fills in dense strides; false where rows of `width` elements would overlap.  Those of an extent of one are never taken, and may be anything.
 bool fill_strides(int64_t &outer, int64_t &inner, int64_t n_outer, int64_t n_inner, int64_t width)
 {
+    if (outer < 0 || inner < 0 || width > kMaxInner || (n_inner > 1 && inner > kMaxInner)) return false;
     if (inner == 0) inner = width;
     if (outer == 0) outer = inner * (n_inner > 1 ? n_inner : 1);
-    if (outer < 0 || inner < 0 || outer > kMaxStride || inner > kMaxInner) return false;
+    if (n_inner <= 1) inner = width;
+    if (n_outer <= 1) outer = width;
+    if (outer > kMaxStride) return false;
     if (n_inner > 1 && inner < width) return false;
     if (n_outer > 1 && outer < width) return false;
     if (n_inner > 1 && n_outer > 1) {

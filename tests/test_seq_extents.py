@@ -58,3 +58,35 @@ def test_the_largest(n):
     need = 4 * ((n + 15) // 16) * 16 * 2 * 4
     assert need < seq.ucd_scan_workspace_size(seq.scan(1, n, 4, 4), seq.BWD) < need + 65 * 4 * (4 * 4 + 4 + 4 * 6)
     assert seq.ucd_group_norm_workspace_size(seq.group_norm(n, 1, 1, 1), seq.FWD) == 0
+
+
+ANY = [1, 1 << 26, 1 << 41, 1 << 62]       # strides that an extent of one never takes
+
+
+@pytest.mark.parametrize("inner", [1] + ANY)
+def test_channels_beyond(inner):
+    """2^25 channels are the most, also where there is a single token whose stride says nothing about them."""
+    n = (1 << 25) + 64
+    desc = seq.group_norm(1, 1, n, 1, x_stride=(0, inner), y_stride=(0, inner))
+    assert seq.ucd_group_norm_workspace_size(desc, seq.FWD) == ucd.WS_NA
+    refused(seq.ucd_group_norm_fwd, desc, P, P, P, P, **WS)
+    desc = seq.causal_conv(1, 1, n, 4, x_stride=(0, inner), y_stride=(0, inner))
+    assert seq.ucd_causal_conv_workspace_size(desc) == ucd.WS_NA
+    refused(seq.ucd_causal_conv_step, desc, P, P, P, P, P, stream=0)
+    for D, N, G in ((n, 4, 1), (1 << 20, 64, 1 << 20)):
+        desc = seq.scan(1, 1, D, N, G, **{k + "_stride": (0, inner) for k in ("u", "dt", "Bm", "Cm", "z", "y")})
+        assert seq.ucd_scan_saved_size(desc) == ucd.WS_NA
+        refused(seq.ucd_scan_step, desc, P, P, P, P, P, P, P, stream=0)
+
+
+@pytest.mark.parametrize("any", ANY)
+def test_strides_of_an_extent_of_one(any):
+    size = seq.ucd_group_norm_workspace_size
+    assert size(seq.group_norm(5, 1, 64, 4, x_stride=(64, any), y_stride=(96, any)), seq.BWD) == size(seq.group_norm(5, 1, 64, 4), seq.BWD)
+    assert size(seq.group_norm(1, 5, 64, 4, x_stride=(any, 64)), seq.BWD) == size(seq.group_norm(1, 5, 64, 4), seq.BWD)
+    size = seq.ucd_causal_conv_workspace_size
+    assert size(seq.causal_conv(5, 1, 64, 4, x_stride=(64, any))) == size(seq.causal_conv(5, 1, 64, 4))
+    assert size(seq.causal_conv(1, 5, 64, 4, y_stride=(any, 64))) == size(seq.causal_conv(1, 5, 64, 4))
+    size, names = seq.ucd_scan_saved_size, ("u", "dt", "Bm", "Cm", "z", "y")
+    assert size(seq.scan(5, 1, 64, 16, **{k + "_stride": (64, any) for k in names})) == size(seq.scan(5, 1, 64, 16))
+    assert size(seq.scan(1, 5, 64, 16, **{k + "_stride": (any, 64) for k in names})) == size(seq.scan(1, 5, 64, 16))
