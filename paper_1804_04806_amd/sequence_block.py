@@ -76,6 +76,24 @@ def _dense(*tensors):
     return (None if t is None else t.contiguous() for t in tensors)
 
 
+class _Once(torch.autograd.Function):
+    """Gradients that raise where they are differentiated again: the operators have no second derivatives."""
+
+    @staticmethod
+    def forward(ctx, n, *tensors):
+        return tensors[n:]
+
+    @staticmethod
+    def backward(ctx, *_):
+        raise RuntimeError("the sequence operators' gradients cannot be differentiated again")
+
+
+def _once(given, grads):
+    """A backward's results, which depend on `given`.  Where a graph of them is built (create_graph) their node is connected to
+    those, so that whatever is differentiated with respect to them reaches it; otherwise the part would be left out."""
+    return _Once.apply(len(given), *given, *grads) if torch.is_grad_enabled() else grads
+
+
 class GroupNorm(torch.autograd.Function):
     """Group norm of single tokens: x (B, L, C)."""
 
@@ -84,23 +102,24 @@ class GroupNorm(torch.autograd.Function):
         _dtype(x)
         c = _tokens("x", x)[2:]
         _check(("x", x, x.shape, x.dtype), ("gamma", gamma, c, torch.float32), ("beta", beta, c, torch.float32))
-        x, gamma, beta = _dense(x, gamma, beta)
+        given = x, gamma, beta
+        x, gamma, beta = _dense(*given)
         n = x.shape[0] * x.shape[1]
         desc = seq.group_norm(n, 1, x.shape[2], groups, act=int(silu), dtype=_dtype(x))
         y, stats = torch.empty_like(x), torch.empty(2, n, groups, device=x.device)
         seq.ucd_group_norm_fwd(desc, x, gamma, beta, y, stats,
                                ws=_workspace(seq.ucd_group_norm_workspace_size(desc, seq.FWD), x.device))
-        ctx.save_for_backward(x, gamma, beta, stats)
+        ctx.save_for_backward(x, gamma, beta, stats, *given)
         ctx.desc = desc
         return y
 
     @staticmethod
     def backward(ctx, dy):
-        x, gamma, beta, stats = ctx.saved_tensors
+        x, gamma, beta, stats, *given = ctx.saved_tensors
         dx, dgamma, dbeta = torch.empty_like(x), torch.empty_like(gamma), torch.empty_like(beta)
         seq.ucd_group_norm_bwd(ctx.desc, x, gamma, beta, stats, dy.contiguous(), dx, dgamma, dbeta,
                                ws=_workspace(seq.ucd_group_norm_workspace_size(ctx.desc, seq.BWD), x.device))
-        return dx, dgamma, dbeta, None, None
+        return _once((dy, *given), (dx, dgamma, dbeta, None, None))
 
 
 class CausalConv(torch.autograd.Function):
@@ -111,23 +130,24 @@ class CausalConv(torch.autograd.Function):
         _dtype(x)
         b, l, d = _tokens("x", x)
         _check(("x", x, x.shape, x.dtype), ("w", w, (d, w.shape[-1]), x.dtype), ("bias", bias, (d,), torch.float32))
+        given = x, w, bias
         x, stride = _rows(x)
         w, bias = _dense(w, bias)
         desc = seq.causal_conv(b, l, d, w.shape[1], act=seq.ACT_SILU, dtype=_dtype(x), x_stride=stride)
         y = torch.empty(b, l, d, dtype=x.dtype, device=x.device)
         seq.ucd_causal_conv_fwd(desc, x, w, bias, y)
-        ctx.save_for_backward(x, w, bias)
+        ctx.save_for_backward(x, w, bias, *given)
         ctx.desc = desc
         return y
 
     @staticmethod
     def backward(ctx, dy):
-        x, w, bias = ctx.saved_tensors
+        x, w, bias, *given = ctx.saved_tensors
         dx = torch.empty_strided(x.shape, x.stride(), dtype=x.dtype, device=x.device)
         dw, dbias = torch.empty(w.shape, device=w.device), torch.empty_like(bias)
         seq.ucd_causal_conv_bwd(ctx.desc, x, w, bias, dy.contiguous(), dx, dw, dbias,
                                 ws=_workspace(seq.ucd_causal_conv_workspace_size(ctx.desc), x.device))
-        return dx, dw.to(w.dtype), dbias
+        return _once((dy, *given), (dx, dw.to(w.dtype), dbias))
 
 
 class Scan(torch.autograd.Function):
@@ -142,6 +162,7 @@ class Scan(torch.autograd.Function):
         _check(("u", u, u.shape, u.dtype), ("dt", dt, u.shape, u.dtype), ("z", z, u.shape, u.dtype), ("Bm", Bm, states[0], u.dtype),
                ("Cm", Cm, states[1], u.dtype), ("A", A, (d, n), torch.float32), ("skip", skip, (d,), torch.float32),
                ("dt_bias", dt_bias, (d,), torch.float32))
+        given = u, dt, A, Bm, Cm, skip, z, dt_bias
         rows = {k: _rows(t) for k, t in dict(u=u, dt=dt, Bm=Bm, Cm=Cm, z=z).items()}
         u, dt, Bm, Cm, z = (rows[k][0] for k in ("u", "dt", "Bm", "Cm", "z"))
         A, skip, dt_bias = _dense(A, skip, dt_bias)
@@ -150,20 +171,19 @@ class Scan(torch.autograd.Function):
         saved = torch.empty(seq.ucd_scan_saved_size(desc), dtype=torch.uint8, device=u.device)
         seq.ucd_scan_fwd(desc, u, dt, A, Bm, Cm, y, skip=skip, z=z, dt_bias=dt_bias, saved=saved,
                          ws=_workspace(seq.ucd_scan_workspace_size(desc, seq.FWD), u.device))
-        ctx.save_for_backward(u, dt, A, Bm, Cm, skip, z, dt_bias, saved)
+        ctx.save_for_backward(u, dt, A, Bm, Cm, skip, z, dt_bias, saved, *given)
         ctx.desc = desc
         return y
 
     @staticmethod
     def backward(ctx, dy):
-        *given, saved = ctx.saved_tensors
-        u, dt, A, Bm, Cm, skip, z, dt_bias = given
+        u, dt, A, Bm, Cm, skip, z, dt_bias, saved, *given = ctx.saved_tensors
         du, ddt, dA, dBm, dCm, dskip, dz, dbias = (torch.empty_strided(t.shape, t.stride(), dtype=t.dtype, device=t.device)
-                                                   for t in given)
+                                                   for t in (u, dt, A, Bm, Cm, skip, z, dt_bias))
         seq.ucd_scan_bwd(ctx.desc, u, dt, A, Bm, Cm, dy.contiguous(), saved, du, ddt, dA, dBm, dCm, skip=skip, dskip=dskip,
                          z=z, dz=dz, dt_bias=dt_bias, ddt_bias=dbias,
                          ws=_workspace(seq.ucd_scan_workspace_size(ctx.desc, seq.BWD), u.device))
-        return du, ddt, dA, dBm, dCm, dskip, dz, dbias
+        return _once((dy, *given), (du, ddt, dA, dBm, dCm, dskip, dz, dbias))
 
 
 class Block(torch.nn.Module):

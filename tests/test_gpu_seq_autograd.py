@@ -159,3 +159,20 @@ def test_block_under_autocast():
     for i, (a, b) in enumerate(zip(*got)):
         assert a.dtype == b.dtype == torch.float32
         assert float((a - b).norm()) <= (10 if i == 0 else 20) * 2.0 ** -8 * float(a.norm()), i
+
+
+def test_gradients_of_gradients():
+    """With create_graph the gradients are the same; a penalty on them raises instead of leaving the operators' part out."""
+    import torch
+    from paper_1804_04806_amd.sequence_block import Block
+    torch.manual_seed(8)
+    block, x = Block(16, 24), torch.randn(2, 9, 16, device="cuda", requires_grad=True)
+    leaves = [x] + list(block.parameters())
+    plain = torch.autograd.grad(block(x).sum(), leaves)
+    graph = torch.autograd.grad(block(x).sum(), leaves, create_graph=True)
+    assert all(torch.equal(a, b) for a, b in zip(plain, graph))
+    for wanted in (leaves, [x], [block.gamma], [block.w_out]):
+        with pytest.raises(RuntimeError, match="differentiated again"):
+            torch.autograd.grad(graph[0].square().sum(), wanted, retain_graph=True)
+    with pytest.raises(RuntimeError, match="differentiated again"):
+        graph[0].square().sum().backward()

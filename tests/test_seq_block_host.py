@@ -141,3 +141,21 @@ def test_workspaces_are_a_calls_own():
     spans = sorted((t.data_ptr(), t.data_ptr() + t.numel()) for t in (first, second, larger))
     assert all(end <= begin for (_, end), (begin, _) in zip(spans, spans[1:]))
     assert [t.numel() for t in (first, second, larger)] == [4096, 64, 1 << 16]
+
+
+@pytest.mark.parametrize("i", range(3), ids=["norm", "conv", "scan"])
+def test_second_derivatives_are_refused(i, monkeypatch):
+    """The operators have none: a gradient of a gradient raises, instead of leaving the operators' part out."""
+    monkeypatch.setattr(sb, "_DEVICE", "cpu", raising=False)
+    for name in sb.seq.EXPORTS:
+        if not name.endswith("_size"):
+            monkeypatch.setattr(sb.seq, name, lambda *a, **k: None)
+    function, args, names = weights()[i]
+    args = [t.clone().requires_grad_() if isinstance(t, torch.Tensor) else t for t in args]
+    leaves = [t for t in args if isinstance(t, torch.Tensor)]
+    y = function.apply(*args)
+    first = torch.autograd.grad(y, leaves, (torch.ones_like(y) * args[0]), create_graph=True)
+    # a penalty on the gradients beside something that is differentiable twice
+    penalty = sum(g.square().sum() for g in first) + args[0].pow(3).sum()
+    with pytest.raises(RuntimeError, match="differentiat"):
+        torch.autograd.grad(penalty, leaves, allow_unused=True)
