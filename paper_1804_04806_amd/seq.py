@@ -1,6 +1,7 @@
 """ctypes binding of the sequence operators: the same entry points as include/ucd_seq.h, argument
 marshalling only.  Device buffers are torch tensors (their ``data_ptr()``), raw integer addresses or
-None; the library is the one ``ucd.lib()`` loads.
+None; the library is the one ``ucd.lib()`` loads.  Kernels are launched on the current device, which has to be the
+buffers', and by default on its current stream.
 """
 import ctypes
 import struct

@@ -13,6 +13,8 @@ tokens by a short causal convolution and all earlier ones by a selective scan.
 Training runs Forward and Backward through ``torch.autograd``; decoding keeps the convolution's last tokens and the
 scan's states of every sequence in pools, fills them from prompts of any lengths and moves on by single tokens.
 """
+import contextlib
+import functools
 import math
 
 import torch
@@ -71,6 +73,15 @@ def _rows(t):
     return t, tuple(stride if n > 1 else 0 for stride, n in zip(t.stride()[:2], t.shape[:2]))
 
 
+def _on_device(method):
+    """The method with its first tensor's device as the current one, on which the operators launch."""
+    @functools.wraps(method)
+    def run(owner, x, *args, **kw):
+        with torch.cuda.device(x.device) if x.is_cuda else contextlib.nullcontext():
+            return method(owner, x, *args, **kw)
+    return run
+
+
 def _dense(*tensors):
     """Tensors without strides of their own, as the operators read weights."""
     return (None if t is None else t.contiguous() for t in tensors)
@@ -98,6 +109,7 @@ class GroupNorm(torch.autograd.Function):
     """Group norm of single tokens: x (B, L, C)."""
 
     @staticmethod
+    @_on_device
     def forward(ctx, x, gamma, beta, groups, silu):
         _dtype(x)
         c = _tokens("x", x)[2:]
@@ -114,6 +126,7 @@ class GroupNorm(torch.autograd.Function):
         return y
 
     @staticmethod
+    @_on_device
     def backward(ctx, dy):
         x, gamma, beta, stats, *given = ctx.saved_tensors
         dx, dgamma, dbeta = torch.empty_like(x), torch.empty_like(gamma), torch.empty_like(beta)
@@ -126,6 +139,7 @@ class CausalConv(torch.autograd.Function):
     """SiLU of the short causal convolution: x (B, L, D), w (D, K) of x's type, bias (D) fp32."""
 
     @staticmethod
+    @_on_device
     def forward(ctx, x, w, bias):
         _dtype(x)
         b, l, d = _tokens("x", x)
@@ -141,6 +155,7 @@ class CausalConv(torch.autograd.Function):
         return y
 
     @staticmethod
+    @_on_device
     def backward(ctx, dy):
         x, w, bias, *given = ctx.saved_tensors
         dx = torch.empty_strided(x.shape, x.stride(), dtype=x.dtype, device=x.device)
@@ -154,6 +169,7 @@ class Scan(torch.autograd.Function):
     """The gated selective scan: u, dt, z (B, L, D) and Bm, Cm (B, L, N) of one type; A (D, N), skip, dt_bias (D) fp32."""
 
     @staticmethod
+    @_on_device
     def forward(ctx, u, dt, A, Bm, Cm, skip, z, dt_bias):
         _dtype(u)
         b, l, d = _tokens("u", u)
@@ -176,6 +192,7 @@ class Scan(torch.autograd.Function):
         return y
 
     @staticmethod
+    @_on_device
     def backward(ctx, dy):
         u, dt, A, Bm, Cm, skip, z, dt_bias, saved, *given = ctx.saved_tensors
         du, ddt, dA, dBm, dCm, dskip, dz, dbias = (torch.empty_strided(t.shape, t.stride(), dtype=t.dtype, device=t.device)
@@ -239,6 +256,7 @@ class Block(torch.nn.Module):
                 torch.zeros(n, self.inner, self.states, device=device))
 
     @torch.no_grad()
+    @_on_device
     def extend(self, x, pools, slots, lengths=None):
         """Outputs for the next tokens x (B, L, width) of the sequences in `slots`, whose states move on; with `lengths`
         prompts of their own lengths, padded to L.  One token takes the single-token kernels."""
