@@ -115,8 +115,8 @@ bool empty(int B, int L) { return B == 0 || L == 0; }
 // Workgroups of the scan's launches, 16 channels each at least: their kernels count them in 32 bits.
 double scan_workgroups(const ucd_scan_t &d) { return (double)d.B * (d.D / 16 + d.G); }
 
-// A pool needs its slots and slots their pool.
-bool slots_ok(int n_slots, const int32_t *slots) { return (n_slots > 0) == (slots != nullptr); }
+// A pool needs its slots, where there are any, and slots their pool.
+bool slots_ok(int B, int n_slots, const int32_t *slots) { return n_slots > 0 ? slots != nullptr || B == 0 : slots == nullptr; }
 
 int scan_inputs(const ucd_scan_t &d, const ucd_scan_in_t *in)
 {
@@ -187,7 +187,7 @@ int ucd_causal_conv_fwd(const ucd_causal_conv_t *conv, const void *x, const void
     return guarded([&]() -> int {
         if (!conv || !w) return UCD_E_NULLPTR;
         ucd_causal_conv_t d;
-        if (!conv_ok(conv, d) || !slots_ok(d.n_slots, slots)) return UCD_E_INVALID;
+        if (!conv_ok(conv, d) || !slots_ok(d.B, d.n_slots, slots)) return UCD_E_INVALID;
         if (!empty(d.B, d.L) && (!x || !y)) return UCD_E_NULLPTR;
         if (!aligned(x, d.dtype) || !aligned(w, d.dtype) || !aligned(y, d.dtype) || !aligned(state_in, d.dtype) ||
             !aligned(state_out, d.dtype) || !aligned4(bias) || !aligned4(lengths) || !aligned4(slots))
@@ -232,7 +232,7 @@ int ucd_causal_conv_step(const ucd_causal_conv_t *conv, const void *x, const voi
     return guarded([&]() -> int {
         if (!conv || !w) return UCD_E_NULLPTR;
         ucd_causal_conv_t d;
-        if (!conv_ok(conv, d) || d.L != 1 || !slots_ok(d.n_slots, slots)) return UCD_E_INVALID;
+        if (!conv_ok(conv, d) || d.L != 1 || !slots_ok(d.B, d.n_slots, slots)) return UCD_E_INVALID;
         if (d.B > 0 && (!x || !y || (d.K > 1 && !state))) return UCD_E_NULLPTR;
         if (!aligned(x, d.dtype) || !aligned(w, d.dtype) || !aligned(y, d.dtype) || !aligned(state, d.dtype) || !aligned4(bias) ||
             !aligned4(slots))
@@ -266,7 +266,7 @@ int ucd_scan_fwd(const ucd_scan_t *scan, const ucd_scan_in_t *in, const float *s
     return guarded([&]() -> int {
         if (!scan || !in) return UCD_E_NULLPTR;
         ucd_scan_t d;
-        if (!scan_ok(scan, d) || !slots_ok(d.n_slots, in->slots)) return UCD_E_INVALID;
+        if (!scan_ok(scan, d) || !slots_ok(d.B, d.n_slots, in->slots)) return UCD_E_INVALID;
         if (!empty(d.B, d.L) && !y) return UCD_E_NULLPTR;
         int rc = scan_inputs(d, in);
         if (rc != UCD_OK) return rc;
@@ -309,7 +309,7 @@ int ucd_scan_step(const ucd_scan_t *scan, const ucd_scan_in_t *in, float *state,
     return guarded([&]() -> int {
         if (!scan || !in) return UCD_E_NULLPTR;
         ucd_scan_t d;
-        if (!scan_ok(scan, d) || d.L != 1 || !slots_ok(d.n_slots, in->slots)) return UCD_E_INVALID;
+        if (!scan_ok(scan, d) || d.L != 1 || !slots_ok(d.B, d.n_slots, in->slots)) return UCD_E_INVALID;
         if (d.B > 0 && (!state || !y)) return UCD_E_NULLPTR;
         const int rc = scan_inputs(d, in);
         if (rc != UCD_OK) return rc;

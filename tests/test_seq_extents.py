@@ -90,3 +90,13 @@ def test_strides_of_an_extent_of_one(any):
     size, names = seq.ucd_scan_saved_size, ("u", "dt", "Bm", "Cm", "z", "y")
     assert size(seq.scan(5, 1, 64, 16, **{k + "_stride": (64, any) for k in names})) == size(seq.scan(5, 1, 64, 16))
     assert size(seq.scan(1, 5, 64, 16, **{k + "_stride": (any, 64) for k in names})) == size(seq.scan(1, 5, 64, 16))
+
+
+def test_pools_of_no_sequences():
+    """A pool beside no sequences: the places, a tensor of no elements, have no address."""
+    conv, one = seq.causal_conv(0, 3, 8, 4, n_slots=5), seq.causal_conv(0, 1, 8, 4, n_slots=5)
+    for slots in (None, P):
+        seq.ucd_causal_conv_fwd(conv, None, P, P, None, slots=slots, state_in=P, state_out=P, stream=0)
+        seq.ucd_causal_conv_step(one, None, P, P, P, None, slots=slots, stream=0)
+        seq.ucd_scan_fwd(seq.scan(0, 3, 8, 4, n_slots=5), None, None, P, None, None, None, slots=slots, state_in=P, state_out=P, **WS)
+        seq.ucd_scan_step(seq.scan(0, 1, 8, 4, n_slots=5), None, None, P, None, None, P, None, slots=slots, stream=0)
