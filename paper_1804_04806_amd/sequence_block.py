@@ -119,8 +119,9 @@ class GroupNorm(torch.autograd.Function):
         n = x.shape[0] * x.shape[1]
         desc = seq.group_norm(n, 1, x.shape[2], groups, act=int(silu), dtype=_dtype(x))
         y, stats = torch.empty_like(x), torch.empty(2, n, groups, device=x.device)
-        seq.ucd_group_norm_fwd(desc, x, gamma, beta, y, stats,
-                               ws=_workspace(seq.ucd_group_norm_workspace_size(desc, seq.FWD), x.device))
+        if n > 0:      # the operator has one sample at least
+            seq.ucd_group_norm_fwd(desc, x, gamma, beta, y, stats,
+                                   ws=_workspace(seq.ucd_group_norm_workspace_size(desc, seq.FWD), x.device))
         ctx.save_for_backward(x, gamma, beta, stats, *given)
         ctx.desc = desc
         return y
@@ -130,8 +131,11 @@ class GroupNorm(torch.autograd.Function):
     def backward(ctx, dy):
         x, gamma, beta, stats, *given = ctx.saved_tensors
         dx, dgamma, dbeta = torch.empty_like(x), torch.empty_like(gamma), torch.empty_like(beta)
-        seq.ucd_group_norm_bwd(ctx.desc, x, gamma, beta, stats, dy.contiguous(), dx, dgamma, dbeta,
-                               ws=_workspace(seq.ucd_group_norm_workspace_size(ctx.desc, seq.BWD), x.device))
+        if ctx.desc.N > 0:
+            seq.ucd_group_norm_bwd(ctx.desc, x, gamma, beta, stats, dy.contiguous(), dx, dgamma, dbeta,
+                                   ws=_workspace(seq.ucd_group_norm_workspace_size(ctx.desc, seq.BWD), x.device))
+        else:
+            dgamma.zero_(), dbeta.zero_()
         return _once((dy, *given), (dx, dgamma, dbeta, None, None))
 
 

@@ -207,3 +207,36 @@ def test_operators_run_on_their_tensors_device(monkeypatch):
     torch.cuda.synchronize()
     assert {n for n, _ in seen} == {n for n in sb.seq.EXPORTS if not n.endswith("_size")}
     assert all(on for _, on in seen), seen
+
+
+@pytest.mark.parametrize("rows", [(0, 5), (3, 0), (0, 0)], ids=str)
+def test_no_tokens(rows):
+    """Of no sequences or no tokens the outputs are as empty, the gradients of the weights 0, and states stay."""
+    import torch
+    from paper_1804_04806_amd.sequence_block import Block
+    block, x = Block(16, 24), torch.randn(*rows, 16, device="cuda", requires_grad=True)
+    y = block(x)
+    assert y.shape == x.shape
+    y.sum().backward()
+    assert x.grad.shape == x.shape
+    for name, p in block.named_parameters():
+        assert p.grad is not None and not p.grad.any(), name
+    pools = [torch.randn_like(t) for t in block.pools(4)]
+    before = [t.clone() for t in pools]
+    slots = torch.arange(rows[0], dtype=torch.int32, device="cuda")
+    assert block.extend(x.detach(), pools, slots).shape == x.shape
+    assert all(torch.equal(a, b) for a, b in zip(pools, before))
+
+
+def test_decoding_from_nothing():
+    """Prompts of no tokens at all: every token is a single one."""
+    import torch
+    from paper_1804_04806_amd.sequence_block import Block, decode
+    torch.manual_seed(9)
+    blocks, x = [Block(16, 24), Block(16, 24)], torch.randn(3, 7, 16, device="cuda")
+    with torch.no_grad():
+        whole = blocks[1](blocks[0](x))
+    out = decode(blocks, x, [0, 0, 0])
+    assert len(out) == 7
+    # fp32, sums in another order: as in the test of decoding behind prompts
+    assert float((torch.stack(out, 1) - whole).abs().max()) <= 1e-3 * float(whole.abs().max())
