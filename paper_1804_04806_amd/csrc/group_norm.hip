@@ -69,6 +69,13 @@ __device__ __forceinline__ void load_weights(float (&v)[VE], const float *at)
     for (int i = 0; i < VE; ++i) v[i] = at[i];
 }
 
+// 1 / sqrt(v); the unit takes numbers below the smallest normal one for 0.
+__device__ __forceinline__ float inverse_root(float v)
+{
+    const bool tiny = v < 0x1p-100f;
+    return __builtin_amdgcn_rsqf(tiny ? v * 0x1p100f : v) * (tiny ? 0x1p50f : 1.f);
+}
+
 // y of one pack
 template <bool SILU, class T, int VE>
 __device__ __forceinline__ Pack<T, VE> norm_pack(const Raw<T, VE, true> &r, float mean, float rstd, const float (&gamma)[VE], const float (&beta)[VE])
@@ -172,7 +179,7 @@ __global__ __launch_bounds__(256) void norm_rows_fwd_kernel(NormParams p)
                 const float v = r[i].get(e) - mean;
                 sq += e >= at.own[i] ? v * v : 0.f;
             }
-        const float rstd = __builtin_amdgcn_rsqf(fmaf(sum_group(sq, p.lanes), p.share, p.d.eps));
+        const float rstd = inverse_root(fmaf(sum_group(sq, p.lanes), p.share, p.d.eps));
 #pragma unroll
         for (int i = 0; i < R; ++i)
             if (at.have[i] && there)
@@ -450,7 +457,7 @@ __global__ __launch_bounds__(kMaxThreads, (slab_waves<T, VE, R>())) void norm_sl
         Slab<T, VE, R> x;
         x.load(p.x, p.d.x_n, p.d.x_s, p, at, n, 0, p.d.S);
         const float2 m = slab_moments<TAIL, T, VE, R>(p, x, at, p.d.S, p.share);
-        const float rstd = __builtin_amdgcn_rsqf(fmaf(m.y, p.share, p.d.eps));
+        const float rstd = inverse_root(fmaf(m.y, p.share, p.d.eps));
         float gamma[VE] = {}, beta[VE] = {};
         if (at.active) {
             load_weights<VE>(gamma, p.gamma + at.c0);
@@ -622,7 +629,7 @@ __device__ __forceinline__ float2 join_parts(const NormParams &p, int n, int g)
         v.y += s[1] + off * off * elements(i);
     }
     v.y = sum_group(v.y, 64);
-    return make_float2(v.x, __builtin_amdgcn_rsqf(fmaf(v.y, p.share, p.d.eps)));
+    return make_float2(v.x, inverse_root(fmaf(v.y, p.share, p.d.eps)));
 }
 
 // Parts, second kernel: y or dx of one part.
