@@ -19,11 +19,12 @@ import math
 
 import torch
 
-from . import seq
+from . import seq, ucd
 
 def _workspace(nbytes, device):
-    """A call's workspace, of the current stream like the call: what other streams or captured graphs hold is never shared."""
-    return torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
+    """A call's workspace, of the current stream like the call: what other streams or captured graphs hold is never shared.
+    None for a descriptor without one, which the call refuses."""
+    return torch.empty(nbytes, dtype=torch.uint8, device=device) if 0 < nbytes < ucd.WS_NA else None
 
 
 _DEVICE = "cuda"
@@ -188,7 +189,7 @@ class Scan(torch.autograd.Function):
         A, skip, dt_bias = _dense(A, skip, dt_bias)
         desc = seq.scan(b, l, d, n, dtype=_dtype(u), **{k + "_stride": s for k, (_, s) in rows.items()})
         y = torch.empty(b, l, d, dtype=u.dtype, device=u.device)
-        saved = torch.empty(seq.ucd_scan_saved_size(desc), dtype=torch.uint8, device=u.device)
+        saved = _workspace(seq.ucd_scan_saved_size(desc), u.device)
         seq.ucd_scan_fwd(desc, u, dt, A, Bm, Cm, y, skip=skip, z=z, dt_bias=dt_bias, saved=saved,
                          ws=_workspace(seq.ucd_scan_workspace_size(desc, seq.FWD), u.device))
         ctx.save_for_backward(u, dt, A, Bm, Cm, skip, z, dt_bias, saved, *given)

@@ -159,3 +159,17 @@ def test_second_derivatives_are_refused(i, monkeypatch):
     penalty = sum(g.square().sum() for g in first) + args[0].pow(3).sum()
     with pytest.raises(RuntimeError, match="differentiat"):
         torch.autograd.grad(penalty, leaves, allow_unused=True)
+
+
+def test_refused_descriptors_raise_the_librarys_error(monkeypatch):
+    """What the library refuses is its error, whichever query or call meets it first."""
+    from paper_1804_04806_amd import ucd
+    monkeypatch.setattr(sb, "_DEVICE", "cpu", raising=False)
+    monkeypatch.setattr(sb.seq, "_raw_stream", lambda: 0)
+    (norm, args, _), (conv, conv_args, _), (scan, scan_args, _) = weights()
+    many = torch.randn(2, 3, 65)
+    for function, bad in ((norm, args[:3] + [3, False]), (norm, args[:3] + [0, False]), (conv, [conv_args[0], torch.randn(8, 9), conv_args[2]]),
+                          (scan, scan_args[:2] + [torch.randn(8, 65), many, many] + scan_args[5:])):
+        with pytest.raises(ucd.UcdError) as e:
+            function.apply(*bad)
+        assert e.value.status == ucd.E_INVALID
