@@ -3,7 +3,9 @@
 // Every token is read once (K - 1 of them once more per run) and every result written once: memory bounds it.  A thread owns VE neighbouring channels
 // and a run of tokens; the last K - 1 tokens of its channels, and in Backward the last K - 1 gradients of u, stay in registers while it walks.
 // Workgroups are 32 packs of 16 bytes (64 of two channels) by 8 (4) runs: whole lines of a row, and neighbouring runs meet their common tokens in the
-// same L1.  8 x 2048 tokens, 2048 channels, 4 taps, bf16: Forward 26 us (5.1 TB/s), Backward 48 (4.2); fp32, 1024 channels: 22 (6.0) and 39 (5.2).
+// same L1.  8 x 2048 tokens, 2048 channels, 4 taps, bf16, on inputs that change from call to call: Forward 32 us (4.2 TB/s; a copy of as many bytes takes
+// 28), Backward 54 (3.7, its join included); fp32, 1024 channels: 30 (4.5) and 45 (4.5).  (Figures at the constants below compare two choices on one set
+// of inputs, part of which stays in the card's cache: 27 and 48 us.)  Rows of few channels leave lanes idle: 16 x 8192 x 64 24 us in Forward, 1.4 TB/s.
 #include <algorithm>
 #include <type_traits>
 
@@ -213,7 +215,7 @@ __global__ __launch_bounds__(256) void conv_fwd_kernel(ConvParams p, unsigned un
 }
 
 // One token: a thread to VE channels of a sequence, few of them, so that single sequences fill some hundred workgroups too; all loads but the state's
-// place are under way at once.  64 sequences, 2048 channels, 4 taps, bf16: 2.8 us, which is a launch's own time.
+// place are under way at once.  64 sequences, 2048 channels, 4 taps, bf16: 3.0 us, which is a launch's own time.
 template <class T, int VE, int K, bool SILU>
 __global__ __launch_bounds__(256) void conv_step_kernel(ConvParams p)
 {

@@ -7,8 +7,10 @@
 //   parts  what fits neither: a first kernel leaves sums of parts of a group, the second joins them and reads its part again.
 // Sums of Forward are means and squares around them (two passes over registers), joined as such: no difference of large numbers is taken.
 // The gradients of gamma and beta are sums over positions, which threads keep per channel while they walk, and a join over the workgroups.
-// bf16, Forward and Backward: rows 8192 x 1 x 2048 in 16 groups 13 us (5.2 TB/s) and 25.5 (4.0; 4 of it the join); slabs 64 x 1024 x 512 in 32 groups with
-// SiLU 35 (3.8) and 58 (3.5): all workgroups read, sum and write at the same time; parts 8 x 4096 x 2000 in one group 94 (2.8) and 182 (2.2).
+// bf16, Forward and Backward, on inputs that change from call to call: rows 8192 x 1 x 2048 in 16 groups 13 us (5.1 TB/s) and 29 (3.5; 4 of it the join);
+// slabs 64 x 1024 x 512 in 32 groups with SiLU 39 (3.4) and 67 (3.0): all workgroups read, sum and write at the same time; parts 8 x 4096 x 2000 in one
+// group 99 (2.6) and 145 (2.7).  (Figures at the constants below compare two choices on one set of inputs, part of which stays in the card's cache:
+// 34 and 58 us for those slabs.)  Few samples are slow: 1 x 1024 x 512 in 32 groups is 8 workgroups of one XCD, 14 us in Forward.
 #include <algorithm>
 
 #include "seq.h"

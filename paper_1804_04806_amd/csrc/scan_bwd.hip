@@ -8,7 +8,7 @@
 // The states come again from those that Forward kept every eight tokens (all of them would be eight times the memory of u, dt, z and y together at 16
 // states; recomputing costs five of the twenty slots that a state and token take).  Sums over the states stay in a channel's lanes, sums over the
 // channels go through the waves' own exchanges, a workgroup's LDS and one row of partial sums per workgroup: no atomics, the order is fixed.
-// The vector units bound it: 8 x 2048 tokens, 2048 channels, 16 states, bf16: 505 to 540 us, issuing in 75 % of the time, and 14 + 4 for the joins.
+// The vector units bound it: 8 x 2048 tokens, 2048 channels, 16 states, bf16: 509 us, issuing in 75 % of the time, and 14 + 5 for the joins.
 #include <algorithm>
 
 #include "scan_common.hpp"

@@ -4,7 +4,7 @@
 //   h_t = exp(d_t A) h_{t-1} + d_t u_t Bm_t,  y_t = (sum_n Cm_t h_t + skip u_t) SiLU(z_t).
 // A state and token cost a multiplication, an exponential (two issue slots), a multiplication and two fused ones, where it moves 1 / N of some
 // bytes: the vector units bound it, and a wave that has its SIMD to itself has to keep them fed.  8 x 2048 tokens, 2048 channels, 16 states, bf16:
-// 200 to 215 us with the states that Backward needs, 180 to 210 without; the units issue in 67 % of the time, and six slots alone would take
+// 196 us with the states that Backward needs, 182 without; the units issue in 67 % of the time, and six slots alone would take
 // 82 us.  The tokens of a sequence follow each other, so lanes are states and channels, tiles of tokens are what is loaded at
 // once, and sequences are cut only where there are too few channels.  (A tile's outputs written behind the next tile's sums: 316 us against 251 then;
 // eight lanes to a channel instead of four: 256 against 205, and 539 against 380 for twice as many sequences.)

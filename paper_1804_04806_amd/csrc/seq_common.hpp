@@ -100,7 +100,9 @@ struct Raw {
     }
 };
 
-// 2^v on the transcendental unit.
+// 2^v on the transcendental unit, to an ulp of the result.  Where v is a rounded product w log2(e), as in sigmoid and in the scan's decays, its rounding
+// adds up to |w| 2^-24 of the result: 6e-7 of a decay to 5e-5, the more the less is left.  exp_full's correction costs six instructions more, which the
+// decays would pay for every state and token.
 __device__ __forceinline__ float exp2_fast(float v) { return __builtin_amdgcn_exp2f(v); }
 
 // exp(v) to about an ulp: the rounding of v * log2(e), up to 2^-24 |v log2(e)| in the exponent, is put back as a factor.
@@ -117,8 +119,8 @@ __device__ __forceinline__ float exp_full(float v)
 __device__ __forceinline__ float sigmoid(float v) { return __builtin_amdgcn_rcpf(1.f + exp2_fast(v * -kLog2e)); }
 
 // log(1 + exp(v)) = max(v, 0) + log1p(e), e = exp(-|v|); with w = 1 + e rounded, log1p(e) = log(w) e / (w - 1) to an ulp or two, because w - 1 is
-// exact and log(w) / (w - 1) hardly changes between 1 + e and w.  Also the function's derivative, 1 / (1 + exp(-v)).  For values that were rounded
-// to 8 bits exp(-|v|) without its correction: |v log2(e)| 2^-24 off.
+// exact and log(w) / (w - 1) hardly changes between 1 + e and w.  Also the function's derivative, 1 / (1 + exp(-v)).  For bf16 activations exp(-|v|)
+// without its correction: |v| 2^-24 of it off at most, which is also what the rounding of v = dt + dt_bias to 32 bits may leave of it.
 template <class T>
 __device__ __forceinline__ float softplus(float v, float *derivative = nullptr)
 {
