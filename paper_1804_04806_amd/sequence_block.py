@@ -13,13 +13,13 @@ tokens by a short causal convolution and all earlier ones by a selective scan.
 Training runs Forward and Backward through ``torch.autograd``; decoding keeps the convolution's last tokens and the
 scan's states of every sequence in pools, fills them from prompts of any lengths and moves on by single tokens.
 """
-import contextlib
 import functools
 import math
 
 import torch
 
 from . import seq, ucd
+
 
 def _workspace(nbytes, device):
     """A call's workspace, of the current stream like the call: what other streams or captured graphs hold is never shared.
@@ -40,16 +40,18 @@ def _dtype(t):
 def _check(*given):
     """The operators are given addresses alone: refuses what is not as they will read it.  Each is a name, a tensor or None,
     its shape and its type; all are on the first one's device."""
-    given = [g for g in given if g[1] is not None]
+    devices = set()
     for name, t, shape, kind in given:
+        if t is None:
+            continue
         if t.dtype != kind:
             raise TypeError(f"{name} is {t.dtype} where {kind} is read")
-        if t.shape != tuple(shape):
+        if t.shape != shape:
             raise ValueError(f"{name} is {tuple(t.shape)} where {tuple(shape)} is read")
-    device = given[0][1].device
-    for name, t, _, _ in given:
-        if t.device != device or device.type != _DEVICE:
-            raise ValueError(f"{name} is on {t.device}, {given[0][0]} on {device}: all are read on one {_DEVICE} device")
+        devices.add(t.get_device())          # -1: the host's memory
+    if len(devices) != 1 or (-1 in devices) == (_DEVICE == "cuda"):
+        raise ValueError(f"all tensors are read on one {_DEVICE} device: " +
+                         ", ".join(f"{name} is on {t.device}" for name, t, _, _ in given if t is not None))
 
 
 def _tokens(name, t):
@@ -62,30 +64,41 @@ def _tokens(name, t):
 def _rows(t):
     """A tensor (B, L, ...) whose rows are dense and apart from each other, and its strides of sequence and token, 0 (the dense
     one) where there is only one.  Copied where it is not such a tensor, as broadcast ones are not: all of their rows are one."""
-    dense, span = True, 1
-    for n, stride in zip(reversed(t.shape[2:]), reversed(t.stride()[2:])):
+    if t.is_contiguous():
+        return t, (0, 0)
+    (b, l), (outer, inner), dense, span = t.shape[:2], t.stride()[:2], True, 1
+    for n, stride in zip(t.shape[:1:-1], t.stride()[:1:-1]):
         dense = dense and (n == 1 or stride == span)
         span *= n
-    for stride, n in sorted(zip(t.stride()[:2], t.shape[:2])):
+    for stride, n in ((outer, b), (inner, l)) if outer < inner else ((inner, l), (outer, b)):
         if n > 1:
             dense = dense and stride >= span
             span += stride * (n - 1)
-    t = t if dense else t.contiguous()
-    return t, tuple(stride if n > 1 else 0 for stride, n in zip(t.stride()[:2], t.shape[:2]))
+    if not dense:
+        return t.contiguous(), (0, 0)
+    return t, (outer if b > 1 else 0, inner if l > 1 else 0)
 
 
 def _on_device(method):
     """The method with its first tensor's device as the current one, on which the operators launch."""
     @functools.wraps(method)
     def run(owner, x, *args, **kw):
-        with torch.cuda.device(x.device) if x.is_cuda else contextlib.nullcontext():
+        device = x.get_device()
+        if device < 0:
+            return method(owner, x, *args, **kw)
+        with torch.cuda.device(device):
             return method(owner, x, *args, **kw)
     return run
 
 
 def _dense(*tensors):
     """Tensors without strides of their own, as the operators read weights."""
-    return (None if t is None else t.contiguous() for t in tensors)
+    return [None if t is None else t.contiguous() for t in tensors]
+
+
+def _save(ctx, used, given, *more):
+    """Saves what a backward reads, `used` and more, and behind it the tensors that `used` were made of where they are others."""
+    ctx.save_for_backward(*used, *more, *(() if list(map(id, used)) == list(map(id, given)) else given))
 
 
 class _Once(torch.autograd.Function):
@@ -123,7 +136,7 @@ class GroupNorm(torch.autograd.Function):
         if n > 0:      # the operator has one sample at least
             seq.ucd_group_norm_fwd(desc, x, gamma, beta, y, stats,
                                    ws=_workspace(seq.ucd_group_norm_workspace_size(desc, seq.FWD), x.device))
-        ctx.save_for_backward(x, gamma, beta, stats, *given)
+        _save(ctx, (x, gamma, beta), given, stats)
         ctx.desc = desc
         return y
 
@@ -137,7 +150,7 @@ class GroupNorm(torch.autograd.Function):
                                    ws=_workspace(seq.ucd_group_norm_workspace_size(ctx.desc, seq.BWD), x.device))
         else:
             dgamma.zero_(), dbeta.zero_()
-        return _once((dy, *given), (dx, dgamma, dbeta, None, None))
+        return _once((dy, *(given or (x, gamma, beta))), (dx, dgamma, dbeta, None, None))
 
 
 class CausalConv(torch.autograd.Function):
@@ -155,7 +168,7 @@ class CausalConv(torch.autograd.Function):
         desc = seq.causal_conv(b, l, d, w.shape[1], act=seq.ACT_SILU, dtype=_dtype(x), x_stride=stride)
         y = torch.empty(b, l, d, dtype=x.dtype, device=x.device)
         seq.ucd_causal_conv_fwd(desc, x, w, bias, y)
-        ctx.save_for_backward(x, w, bias, *given)
+        _save(ctx, (x, w, bias), given)
         ctx.desc = desc
         return y
 
@@ -167,7 +180,7 @@ class CausalConv(torch.autograd.Function):
         dw, dbias = torch.empty(w.shape, device=w.device), torch.empty_like(bias)
         seq.ucd_causal_conv_bwd(ctx.desc, x, w, bias, dy.contiguous(), dx, dw, dbias,
                                 ws=_workspace(seq.ucd_causal_conv_workspace_size(ctx.desc), x.device))
-        return _once((dy, *given), (dx, dw.to(w.dtype), dbias))
+        return _once((dy, *(given or (x, w, bias))), (dx, dw.to(w.dtype), dbias))
 
 
 class Scan(torch.autograd.Function):
@@ -192,7 +205,7 @@ class Scan(torch.autograd.Function):
         saved = _workspace(seq.ucd_scan_saved_size(desc), u.device)
         seq.ucd_scan_fwd(desc, u, dt, A, Bm, Cm, y, skip=skip, z=z, dt_bias=dt_bias, saved=saved,
                          ws=_workspace(seq.ucd_scan_workspace_size(desc, seq.FWD), u.device))
-        ctx.save_for_backward(u, dt, A, Bm, Cm, skip, z, dt_bias, saved, *given)
+        _save(ctx, (u, dt, A, Bm, Cm, skip, z, dt_bias), given, saved)
         ctx.desc = desc
         return y
 
@@ -200,12 +213,13 @@ class Scan(torch.autograd.Function):
     @_on_device
     def backward(ctx, dy):
         u, dt, A, Bm, Cm, skip, z, dt_bias, saved, *given = ctx.saved_tensors
+        used = u, dt, A, Bm, Cm, skip, z, dt_bias
         du, ddt, dA, dBm, dCm, dskip, dz, dbias = (torch.empty_strided(t.shape, t.stride(), dtype=t.dtype, device=t.device)
-                                                   for t in (u, dt, A, Bm, Cm, skip, z, dt_bias))
+                                                   for t in used)
         seq.ucd_scan_bwd(ctx.desc, u, dt, A, Bm, Cm, dy.contiguous(), saved, du, ddt, dA, dBm, dCm, skip=skip, dskip=dskip,
                          z=z, dz=dz, dt_bias=dt_bias, ddt_bias=dbias,
                          ws=_workspace(seq.ucd_scan_workspace_size(ctx.desc, seq.BWD), u.device))
-        return _once((dy, *given), (du, ddt, dA, dBm, dCm, dskip, dz, dbias))
+        return _once((dy, *(given or used)), (du, ddt, dA, dBm, dCm, dskip, dz, dbias))
 
 
 class Block(torch.nn.Module):
