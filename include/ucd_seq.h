@@ -9,6 +9,7 @@
  *     An extent is at most 2^30, a row 2^25 elements, a tensor 2^40; rows must not overlap, a
  *     token's stride is at most 2^25 and a sequence's 2^40 (UCD_E_INVALID otherwise), but for
  *     those of an extent of one, which are not taken; a gradient has the strides of its tensor.
+ *     Calls that would be 2^31 workgroups (the scan's 2^30) are UCD_E_UNSUPPORTED.
  *   - dtype 0: activations (and their gradients, filters and convolution states) fp32; dtype 1:
  *     bfloat16, rounded to nearest-even once.  Everything else is fp32: norm weights, biases, A,
  *     skip, scan states, statistics, gradients of all weights; and so is all arithmetic.
@@ -24,7 +25,7 @@
  *   - slots (may be NULL): device, int32 per sequence, its place in a pool of n_slots states.  A
  *     place outside 0 .. n_slots-1 marks an idle sequence: no state is read or written and its
  *     outputs are 0.  Sequences of one call have places of their own.  Without slots the states
- *     are one per sequence (n_slots = 0).
+ *     are one per sequence (n_slots = 0); a pool without slots goes with no sequences alone.
  */
 #ifndef UCD_SEQ_H
 #define UCD_SEQ_H
