@@ -100,3 +100,17 @@ def test_pools_of_no_sequences():
         seq.ucd_causal_conv_step(one, None, P, P, P, None, slots=slots, stream=0)
         seq.ucd_scan_fwd(seq.scan(0, 3, 8, 4, n_slots=5), None, None, P, None, None, None, slots=slots, state_in=P, state_out=P, **WS)
         seq.ucd_scan_step(seq.scan(0, 1, 8, 4, n_slots=5), None, None, P, None, None, P, None, slots=slots, stream=0)
+
+
+def test_too_many_workgroups():
+    """Extents that are allowed each, in calls that are too large to be counted."""
+    def unsupported(call, *args, **kw):
+        with pytest.raises(ucd.UcdError) as e:
+            call(*args, **kw)
+        assert e.value.status == ucd.E_UNSUPPORTED, e.value.status
+    conv = seq.causal_conv(MOST, 8, 1, 4)
+    unsupported(seq.ucd_causal_conv_fwd, conv, P, P, P, P, stream=0)
+    unsupported(seq.ucd_causal_conv_bwd, conv, P, P, P, P, P, P, P, **WS)
+    scan = seq.scan(MOST, 1, 16, 4)
+    unsupported(seq.ucd_scan_fwd, scan, P, P, P, P, P, P, **WS)
+    unsupported(seq.ucd_scan_step, scan, P, P, P, P, P, P, P, stream=0)
