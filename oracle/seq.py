@@ -1,5 +1,5 @@
 """TEST INFRASTRUCTURE ONLY: the sequence operators (group norm with an activation, short causal
-convolution, selective state space scan) and their gradients in numpy, 64 bits, written from the
+convolution, selective state space scan, linear attention, gated projection) and their gradients in numpy, 64 bits, written from the
 formulas in include/ucd_seq.h token by token.  Shares no code with the library.
 """
 import numpy as np
@@ -172,3 +172,90 @@ def scan_bwd(u, dt, A, Bm, Cm, dy, skip=None, z=None, dt_bias=None, softplus=Tru
             dh = dh * a
         g["state"][b] = dh
     return g
+
+
+# ---- linear attention ------------------------------------------------------------------------
+
+
+def _log_decays(g, decay, b, n, H):
+    ld = np.zeros((n, H))
+    if g is not None:
+        ld = ld + g[b, :n].astype(np.float64)
+    if decay is not None:
+        ld = ld + decay.astype(np.float64)
+    return ld
+
+
+def attention_fwd(q, k, v, scale, g=None, decay=None, lengths=None, state=None, keep=False):
+    """(y, new state): q, k (B, L, Hk, Dk), v (B, L, H, Dv), g (B, L, H), decay (H), state (B, H, Dk, Dv).  keep: also
+    every token's state."""
+    B, L, H, Dv = v.shape
+    shared, Dk = H // q.shape[2], q.shape[3]
+    y, out = np.zeros((B, L, H, Dv)), np.zeros((B, H, Dk, Dv))
+    all_s = np.zeros((B, L + 1, H, Dk, Dv)) if keep else None
+    for b in range(B):
+        n = L if lengths is None else int(lengths[b])
+        ld = _log_decays(g, decay, b, n, H)
+        s = np.zeros((H, Dk, Dv)) if state is None else state[b].astype(np.float64)
+        if keep:
+            all_s[b, 0] = s
+        for t in range(n):
+            qt, kt = (np.repeat(m[b, t].astype(np.float64), shared, axis=0) for m in (q, k))
+            s = np.exp(ld[t])[:, None, None] * s + kt[:, :, None] * v[b, t].astype(np.float64)[:, None, :]
+            y[b, t] = scale * (qt[:, :, None] * s).sum(1)
+            if keep:
+                all_s[b, t + 1] = s
+        out[b] = s
+    return (y, out, all_s) if keep else (y, out)
+
+
+def attention_bwd(q, k, v, scale, dy, g=None, decay=None, lengths=None, state=None, dstate_out=None):
+    """Dict of the gradients of q, k, v, g (of the log decays) and state."""
+    B, L, H, Dv = v.shape
+    Hk, Dk = q.shape[2:]
+    shared = H // Hk
+    _, _, all_s = attention_fwd(q, k, v, scale, g, decay, lengths, state, keep=True)
+    out = {"q": np.zeros((B, L, Hk, Dk)), "k": np.zeros((B, L, Hk, Dk)), "v": np.zeros((B, L, H, Dv)), "g": np.zeros((B, L, H)),
+           "state": np.zeros((B, H, Dk, Dv))}
+    for b in range(B):
+        n = L if lengths is None else int(lengths[b])
+        ld = _log_decays(g, decay, b, n, H)
+        ds = np.zeros((H, Dk, Dv)) if dstate_out is None else dstate_out[b].astype(np.float64)
+        for t in reversed(range(n)):
+            qt, kt = (np.repeat(m[b, t].astype(np.float64), shared, axis=0) for m in (q, k))
+            vt, dyt = v[b, t].astype(np.float64), dy[b, t].astype(np.float64)
+            ds = ds + scale * qt[:, :, None] * dyt[:, None, :]
+            out["q"][b, t] = (scale * (all_s[b, t + 1] * dyt[:, None, :]).sum(2)).reshape(Hk, shared, Dk).sum(1)
+            out["k"][b, t] = (ds * vt[:, None, :]).sum(2).reshape(Hk, shared, Dk).sum(1)
+            out["v"][b, t] = (ds * kt[:, :, None]).sum(1)
+            ds = np.exp(ld[t])[:, None, None] * ds
+            out["g"][b, t] = (ds * all_s[b, t]).sum((1, 2))
+        out["state"][b] = ds
+    return out
+
+
+# ---- gated projection ------------------------------------------------------------------------
+
+
+def gate_act(v, act):
+    """act(v), and its derivative; 0: none, 1: SiLU, 2: GELU in its tanh form, v sigmoid(2 sqrt(2/pi) (v + 0.044715 v^3))."""
+    if act == 0:
+        return v, np.ones_like(v)
+    if act == 1:
+        return act_fwd(v, True), act_bwd(v, True)
+    c = 2 * np.sqrt(2 / np.pi)
+    s = sigmoid(c * (v + 0.044715 * v ** 3))
+    return v * s, s * (1 + v * (1 - s) * c * (1 + 3 * 0.044715 * v * v))
+
+
+def gated_fwd(x, w_gate, w_up, act):
+    x, w_gate, w_up = (a.astype(np.float64) for a in (x, w_gate, w_up))
+    return gate_act(x @ w_gate.T, act)[0] * (x @ w_up.T)
+
+
+def gated_bwd(x, w_gate, w_up, act, dy):
+    """(dx, dw_gate, dw_up)."""
+    x, w_gate, w_up, dy = (a.astype(np.float64) for a in (x, w_gate, w_up, dy))
+    value, slope = gate_act(x @ w_gate.T, act)
+    dgate, dup = dy * (x @ w_up.T) * slope, dy * value
+    return dgate @ w_gate + dup @ w_up, dgate.T @ x, dup.T @ x

@@ -1,0 +1,631 @@
+// Gated projection: y = act(x Wg^T) * (x Wu^T), and its gradients.
+//
+// Products bound it from some hundred tokens on, the weights' bytes below.  Forward is one product whose tiles hold the same columns of both
+// projections, so that a lane has both sides of a gate in registers and writes y alone (for Backward, both sides in fp32 too).  Backward first turns
+// dy and what was kept into dG = [dgate | dup], bfloat16 (rounded once: the products' operand), then dx = dG [Wg; Wu] and [dWg; dWu] = dG^T x, each
+// one product.  Operands that the products cannot read as they lie (fp32, rows of no whole 16 bytes) are copied first.
+#include <algorithm>
+
+#include "product.hpp"
+#include "seq.h"
+
+namespace ucd {
+namespace {
+using namespace seq;
+using namespace product;
+
+constexpr float kGelu = 1.59576912160573071176f, kCube = 0.044715f;    // 2 sqrt(2 / pi)
+
+// act(v) and its derivative; GELU in its tanh form is v sigmoid(2 sqrt(2/pi) (v + 0.044715 v^3)).  The cube of a v beyond 1e12 overflows to an infinity of
+// its sign, whose sigmoid is 0 or 1 as it should be; v times 0 is left out there.
+__device__ __forceinline__ float gate_sigmoid(int act, float v)
+{
+    const float w = act == UCD_ACT_GELU ? kGelu * fmaf(kCube * v * v, v, v) : v;
+    return __builtin_amdgcn_rcpf(1.f + exp_full(-w));
+}
+__device__ __forceinline__ float gate_act(int act, float v)
+{
+    return act == UCD_ACT_NONE ? v : v * gate_sigmoid(act, v);
+}
+__device__ __forceinline__ float gate_slope(int act, float v, float &value)
+{
+    value = v;
+    if (act == UCD_ACT_NONE) return 1.f;
+    const float s = gate_sigmoid(act, v), inner = act == UCD_ACT_GELU ? kGelu * fmaf(3.f * kCube * v, v, 1.f) : 1.f;
+    value = v * s;
+    const float rest = s * (1.f - s);
+    return rest == 0.f ? s : fmaf(v * inner, rest, s);
+}
+
+inline long round_up(long n, long to) { return (n + to - 1) / to * to; }
+
+// ---- copies --------------------------------------------------------------------------------------------------------
+
+// The three bfloat16 parts of an fp32 value: the first is the largest finite one where it would be rounded to an infinity.
+__device__ __forceinline__ void parts_of(float v, bf16_t &h, bf16_t &m, bf16_t &l)
+{
+    constexpr float kMost = 3.38953139e38f;
+    h = (bf16_t)(fabsf(v) < INFINITY ? fminf(fmaxf(v, -kMost), kMost) : v);
+    const float a = v - (float)h;
+    m = (bf16_t)a;
+    l = (bf16_t)(a - (float)m);
+}
+
+template <class T>
+struct Planes {
+    static constexpr int N = sizeof(T) == 4 ? 3 : 1;
+};
+
+template <class T>
+__device__ __forceinline__ void store_planes(bf16_t *to, long plane, const float (&v)[8])
+{
+    Pack<bf16_t, 8> p[3];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        if (sizeof(T) == 4) parts_of(v[i], p[0].v[i], p[1].v[i], p[2].v[i]);
+        else p[0].v[i] = from_f<bf16_t>(v[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < Planes<T>::N; ++i) *reinterpret_cast<Pack<bf16_t, 8> *>(to + i * plane) = p[i];
+}
+
+// rows x cols elements, rows `stride` apart -> planes of rows of `width`, a multiple of 8 from cols on, filled up with 0
+template <class T>
+__global__ __launch_bounds__(256) void copy_rows_kernel(const T *from, long stride, long rows, int cols, bf16_t *to, int width, long plane)
+{
+    const int packs = width / 8;
+    for (long i = blockIdx.x * 256l + threadIdx.x; i < rows * packs; i += gridDim.x * 256l) {
+        const long row = i / packs;
+        const int c = (int)(i % packs) * 8, have = min(8, cols - c);
+        const T *src = from + row * stride + c;
+        float v[8];
+        if (have == 8) {
+            const Pack<T, 8> p = loose_load<T, 8>(src);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = to_f(p.v[j]);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = j < have ? to_f(src[j]) : 0.f;
+        }
+        store_planes<T>(to + row * width + c, plane, v);
+    }
+}
+
+// ---- forward -------------------------------------------------------------------------------------------------------
+
+struct GateOut {
+    void *y;
+    long y_m;
+    float *saved;      // M rows of two rows of `wide` floats, or null
+    int M, F, wide, act;
+};
+
+template <class T>
+__device__ __forceinline__ void gate_store(const GateOut &o, long m, int f, const Pack<float, 4> &g, const Pack<float, 4> &u)
+{
+    const int have = min(4, o.F - f);
+    if (m >= o.M || have <= 0) return;
+    Pack<T, 4> y;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) y.v[i] = from_f<T>(gate_act(o.act, g.v[i]) * u.v[i]);
+    T *at = (T *)o.y + m * o.y_m + f;
+    if (have == 4) loose_store<T, 4>(at, y);
+    else store_pack<false, T, 4>(at, y, have);
+    if (o.saved) {      // whole packs: rows are a multiple of 4
+        float *s = o.saved + m * 2 * o.wide + f;
+        *reinterpret_cast<Pack<float, 4> *>(s) = g;
+        *reinterpret_cast<Pack<float, 4> *>(s + o.wide) = u;
+    }
+}
+
+template <class TILE, class T>
+__global__ __launch_bounds__(TILE::THREADS) void gated_forward_kernel(Problem p, GateOut o, float *part)
+{
+    __shared__ __attribute__((aligned(16))) char lds[TILE::LDS];
+    const int tm = blockIdx.x % p.tiles_m, tn = blockIdx.x / p.tiles_m;
+    const int m0 = tm * TILE::BM, f0 = tn * (TILE::BN / 2);
+    int t0, t1;
+    split_range(p, blockIdx.y, t0, t1);
+    TILE tile;
+    tile.run(p, m0, f0, t0, t1, lds);
+    if (part) {
+        // partial sums: for every split and row a row of both sides
+        float *at = part + (long)blockIdx.y * o.M * 2 * o.wide;
+        tile.each([&](int m, int n, const Pack<float, 4> &v) {
+            const int side = n >= TILE::BN / 2, f = f0 + n - side * (TILE::BN / 2);
+            if (m0 + m < o.M && f < o.F) *reinterpret_cast<Pack<float, 4> *>(at + (m0 + m) * 2l * o.wide + side * o.wide + f) = v;
+        });
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < TILE::FM; ++j)
+#pragma unroll
+        for (int i = 0; i < TILE::FN / 2; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                Pack<float, 4> g, u;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    g.v[e] = tile.acc[i][j][4 * r + e];
+                    u.v[e] = tile.acc[i + TILE::FN / 2][j][4 * r + e];
+                }
+                gate_store<T>(o, m0 + tile.wm * TILE::WM + 32 * j + tile.lane % 32, f0 + tile.n_first(i) + 8 * r + 4 * (tile.lane / 32), g, u);
+            }
+}
+
+template <class T>
+__global__ __launch_bounds__(256) void gated_join_kernel(const float *part, int splits, GateOut o)
+{
+    const int packs = o.wide / 4;
+    const long size = (long)o.M * 2 * o.wide;
+    for (long i = blockIdx.x * 256l + threadIdx.x; i < (long)o.M * packs; i += gridDim.x * 256l) {
+        const long m = i / packs;
+        const int f = (int)(i % packs) * 4;
+        const float *at = part + m * 2 * o.wide + f;
+        Pack<float, 4> g{}, u{};
+        for (int s = 0; s < splits; ++s) {
+            const auto a = *reinterpret_cast<const Pack<float, 4> *>(at + s * size), b = *reinterpret_cast<const Pack<float, 4> *>(at + s * size + o.wide);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) g.v[e] += a.v[e], u.v[e] += b.v[e];
+        }
+        gate_store<T>(o, m, f, g, u);
+    }
+}
+
+// ---- few tokens ----------------------------------------------------------------------------------------------------
+//
+// Up to 64 tokens: the weights are read once, straight into the matrix instructions' operands, 16 bytes a lane.  A workgroup has 16 columns of both
+// sides and all tokens; its eight waves share the reduction out, a step of 32 (16 for fp32) each by turns, and join their sums in LDS.
+
+constexpr int kFewWaves = 8, kFewTokens = 64;
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+// 16 bytes of a row; elements from `have` on are 0
+template <class T>
+__device__ __forceinline__ Pack<T, 16 / sizeof(T)> load_piece(const T *p, int have)
+{
+    constexpr int N = 16 / sizeof(T);
+    if (have >= N) return loose_load<T, N>(p);
+    return load_pack<false, T, N>(p, have);
+}
+
+__device__ __forceinline__ f32x4 few_product(const Pack<bf16_t, 8> &w, const Pack<bf16_t, 8> &x, f32x4 acc)
+{
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w), __builtin_bit_cast(bf16x8, x), acc, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4 few_product(const Pack<float, 4> &w, const Pack<float, 4> &x, f32x4 acc)
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(w.v[i], x.v[i], acc, 0, 0, 0);
+    return acc;
+}
+
+template <class T, int MT>
+__global__ __launch_bounds__(64 * kFewWaves) void gated_few_kernel(const T *x, long x_m, const T *wg, const T *wu, int D, GateOut o)
+{
+    constexpr int N = 16 / sizeof(T), STEP = 4 * N;
+    __shared__ f32x4 sums[kFewWaves][2 * MT][64];
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, row = lane % 16;
+    const long f0 = blockIdx.x * 16l, f = f0 + row;
+    const bool real = f < o.F;
+    f32x4 g[MT] = {}, u[MT] = {};
+#pragma unroll 4
+    for (int k0 = wave * STEP; k0 < D; k0 += kFewWaves * STEP) {
+        const int k = k0 + lane / 16 * N, have = D - k;
+        const auto a = load_piece<T>(wg + f * D + k, real ? have : 0), b = load_piece<T>(wu + f * D + k, real ? have : 0);
+#pragma unroll
+        for (int t = 0; t < MT; ++t) {
+            const int m = 16 * t + row;
+            const auto v = load_piece<T>(x + m * x_m + k, m < o.M ? have : 0);
+            g[t] = few_product(a, v, g[t]);
+            u[t] = few_product(b, v, u[t]);
+        }
+    }
+#pragma unroll
+    for (int t = 0; t < MT; ++t) sums[wave][2 * t][lane] = g[t], sums[wave][2 * t + 1][lane] = u[t];
+    __syncthreads();
+    // a lane's sums: column 4 (lane / 16) + 0 .. 3, token lane % 16
+    for (int t = wave; t < MT; t += kFewWaves) {
+        Pack<float, 4> gate{}, up{};
+        for (int w = 0; w < kFewWaves; ++w)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) gate.v[e] += sums[w][2 * t][lane][e], up.v[e] += sums[w][2 * t + 1][lane][e];
+        gate_store<T>(o, 16 * t + row, (int)f0 + 4 * (lane / 16), gate, up);
+    }
+}
+
+// ---- backward ------------------------------------------------------------------------------------------------------
+
+// dG's planes, M rows of 2 * half: [dgate | dup], columns behind F are 0
+template <class T>
+__global__ __launch_bounds__(256) void gated_gradient_kernel(const T *dy, long dy_m, const float *saved, GateOut o, int half, bf16_t *out, long plane)
+{
+    const int packs = half / 8;
+    for (long i = blockIdx.x * 256l + threadIdx.x; i < (long)o.M * packs; i += gridDim.x * 256l) {
+        const long m = i / packs;
+        const int f = (int)(i % packs) * 8, have = min(8, o.F - f);
+        float dg[8] = {}, du[8] = {};
+        if (have > 0) {
+            const T *d = dy + m * dy_m + f;
+            const float *s = saved + m * 2 * o.wide + f;
+            Pack<T, 8> v;
+            Pack<float, 8> g, u;
+            if (have == 8) {
+                v = loose_load<T, 8>(d);
+                g = loose_load<float, 8>(s);
+                u = loose_load<float, 8>(s + o.wide);
+            } else {
+                v = load_pack<false, T, 8>(d, have);
+                g = load_pack<false, float, 8>(s, have);
+                u = load_pack<false, float, 8>(s + o.wide, have);
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                float value;
+                const float slope = gate_slope(o.act, g.v[e], value), dv = to_f(v.v[e]);
+                dg[e] = e < have ? dv * u.v[e] * slope : 0.f;
+                du[e] = e < have ? dv * value : 0.f;
+            }
+        }
+        store_planes<T>(out + m * 2 * half + f, plane, dg);
+        store_planes<T>(out + m * 2 * half + half + f, plane, du);
+    }
+}
+
+// out(m, n), rows `stride` apart, of one matrix or of two: rows from `half` on are the second's
+struct MatrixOut {
+    void *p[2];
+    long stride;
+    long rows, half;      // rows of each; rows from `half` on are the second's, which one alone has beyond any tile
+    int cols;
+    bool add;
+};
+
+template <class T>
+__device__ __forceinline__ void matrix_store(const MatrixOut &o, long m, int n, const Pack<float, 4> &v)
+{
+    const int second = m >= o.half, have = min(4, o.cols - n);
+    m -= second ? o.half : 0;
+    if (m >= o.rows || have <= 0) return;
+    T *at = (T *)o.p[second] + m * o.stride + n;
+    Pack<T, 4> r;
+    if (have == 4) {
+        Pack<T, 4> old{};
+        if (o.add) old = loose_load<T, 4>(at);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) r.v[e] = from_f<T>(o.add ? to_f(old.v[e]) + v.v[e] : v.v[e]);
+        loose_store<T, 4>(at, r);
+    } else {
+        for (int e = 0; e < have; ++e) at[e] = from_f<T>(o.add ? to_f(at[e]) + v.v[e] : v.v[e]);
+    }
+}
+
+template <class TILE, class T>
+__global__ __launch_bounds__(TILE::THREADS) void product_kernel(Problem p, MatrixOut o, float *part, long part_rows, int part_cols)
+{
+    __shared__ __attribute__((aligned(16))) char lds[TILE::LDS];
+    const int tm = blockIdx.x % p.tiles_m, tn = blockIdx.x / p.tiles_m;
+    const int m0 = tm * TILE::BM, n0 = tn * TILE::BN;
+    int t0, t1;
+    split_range(p, blockIdx.y, t0, t1);
+    TILE tile;
+    tile.run(p, m0, n0, t0, t1, lds);
+    if (part) {
+        float *at = part + (long)blockIdx.y * part_rows * part_cols;
+        tile.each([&](int m, int n, const Pack<float, 4> &v) {
+            if (m0 + m < part_rows && n0 + n < part_cols) *reinterpret_cast<Pack<float, 4> *>(at + (long)(m0 + m) * part_cols + n0 + n) = v;
+        });
+        return;
+    }
+    tile.each([&](int m, int n, const Pack<float, 4> &v) { matrix_store<T>(o, (long)m0 + m, n0 + n, v); });
+}
+
+template <class T>
+__global__ __launch_bounds__(256) void product_join_kernel(const float *part, int splits, MatrixOut o, long rows, int cols)
+{
+    const int packs = cols / 4;
+    for (long i = blockIdx.x * 256l + threadIdx.x; i < rows * packs; i += gridDim.x * 256l) {
+        const long m = i / packs;
+        const int n = (int)(i % packs) * 4;
+        Pack<float, 4> v{};
+        for (int s = 0; s < splits; ++s) {
+            const auto a = *reinterpret_cast<const Pack<float, 4> *>(part + (s * rows + m) * cols + n);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v.v[e] += a.v[e];
+        }
+        matrix_store<T>(o, m, n, v);
+    }
+}
+
+__global__ __launch_bounds__(256) void clear_kernel(char *p, long row_bytes, long rows, long stride_bytes)
+{
+    for (long i = blockIdx.x * 256l + threadIdx.x; i < rows * row_bytes; i += gridDim.x * 256l) p[i / row_bytes * stride_bytes + i % row_bytes] = 0;
+}
+
+// ---- plans ---------------------------------------------------------------------------------------------------------
+
+unsigned grid_for(long n) { return (unsigned)std::min((n + 255) / 256, 1l << 16); }
+
+constexpr int kUnits = 256;      // compute units
+
+// Tiles of 256 by 256 where they fill the card, of 128 by 128 otherwise; the reduction in parts where even those are too few.
+struct Shape {
+    bool large;
+    int tiles_m, tiles_n, splits;
+};
+
+Shape shape_of(long m, long n, long steps)
+{
+    Shape s;
+    const long big = (m + 255) / 256 * ((n + 255) / 256);
+    s.large = big >= kUnits;
+    const int side = s.large ? 256 : 128;
+    s.tiles_m = (int)((m + side - 1) / side);
+    s.tiles_n = (int)((n + side - 1) / side);
+    const long tiles = (long)s.tiles_m * s.tiles_n;
+    s.splits = 1;
+    // parts of 8 steps at least; two workgroups to a unit
+    if (!s.large) s.splits = (int)std::max(1l, std::min(2 * kUnits / tiles, steps / 8));
+    return s;
+}
+
+// What a call has in its workspace, in bytes from its begin; a part of no bytes is not needed.
+struct Layout {
+    int planes, phases;
+    int width;               // a row of x's and the weights' copies
+    bool copy_x, copy_w;
+    size_t x, wg, wu, dg, part, bytes;
+    int half;                // dG's columns of one side
+    long x_plane, w_plane, dg_plane;
+    bool few;
+    Shape fwd, dx, dw;
+};
+
+int wide_of(const ucd_gated_projection_t &d) { return (int)round_up(d.F, 4); }
+
+Layout layout_of(const ucd_gated_projection_t &d, int dir, bool x_aligned, bool w_aligned)
+{
+    Layout l{};
+    const bool f32 = d.dtype == 0;
+    l.planes = f32 ? 3 : 1;
+    l.phases = f32 ? 6 : 1;
+    l.width = (int)round_up(d.D, 8);
+    l.half = (int)round_up(d.F, BK);
+    l.few = d.M <= kFewTokens;
+    l.copy_w = f32 || d.D % 8 != 0 || !w_aligned;
+    l.copy_x = f32 || d.D % 8 != 0 || !x_aligned || (d.M > 1 && d.x_m % 8 != 0);
+    size_t at = 0;
+    auto take = [&](size_t n) {
+        const size_t here = at;
+        at += (n + 255) / 256 * 256;
+        return here;
+    };
+    l.x_plane = round_up((long)d.M * l.width, 128);
+    l.w_plane = round_up((long)d.F * l.width, 128);
+    const long d_steps = (l.width + BK - 1) / BK * l.phases;
+    if (dir == UCD_SEQ_FWD) {
+        l.fwd = shape_of(d.M, 2l * d.F, d_steps);
+        if (l.few) {
+            l.bytes = 0;
+            return l;
+        }
+    } else {
+        l.dx = shape_of(d.M, d.D, 2l * l.half / BK * l.phases);
+        l.dw = shape_of(2l * l.half, d.D, ((long)d.M + BK - 1) / BK * l.phases);
+        l.dg_plane = (long)d.M * 2 * l.half;
+        l.dg = take((size_t)l.planes * l.dg_plane * 2);
+    }
+    if (l.copy_x) l.x = take((size_t)l.planes * l.x_plane * 2);
+    if (l.copy_w) {
+        l.wg = take((size_t)l.planes * l.w_plane * 2);
+        l.wu = take((size_t)l.planes * l.w_plane * 2);
+    }
+    size_t part = 0;
+    if (dir == UCD_SEQ_FWD) {
+        if (l.fwd.splits > 1) part = (size_t)l.fwd.splits * d.M * 2 * wide_of(d) * 4;
+    } else {
+        const size_t cols = (size_t)round_up(d.D, 4);
+        if (l.dx.splits > 1) part = (size_t)l.dx.splits * d.M * cols * 4;
+        if (l.dw.splits > 1) part = std::max(part, (size_t)l.dw.splits * 2 * l.half * cols * 4);
+    }
+    l.part = take(part);
+    l.bytes = at;
+    return l;
+}
+
+bool aligned16(const void *p) { return ((uintptr_t)p & 15u) == 0; }
+
+template <class T>
+hipError_t copy_rows(const void *from, long stride, long rows, int cols, bf16_t *to, int width, long plane, hipStream_t s)
+{
+    copy_rows_kernel<T><<<grid_for(rows * (width / 8)), 256, 0, s>>>((const T *)from, stride, rows, cols, to, width, plane);
+    return hipGetLastError();
+}
+
+// x and the weights as operands, copied where they have to be
+template <class T>
+hipError_t operands(const ucd_gated_projection_t &d, const Layout &l, const void *x, const void *wg, const void *wu, char *ws, Operand &ox, Operand &ow,
+                    hipStream_t s)
+{
+    hipError_t e = hipSuccess;
+    ox.p[0] = ox.p[1] = (const bf16_t *)x;
+    ox.stride = d.x_m;
+    ow.p[0] = (const bf16_t *)wg;
+    ow.p[1] = (const bf16_t *)wu;
+    ow.stride = d.D;
+    ox.plane = l.x_plane;
+    ow.plane = l.w_plane;
+    if (l.copy_x) {
+        ox.p[0] = ox.p[1] = (bf16_t *)(ws + l.x);
+        ox.stride = l.width;
+        if ((e = copy_rows<T>(x, d.x_m, d.M, d.D, (bf16_t *)(ws + l.x), l.width, l.x_plane, s)) != hipSuccess) return e;
+    }
+    if (l.copy_w) {
+        ow.p[0] = (bf16_t *)(ws + l.wg);
+        ow.p[1] = (bf16_t *)(ws + l.wu);
+        ow.stride = l.width;
+        if ((e = copy_rows<T>(wg, d.D, d.F, d.D, (bf16_t *)(ws + l.wg), l.width, l.w_plane, s)) != hipSuccess) return e;
+        if ((e = copy_rows<T>(wu, d.D, d.F, d.D, (bf16_t *)(ws + l.wu), l.width, l.w_plane, s)) != hipSuccess) return e;
+    }
+    return e;
+}
+
+template <class T>
+hipError_t few(const ucd_gated_projection_t &d, const void *x, const void *wg, const void *wu, const GateOut &o, hipStream_t s)
+{
+    const unsigned grid = (unsigned)((d.F + 15) / 16);
+    const int mt = (d.M + 15) / 16;
+    const T *px = (const T *)x, *pg = (const T *)wg, *pu = (const T *)wu;
+    if (mt == 1) gated_few_kernel<T, 1><<<grid, 64 * kFewWaves, 0, s>>>(px, d.x_m, pg, pu, d.D, o);
+    else if (mt == 2) gated_few_kernel<T, 2><<<grid, 64 * kFewWaves, 0, s>>>(px, d.x_m, pg, pu, d.D, o);
+    else gated_few_kernel<T, 4><<<grid, 64 * kFewWaves, 0, s>>>(px, d.x_m, pg, pu, d.D, o);
+    return hipGetLastError();
+}
+
+template <class T, class TILE>
+hipError_t forward(const Problem &p, const GateOut &o, float *part, hipStream_t s)
+{
+    gated_forward_kernel<TILE, T><<<dim3((unsigned)(p.tiles_m * p.tiles_n), (unsigned)p.splits), TILE::THREADS, 0, s>>>(p, o, part);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || !part) return e;
+    gated_join_kernel<T><<<grid_for((long)o.M * (o.wide / 4)), 256, 0, s>>>(part, p.splits, o);
+    return hipGetLastError();
+}
+
+template <class T, class TILE>
+hipError_t multiply(const Problem &p, const MatrixOut &o, float *part, long rows, hipStream_t s)
+{
+    const int cols = (int)round_up(o.cols, 4);
+    product_kernel<TILE, T><<<dim3((unsigned)(p.tiles_m * p.tiles_n), (unsigned)p.splits), TILE::THREADS, 0, s>>>(p, o, part, rows, cols);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || !part) return e;
+    product_join_kernel<T><<<grid_for(rows * (cols / 4)), 256, 0, s>>>(part, p.splits, o, rows, cols);
+    return hipGetLastError();
+}
+
+void shape_into(Problem &p, const Shape &s)
+{
+    p.tiles_m = s.tiles_m;
+    p.tiles_n = s.tiles_n;
+    p.splits = s.splits;
+}
+
+template <class T>
+hipError_t fwd(const ucd_gated_projection_t &d, const void *x, const void *wg, const void *wu, const GateOut &o, char *ws, hipStream_t s)
+{
+    const Layout l = layout_of(d, UCD_SEQ_FWD, aligned16(x), aligned16(wg) && aligned16(wu));
+    if (l.few) return few<T>(d, x, wg, wu, o, s);
+    Problem p{};
+    const hipError_t e = operands<T>(d, l, x, wg, wu, ws, p.m, p.n, s);
+    if (e != hipSuccess) return e;
+    p.m.rows = d.M;
+    p.n.rows = d.F;
+    p.m.k = p.n.k = l.width;
+    p.k_tiles = (l.width + BK - 1) / BK;
+    p.phases = l.phases;
+    shape_into(p, l.fwd);
+    float *part = p.splits > 1 ? (float *)(ws + l.part) : nullptr;
+    if (l.fwd.large) return forward<T, Tile<256, 256, 2, 4, true, true, true>>(p, o, part, s);
+    return forward<T, Tile<128, 128, 2, 2, true, true, true>>(p, o, part, s);
+}
+
+template <class T>
+hipError_t bwd(const ucd_gated_projection_t &d, const void *x, const void *wg, const void *wu, const void *dy, const GateOut &o, void *dx, void *dwg,
+               void *dwu, bool add, char *ws, hipStream_t s)
+{
+    const Layout l = layout_of(d, UCD_SEQ_BWD, aligned16(x), aligned16(wg) && aligned16(wu));
+    Operand ox{}, ow{}, og{};
+    hipError_t e = operands<T>(d, l, x, wg, wu, ws, ox, ow, s);
+    if (e != hipSuccess) return e;
+    gated_gradient_kernel<T><<<grid_for((long)d.M * (l.half / 8)), 256, 0, s>>>((const T *)dy, d.y_m, o.saved, o, l.half, (bf16_t *)(ws + l.dg), l.dg_plane);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+    og.p[0] = og.p[1] = (const bf16_t *)(ws + l.dg);
+    og.stride = 2l * l.half;
+    og.plane = l.dg_plane;
+    // dx = dG [Wg; Wu]: dG along its rows, the weights across
+    Problem p{};
+    p.m = og;
+    p.m.rows = d.M;
+    p.m.k = 2 * l.half;
+    p.n = ow;
+    p.n.rows = l.width;
+    p.n.k = d.F;
+    p.n.half = l.half;
+    p.k_tiles = 2 * l.half / BK;
+    p.phases = l.phases;
+    shape_into(p, l.dx);
+    MatrixOut out{};
+    out.p[0] = out.p[1] = dx;
+    out.stride = d.x_m;
+    out.rows = d.M;
+    out.half = 1l << 40;
+    out.cols = d.D;
+    float *part = p.splits > 1 ? (float *)(ws + l.part) : nullptr;
+    e = l.dx.large ? multiply<T, Tile<256, 256, 2, 4, true, false, true>>(p, out, part, d.M, s)
+                   : multiply<T, Tile<128, 128, 2, 2, true, false, true>>(p, out, part, d.M, s);
+    if (e != hipSuccess) return e;
+    // [dWg; dWu] = dG^T x: both across
+    p.m = og;
+    p.m.rows = 2 * l.half;
+    p.m.k = d.M;
+    p.n = ox;
+    p.n.rows = l.width;
+    p.n.k = d.M;
+    p.k_tiles = (d.M + BK - 1) / BK;
+    shape_into(p, l.dw);
+    out.p[0] = dwg;
+    out.p[1] = dwu;
+    out.stride = d.D;
+    out.rows = d.F;
+    out.half = l.half;
+    out.add = add;
+    part = p.splits > 1 ? (float *)(ws + l.part) : nullptr;
+    return l.dw.large ? multiply<T, Tile<256, 256, 2, 4, false, false, false>>(p, out, part, 2l * l.half, s)
+                      : multiply<T, Tile<128, 128, 2, 2, false, false, false>>(p, out, part, 2l * l.half, s);
+}
+
+GateOut gate_out(const ucd_gated_projection_t &d, void *y, float *saved)
+{
+    return GateOut{y, (long)d.y_m, saved, d.M, d.F, wide_of(d), d.act};
+}
+
+}  // namespace
+
+size_t gated_projection_ws_bytes(const ucd_gated_projection_t &d, int dir)
+{
+    if (d.M == 0) return 0;
+    return layout_of(d, dir, false, false).bytes;
+}
+
+size_t gated_projection_saved_bytes(const ucd_gated_projection_t &d) { return (size_t)d.M * 2 * wide_of(d) * 4; }
+
+bool gated_projection_countable(const ucd_gated_projection_t &d)
+{
+    // tiles of the smaller kind, 128 by 128 (64 columns of either side): a grid has fewer than 2^32 threads
+    const double m = (d.M + 127) / 128, f = (d.F + 63) / 64, c = (d.D + 127) / 128;
+    return m * f < 1 << 23 && m * c < 1 << 23 && 2 * f * c < 1 << 23;
+}
+
+hipError_t gated_projection_fwd(const ucd_gated_projection_t &d, const void *x, const void *wg, const void *wu, void *y, float *saved, void *ws,
+                                hipStream_t s)
+{
+    const GateOut o = gate_out(d, y, saved);
+    return d.dtype == 1 ? fwd<bf16_t>(d, x, wg, wu, o, (char *)ws, s) : fwd<float>(d, x, wg, wu, o, (char *)ws, s);
+}
+
+hipError_t gated_projection_bwd(const ucd_gated_projection_t &d, const void *x, const void *wg, const void *wu, const void *dy, const float *saved,
+                                void *dx, void *dwg, void *dwu, bool add, void *ws, hipStream_t s)
+{
+    if (d.M == 0) {
+        if (add) return hipSuccess;
+        const long bytes = (long)d.F * d.D * (d.dtype == 1 ? 2 : 4);
+        clear_kernel<<<grid_for(bytes), 256, 0, s>>>((char *)dwg, bytes, 1, 0);
+        clear_kernel<<<grid_for(bytes), 256, 0, s>>>((char *)dwu, bytes, 1, 0);
+        return hipGetLastError();
+    }
+    const GateOut o = gate_out(d, nullptr, const_cast<float *>(saved));
+    return d.dtype == 1 ? bwd<bf16_t>(d, x, wg, wu, dy, o, dx, dwg, dwu, add, (char *)ws, s)
+                        : bwd<float>(d, x, wg, wu, dy, o, dx, dwg, dwu, add, (char *)ws, s);
+}
+
+}  // namespace ucd

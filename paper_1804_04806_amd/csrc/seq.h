@@ -42,4 +42,24 @@ hipError_t scan_bwd(const ucd_scan_t &d, const ucd_scan_in_t &in, const void *dy
                     const float *saved, const ucd_scan_grad_t &g, bool add, void *ws, hipStream_t s);
 hipError_t scan_step(const ucd_scan_t &d, const ucd_scan_in_t &in, float *state, void *y, hipStream_t s);
 
+size_t linear_attention_ws_bytes(const ucd_linear_attention_t &d, int dir);
+size_t linear_attention_saved_bytes(const ucd_linear_attention_t &d);
+bool linear_attention_countable(const ucd_linear_attention_t &d);
+hipError_t linear_attention_fwd(const ucd_linear_attention_t &d, const ucd_linear_attention_in_t &in, const float *state_in,
+                                float *state_out, void *y, float *saved, void *ws, hipStream_t s);
+hipError_t linear_attention_bwd(const ucd_linear_attention_t &d, const ucd_linear_attention_in_t &in, const void *dy,
+                                const float *dstate_out, const float *saved, const ucd_linear_attention_grad_t &grad,
+                                void *ws, hipStream_t s);
+hipError_t linear_attention_step(const ucd_linear_attention_t &d, const ucd_linear_attention_in_t &in, float *state, void *y,
+                                 hipStream_t s);
+
+size_t gated_projection_ws_bytes(const ucd_gated_projection_t &d, int dir);
+size_t gated_projection_saved_bytes(const ucd_gated_projection_t &d);
+bool gated_projection_countable(const ucd_gated_projection_t &d);
+hipError_t gated_projection_fwd(const ucd_gated_projection_t &d, const void *x, const void *wg, const void *wu, void *y,
+                                float *saved, void *ws, hipStream_t s);
+hipError_t gated_projection_bwd(const ucd_gated_projection_t &d, const void *x, const void *wg, const void *wu,
+                                const void *dy, const float *saved, void *dx, void *dwg, void *dwu, bool add, void *ws,
+                                hipStream_t s);
+
 }  // namespace ucd

@@ -1,6 +1,7 @@
 // C-ABI of the sequence operators: validation and the calls of their launchers.  See include/ucd_seq.h for the contract.
 #include "ucd_seq.h"
 
+#include <algorithm>
 #include <cmath>
 #include <cstdio>
 #include <cstdlib>
@@ -126,6 +127,41 @@ int scan_inputs(const ucd_scan_t &d, const ucd_scan_in_t *in)
         !aligned4(in->lengths) || !aligned4(in->slots))
         return UCD_E_INVALID;
     return UCD_OK;
+}
+
+bool attention_ok(const ucd_linear_attention_t *in, ucd_linear_attention_t &d)
+{
+    d = *in;
+    if (!extent_ok(d.B, 0) || !extent_ok(d.L, 0) || !extent_ok(d.H, 1) || d.Hk < 1 || d.H % d.Hk != 0 || d.Dk < 1 || d.Dk > 128 || d.Dv < 1 ||
+        d.Dv > 128 || !dtype_ok(d.dtype) || d.n_slots < 0 || !std::isfinite(d.scale))
+        return false;
+    const int64_t qk = (int64_t)d.Hk * d.Dk, v = (int64_t)d.H * d.Dv;
+    if ((double)d.B * (d.L + 1.) * std::max(std::max(qk, v), (int64_t)d.H * d.Dk) > (double)kMaxElements) return false;
+    if ((double)d.B * d.H * d.Dk * d.Dv > (double)kMaxElements) return false;
+    return fill_strides(d.q_b, d.q_l, d.B, d.L, qk) && fill_strides(d.k_b, d.k_l, d.B, d.L, qk) && fill_strides(d.v_b, d.v_l, d.B, d.L, v) &&
+           fill_strides(d.g_b, d.g_l, d.B, d.L, d.H) && fill_strides(d.y_b, d.y_l, d.B, d.L, v);
+}
+
+int attention_inputs(const ucd_linear_attention_t &d, const ucd_linear_attention_in_t *in)
+{
+    if (!empty(d.B, d.L) && (!in->q || !in->k || !in->v)) return UCD_E_NULLPTR;
+    if (!aligned(in->q, d.dtype) || !aligned(in->k, d.dtype) || !aligned(in->v, d.dtype) || !aligned(in->g, d.dtype) ||
+        !aligned4(in->decay) || !aligned4(in->lengths) || !aligned4(in->slots))
+        return UCD_E_INVALID;
+    return UCD_OK;
+}
+
+constexpr int32_t kMaxWidth = 1 << 20;      // a tile of 256 rows in 32-bit offsets of bytes
+
+bool gated_ok(const ucd_gated_projection_t *in, ucd_gated_projection_t &d)
+{
+    d = *in;
+    if (!extent_ok(d.M, 0) || d.D < 1 || d.D > kMaxWidth || d.F < 1 || d.F > kMaxWidth || !dtype_ok(d.dtype)) return false;
+    if (!act_ok(d.act) && d.act != UCD_ACT_GELU) return false;
+    int64_t one = 0, two = 0;
+    if ((double)d.M * std::max(d.D, d.F) > (double)kMaxElements) return false;
+    if (!fill_strides(one, d.x_m, 1, d.M, d.D) || !fill_strides(two, d.y_m, 1, d.M, d.F)) return false;
+    return d.M <= 1 || d.x_m <= 2 * kMaxWidth;
 }
 
 }  // namespace
@@ -318,6 +354,135 @@ int ucd_scan_step(const ucd_scan_t *scan, const ucd_scan_in_t *in, float *state,
         if (d.B == 0) return UCD_OK;
         (void)hipGetLastError();
         return hip_status(scan_step(d, *in, state, y, (hipStream_t)stream));
+    });
+}
+
+size_t ucd_linear_attention_workspace_size(const ucd_linear_attention_t *attention, int dir)
+{
+    ucd_linear_attention_t d;
+    if (!attention || !attention_ok(attention, d) || (dir != UCD_SEQ_FWD && dir != UCD_SEQ_BWD)) return UCD_WS_NA;
+    return linear_attention_ws_bytes(d, dir);
+}
+
+size_t ucd_linear_attention_saved_size(const ucd_linear_attention_t *attention)
+{
+    ucd_linear_attention_t d;
+    if (!attention || !attention_ok(attention, d)) return UCD_WS_NA;
+    return linear_attention_saved_bytes(d);
+}
+
+int ucd_linear_attention_fwd(const ucd_linear_attention_t *attention, const ucd_linear_attention_in_t *in, const float *state_in,
+                             float *state_out, void *y, void *saved, size_t saved_bytes, void *ws, size_t ws_bytes, void *stream)
+{
+    return guarded([&]() -> int {
+        if (!attention || !in) return UCD_E_NULLPTR;
+        ucd_linear_attention_t d;
+        if (!attention_ok(attention, d) || !slots_ok(d.B, d.n_slots, in->slots)) return UCD_E_INVALID;
+        if (!empty(d.B, d.L) && !y) return UCD_E_NULLPTR;
+        int rc = attention_inputs(d, in);
+        if (rc != UCD_OK) return rc;
+        if (!aligned(y, d.dtype) || !aligned4(state_in) || !aligned4(state_out)) return UCD_E_INVALID;
+        if (saved && (rc = ws_status(linear_attention_saved_bytes(d), saved, saved_bytes)) != UCD_OK) return rc;
+        if ((rc = ws_status(linear_attention_ws_bytes(d, UCD_SEQ_FWD), ws, ws_bytes)) != UCD_OK) return rc;
+        if (!linear_attention_countable(d)) return UCD_E_UNSUPPORTED;
+        if (d.B == 0) return UCD_OK;
+        (void)hipGetLastError();
+        return hip_status(linear_attention_fwd(d, *in, state_in, state_out, y, (float *)saved, ws, (hipStream_t)stream));
+    });
+}
+
+int ucd_linear_attention_bwd(const ucd_linear_attention_t *attention, const ucd_linear_attention_in_t *in, const void *dy,
+                             const float *dstate_out, const void *saved, size_t saved_bytes, const ucd_linear_attention_grad_t *grad,
+                             void *ws, size_t ws_bytes, void *stream)
+{
+    return guarded([&]() -> int {
+        if (!attention || !in || !grad) return UCD_E_NULLPTR;
+        ucd_linear_attention_t d;
+        if (!attention_ok(attention, d) || d.n_slots != 0 || in->slots || (grad->g && !in->g)) return UCD_E_INVALID;
+        int rc = attention_inputs(d, in);
+        if (rc != UCD_OK) return rc;
+        if (!empty(d.B, d.L) && (!dy || !grad->q || !grad->k || !grad->v)) return UCD_E_NULLPTR;
+        if (!aligned(dy, d.dtype) || !aligned(grad->q, d.dtype) || !aligned(grad->k, d.dtype) || !aligned(grad->v, d.dtype) ||
+            !aligned(grad->g, d.dtype) || !aligned4(grad->state) || !aligned4(dstate_out))
+            return UCD_E_INVALID;
+        if ((rc = ws_status(linear_attention_saved_bytes(d), saved, saved_bytes)) != UCD_OK) return rc;
+        if ((rc = ws_status(linear_attention_ws_bytes(d, UCD_SEQ_BWD), ws, ws_bytes)) != UCD_OK) return rc;
+        if (!linear_attention_countable(d)) return UCD_E_UNSUPPORTED;
+        if (d.B == 0) return UCD_OK;
+        (void)hipGetLastError();
+        return hip_status(linear_attention_bwd(d, *in, dy, dstate_out, (const float *)saved, *grad, ws, (hipStream_t)stream));
+    });
+}
+
+int ucd_linear_attention_step(const ucd_linear_attention_t *attention, const ucd_linear_attention_in_t *in, float *state, void *y,
+                              void *stream)
+{
+    return guarded([&]() -> int {
+        if (!attention || !in) return UCD_E_NULLPTR;
+        ucd_linear_attention_t d;
+        if (!attention_ok(attention, d) || d.L != 1 || !slots_ok(d.B, d.n_slots, in->slots)) return UCD_E_INVALID;
+        if (d.B > 0 && (!state || !y)) return UCD_E_NULLPTR;
+        const int rc = attention_inputs(d, in);
+        if (rc != UCD_OK) return rc;
+        if (!aligned(y, d.dtype) || !aligned4(state)) return UCD_E_INVALID;
+        if (!linear_attention_countable(d)) return UCD_E_UNSUPPORTED;
+        if (d.B == 0) return UCD_OK;
+        (void)hipGetLastError();
+        return hip_status(linear_attention_step(d, *in, state, y, (hipStream_t)stream));
+    });
+}
+
+size_t ucd_gated_projection_workspace_size(const ucd_gated_projection_t *gated, int dir)
+{
+    ucd_gated_projection_t d;
+    if (!gated || !gated_ok(gated, d) || (dir != UCD_SEQ_FWD && dir != UCD_SEQ_BWD)) return UCD_WS_NA;
+    return gated_projection_ws_bytes(d, dir);
+}
+
+size_t ucd_gated_projection_saved_size(const ucd_gated_projection_t *gated)
+{
+    ucd_gated_projection_t d;
+    if (!gated || !gated_ok(gated, d)) return UCD_WS_NA;
+    return gated_projection_saved_bytes(d);
+}
+
+int ucd_gated_projection_fwd(const ucd_gated_projection_t *gated, const void *x, const void *w_gate, const void *w_up, void *y,
+                             void *saved, size_t saved_bytes, void *ws, size_t ws_bytes, void *stream)
+{
+    return guarded([&]() -> int {
+        if (!gated || !w_gate || !w_up) return UCD_E_NULLPTR;
+        ucd_gated_projection_t d;
+        if (!gated_ok(gated, d)) return UCD_E_INVALID;
+        if (d.M > 0 && (!x || !y)) return UCD_E_NULLPTR;
+        if (!aligned(x, d.dtype) || !aligned(w_gate, d.dtype) || !aligned(w_up, d.dtype) || !aligned(y, d.dtype)) return UCD_E_INVALID;
+        int rc;
+        if (saved && (rc = ws_status(gated_projection_saved_bytes(d), saved, saved_bytes)) != UCD_OK) return rc;
+        if ((rc = ws_status(gated_projection_ws_bytes(d, UCD_SEQ_FWD), ws, ws_bytes)) != UCD_OK) return rc;
+        if (!gated_projection_countable(d)) return UCD_E_UNSUPPORTED;
+        if (d.M == 0) return UCD_OK;
+        (void)hipGetLastError();
+        return hip_status(gated_projection_fwd(d, x, w_gate, w_up, y, (float *)saved, ws, (hipStream_t)stream));
+    });
+}
+
+int ucd_gated_projection_bwd(const ucd_gated_projection_t *gated, const void *x, const void *w_gate, const void *w_up,
+                             const void *dy, const void *saved, size_t saved_bytes, void *dx, void *dw_gate, void *dw_up, float beta,
+                             void *ws, size_t ws_bytes, void *stream)
+{
+    return guarded([&]() -> int {
+        if (!gated || !w_gate || !w_up || !dw_gate || !dw_up) return UCD_E_NULLPTR;
+        ucd_gated_projection_t d;
+        if (!gated_ok(gated, d) || !beta_ok(beta)) return UCD_E_INVALID;
+        if (d.M > 0 && (!x || !dy || !dx)) return UCD_E_NULLPTR;
+        if (!aligned(x, d.dtype) || !aligned(w_gate, d.dtype) || !aligned(w_up, d.dtype) || !aligned(dy, d.dtype) || !aligned(dx, d.dtype) ||
+            !aligned(dw_gate, d.dtype) || !aligned(dw_up, d.dtype))
+            return UCD_E_INVALID;
+        int rc = ws_status(gated_projection_saved_bytes(d), saved, saved_bytes);
+        if (rc != UCD_OK) return rc;
+        if ((rc = ws_status(gated_projection_ws_bytes(d, UCD_SEQ_BWD), ws, ws_bytes)) != UCD_OK) return rc;
+        if (!gated_projection_countable(d)) return UCD_E_UNSUPPORTED;
+        (void)hipGetLastError();
+        return hip_status(gated_projection_bwd(d, x, w_gate, w_up, dy, (const float *)saved, dx, dw_gate, dw_up, beta != 0.f, ws, (hipStream_t)stream));
     });
 }
 
