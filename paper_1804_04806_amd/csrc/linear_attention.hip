@@ -31,13 +31,14 @@ struct Rows {
     int div;        // heads that share a row of it
     int width;
     template <class T>
-    __device__ __forceinline__ const T *at(int seq, int head, long t) const { return (const T *)p + seq * b + t * l + (long)(head / div) * width; }
+    __device__ __forceinline__ const T *at(int seq, int head) const { return (const T *)p + seq * b + (long)(head / div) * width; }
 };
 
 struct Mix {
     Rows q, k, v, dot;           // dot: rows like the output's, multiplied with the part of the state at the chunk's start; may be none
     void *out;
     long out_b, out_l;
+    bool out_f32;
     float p_scale, first_scale, last_scale;
     Decays decays;
     const int32_t *lengths, *slots;
@@ -45,16 +46,16 @@ struct Mix {
     // states: of a slot and head rows (of q's width) and columns (of v's) apart
     const float *state_in;
     float *state_out;
-    long s_row, s_col, s_head, s_out_row, s_out_col;
+    long s_row, s_col, s_head;
     float *starts;               // (segments, B, H, rows, columns) with the strides of state_in, or null
     float *segment_decay;        // (segments, B, H)
     float *dots;                 // (column tiles, B, H, L), or null
-    void *chunk_states;          // states at the chunks' starts, by workgroup, chunk and thread; or null
+    void *chunk_states;          // states at the chunks' starts, by workgroup, chunk and thread
     float *passes;               // (column tiles, B, H, chunks): c
     int tiles;
 };
 
-// Places of a launch: column tile, head, sequence, segment.  Column tiles of a head are neighbours that share q and k.
+// Places of a launch: column tile, head, segment, sequence.  Column tiles of a head are neighbours that share q and k.
 struct Place {
     int tile, head, seq, segment;
 };
@@ -71,21 +72,26 @@ __device__ __forceinline__ Place place_of(const Mix &p, int segments)
     return r;
 }
 
-enum { KEEP_NONE = 0, KEEP_WRITE = 1, KEEP_READ = 2 };
+// What a walk is for: outputs; outputs and what the gradient of the decays takes of them (forward: the states at the chunks' starts are kept, backward
+// they are read); a segment's own state alone, from nothing.
+enum { OUTPUTS, DECAYS, STATES };
 
-// DK: q's width, 64 or 128.  STATES: only the segment's own state, from nothing.
-template <class T, class OUT, int DK, bool REV, bool STATES, int KEEP>
-__global__ __launch_bounds__(kThreads) void mix_kernel(Mix p)
+// DK: q's width, 64 or 128.  WHOLE: of rows (Fetch).
+template <class T, int DK, bool REV, int FOR, bool WHOLE>
+__global__ __launch_bounds__(kThreads, sizeof(T) == 2 || DK == 64 ? 2 : 1) void mix_kernel(Mix p)
 {
+    constexpr bool OUT = FOR != STATES, DG = FOR == DECAYS;
+    // what is added to a state that a caller gets, or the next segment, is as exact as the state; states that only go into 16-bit operands need less
+    constexpr int PARTS = sizeof(T) == 4 ? 1 : DG ? 2 : 3;
     typedef Mma<T> M;
     typedef TileLds<T, DK> TQ;
     typedef TileLds<T, kCols> TV;
     constexpr int SD = DK / 64;         // a wave's tiles of the state: DK = 128: 32 rows and all 64 columns; 64: 32 rows and 32 columns
-    __shared__ __attribute__((aligned(16))) char lds_q[STATES ? 16 : TQ::BYTES], lds_k[TQ::BYTES], lds_v[TV::BYTES],
-        lds_p[STATES ? 16 : TV::BYTES], lds_s[STATES ? 16 : TQ::BYTES];      // lds_s: the state's columns as rows of DK
-    __shared__ ChunkDecays dec;
+    __shared__ __attribute__((aligned(16))) char lds_q[OUT ? TQ::BYTES : 16], lds_k[TQ::BYTES], lds_v[TV::BYTES],
+        lds_p[OUT ? TV::BYTES : 16], lds_s[OUT ? TQ::BYTES : 16];      // lds_s: the state's columns as rows of DK
+    __shared__ ChunkDecays decays[2];
     __shared__ float lds_dot[2][kChunk], lds_pass[4];
-    const Place at = place_of(p, STATES ? p.segments - 1 : p.segments);
+    const Place at = place_of(p, OUT ? p.segments : p.segments - 1);
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), row = lane % 32, half = lane / 32;
     const int col0 = at.tile * kCols, cols = min(kCols, p.v.width - col0);
     const int n = p.lengths ? max(0, min(p.L, p.lengths[at.seq])) : p.L;
@@ -93,6 +99,21 @@ __global__ __launch_bounds__(kThreads) void mix_kernel(Mix p)
     const bool idle = p.slots && (slot < 0 || slot >= p.n_slots);
     const int chunks = (p.L + kChunk - 1) / kChunk;
     const int c0 = at.segment * p.per_segment, c1 = min(chunks, c0 + p.per_segment);       // in walking order
+    // a chunk's first token, and the token of one of its rows
+    auto token0 = [&](int chunk) { return (REV ? chunks - 1 - chunk : chunk) * kChunk; };
+    auto token = [&](int chunk, int r) { return token0(chunk) + (REV ? kChunk - 1 - r : r); };
+    const int osize = p.out_f32 ? 4 : (int)sizeof(T);
+    const long o_l = p.out_l * osize;
+    char *out = (char *)p.out + (at.seq * p.out_b + (long)at.head * p.v.width + col0) * osize;
+
+    if (idle) {
+        for (int c = c0; c < c1 && OUT; ++c)
+            for (int i = threadIdx.x; i < kChunk * kCols; i += kThreads) {
+                const int t = token(c, i / kCols), x = i % kCols;
+                if (t < p.L && x < cols) *(T *)(out + t * o_l + x * sizeof(T)) = from_f<T>(0.f);
+            }
+        return;
+    }
 
     // places of a wave's tiles of the state
     const int s_row = DK == 128 ? wave * 32 : wave % 2 * 32;
@@ -100,7 +121,7 @@ __global__ __launch_bounds__(kThreads) void mix_kernel(Mix p)
     f32x16 state[SD];
 #pragma unroll
     for (int i = 0; i < SD; ++i) state[i] = f32x16{};
-    if (!STATES && !idle) {
+    if (OUT) {
         const float *from = p.starts ? p.starts + (((long)at.segment * p.B + at.seq) * p.H + at.head) * p.s_head
                                      : p.state_in ? p.state_in + ((long)slot * p.H + at.head) * p.s_head : nullptr;
         if (from)
@@ -113,92 +134,120 @@ __global__ __launch_bounds__(kThreads) void mix_kernel(Mix p)
                 }
     }
 
-    auto token = [&](int chunk, int r) { return (REV ? chunks - 1 - chunk : chunk) * kChunk + (REV ? kChunk - 1 - r : r); };
-    Fetch<T, DK> fq, fk;
-    Fetch<T, kCols> fv;
+    Fetch<T, DK, WHOLE> fq, fk;
+    Fetch<T, kCols, WHOLE> fv;
+    const long q_l = p.q.l * sizeof(T), k_l = p.k.l * sizeof(T), v_l = p.v.l * sizeof(T);
+    const T *qp = p.q.template at<T>(at.seq, at.head), *kp = p.k.template at<T>(at.seq, at.head), *vp = p.v.template at<T>(at.seq, at.head) + col0;
+    if (OUT) fq.init(p.q.width, q_l, REV);
+    fk.init(p.k.width, k_l, REV);
+    fv.init(cols, v_l, REV);
     auto fetch = [&](int chunk) {
-        auto rows = [&](const Rows &s) {
-            return [&s, &at, n, chunk, token](int r) {
-                const int t = token(chunk, r);
-                return t < n ? s.template at<T>(at.seq, at.head, t) : nullptr;
-            };
-        };
-        if (!STATES) fq.load(rows(p.q), p.q.width);
-        fk.load(rows(p.k), p.k.width);
-        auto v = rows(p.v);
-        fv.load([&](int r) { const T *s = v(r); return s ? s + col0 : nullptr; }, cols);
+        const long t = token0(chunk);
+        const int there = n - (int)t;
+        if (OUT) fq.load((const char *)qp + t * q_l, q_l, there);
+        fk.load((const char *)kp + t * k_l, k_l, there);
+        fv.load((const char *)vp + t * v_l, v_l, there);
     };
-    auto own_decay = [&](int chunk) {
+    // a lane's outputs: row t, columns x0 + 8 i + 4 half + 0 .. 3
+    const int t0 = wave % 2 * 32, x0 = wave / 2 * 32, t_row = t0 + row, t_at = REV ? kChunk - 1 - t_row : t_row;
+    const uint32_t o_first = (uint32_t)(t_at * o_l) + (x0 + 4 * half) * osize;
+    const long d_l = DG ? p.dot.l * (long)sizeof(T) : 0;
+    const T *dp = DG ? p.dot.template at<T>(at.seq, at.head) + col0 : nullptr;
+    // the first wave has the decays of the chunk that comes, and those of the one behind it on their way
+    T raw_decay = from_f<T>(0.f);
+    auto fetch_decay = [&](int chunk) {
         const int t = token(chunk, lane) + (REV ? 1 : 0);
-        return t < n ? p.decays.get<T>(at.seq, at.head, t) : 0.f;
+        raw_decay = chunk < c1 && t < n ? p.decays.raw<T>(at.seq, at.head, t) : from_f<T>(0.f);
+    };
+    auto set_decays = [&](int chunk) {
+        const int t = token(chunk, lane) + (REV ? 1 : 0);
+        decays[chunk & 1].set(t < n ? p.decays.get<T>(at.head, raw_decay) : 0.f, p.first_scale, p.last_scale);
+        fetch_decay(chunk + 1);
     };
     double segment_decay = 0;
-
-    if (idle) {
-        for (int c = c0; c < c1 && !STATES; ++c)
-            for (int i = threadIdx.x; i < kChunk * kCols; i += kThreads) {
-                const int t = token(c, i / kCols), x = i % kCols;
-                if (t < p.L && x < cols) ((OUT *)p.out + at.seq * p.out_b + t * p.out_l + (long)at.head * p.v.width + col0)[x] = from_f<OUT>(0.f);
-            }
-        return;
-    }
-    if (c0 < c1) fetch(c0);
-    for (int c = c0; c < c1; ++c) {
-        if (!STATES) fq.store(lds_q);
-        fk.store(lds_k);
-        fv.store(lds_v);
+    // states at the chunks' starts: pieces of 16 bytes, a workgroup's threads side by side
+    constexpr int PER = 16 / sizeof(T), PIECES = 16 * SD / PER;
+    typedef Pack<T, PER> Piece;
+    auto kept = [&](int c) {
+        const long chunk = REV ? chunks - 1 - c : c;
+        return (Piece *)p.chunk_states + ((((long)at.seq * p.H + at.head) * p.tiles + at.tile) * chunks + chunk) * (PIECES * kThreads) + threadIdx.x;
+    };
+    Piece before[DG && REV ? PIECES : 1];
+    if (c0 < c1) {
+        fetch(c0);
         if (wave == 0) {
-            const float own = own_decay(c);
-            dec.set(own, p.first_scale, p.last_scale);
+            fetch_decay(c0);
+            set_decays(c0);
         }
-        if (!STATES) {
+    }
+    for (int c = c0; c < c1; ++c) {
+        const ChunkDecays &dec = decays[c & 1];
+        if (DG && REV) {
+            const Piece *from = kept(c);
+#pragma unroll
+            for (int i = 0; i < PIECES; ++i) before[i] = from[i * kThreads];
+        }
+        {
+            const long t = token0(c);
+            if (OUT) fq.store(lds_q, (const char *)qp + t * q_l);
+            fk.store(lds_k, (const char *)kp + t * k_l);
+            fv.store(lds_v, (const char *)vp + t * v_l);
+        }
+        if (OUT) {
             // the state as an operand, rounded once to its type
 #pragma unroll
             for (int i = 0; i < SD; ++i)
 #pragma unroll
-                for (int r = 0; r < 16; r += 4) {
-                    Pack<T, 4> v;
+                for (int r = 0; r < 16; r += 4)
+                    *reinterpret_cast<Pack<T, 4> *>(lds_s + TQ::at(s_col(i) + row, s_row + 2 * r + 4 * half)) =
+                        pack_four<T>(state[i][r], state[i][r + 1], state[i][r + 2], state[i][r + 3]);
+            if (DG && !REV) {
+                Piece *to = kept(c);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) v.v[e] = from_f<T>(state[i][r + e]);
-                    *reinterpret_cast<Pack<T, 4> *>(lds_s + TQ::at(s_col(i) + row, s_row + 2 * r + 4 * half)) = v;
-                }
-            if (KEEP == KEEP_WRITE || KEEP == KEEP_READ) {
-                // by thread: 16 SD values of T
-                const long chunk = REV ? chunks - 1 - c : c;
-                T *keep = (T *)p.chunk_states + (((((long)at.seq * p.H + at.head) * p.tiles + at.tile) * chunks + chunk) * kThreads + threadIdx.x) * (16 * SD);
-                float pass = 0.f;
+                for (int i = 0; i < PIECES; ++i) {
+                    Piece v;
 #pragma unroll
-                for (int i = 0; i < SD; ++i)
-#pragma unroll
-                    for (int r = 0; r < 16; r += 4) {
-                        Pack<T, 4> v;
-                        if (KEEP == KEEP_WRITE) {
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) v.v[e] = from_f<T>(state[i][r + e]);
-                            *reinterpret_cast<Pack<T, 4> *>(keep + 16 * i + r) = v;
-                        } else {
-                            v = *reinterpret_cast<const Pack<T, 4> *>(keep + 16 * i + r);
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) pass = fmaf(to_f(v.v[e]), state[i][r + e], pass);
-                        }
-                    }
-                if (KEEP == KEEP_READ) {
-                    pass = sum_group(pass, 64);
-                    if (lane == 0) lds_pass[wave] = pass;
+                    for (int e = 0; e < PER; ++e) v.v[e] = from_f<T>(state[i * PER / 16][i * PER % 16 + e]);
+                    to[i * kThreads] = v;
                 }
             }
         }
-        __syncthreads();
-        if (c + 1 < c1) fetch(c + 1);
-        if (KEEP == KEEP_READ && threadIdx.x == 0) {
-            const int chunk = chunks - 1 - c;
-            const float own = chunk * kChunk < n ? p.decays.get<T>(at.seq, at.head, (long)chunk * kChunk) : 0.f;
-            p.passes[(((long)at.tile * p.B + at.seq) * p.H + at.head) * chunks + chunk] =
-                dec.whole * exp_full(own) * ((lds_pass[0] + lds_pass[1]) + (lds_pass[2] + lds_pass[3]));
+        lds_barrier();
+        if (DG && REV) {
+            float pass = 0.f;
+#pragma unroll
+            for (int i = 0; i < PIECES; ++i)
+#pragma unroll
+                for (int e = 0; e < PER; ++e) pass = fmaf(to_f(before[i % (DG && REV ? PIECES : 1)].v[e]), state[i * PER / 16][i * PER % 16 + e], pass);
+            pass = sum_group(pass, 64);
+            if (lane == 0) lds_pass[wave] = pass;
         }
-        if (!STATES) {
+        if (wave == 0 && c + 1 < c1) set_decays(c + 1);       // ahead of the loads, which it would wait for
+        if (c + 1 < c1) fetch(c + 1);
+        if (OUT) {
             // P[t, s]: a lane has row t and 16 s
-            const int t0 = wave % 2 * 32, s0 = wave / 2 * 32, t = t0 + row;
+            const int s0 = x0, t = t_row, tok0 = token0(c);
+            const bool real = t_at < n - tok0;
+            // what the part of the first state is multiplied with: on its way
+            uint32_t dots[DG ? 4 : 1][4];
+            if (DG) {
+                const auto rsrc = buffer_of((const char *)dp + tok0 * d_l, chunk_bytes(d_l, n - tok0));
+                const uint32_t first = (uint32_t)(t_at * d_l) + (x0 + 4 * half) * (uint32_t)sizeof(T);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int have = cols - (x0 + 8 * r + 4 * half);
+                    const uint32_t o = first + 8 * r * (uint32_t)sizeof(T);
+                    if (WHOLE && sizeof(T) == 2) {
+                        const u32x2 x = __builtin_amdgcn_raw_buffer_load_b64(rsrc, have > 0 ? o : kOut, 0, 0);
+                        dots[r][0] = x[0], dots[r][1] = x[1];
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            dots[r][e] = sizeof(T) == 4 ? __builtin_amdgcn_raw_buffer_load_b32(rsrc, e < have ? o + 4 * e : kOut, 0, 0)
+                                                        : (uint32_t)__builtin_amdgcn_raw_buffer_load_b16(rsrc, e < have ? o + 2 * e : kOut, 0, 0);
+                    }
+                }
+            }
             f32x16 acc{};
             if (s0 <= t0)
 #pragma unroll
@@ -206,35 +255,39 @@ __global__ __launch_bounds__(kThreads) void mix_kernel(Mix p)
             const float hi = dec.hi[t], lo = dec.lo[t];
 #pragma unroll
             for (int r = 0; r < 16; r += 4) {
-                Pack<T, 4> v;
                 const int s = s0 + 2 * r + 4 * half;
                 const auto shi = *reinterpret_cast<const Pack<float, 4> *>(&dec.hi[s]), slo = *reinterpret_cast<const Pack<float, 4> *>(&dec.lo[s]);
+                float v[4];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const float w = exp2_fast((hi - shi.v[e]) + (lo - slo.v[e])) * p.p_scale;
-                    v.v[e] = from_f<T>(s + e <= t ? acc[r + e] * w : 0.f);
+                    const float w = ChunkDecays::pair<T>(hi, lo, shi.v[e], slo.v[e]) * p.p_scale;
+                    v[e] = s + e <= t ? acc[r + e] * w : 0.f;
                 }
-                *reinterpret_cast<Pack<T, 4> *>(lds_p + TV::at(t, s)) = v;
+                *reinterpret_cast<Pack<T, 4> *>(lds_p + TV::at(t, s)) = pack_four<T>(v[0], v[1], v[2], v[3]);
             }
-            __syncthreads();
+            lds_barrier();
+            if (DG && REV && threadIdx.x == 0) {
+                const int chunk = chunks - 1 - c;
+                const float own = chunk * kChunk < n ? p.decays.get<T>(at.seq, at.head, (long)chunk * kChunk) : 0.f;
+                p.passes[(((long)at.tile * p.B + at.seq) * p.H + at.head) * chunks + chunk] =
+                    dec.whole * exp_full(own) * ((lds_pass[0] + lds_pass[1]) + (lds_pass[2] + lds_pass[3]));
+            }
             // outputs: a lane has row t and 16 columns
-            const int x0 = wave / 2 * 32;
             f32x16 y{};
 #pragma unroll
             for (int k = 0; k < DK; k += M::K) y = M::product(M::template along<DK>(lds_s, x0, k), M::template along<DK>(lds_q, t0, k), y);
             const float first = dec.first[t];
 #pragma unroll
             for (int r = 0; r < 16; ++r) y[r] *= first;
-            const int tok = token(c, t);
-            if (p.dots) {
-                const T *d = tok < n ? p.dot.template at<T>(at.seq, at.head, tok) + col0 : nullptr;
+            if (DG) {
                 float sum = 0.f;
 #pragma unroll
-                for (int r = 0; r < 16; r += 4) {
-                    const int x = x0 + 2 * r + 4 * half, have = d ? cols - x : 0;
-                    const Pack<T, 4> v = have >= 4 ? loose_load<T, 4>(d + x) : load_pack<false, T, 4>(d + x, have);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) sum = fmaf(to_f(v.v[e]), y[r + e], sum);
+                for (int r = 0; r < 16; ++r) {
+                    const uint32_t(&d)[4] = dots[DG ? r / 4 : 0];
+                    const float v = sizeof(T) == 4 ? __uint_as_float(d[r % 4])
+                                    : WHOLE        ? __uint_as_float(r % 2 ? d[r % 4 / 2] & 0xFFFF0000u : d[r % 4 / 2] << 16)
+                                                   : __uint_as_float(d[r % 4] << 16);
+                    sum = fmaf(v, y[r], sum);
                 }
                 float other = sum;
                 swap_halves(sum, other);
@@ -243,17 +296,31 @@ __global__ __launch_bounds__(kThreads) void mix_kernel(Mix p)
             }
 #pragma unroll
             for (int k = 0; k < kChunk; k += M::K)
-                if (k < t0 + 32) y = M::product(M::template across<kCols>(lds_v, x0, k), M::template along<kCols>(lds_p, t0, k), y);
-            if (tok < p.L) {
-                OUT *to = (OUT *)p.out + at.seq * p.out_b + tok * p.out_l + (long)at.head * p.v.width + col0;
+                if (k < 32 || t0 == 32) y = M::product(M::template across<kCols>(lds_v, x0, k), M::template along<kCols>(lds_p, t0, k), y);
+            const auto rsrc = buffer_of(out + tok0 * o_l, chunk_bytes(o_l, p.L - tok0));
 #pragma unroll
-                for (int r = 0; r < 16; r += 4) {
-                    const int x = x0 + 2 * r + 4 * half, have = min(4, cols - x);
-                    Pack<OUT, 4> v;
+            for (int r = 0; r < 16; ++r) y[r] = real ? y[r] : 0.f;
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) v.v[e] = from_f<OUT>(tok < n ? y[r + e] : 0.f);
-                    if (have == 4) loose_store<OUT, 4>(to + x, v);
-                    else if (have > 0) store_pack<false, OUT, 4>(to + x, v, have);
+            for (int r = 0; r < 4; ++r) {
+                const int have = cols - (x0 + 8 * r + 4 * half);
+                const uint32_t o = o_first + 8 * r * osize;
+                const auto four = pack_four<T>(y[4 * r], y[4 * r + 1], y[4 * r + 2], y[4 * r + 3]);
+                if (sizeof(T) == 4 || p.out_f32) {
+                    if (WHOLE) {
+                        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, pack_four<float>(y[4 * r], y[4 * r + 1], y[4 * r + 2], y[4 * r + 3])), rsrc,
+                                                               have > 0 ? o : kOut, 0, 0);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(y[4 * r + e]), rsrc, e < have ? o + 4 * e : kOut, 0, 0);
+                    }
+                } else if constexpr (sizeof(T) == 2) {
+                    if (WHOLE) {
+                        __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, four), rsrc, have > 0 ? o : kOut, 0, 0);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(uint16_t, four.v[e]), rsrc, e < have ? o + 2 * e : kOut, 0, 0);
+                    }
                 }
             }
         }
@@ -268,28 +335,29 @@ __global__ __launch_bounds__(kThreads) void mix_kernel(Mix p)
             constexpr int E = M::K / 2;
             float w[E];
 #pragma unroll
-            for (int e = 0; e < E; e += 4) *reinterpret_cast<Pack<float, 4> *>(w + e) = *reinterpret_cast<const Pack<float, 4> *>(&dec.last[k + half * E + e]);
-            typename M::Frag a[M::PARTS];
-            M::weighted(M::template across<DK>(lds_k, s_row, k), w, a);
+            for (int e = 0; e < E; e += 4) {
+                const auto four = *reinterpret_cast<const Pack<float, 4> *>(&dec.last[k + half * E + e]);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) w[e + i] = four.v[i];
+            }
+            typename M::Frag a[PARTS];
+            M::template weighted<PARTS>(M::template across<DK>(lds_k, s_row, k), w, a);
 #pragma unroll
             for (int i = 0; i < SD; ++i) {
                 const auto b = M::template across<kCols>(lds_v, s_col(i), k);
 #pragma unroll
-                for (int e = M::PARTS; e-- > 0;) state[i] = M::product(a[e], b, state[i]);
+                for (int e = PARTS; e-- > 0;) state[i] = M::product(a[e], b, state[i]);
             }
         }
-        if (STATES && threadIdx.x < 64) {
-            const double all = (double)dec.hi[63] + (double)dec.lo[63];
-            segment_decay += all;
-        }
-        __syncthreads();
-        if (!STATES && p.dots && threadIdx.x < kChunk) {
+        if (!OUT && threadIdx.x < 64) segment_decay += (double)dec.hi[63] + (double)dec.lo[63];
+        lds_barrier();
+        if (DG && threadIdx.x < kChunk) {
             const int t = token(c, threadIdx.x);
             if (t < p.L) p.dots[(((long)at.tile * p.B + at.seq) * p.H + at.head) * p.L + t] = lds_dot[0][threadIdx.x] + lds_dot[1][threadIdx.x];
         }
     }
 
-    if (STATES) {
+    if (!OUT) {
         float *to = p.starts + ((((long)at.segment + 1) * p.B + at.seq) * p.H + at.head) * p.s_head;
 #pragma unroll
         for (int i = 0; i < SD; ++i)
@@ -342,7 +410,7 @@ struct Pairs {
     float *out;
 };
 
-template <class T, int DK, int DV>
+template <class T, int DK, int DV, bool WHOLE>
 __global__ __launch_bounds__(kThreads) void pairs_kernel(Pairs p)
 {
     typedef Mma<T> M;
@@ -356,42 +424,40 @@ __global__ __launch_bounds__(kThreads) void pairs_kernel(Pairs p)
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), row = lane % 32, half = lane / 32;
     const int n = p.lengths ? max(0, min(p.L, p.lengths[seq])) : p.L, first = chunk * kChunk;
     float *out = p.out + ((long)seq * p.H + head) * p.L + first;
-    auto rows = [&](const Rows &s) {
-        return [&s, seq, head, n, first](int r) { return first + r < n ? s.template at<T>(seq, head, first + r) : nullptr; };
+    Fetch<T, DK, WHOLE> fq, fk;
+    Fetch<T, DV, WHOLE> fv, fo;
+    auto load = [&](auto &f, const Rows &r) {
+        f.init(r.width, r.l * sizeof(T), false);
+        f.load(r.template at<T>(seq, head) + first * r.l, r.l * sizeof(T), n - first);
     };
+    auto store = [&](const auto &f, const Rows &r, char *to) { f.store(to, r.template at<T>(seq, head) + first * r.l); };
+    load(fq, p.q);
+    load(fk, p.k);
+    load(fo, p.dy);
+    load(fv, p.v);
     const int t0 = wave % 2 * 32, s0 = wave / 2 * 32, t = t0 + row;
     f32x16 acc{}, acc2{};
-    {
-        Fetch<T, DK> f;
-        f.load(rows(p.q), p.q.width);
-        f.store(lds_a);
-        f.load(rows(p.k), p.k.width);
-        f.store(lds_b);
-    }
     if (wave == 0) dec.set(first + lane < n ? p.decays.get<T>(seq, head, first + lane) : 0.f, 1.f, 1.f);
-    __syncthreads();
+    store(fq, p.q, lds_a);
+    store(fk, p.k, lds_b);
+    lds_barrier();
     if (s0 <= t0)
 #pragma unroll
         for (int k = 0; k < DK; k += M::K) acc = M::product(M::template along<DK>(lds_b, s0, k), M::template along<DK>(lds_a, t0, k), acc);
-    __syncthreads();
-    {
-        Fetch<T, DV> f;
-        f.load(rows(p.dy), p.dy.width);
-        f.store(lds_a);
-        f.load(rows(p.v), p.v.width);
-        f.store(lds_b);
-    }
-    __syncthreads();
+    lds_barrier();
+    store(fo, p.dy, lds_a);
+    store(fv, p.v, lds_b);
+    lds_barrier();
     if (s0 <= t0)
 #pragma unroll
         for (int k = 0; k < DV; k += M::K) acc2 = M::product(M::template along<DV>(lds_b, s0, k), M::template along<DV>(lds_a, t0, k), acc2);
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
         const int s = s0 + 8 * (r / 4) + 4 * half + r % 4;
-        const float d = exp2_fast((dec.hi[t] - dec.hi[s]) + (dec.lo[t] - dec.lo[s]));
+        const float d = ChunkDecays::pair<float>(dec.hi[t], dec.lo[t], dec.hi[s], dec.lo[s]);
         w[t][s] = s < t ? p.scale * acc[r] * acc2[r] * d : 0.f;
     }
-    __syncthreads();
+    lds_barrier();
     // four threads to a token: half of its row, half of its column
     const int token = threadIdx.x % 64, part = threadIdx.x / 64;
     float sum = 0.f;
@@ -400,7 +466,7 @@ __global__ __launch_bounds__(kThreads) void pairs_kernel(Pairs p)
         sum += part < 2 ? w[token][o] : -w[o][token];
     }
     parts[threadIdx.x] = sum;
-    __syncthreads();
+    lds_barrier();
     if (threadIdx.x < 64 && first + token < p.L) out[token] = (parts[token] + parts[64 + token]) + (parts[128 + token] + parts[192 + token]);
 }
 
@@ -512,11 +578,11 @@ __global__ __launch_bounds__(256) void attention_step_kernel(StepParams p)
 int chunks_of(int L) { return (L + kChunk - 1) / kChunk; }
 int tiles_of(int width) { return (width + kCols - 1) / kCols; }
 
-// Segments of a walk: as many as fill the card with two workgroups to a unit, of 4 chunks at least.
+// Segments of a walk: as many as fill the card with two workgroups to a unit, where there is not one to each anyway.
 void segments_of(int B, int L, int H, int width, int &segments, int &per)
 {
     const long have = (long)B * H * tiles_of(width), chunks = std::max(1, chunks_of(L));
-    const long want = std::max(1l, std::min(512 / std::max(1l, have), chunks / 4));
+    const long want = have >= 256 ? 1 : std::max(1l, std::min(512 / std::max(1l, have), chunks));
     per = (int)((chunks + want - 1) / want);
     segments = (int)((chunks + per - 1) / per);
 }
@@ -564,35 +630,52 @@ Layout layout_of(const ucd_linear_attention_t &d, int dir)
     return l;
 }
 
-template <class T, class OUT, int DK, bool REV>
-hipError_t run_mix(Mix &p, int keep, hipStream_t s)
+// Rows that Fetch can read by whole pieces
+template <class T>
+bool whole_rows(const Rows &r)
 {
-    p.tiles = tiles_of(p.v.width);
+    constexpr int PER = 16 / sizeof(T), WORD = 4 / sizeof(T);
+    return r.width % PER == 0 && r.l % WORD == 0 && r.b % WORD == 0 && ((uintptr_t)r.p & 3u) == 0;
+}
+
+template <class T, int DK, bool REV, bool WHOLE>
+hipError_t run_mix(const Mix &p, hipStream_t s)
+{
     const unsigned groups = (unsigned)((long)p.B * p.H * p.tiles);
     if (p.segments > 1) {
-        mix_kernel<T, OUT, DK, REV, true, KEEP_NONE><<<groups * (p.segments - 1), kThreads, 0, s>>>(p);
-        hipError_t e = hipGetLastError();
+        mix_kernel<T, DK, REV, STATES, WHOLE><<<groups * (p.segments - 1), kThreads, 0, s>>>(p);
+        const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
-        const int size = (int)p.s_head;
-        join_states_kernel<<<dim3((unsigned)std::min(64, (size + 255) / 256), (unsigned)std::min(65535l, (long)p.B * p.H)), 256, 0, s>>>(p, size);
-        if ((e = hipGetLastError()) != hipSuccess) return e;
-    } else if (p.starts) {      // Forward keeps the state that it begins with
+    }
+    if (p.starts) {      // also of one segment, where Forward keeps the state that it begins with
         const int size = (int)p.s_head;
         join_states_kernel<<<dim3((unsigned)std::min(64, (size + 255) / 256), (unsigned)std::min(65535l, (long)p.B * p.H)), 256, 0, s>>>(p, size);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
-    const unsigned grid = groups * p.segments;
-    if (keep == KEEP_NONE) mix_kernel<T, OUT, DK, REV, false, KEEP_NONE><<<grid, kThreads, 0, s>>>(p);
-    else if (!REV) mix_kernel<T, OUT, DK, REV, false, KEEP_WRITE><<<grid, kThreads, 0, s>>>(p);
-    else mix_kernel<T, OUT, DK, REV, false, KEEP_READ><<<grid, kThreads, 0, s>>>(p);
+    if (p.dots) mix_kernel<T, DK, REV, DECAYS, WHOLE><<<groups * p.segments, kThreads, 0, s>>>(p);
+    else mix_kernel<T, DK, REV, OUTPUTS, WHOLE><<<groups * p.segments, kThreads, 0, s>>>(p);
     return hipGetLastError();
 }
 
-template <class T, class OUT, bool REV>
-hipError_t run_mix(Mix &p, int keep, hipStream_t s)
+template <class T, bool REV>
+hipError_t run_mix(Mix &p, hipStream_t s)
 {
-    return p.q.width > 64 ? run_mix<T, OUT, 128, REV>(p, keep, s) : run_mix<T, OUT, 64, REV>(p, keep, s);
+    p.tiles = tiles_of(p.v.width);
+    const Rows out{p.out, p.out_b, p.out_l, 1, p.v.width};
+    const bool whole = whole_rows<T>(p.q) && whole_rows<T>(p.k) && whole_rows<T>(p.v) && whole_rows<T>(out) && (!p.dots || whole_rows<T>(p.dot));
+    if (whole) return p.q.width > 64 ? run_mix<T, 128, REV, true>(p, s) : run_mix<T, 64, REV, true>(p, s);
+    return p.q.width > 64 ? run_mix<T, 128, REV, false>(p, s) : run_mix<T, 64, REV, false>(p, s);
+}
+
+template <class T, bool WHOLE>
+hipError_t run_pairs(const Pairs &r, unsigned grid, hipStream_t s)
+{
+    if (r.k.width > 64 && r.v.width > 64) pairs_kernel<T, 128, 128, WHOLE><<<grid, kThreads, 0, s>>>(r);
+    else if (r.k.width > 64) pairs_kernel<T, 128, 64, WHOLE><<<grid, kThreads, 0, s>>>(r);
+    else if (r.v.width > 64) pairs_kernel<T, 64, 128, WHOLE><<<grid, kThreads, 0, s>>>(r);
+    else pairs_kernel<T, 64, 64, WHOLE><<<grid, kThreads, 0, s>>>(r);
+    return hipGetLastError();
 }
 
 Mix mix_base(const ucd_linear_attention_t &d, const ucd_linear_attention_in_t &in)
@@ -632,7 +715,7 @@ hipError_t fwd(const ucd_linear_attention_t &d, const ucd_linear_attention_in_t 
     p.per_segment = l.per;
     p.starts = saved ? saved : l.segments > 1 ? (float *)(ws + l.starts) : nullptr;
     p.segment_decay = (float *)(ws + l.decay);
-    return run_mix<T, T, false>(p, KEEP_NONE, s);
+    return run_mix<T, false>(p, s);
 }
 
 template <class T>
@@ -663,7 +746,7 @@ hipError_t bwd(const ucd_linear_attention_t &d, const ucd_linear_attention_in_t 
     p.per_segment = l.per;
     p.starts = l.segments > 1 ? (float *)(ws + l.starts) : nullptr;
     p.segment_decay = (float *)(ws + l.decay);
-    if ((e = run_mix<T, T, true>(p, KEEP_NONE, s)) != hipSuccess) return e;
+    if ((e = run_mix<T, true>(p, s)) != hipSuccess) return e;
     // dq: the states again, transposed
     Mix a = mix_base(d, in);
     a.q = o;
@@ -683,17 +766,12 @@ hipError_t bwd(const ucd_linear_attention_t &d, const ucd_linear_attention_in_t 
     a.chunk_states = ws + l.keep;
     a.passes = (float *)(ws + l.c);
     auto heads = [&](Mix &m, void *out, long o_b, long o_l, bool rev) {
-        const int keep = !decays ? KEEP_NONE : rev ? KEEP_READ : KEEP_WRITE;
-        if (shared == 1) {
-            m.out = out;
-            m.out_b = o_b;
-            m.out_l = o_l;
-            return rev ? run_mix<T, T, true>(m, keep, s) : run_mix<T, T, false>(m, keep, s);
-        }
-        m.out = ws + l.heads;
-        m.out_l = (long)d.H * d.Dk;
-        m.out_b = m.out_l * d.L;
-        const hipError_t e = rev ? run_mix<T, float, true>(m, keep, s) : run_mix<T, float, false>(m, keep, s);
+        m.out_f32 = shared > 1;
+        m.out = shared > 1 ? ws + l.heads : out;
+        m.out_l = shared > 1 ? (long)d.H * d.Dk : o_l;
+        m.out_b = shared > 1 ? m.out_l * d.L : o_b;
+        const hipError_t e = rev ? run_mix<T, true>(m, s) : run_mix<T, false>(m, s);
+        if (shared == 1) return e;
         const long tokens = (long)d.B * d.L;
         if (e != hipSuccess || tokens == 0) return e;
         const unsigned grid = (unsigned)std::min((tokens * d.Hk * d.Dk + 255) / 256, 1l << 16);
@@ -715,11 +793,8 @@ hipError_t bwd(const ucd_linear_attention_t &d, const ucd_linear_attention_in_t 
     if (!decays || d.L == 0) return hipSuccess;
     Pairs r{q, k, v, o, d.scale, a.decays, in.lengths, d.B, d.L, d.H, (float *)(ws + l.pairs)};
     const unsigned grid = (unsigned)((long)d.B * d.H * chunks_of(d.L));
-    if (d.Dk > 64 && d.Dv > 64) pairs_kernel<T, 128, 128><<<grid, kThreads, 0, s>>>(r);
-    else if (d.Dk > 64) pairs_kernel<T, 128, 64><<<grid, kThreads, 0, s>>>(r);
-    else if (d.Dv > 64) pairs_kernel<T, 64, 128><<<grid, kThreads, 0, s>>>(r);
-    else pairs_kernel<T, 64, 64><<<grid, kThreads, 0, s>>>(r);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
+    const bool whole = whole_rows<T>(q) && whole_rows<T>(k) && whole_rows<T>(v) && whole_rows<T>(o);
+    if ((e = whole ? run_pairs<T, true>(r, grid, s) : run_pairs<T, false>(r, grid, s)) != hipSuccess) return e;
     decay_gradient_kernel<T><<<std::min(grid, 1u << 20), 64, 0, s>>>(r.out, a.dots, b.dots, a.passes, tiles_of(d.Dk), d.B, d.L, d.H, in.lengths, (T *)grad.g,
                                                                     d.g_b, d.g_l);
     return hipGetLastError();

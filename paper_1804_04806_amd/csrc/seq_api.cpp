@@ -138,8 +138,11 @@ bool attention_ok(const ucd_linear_attention_t *in, ucd_linear_attention_t &d)
     const int64_t qk = (int64_t)d.Hk * d.Dk, v = (int64_t)d.H * d.Dv;
     if ((double)d.B * (d.L + 1.) * std::max(std::max(qk, v), (int64_t)d.H * d.Dk) > (double)kMaxElements) return false;
     if ((double)d.B * d.H * d.Dk * d.Dv > (double)kMaxElements) return false;
-    return fill_strides(d.q_b, d.q_l, d.B, d.L, qk) && fill_strides(d.k_b, d.k_l, d.B, d.L, qk) && fill_strides(d.v_b, d.v_l, d.B, d.L, v) &&
-           fill_strides(d.g_b, d.g_l, d.B, d.L, d.H) && fill_strides(d.y_b, d.y_l, d.B, d.L, v);
+    if (!fill_strides(d.q_b, d.q_l, d.B, d.L, qk) || !fill_strides(d.k_b, d.k_l, d.B, d.L, qk) || !fill_strides(d.v_b, d.v_l, d.B, d.L, v) ||
+        !fill_strides(d.g_b, d.g_l, d.B, d.L, d.H) || !fill_strides(d.y_b, d.y_l, d.B, d.L, v))
+        return false;
+    constexpr int64_t kMost = int64_t(1) << 23;      // 64 tokens in 32-bit offsets of bytes
+    return d.q_l <= kMost && d.k_l <= kMost && d.v_l <= kMost && d.y_l <= kMost;
 }
 
 int attention_inputs(const ucd_linear_attention_t &d, const ucd_linear_attention_in_t *in)
