@@ -167,8 +167,8 @@ int ucd_scan_step(const ucd_scan_t *scan, const ucd_scan_in_t *in, float *state,
  * exp of which is as good as 0: -infinity forgets what was before the token.  Tokens are taken 64 at a
  * time, from a sequence's first on: a value that is not finite may reach all 64 outputs and gradients
  * around it, beside those of the formulas.  1 <= Dk, Dv <= 128 (wider heads of v are more heads of v to
- * one of q and k); Hk divides H; B, L >= 0.  Rows of q, k, v and y, and a token's stride of theirs,
- * are at most 2^23 elements. */
+ * one of q and k); Hk divides H; B, L >= 0.  Rows of q, k, v, g and y, and a token's stride of
+ * theirs, are at most 2^23 elements. */
 typedef struct {
     int32_t B, L, H, Hk, Dk, Dv, dtype;
     int32_t n_slots;

@@ -7,26 +7,26 @@ namespace ucd {
 namespace attention {
 using namespace seq;
 
-constexpr int kChunk = 64, kThreads = 256, kCols = 64;      // tokens of a chunk; columns of a state that a workgroup has
+constexpr int kChunk = 64;      // tokens of a chunk
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 // exp(-80) is as good as 0, and sums of 64 of them and their differences stay finite: what is below counts as -80.  A NaN stays one.
 constexpr float kLeast = -80.f;
 
-// A tile of rows of COLS elements in LDS, in cells of 16 bytes.  Cell c of row r stands at c ^ swizzle(r): 16 lanes that read a cell each of 16 rows meet
-// no bank twice, and neither do transposing reads of 4 rows by 4 cells (bfloat16).
+// A tile of rows of COLS elements in LDS.  Rows are 16 bytes longer than their elements and stand, 16 at a time, in an order of their own: 16 lanes that
+// read 16 bytes each of 16 rows meet no bank twice (rows are an odd number of 16 bytes apart), and neither do transposing reads of 4 neighbouring rows by 64
+// bytes (those rows are 64 bytes apart modulo 256).  An address is a lane's own plus a constant.
 template <class T, int COLS>
 struct TileLds {
-    static constexpr int PER = 16 / sizeof(T), CELLS = COLS / PER, BYTES = kChunk * COLS * (int)sizeof(T);
-    __device__ static __forceinline__ int swizzle(int r)
-    {
-        if (CELLS >= 16) return sizeof(T) == 2 ? (r & 3) << 2 | (r >> 2 & 3) : r & 15;
-        return (r >> 1 & 1) << 2 | (r >> 2 & 3);
-    }
-    __device__ static __forceinline__ int cell(int r, int c) { return (r * CELLS + (c ^ swizzle(r))) * 16; }
-    __device__ static __forceinline__ int at(int r, int col) { return cell(r, col / PER) + col % PER * (int)sizeof(T); }
+    static constexpr int PER = 16 / sizeof(T), CELLS = COLS / PER, ROW = COLS * (int)sizeof(T) + 16, BYTES = kChunk * ROW;
+    static constexpr int STEP = ROW / 16 % 16;                  // of rows, in 16 bytes modulo 256
+    static_assert(STEP == 1 || STEP == 9, "its own inverse modulo 16");
+    __device__ static __forceinline__ int place(int r) { return (r & ~15) | ((STEP * ((r & 3) << 2 | (r >> 2 & 3))) & 15); }
+    __device__ static __forceinline__ int cell(int r, int c) { return place(r) * ROW + c * 16; }
+    __device__ static __forceinline__ int at(int r, int col) { return place(r) * ROW + col * (int)sizeof(T); }
 };
 
 // Operands of v_mfma_f32_32x32: K reduction steps of a fragment; lanes 0-31 have the first half of them, lanes 32-63 the second, row lane % 32.
@@ -57,24 +57,62 @@ template <> struct Mma<bf16_t> {
     __device__ static __forceinline__ Frag along(const char *tile, int first, int k0)
     {
         const int lane = threadIdx.x % 64;
-        return *reinterpret_cast<const Frag *>(tile + TileLds<bf16_t, COLS>::cell(first + lane % 32, k0 / 8 + lane / 32));
+        return *reinterpret_cast<const Frag *>(tile + TileLds<bf16_t, COLS>::cell(lane % 32, lane / 32) + first * TileLds<bf16_t, COLS>::ROW + k0 * 2);
     }
+    // sums i, i + 1, ... of a tile of them as an operand: lanes 0-31 have rows 0 .. 3 and 8 .. 11 of 16, lanes 32-63 rows 4 .. 7 and 12 .. 15.  What is
+    // multiplied with them is stored in that order (SUMS_ORDER): 8, 8, 8 and 8 bytes of 32 as 0, 2, 1, 3
+    __device__ static __forceinline__ Frag from_sums(const f32x16 &s, int i)
+    {
+        struct Words {
+            uint32_t w[4];
+        };
+        return __builtin_bit_cast(Frag, Words{{pack_bf16(s[i], s[i + 1]), pack_bf16(s[i + 2], s[i + 3]), pack_bf16(s[i + 4], s[i + 5]), pack_bf16(s[i + 6], s[i + 7])}});
+    }
+    static constexpr int SUMS = 8;      // of an operand
+    static constexpr bool SUMS_ORDER = true;
     // columns first .. first + 31, reduction over rows from k0 on: 16 lanes fetch 4 rows of 16 columns each and get 4 rows of a column each
     template <int COLS>
     __device__ static __forceinline__ Frag across(const char *tile, int first, int k0)
     {
-        const int lane = threadIdx.x % 64, col = first + lane / 16 % 2 * 16 + lane % 4 * 4, k = k0 + lane / 32 * 8 + lane % 16 / 4;
+        typedef TileLds<bf16_t, COLS> Tile;
+        const int lane = threadIdx.x % 64, col = lane / 16 % 2 * 16 + lane % 4 * 4, k = lane / 32 * 8 + lane % 16 / 4;
+        const char *p = tile + k0 * Tile::ROW + first * 2;
         typedef __attribute__((address_space(3))) s16x4 lds_t;
         struct Both {
             s16x4 lo, hi;
         } v;
-        v.lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_t *)(tile + TileLds<bf16_t, COLS>::at(k, col)));
-        v.hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_t *)(tile + TileLds<bf16_t, COLS>::at(k + 4, col)));
+        v.lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_t *)(p + Tile::at(k, col)));
+        v.hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_t *)(p + Tile::at(k + 4, col)));
         return __builtin_bit_cast(Frag, v);
     }
     __device__ static __forceinline__ f32x16 product(const Frag &a, const Frag &b, f32x16 c)
     {
         return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+    }
+    // 16 rows by 32 steps, and their product: row lane % 16, steps 8 (lane / 16) + 0 .. 7
+    static constexpr int K16 = 32;
+    template <int COLS>
+    __device__ static __forceinline__ Frag along16(const char *tile, int first, int k0)
+    {
+        const int lane = threadIdx.x % 64;
+        return *reinterpret_cast<const Frag *>(tile + TileLds<bf16_t, COLS>::cell(lane % 16, lane / 16) + first * TileLds<bf16_t, COLS>::ROW + k0 * 2);
+    }
+    // those steps of a tile in its own order that along16 gives of one in the sums'
+    template <int COLS>
+    __device__ static __forceinline__ Frag along16_other(const char *tile, int first, int k0)
+    {
+        const int lane = threadIdx.x % 64, g = lane / 16;
+        const char *p = tile + TileLds<bf16_t, COLS>::cell(lane % 16, g / 2 * 2) + g % 2 * 8 + first * TileLds<bf16_t, COLS>::ROW + k0 * 2;
+        struct Both {
+            s16x4 lo, hi;
+        } v;
+        v.lo = *reinterpret_cast<const s16x4 *>(p);
+        v.hi = *reinterpret_cast<const s16x4 *>(p + 16);
+        return __builtin_bit_cast(Frag, v);
+    }
+    __device__ static __forceinline__ f32x4 product16(const Frag &a, const Frag &b, f32x4 c)
+    {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
     }
     // w a in PARTS bfloat16 parts, the largest first: three are as exact as the sums' 32 bits, two leave 2^-17
     template <int PARTS>
@@ -110,21 +148,41 @@ template <> struct Mma<float> {
     __device__ static __forceinline__ Frag along(const char *tile, int first, int k0)
     {
         const int lane = threadIdx.x % 64;
-        return *reinterpret_cast<const Frag *>(tile + TileLds<float, COLS>::cell(first + lane % 32, k0 / 4 + lane / 32));
+        return *reinterpret_cast<const Frag *>(tile + TileLds<float, COLS>::cell(lane % 32, lane / 32) + first * TileLds<float, COLS>::ROW + k0 * 4);
     }
+    template <int COLS>
+    __device__ static __forceinline__ Frag along16_other(const char *tile, int first, int k0) { return along16<COLS>(tile, first, k0); }
+    __device__ static __forceinline__ Frag from_sums(const f32x16 &s, int i) { return Frag{{s[i], s[i + 1], s[i + 2], s[i + 3]}}; }
+    static constexpr int SUMS = 4;
+    static constexpr bool SUMS_ORDER = false;
     template <int COLS>
     __device__ static __forceinline__ Frag across(const char *tile, int first, int k0)
     {
         const int lane = threadIdx.x % 64;
         Frag v;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v.v[i] = *reinterpret_cast<const float *>(tile + TileLds<float, COLS>::at(k0 + lane / 32 * 4 + i, first + lane % 32));
+        for (int i = 0; i < 4; ++i)      // row 4 (lane / 32) + i of 8, from k0, of which there may be an odd number in 16
+            v.v[i] = *reinterpret_cast<const float *>(tile + TileLds<float, COLS>::at(k0 % 16 + lane / 32 * 4 + i, lane % 32) + k0 / 16 * 16 * TileLds<float, COLS>::ROW +
+                                                      first * 4);
         return v;
     }
     __device__ static __forceinline__ f32x16 product(const Frag &a, const Frag &b, f32x16 c)
     {
 #pragma unroll
         for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a.v[i], b.v[i], c, 0, 0, 0);
+        return c;
+    }
+    static constexpr int K16 = 16;
+    template <int COLS>
+    __device__ static __forceinline__ Frag along16(const char *tile, int first, int k0)
+    {
+        const int lane = threadIdx.x % 64;
+        return *reinterpret_cast<const Frag *>(tile + TileLds<float, COLS>::cell(lane % 16, lane / 16) + first * TileLds<float, COLS>::ROW + k0 * 4);
+    }
+    __device__ static __forceinline__ f32x4 product16(const Frag &a, const Frag &b, f32x4 c)
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a.v[i], b.v[i], c, 0, 0, 0);
         return c;
     }
     template <int PARTS>
@@ -134,6 +192,14 @@ template <> struct Mma<float> {
         for (int i = 0; i < 4; ++i) out[0].v[i] = a.v[i] * w[i];
     }
 };
+
+// The place of a workgroup among all: workgroups are dealt to the 8 XCDs in turn, and each XCD takes neighbours here.  Heads are neighbours, whose rows lie side
+// by side in a token: an XCD that had every eighth head would use two of its L2's 16 channels.
+__device__ __forceinline__ unsigned xcd_place()
+{
+    const unsigned n = gridDim.x, xcd = blockIdx.x % 8;
+    return xcd * (n / 8) + min(xcd, n % 8) + blockIdx.x / 8;
+}
 
 // Reads behind a buffer's end give 0.
 constexpr uint32_t kOut = 0x80000000u;
@@ -152,13 +218,13 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_of(const void *p, uint3
 // What is there of a chunk: bytes of its tokens.
 __device__ __forceinline__ uint32_t chunk_bytes(long stride, int tokens) { return (uint32_t)(max(0, min(kChunk, tokens)) * stride); }
 
-// A tile's pieces of 16 bytes on their way from memory: thread i has cells i, i + 256, ...  They are words that nothing looks at before they are stored
+// A tile's pieces of 16 bytes on their way from memory: thread i has cells i, i + THREADS, ...  They are words that nothing looks at before they are stored
 // (elements of 16 bits would be taken apart, and waited for, right behind the load), and are read through a buffer that ends behind the last token that
 // there is: no branches.  WHOLE: rows of whole pieces at multiples of 4 bytes.  Otherwise word by word: those that begin before the row's end, from the
 // multiple of 4 bytes at or below the piece's begin; what does not belong to the piece goes when it is stored.
-template <class T, int COLS, bool WHOLE>
+template <class T, int COLS, bool WHOLE, int THREADS>
 struct Fetch {
-    static constexpr int PER = 16 / sizeof(T), CELLS = COLS / PER, N = kChunk * CELLS / kThreads, ROWS = kThreads / CELLS;
+    static constexpr int PER = 16 / sizeof(T), CELLS = COLS / PER, N = kChunk * CELLS / THREADS, ROWS = THREADS / CELLS;
     static constexpr int WORDS = WHOLE || sizeof(T) == 4 ? 4 : 5;
     uint32_t v[N][WORDS];
     uint32_t first, step;      // offsets: of the thread's first piece, from piece to piece
@@ -196,6 +262,7 @@ struct Fetch {
             }
         }
     }
+    template <bool SUMS_ORDER = false>
     __device__ __forceinline__ void store(char *tile, const void *base) const
     {
         const int r = threadIdx.x / CELLS, c = threadIdx.x % CELLS;
@@ -213,7 +280,14 @@ struct Fetch {
                     x[w] = have >= 2 * w + 2 ? y : have == 2 * w + 1 ? y & 0xFFFFu : 0;
                 }
             }
-            *reinterpret_cast<u32x4 *>(tile + TileLds<T, COLS>::cell(r + i * ROWS, c)) = x;
+            char *to = tile + TileLds<T, COLS>::cell(ROWS % 16 == 0 ? r : r + i * ROWS, SUMS_ORDER ? c & ~1 : c) + (ROWS % 16 == 0 ? i * ROWS * TileLds<T, COLS>::ROW : 0);
+            if (SUMS_ORDER) {
+                to += c % 2 * 8;
+                *reinterpret_cast<u32x2 *>(to) = u32x2{x[0], x[1]};
+                *reinterpret_cast<u32x2 *>(to + 16) = u32x2{x[2], x[3]};
+            } else {
+                *reinterpret_cast<u32x4 *>(to) = x;
+            }
         }
     }
 };
@@ -223,16 +297,28 @@ struct Decays {
     const void *g;
     long g_b, g_l;
     const float *decay;
+    // the words of 64 tokens from t on, `tokens` of them there, one lane each, from the last to the first where reversed
     template <class T>
-    __device__ __forceinline__ T raw(int b, int h, long t) const { return g ? ((const T *)g)[b * g_b + t * g_l + h] : from_f<T>(0.f); }
-    template <class T>
-    __device__ __forceinline__ float get(int h, T raw) const
+    __device__ __forceinline__ uint32_t raw(int b, int h, long t, int tokens, bool reversed) const
     {
-        const float v = (decay ? decay[h] : 0.f) + to_f(raw);
+        const long l = g_l * (long)sizeof(T);
+        const auto rsrc = buffer_of((const T *)g + b * g_b + t * g_l + h, g ? chunk_bytes(l, tokens) : 0u);
+        const int lane = threadIdx.x % 64;
+        const uint32_t at = (uint32_t)((reversed ? kChunk - 1 - lane : lane) * l);
+        return sizeof(T) == 4 ? __builtin_amdgcn_raw_buffer_load_b32(rsrc, at, 0, 0) : (uint32_t)__builtin_amdgcn_raw_buffer_load_b16(rsrc, at, 0, 0);
+    }
+    template <class T>
+    __device__ __forceinline__ static float sum(float of_head, uint32_t raw)
+    {
+        const float v = of_head + (sizeof(T) == 4 ? __uint_as_float(raw) : __uint_as_float(raw << 16));
         return v < kLeast ? kLeast : v;
     }
     template <class T>
-    __device__ __forceinline__ float get(int b, int h, long t) const { return get<T>(h, raw<T>(b, h, t)); }
+    __device__ __forceinline__ float get(int b, int h, long t) const
+    {
+        const float v = (decay ? decay[h] : 0.f) + (g ? to_f(((const T *)g)[b * g_b + t * g_l + h]) : 0.f);
+        return v < kLeast ? kLeast : v;
+    }
 };
 
 // A chunk's decays from its rows' own: `hi` + `lo` sums over the rows up to each, in units of 2 (two floats: their differences are exact to 32 bits
@@ -276,6 +362,61 @@ struct ChunkDecays {
         return exp2_fast(sizeof(T) == 2 ? t_hi - s_hi : (t_hi - s_hi) + (t_lo - s_lo));
     }
 };
+
+// ---- a walk --------------------------------------------------------------------------------------------------------
+
+struct Rows {
+    const void *p;
+    long b, l;      // strides
+    int div;        // heads that share a row of it
+    int width;
+    template <class T>
+    __device__ __forceinline__ const T *at(int seq, int head) const { return (const T *)p + seq * b + (long)(head / div) * width; }
+};
+
+struct Mix {
+    Rows q, k, v, dot;           // dot: rows like the output's, multiplied with the part of the state at the chunk's start; may be none
+    void *out;
+    long out_b, out_l;
+    bool out_f32;                // parts of T = bfloat16, for the heads that share a row of it
+    float p_scale, first_scale, last_scale;
+    Decays decays;
+    const int32_t *lengths, *slots;
+    int B, L, H, n_slots, segments, per_segment;     // chunks of a segment
+    // states: of a slot and head rows (of q's width) and columns (of v's) apart
+    const float *state_in;
+    float *state_out;
+    long s_row, s_col, s_head;
+    float *starts;               // (segments, B, H, rows, columns) with the strides of state_in, or null
+    bool started;                // starts are there already, from a walk over the same states
+    float *segment_decay;        // (segments, B, H)
+    float *dots;                 // (column tiles, B, H, L), or null
+    void *chunk_states;          // states at the chunks' starts, by workgroup, chunk and thread
+    float *passes;               // (column tiles, B, H, chunks): c
+    int tiles;
+};
+
+// Starts of the segments from their own states.
+hipError_t join_states(const Mix &p, hipStream_t s);
+
+// A walk, forward or (REV) backward in time; `whole`: whole_rows of all.  Sets p.tiles.
+template <class T, bool REV>
+hipError_t run_mix(Mix &p, bool whole, hipStream_t s);
+
+inline int chunks_of(int L) { return (L + kChunk - 1) / kChunk; }
+inline int tiles_of(int width, int cols) { return (width + cols - 1) / cols; }
+
+// Columns of a state to a workgroup, 32 to a wave: all of them, so that pairs of tokens are computed once.  fp32 states of many rows have four waves also for
+// few columns (two are out of registers: 5 x 677 tokens of 6 heads of 72 by 41, Forward 87 us against 38).
+inline int cols_of(int rows, int cols, bool f32) { return cols > 64 || (f32 && rows > 64) ? 128 : 64; }
+
+// Rows that Fetch can read by whole pieces
+template <class T>
+bool whole_rows(const Rows &r)
+{
+    constexpr int PER = 16 / sizeof(T), WORD = 4 / sizeof(T);
+    return r.width % PER == 0 && r.l % WORD == 0 && r.b % WORD == 0 && ((uintptr_t)r.p & 3u) == 0;
+}
 
 }  // namespace attention
 }  // namespace ucd

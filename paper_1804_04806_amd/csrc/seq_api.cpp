@@ -142,7 +142,7 @@ bool attention_ok(const ucd_linear_attention_t *in, ucd_linear_attention_t &d)
         !fill_strides(d.g_b, d.g_l, d.B, d.L, d.H) || !fill_strides(d.y_b, d.y_l, d.B, d.L, v))
         return false;
     constexpr int64_t kMost = int64_t(1) << 23;      // 64 tokens in 32-bit offsets of bytes
-    return d.q_l <= kMost && d.k_l <= kMost && d.v_l <= kMost && d.y_l <= kMost;
+    return d.q_l <= kMost && d.k_l <= kMost && d.v_l <= kMost && d.g_l <= kMost && d.y_l <= kMost;
 }
 
 int attention_inputs(const ucd_linear_attention_t &d, const ucd_linear_attention_in_t *in)
