@@ -10,7 +10,7 @@
 #include "seq.h"
 
 namespace ucd {
-namespace {
+namespace gated {
 using namespace seq;
 using namespace product;
 
@@ -320,6 +320,12 @@ __global__ __launch_bounds__(TILE::THREADS) void product_kernel(Problem p, Matri
     tile.each([&](int m, int n, const Pack<float, 4> &v) { matrix_store<T>(o, (long)m0 + m, n0 + n, v); });
 }
 
+// dx's and the weights' products
+template <class T> using LargeAlong = Tile<T, 256, 256, 2, 4, true, false, true>;
+template <class T> using SmallAlong = Tile<T, 128, 128, 2, 2, true, false, true>;
+template <class T> using LargeAcross = Tile<T, 256, 256, 2, 4, false, false, false>;
+template <class T> using SmallAcross = Tile<T, 128, 128, 2, 2, false, false, false>;
+
 template <class T>
 __global__ __launch_bounds__(256) void product_join_kernel(const float *part, int splits, MatrixOut o, long rows, int cols)
 {
@@ -525,8 +531,8 @@ hipError_t fwd(const ucd_gated_projection_t &d, const void *x, const void *wg, c
     p.phases = l.phases;
     shape_into(p, l.fwd);
     float *part = p.splits > 1 ? (float *)(ws + l.part) : nullptr;
-    if (l.fwd.large) return forward<T, Tile<256, 256, 2, 4, true, true, true>>(p, o, part, s);
-    return forward<T, Tile<128, 128, 2, 2, true, true, true>>(p, o, part, s);
+    if (l.fwd.large) return forward<T, Tile<T, 256, 256, 2, 4, true, true, true>>(p, o, part, s);
+    return forward<T, Tile<T, 128, 128, 2, 2, true, true, true>>(p, o, part, s);
 }
 
 template <class T>
@@ -561,8 +567,8 @@ hipError_t bwd(const ucd_gated_projection_t &d, const void *x, const void *wg, c
     out.half = 1l << 40;
     out.cols = d.D;
     float *part = p.splits > 1 ? (float *)(ws + l.part) : nullptr;
-    e = l.dx.large ? multiply<T, Tile<256, 256, 2, 4, true, false, true>>(p, out, part, d.M, s)
-                   : multiply<T, Tile<128, 128, 2, 2, true, false, true>>(p, out, part, d.M, s);
+    e = l.dx.large ? multiply<T, LargeAlong<T>>(p, out, part, d.M, s)
+                   : multiply<T, SmallAlong<T>>(p, out, part, d.M, s);
     if (e != hipSuccess) return e;
     // [dWg; dWu] = dG^T x: both across
     p.m = og;
@@ -580,8 +586,8 @@ hipError_t bwd(const ucd_gated_projection_t &d, const void *x, const void *wg, c
     out.half = l.half;
     out.add = add;
     part = p.splits > 1 ? (float *)(ws + l.part) : nullptr;
-    return l.dw.large ? multiply<T, Tile<256, 256, 2, 4, false, false, false>>(p, out, part, 2l * l.half, s)
-                      : multiply<T, Tile<128, 128, 2, 2, false, false, false>>(p, out, part, 2l * l.half, s);
+    return l.dw.large ? multiply<T, LargeAcross<T>>(p, out, part, 2l * l.half, s)
+                      : multiply<T, SmallAcross<T>>(p, out, part, 2l * l.half, s);
 }
 
 GateOut gate_out(const ucd_gated_projection_t &d, void *y, float *saved)
@@ -589,7 +595,9 @@ GateOut gate_out(const ucd_gated_projection_t &d, void *y, float *saved)
     return GateOut{y, (long)d.y_m, saved, d.M, d.F, wide_of(d), d.act};
 }
 
-}  // namespace
+}  // namespace gated
+
+using namespace gated;
 
 size_t gated_projection_ws_bytes(const ucd_gated_projection_t &d, int dir)
 {

@@ -22,8 +22,7 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 constexpr int BK = 64;
-constexpr uint32_t kOut = 0xFFFFFFF0u;            // behind any buffer's end: reads as 0
-constexpr uint32_t kRecords = 0x80000000u;
+constexpr uint32_t kOut = 0x80000000u;            // behind any buffer's end: reads as 0
 
 // An operand.  along: `rows` rows of `k` elements.  across: `k` rows of `rows` elements.  Rows are `stride` elements apart, a multiple of 8 like the
 // length of a row, addresses are multiples of 16 bytes.  There may be two such matrices, p[0] and p[1]: along, the tile's first half of rows
@@ -43,37 +42,52 @@ struct Problem {
     int splits;           // of the steps of all phases
 };
 
+__device__ __forceinline__ uint64_t uniform(const void *p)
+{
+    const uint64_t u = (uint64_t)p;
+    return (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(u >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)u);
+}
+
+// One operand's way to LDS, step by step.  A lane's offsets stay; what moves from step to step is the buffer, which ends behind the last row that there is.
 template <int R, bool ALONG, bool PAIR, int THREADS>
 struct Stage {
     static constexpr int BYTES = R * BK * 2, LOADS = BYTES / (THREADS * 16);
     static_assert(LOADS * THREADS * 16 == BYTES, "whole loads");
+    static constexpr int CELLS = ALONG ? BK / 8 : R / 8, ROWS = THREADS / CELLS;      // cells of a row; rows of a load
+    static_assert(ROWS % 16 == 0 || (!ALONG && ROWS % 4 == 0), "all of a lane's cells have one place in their rows");
+    uint32_t offset[LOADS];
+    int column;                // of the lane's cells, in elements
 
-    // Moves step k0 of a plane, rows (columns) from `origin` on, to `lds`.
-    __device__ static __forceinline__ void move(const Operand &o, int plane, int k0, int origin, char *lds)
+    __device__ __forceinline__ void init(const Operand &o, int origin)
     {
-        const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+        const int r = threadIdx.x / CELLS, c = (threadIdx.x % CELLS) ^ (ALONG ? r / 2 % 8 : r % 4 * 4);
+        column = 8 * c;
+        const bool there = ALONG || origin + column < o.rows;
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
-            const int first = (i * (THREADS / 64) + wave) * 64;        // cell
-            const int cell = first + lane;
-            uint32_t offset;
-            const bf16_t *base;
-            if (ALONG) {
-                const int r = cell / 8, c = (cell % 8) ^ (r / 2 % 8);
-                const bool second = PAIR && first / 8 >= R / 2;
-                const int row = PAIR ? r % (R / 2) : r;
-                base = o.p[second ? 1 : 0] + plane * o.plane + origin * o.stride + k0;
-                offset = origin + row < o.rows && k0 + 8 * c < o.k ? (uint32_t)row * (uint32_t)o.stride * 2u + 16u * c : kOut;
-            } else {
-                constexpr int CELLS = R / 8;
-                const int r = cell / CELLS, c = (cell % CELLS) ^ (r % 4 * 4);
-                const bool second = PAIR && k0 >= o.half;
-                const int k = k0 - (second ? o.half : 0);
-                base = o.p[second ? 1 : 0] + plane * o.plane + k * o.stride + origin;
-                offset = k + r < o.k && origin + 8 * c < o.rows ? (uint32_t)r * (uint32_t)o.stride * 2u + 16u * c : kOut;
-            }
-            const auto rsrc = __builtin_amdgcn_make_buffer_rsrc((void *)base, 0, kRecords, 0x00020000);
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void *)(lds + first * 16), 16, offset, 0, 0, 0);
+            // along, a pair's second matrix has a buffer of its own
+            const int row = ALONG && PAIR ? (r + i * ROWS) % (R / 2) : r + i * ROWS;
+            offset[i] = there ? (uint32_t)row * (uint32_t)o.stride * 2u + 16u * c : kOut;
+        }
+    }
+
+    // Moves step k0 of a plane, rows (columns) from `origin` on, to `lds`.
+    __device__ __forceinline__ void move(const Operand &o, int plane, int k0, int origin, char *lds) const
+    {
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+        const bool second = !ALONG && PAIR && k0 >= o.half;
+        const int k = k0 - (second ? o.half : 0);
+        const long from = plane * o.plane + (ALONG ? origin * o.stride + k : k * o.stride + origin);
+        const int rows = ALONG ? max(0, min(ALONG && PAIR ? R / 2 : R, o.rows - origin)) : max(0, min(BK, o.k - k));
+        const uint32_t bytes = rows ? (uint32_t)(ALONG ? (rows - 1) * o.stride * 2 + (o.k - k) * 2 : rows * o.stride * 2) : 0u;
+        const bool there = !ALONG || k + column < o.k;
+        const uint64_t first = uniform(o.p[second ? 1 : 0] + from), other = ALONG && PAIR ? uniform(o.p[1] + from) : first;
+        const int size = __builtin_amdgcn_readfirstlane((int)bytes);
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            typedef __attribute__((address_space(3))) void lds_t;
+            const auto rsrc = __builtin_amdgcn_make_buffer_rsrc((void *)(i >= LOADS / 2 ? other : first), 0, size, 0x00020000);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_t *)(lds + (i * THREADS + wave * 64) * 16), 16, there ? offset[i] : kOut, 0, 0, 0);
         }
     }
 
@@ -82,13 +96,13 @@ struct Stage {
     {
         const int lane = threadIdx.x % 64;
         if (ALONG) {
-            const int r = first + lane % 32, c = (2 * kk + lane / 32) ^ (r / 2 % 8);
-            return *reinterpret_cast<const bf16x8 *>(lds + r * (BK * 2) + c * 16);
+            const int r = lane % 32, c = (lane / 32) ^ (r / 2 % 8) ^ (2 * kk);
+            return *reinterpret_cast<const bf16x8 *>(lds + r * (BK * 2) + c * 16 + first * (BK * 2));
         }
         // 16 lanes fetch 4 rows of 16 columns each, 4 columns a lane, and get a column each
-        const int at = first + lane / 16 % 2 * 16 + lane % 4 * 4, k = 16 * kk + lane / 32 * 8 + lane % 16 / 4;
+        const int at = first + lane / 16 % 2 * 16 + lane % 4 * 4, k = lane / 32 * 8 + lane % 16 / 4;
         const int cell = (at / 8) ^ (k % 4 * 4);
-        const char *p = lds + k * (R * 2) + cell * 16 + at % 8 * 2;
+        const char *p = lds + k * (R * 2) + cell * 16 + at % 8 * 2 + kk * (32 * R);
         typedef __attribute__((address_space(3))) s16x4 lds_t;
         struct Both {
             s16x4 lo, hi;
@@ -103,8 +117,8 @@ struct Stage {
 __device__ __forceinline__ int plane_m(int phase) { return phase == 2 || phase == 3 ? 1 : phase == 5 ? 2 : 0; }
 __device__ __forceinline__ int plane_n(int phase) { return phase == 1 || phase == 3 ? 1 : phase == 4 ? 2 : 0; }
 
-// WM by WN waves' tiles; NPAIR: the n side's tile is two matrices' rows, and a wave has the same rows of both.
-template <int BM_, int BN_, int WAVES_M, int WAVES_N, bool M_ALONG, bool N_ALONG, bool N_PAIR>
+// Of T, the outputs' type: a tile for each.  N_PAIR: the n side is two matrices; along, its tile is the same rows of both, and so is a wave's part of it.
+template <class T, int BM_, int BN_, int WAVES_M, int WAVES_N, bool M_ALONG, bool N_ALONG, bool N_PAIR>
 struct Tile {
     static constexpr int BM = BM_, BN = BN_, THREADS = 64 * WAVES_M * WAVES_N;
     static constexpr int WM = BM / WAVES_M, WN = BN / WAVES_N, FM = WM / 32, FN = WN / 32;
@@ -133,10 +147,14 @@ struct Tile {
             for (int j = 0; j < FM; ++j) acc[i][j] = f32x16{};
         if (t0 >= t1) return;
         int phase = t0 / p.k_tiles, k0 = t0 % p.k_tiles * BK;
+        SM sm;
+        SN sn;
+        sm.init(p.m, m0);
+        sn.init(p.n, n0);
         auto stage = [&](int buffer) {
             char *at = lds + buffer * (SM::BYTES + SN::BYTES);
-            SM::move(p.m, plane_m(phase), k0, m0, at);
-            SN::move(p.n, plane_n(phase), k0, n0, at + SM::BYTES);
+            sm.move(p.m, plane_m(phase), k0, m0, at);
+            sn.move(p.n, plane_n(phase), k0, n0, at + SM::BYTES);
             k0 += BK;
             if (k0 == p.k_tiles * BK) k0 = 0, ++phase;
         };
@@ -144,20 +162,26 @@ struct Tile {
         for (int t = t0; t < t1; ++t) {
             const int buffer = (t - t0) & 1;
             __builtin_amdgcn_s_waitcnt(0x0F70);      // vmcnt(0): this wave's part of the step has come
-            __syncthreads();                         // everybody's has, and nobody reads the step before any more
+            lds_barrier();                           // everybody's has, and nobody reads the step before any more
             if (t + 1 < t1) stage(buffer ^ 1);
             const char *at = lds + buffer * (SM::BYTES + SN::BYTES);
+            // operands are read 16 k ahead of their products
+            bf16x8 n[2][FN], m[2][FM];
+            auto read = [&](int kk) {
+#pragma unroll
+                for (int i = 0; i < FN; ++i) n[kk % 2][i] = SN::read(at + SM::BYTES, n_first(i), kk);
+#pragma unroll
+                for (int j = 0; j < FM; ++j) m[kk % 2][j] = SM::read(at, wm * WM + 32 * j, kk);
+            };
+            read(0);
 #pragma unroll
             for (int kk = 0; kk < BK / 16; ++kk) {
-                bf16x8 n[FN], m[FM];
+                if (kk + 1 < BK / 16) read(kk + 1);
+                __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int i = 0; i < FN; ++i) n[i] = SN::read(at + SM::BYTES, n_first(i), kk);
+                for (int j = 0; j < FM; ++j)
 #pragma unroll
-                for (int j = 0; j < FM; ++j) m[j] = SM::read(at, wm * WM + 32 * j, kk);
-#pragma unroll
-                for (int i = 0; i < FN; ++i)
-#pragma unroll
-                    for (int j = 0; j < FM; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(n[i], m[j], acc[i][j], 0, 0, 0);
+                    for (int i = 0; i < FN; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(n[kk % 2][i], m[kk % 2][j], acc[i][j], 0, 0, 0);
             }
         }
     }
