@@ -238,7 +238,7 @@ __global__ __launch_bounds__(64 * kFewWaves) void gated_few_kernel(const T *x, l
 
 // dG's planes, M rows of 2 * half: [dgate | dup], columns behind F are 0
 template <class T>
-__global__ __launch_bounds__(256) void gated_gradient_kernel(const T *dy, long dy_m, const float *saved, GateOut o, int half, bf16_t *out, long plane)
+__global__ __launch_bounds__(256) void gated_gradient_kernel(const T *dy, long dy_m, const float *saved, GateOut o, int half, long row, bf16_t *out, long plane)
 {
     const int packs = half / 8;
     for (long i = blockIdx.x * 256l + threadIdx.x; i < (long)o.M * packs; i += gridDim.x * 256l) {
@@ -267,8 +267,8 @@ __global__ __launch_bounds__(256) void gated_gradient_kernel(const T *dy, long d
                 du[e] = e < have ? dv * value : 0.f;
             }
         }
-        store_planes<T>(out + m * 2 * half + f, plane, dg);
-        store_planes<T>(out + m * 2 * half + half + f, plane, du);
+        store_planes<T>(out + m * row + f, plane, dg);
+        store_planes<T>(out + m * row + half + f, plane, du);
     }
 }
 
@@ -321,10 +321,10 @@ __global__ __launch_bounds__(TILE::THREADS) void product_kernel(Problem p, Matri
 }
 
 // dx's and the weights' products
-template <class T> using LargeAlong = Tile<T, 256, 256, 2, 4, true, false, true>;
-template <class T> using SmallAlong = Tile<T, 128, 128, 2, 2, true, false, true>;
-template <class T> using LargeAcross = Tile<T, 256, 256, 2, 4, false, false, false>;
-template <class T> using SmallAcross = Tile<T, 128, 128, 2, 2, false, false, false>;
+template <class T> using LargeAlong = Tile<T, 256, 256, 2, 4, 2, true, false, true>;
+template <class T> using SmallAlong = Tile<T, 128, 128, 2, 2, 4, true, false, true>;
+template <class T> using LargeAcross = Tile<T, 256, 256, 2, 4, 2, false, false, false>;
+template <class T> using SmallAcross = Tile<T, 128, 128, 2, 2, 4, false, false, false>;
 
 template <class T>
 __global__ __launch_bounds__(256) void product_join_kernel(const float *part, int splits, MatrixOut o, long rows, int cols)
@@ -354,7 +354,8 @@ unsigned grid_for(long n) { return (unsigned)std::min((n + 255) / 256, 1l << 16)
 
 constexpr int kUnits = 256;      // compute units
 
-// Tiles of 256 by 256 where they fill the card, of 128 by 128 otherwise; the reduction in parts where even those are too few.
+// Tiles of 256 by 256 or of 128 by 128, whichever take less time in whole rounds of a workgroup to a unit (a small one has a quarter of the work at about
+// 0.7 of the rate); the reduction in parts of 8 steps at least where small ones are too few.
 struct Shape {
     bool large;
     int tiles_m, tiles_n, splits;
@@ -362,16 +363,15 @@ struct Shape {
 
 Shape shape_of(long m, long n, long steps)
 {
+    auto tiles = [&](long side) { return ((m + side - 1) / side) * ((n + side - 1) / side); };
+    auto rounds = [](long t) { return (double)((t + kUnits - 1) / kUnits); };
     Shape s;
-    const long big = (m + 255) / 256 * ((n + 255) / 256);
-    s.large = big >= kUnits;
+    const double large = rounds(tiles(256)), small = rounds(tiles(128)) * 0.25 / 0.7;
+    s.large = large <= small;
     const int side = s.large ? 256 : 128;
     s.tiles_m = (int)((m + side - 1) / side);
     s.tiles_n = (int)((n + side - 1) / side);
-    const long tiles = (long)s.tiles_m * s.tiles_n;
-    s.splits = 1;
-    // parts of 8 steps at least; two workgroups to a unit
-    if (!s.large) s.splits = (int)std::max(1l, std::min(2 * kUnits / tiles, steps / 8));
+    s.splits = s.large ? 1 : (int)std::max(1l, std::min(kUnits / tiles(128), steps / 8));
     return s;
 }
 
@@ -382,6 +382,7 @@ struct Layout {
     bool copy_x, copy_w;
     size_t x, wg, wu, dg, part, bytes;
     int half;                // dG's columns of one side
+    long dg_row;             // elements from row to row
     long x_plane, w_plane, dg_plane;
     bool few;
     Shape fwd, dx, dw;
@@ -397,6 +398,7 @@ Layout layout_of(const ucd_gated_projection_t &d, int dir, bool x_aligned, bool 
     l.phases = f32 ? 6 : 1;
     l.width = (int)round_up(d.D, 8);
     l.half = (int)round_up(d.F, BK);
+    l.dg_row = 2l * l.half + BK;      // rows that are a power of two apart meet in few of the caches' channels (dx of 8192 x 2048 x 8192: 870 TFLOP/s against 979)
     l.few = d.M <= kFewTokens;
     l.copy_w = f32 || d.D % 8 != 0 || !w_aligned;
     l.copy_x = f32 || d.D % 8 != 0 || !x_aligned || (d.M > 1 && d.x_m % 8 != 0);
@@ -418,7 +420,7 @@ Layout layout_of(const ucd_gated_projection_t &d, int dir, bool x_aligned, bool 
     } else {
         l.dx = shape_of(d.M, d.D, 2l * l.half / BK * l.phases);
         l.dw = shape_of(2l * l.half, d.D, ((long)d.M + BK - 1) / BK * l.phases);
-        l.dg_plane = (long)d.M * 2 * l.half;
+        l.dg_plane = (long)d.M * l.dg_row;
         l.dg = take((size_t)l.planes * l.dg_plane * 2);
     }
     if (l.copy_x) l.x = take((size_t)l.planes * l.x_plane * 2);
@@ -531,8 +533,8 @@ hipError_t fwd(const ucd_gated_projection_t &d, const void *x, const void *wg, c
     p.phases = l.phases;
     shape_into(p, l.fwd);
     float *part = p.splits > 1 ? (float *)(ws + l.part) : nullptr;
-    if (l.fwd.large) return forward<T, Tile<T, 256, 256, 2, 4, true, true, true>>(p, o, part, s);
-    return forward<T, Tile<T, 128, 128, 2, 2, true, true, true>>(p, o, part, s);
+    if (l.fwd.large) return forward<T, Tile<T, 256, 256, 2, 4, 2, true, true, true>>(p, o, part, s);
+    return forward<T, Tile<T, 128, 128, 2, 2, 4, true, true, true>>(p, o, part, s);
 }
 
 template <class T>
@@ -543,10 +545,10 @@ hipError_t bwd(const ucd_gated_projection_t &d, const void *x, const void *wg, c
     Operand ox{}, ow{}, og{};
     hipError_t e = operands<T>(d, l, x, wg, wu, ws, ox, ow, s);
     if (e != hipSuccess) return e;
-    gated_gradient_kernel<T><<<grid_for((long)d.M * (l.half / 8)), 256, 0, s>>>((const T *)dy, d.y_m, o.saved, o, l.half, (bf16_t *)(ws + l.dg), l.dg_plane);
+    gated_gradient_kernel<T><<<grid_for((long)d.M * (l.half / 8)), 256, 0, s>>>((const T *)dy, d.y_m, o.saved, o, l.half, l.dg_row, (bf16_t *)(ws + l.dg), l.dg_plane);
     if ((e = hipGetLastError()) != hipSuccess) return e;
     og.p[0] = og.p[1] = (const bf16_t *)(ws + l.dg);
-    og.stride = 2l * l.half;
+    og.stride = l.dg_row;
     og.plane = l.dg_plane;
     // dx = dG [Wg; Wu]: dG along its rows, the weights across
     Problem p{};

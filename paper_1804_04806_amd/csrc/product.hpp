@@ -2,7 +2,7 @@
 // operand is read along its rows (k contiguous) or across them (m or n contiguous).
 //
 // A workgroup has a tile of BM by BN outputs and walks over k in steps of 64.  Both operands' steps go from memory to LDS directly, 16 bytes a lane,
-// one step ahead of the products (two buffers, one barrier a step).  Lanes fetch permuted pieces, so that reads of LDS meet no bank twice:
+// ahead of the products (a ring of buffers, one barrier a step).  Lanes fetch permuted pieces, so that reads of LDS meet no bank twice:
 //   along: rows of 64 k, 8 cells of 16 bytes; cell c of row r stands at c ^ (r / 2 % 8), a lane reads one cell (8 neighbouring k of its row);
 //   across: rows of BM or BN columns, one for each k; cell c of row k stands at c ^ (k % 4 * 4), transposing reads (ds_read_b64_tr_b16) give a lane 4
 //   neighbouring k of its column.
@@ -71,24 +71,29 @@ struct Stage {
         }
     }
 
-    // Moves step k0 of a plane, rows (columns) from `origin` on, to `lds`.
-    __device__ __forceinline__ void move(const Operand &o, int plane, int k0, int origin, char *lds) const
+    // Step k0 of a plane, rows (columns) from `origin` on, is what comes next; 0 where it is no real one.
+    uint64_t first, other;
+    int size;
+    bool there;
+    __device__ __forceinline__ void aim(const Operand &o, int plane, int k0, int origin, bool real)
     {
-        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
         const bool second = !ALONG && PAIR && k0 >= o.half;
         const int k = k0 - (second ? o.half : 0);
         const long from = plane * o.plane + (ALONG ? origin * o.stride + k : k * o.stride + origin);
         const int rows = ALONG ? max(0, min(ALONG && PAIR ? R / 2 : R, o.rows - origin)) : max(0, min(BK, o.k - k));
-        const uint32_t bytes = rows ? (uint32_t)(ALONG ? (rows - 1) * o.stride * 2 + (o.k - k) * 2 : rows * o.stride * 2) : 0u;
-        const bool there = !ALONG || k + column < o.k;
-        const uint64_t first = uniform(o.p[second ? 1 : 0] + from), other = ALONG && PAIR ? uniform(o.p[1] + from) : first;
-        const int size = __builtin_amdgcn_readfirstlane((int)bytes);
-#pragma unroll
-        for (int i = 0; i < LOADS; ++i) {
-            typedef __attribute__((address_space(3))) void lds_t;
-            const auto rsrc = __builtin_amdgcn_make_buffer_rsrc((void *)(i >= LOADS / 2 ? other : first), 0, size, 0x00020000);
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_t *)(lds + (i * THREADS + wave * 64) * 16), 16, there ? offset[i] : kOut, 0, 0, 0);
-        }
+        const uint32_t bytes = real && rows ? (uint32_t)(ALONG ? (rows - 1) * o.stride * 2 + (o.k - k) * 2 : rows * o.stride * 2) : 0u;
+        there = !ALONG || k + column < o.k;
+        first = uniform(o.p[second ? 1 : 0] + from);
+        other = ALONG && PAIR ? uniform(o.p[1] + from) : first;
+        size = __builtin_amdgcn_readfirstlane((int)bytes);
+    }
+    // Load i of it, to `lds`.
+    __device__ __forceinline__ void move(int i, char *lds) const
+    {
+        typedef __attribute__((address_space(3))) void lds_t;
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+        const auto rsrc = __builtin_amdgcn_make_buffer_rsrc((void *)(i >= LOADS / 2 ? other : first), 0, size, 0x00020000);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_t *)(lds + (i * THREADS + wave * 64) * 16), 16, there ? offset[i] : kOut, 0, 0, 0);
     }
 
     // A lane's 8 elements of 16 k from 16 kk on, of the 32 rows (columns) from `first` on: row lane % 32, k 8 (lane / 32) + 0 .. 7.
@@ -118,16 +123,19 @@ __device__ __forceinline__ int plane_m(int phase) { return phase == 2 || phase =
 __device__ __forceinline__ int plane_n(int phase) { return phase == 1 || phase == 3 ? 1 : phase == 4 ? 2 : 0; }
 
 // Of T, the outputs' type: a tile for each.  N_PAIR: the n side is two matrices; along, its tile is the same rows of both, and so is a wave's part of it.
-template <class T, int BM_, int BN_, int WAVES_M, int WAVES_N, bool M_ALONG, bool N_ALONG, bool N_PAIR>
+template <class T, int BM_, int BN_, int WAVES_M, int WAVES_N, int BUFFERS, bool M_ALONG, bool N_ALONG, bool N_PAIR>
 struct Tile {
     static constexpr int BM = BM_, BN = BN_, THREADS = 64 * WAVES_M * WAVES_N;
     static constexpr int WM = BM / WAVES_M, WN = BN / WAVES_N, FM = WM / 32, FN = WN / 32;
     static constexpr bool ROW_PAIR = N_PAIR && N_ALONG;
     typedef Stage<BM, M_ALONG, false, THREADS> SM;
     typedef Stage<BN, N_ALONG, N_PAIR, THREADS> SN;
-    static constexpr int LDS = 2 * (SM::BYTES + SN::BYTES);
+    static constexpr int STEP = SM::BYTES + SN::BYTES, LDS = BUFFERS * STEP;
     f32x16 acc[FN][FM];
     int wm, wn, lane;
+    bf16x8 n[2][FN], m[2][FM];      // operands, 16 k ahead of their products
+    SM sm;
+    SN sn;
 
     // first row of fragment i within the tile's n side
     __device__ __forceinline__ int n_first(int i) const
@@ -135,8 +143,52 @@ struct Tile {
         return ROW_PAIR ? (i < FN / 2 ? 0 : BN / 2) + wn * (WN / 2) + i % (FN / 2) * 32 : wn * WN + 32 * i;
     }
 
+    __device__ __forceinline__ void read(const char *at, int kk)
+    {
+#pragma unroll
+        for (int i = 0; i < FN; ++i) n[kk % 2][i] = SN::read(at + SM::BYTES, n_first(i), kk);
+#pragma unroll
+        for (int j = 0; j < FM; ++j) m[kk % 2][j] = SM::read(at, wm * WM + 32 * j, kk);
+    }
+    __device__ __forceinline__ void multiply(int kk)
+    {
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int j = 0; j < FM; ++j)
+#pragma unroll
+            for (int i = 0; i < FN; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(n[kk % 2][i], m[kk % 2][j], acc[i][j], 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    // A step's loads in three parts between products: all at once they would hold up the waves that issue them.
+    __device__ __forceinline__ void load(int part, char *into) const
+    {
+        constexpr int ALL = SM::LOADS + SN::LOADS;
+#pragma unroll
+        for (int i = ALL * part * 3 / 8; i < min(ALL, ALL * (part + 1) * 3 / 8); ++i) {
+            if (i < SM::LOADS) sm.move(i, into);
+            else sn.move(i - SM::LOADS, into + SM::BYTES);
+        }
+    }
+    // Between two barriers: the last products of the step before, this step's others, and loads of a later step.  The pointers are told to be of different
+    // memory, as they are: otherwise every transposing read waits for all loads on their way.
+    __device__ __forceinline__ void step(const char *__restrict__ at, char *__restrict__ into)
+    {
+        load(0, into);
+        read(at, 0);
+        multiply(3);
+        load(1, into);
+        read(at, 1);
+        multiply(0);
+        load(2, into);
+        read(at, 2);
+        multiply(1);
+        read(at, 3);
+        multiply(2);
+    }
+
     __device__ __forceinline__ void run(const Problem &p, int m0, int n0, int t0, int t1, char *lds)
     {
+        static_assert(BK == 64, "four reads a step");
         lane = threadIdx.x % 64;
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
         wm = wave % WAVES_M;
@@ -146,44 +198,42 @@ struct Tile {
 #pragma unroll
             for (int j = 0; j < FM; ++j) acc[i][j] = f32x16{};
         if (t0 >= t1) return;
-        int phase = t0 / p.k_tiles, k0 = t0 % p.k_tiles * BK;
-        SM sm;
-        SN sn;
+        // the first step's "last products of the step before" are of zeros
+#pragma unroll
+        for (int i = 0; i < FN; ++i) n[1][i] = bf16x8{};
+#pragma unroll
+        for (int j = 0; j < FM; ++j) m[1][j] = bf16x8{};
+        int phase = t0 / p.k_tiles, k0 = t0 % p.k_tiles * BK, aimed = t0;
         sm.init(p.m, m0);
         sn.init(p.n, n0);
-        auto stage = [&](int buffer) {
-            char *at = lds + buffer * (SM::BYTES + SN::BYTES);
-            sm.move(p.m, plane_m(phase), k0, m0, at);
-            sn.move(p.n, plane_n(phase), k0, n0, at + SM::BYTES);
+        // Steps stand in a ring of buffers, BUFFERS - 1 of them on their way or there; behind the last one nothing is read, but as many loads stand in the
+        // queue.
+        auto aim = [&]() {
+            sm.aim(p.m, plane_m(phase), k0, m0, aimed < t1);
+            sn.aim(p.n, plane_n(phase), k0, n0, aimed < t1);
+            ++aimed;
             k0 += BK;
             if (k0 == p.k_tiles * BK) k0 = 0, ++phase;
         };
-        stage(0);
-        for (int t = t0; t < t1; ++t) {
-            const int buffer = (t - t0) & 1;
-            __builtin_amdgcn_s_waitcnt(0x0F70);      // vmcnt(0): this wave's part of the step has come
-            lds_barrier();                           // everybody's has, and nobody reads the step before any more
-            if (t + 1 < t1) stage(buffer ^ 1);
-            const char *at = lds + buffer * (SM::BYTES + SN::BYTES);
-            // operands are read 16 k ahead of their products
-            bf16x8 n[2][FN], m[2][FM];
-            auto read = [&](int kk) {
+        constexpr int LOADS = (SM::LOADS + SN::LOADS) * (BUFFERS - 2);      // in the queue behind the step that is waited for
+        static_assert(LOADS < 64, "counted in six bits");
+        constexpr int WAIT = (LOADS & 15) | LOADS >> 4 << 14 | 0x70;        // vmcnt(LOADS) lgkmcnt(0)
 #pragma unroll
-                for (int i = 0; i < FN; ++i) n[kk % 2][i] = SN::read(at + SM::BYTES, n_first(i), kk);
-#pragma unroll
-                for (int j = 0; j < FM; ++j) m[kk % 2][j] = SM::read(at, wm * WM + 32 * j, kk);
-            };
-            read(0);
-#pragma unroll
-            for (int kk = 0; kk < BK / 16; ++kk) {
-                if (kk + 1 < BK / 16) read(kk + 1);
-                __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-                for (int j = 0; j < FM; ++j)
-#pragma unroll
-                    for (int i = 0; i < FN; ++i) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(n[kk % 2][i], m[kk % 2][j], acc[i][j], 0, 0, 0);
-            }
+        for (int i = 0; i < BUFFERS - 1; ++i) {
+            aim();
+            load(0, lds + i * STEP), load(1, lds + i * STEP), load(2, lds + i * STEP);
         }
+        int at = 0, into = (BUFFERS - 1) * STEP;
+        for (int t = t0; t < t1; ++t) {
+            __builtin_amdgcn_s_waitcnt(WAIT);      // this wave's part of the step has come, and it has read all of the one before
+            lds_barrier();
+            aim();
+            step(lds + at, lds + into);
+            at = at + STEP == LDS ? 0 : at + STEP;
+            into = into + STEP == LDS ? 0 : into + STEP;
+        }
+        multiply(3);
+        __builtin_amdgcn_s_waitcnt(0x0F70);      // vmcnt(0): nothing is on its way to this LDS any more
     }
 
     // f(m, n, values): four neighbours in n, places within the tile; each fragment of the n side by itself
