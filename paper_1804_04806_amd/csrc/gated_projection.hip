@@ -128,29 +128,36 @@ __global__ __launch_bounds__(TILE::THREADS) void gated_forward_kernel(Problem p,
     split_range(p, blockIdx.y, t0, t1);
     TILE tile;
     tile.run(p, m0, f0, t0, t1, lds);
-    if (part) {
-        // partial sums: for every split and row a row of both sides
-        float *at = part + (long)blockIdx.y * o.M * 2 * o.wide;
-        tile.each([&](int m, int n, const Pack<float, 4> &v) {
+    constexpr int SIDE = TILE::FN / 2;
+    auto sums = [&](int i, int j, int r) { return tile.sums(i, j, r); };
+    // both sides in fp32: partial sums, for every split and row a row of either side, or what Backward reads
+    float *both = part ? part + (long)blockIdx.y * o.M * 2 * o.wide : o.saved;
+    if (both) {
+        auto sink = [&](int m, int n, const Pack<float, 4> &v) {
             const int side = n >= TILE::BN / 2, f = f0 + n - side * (TILE::BN / 2);
-            if (m0 + m < o.M && f < o.F) *reinterpret_cast<Pack<float, 4> *>(at + (m0 + m) * 2l * o.wide + side * o.wide + f) = v;
-        });
-        return;
+            if (m0 + m < o.M && f < o.F) *reinterpret_cast<Pack<float, 4> *>(both + (m0 + m) * 2l * o.wide + side * o.wide + f) = v;
+        };
+        tile.template rows<float, 0, SIDE>(lds, sums, sink);
+        tile.template rows<float, SIDE, SIDE>(lds, sums, sink);
     }
+    if (part) return;
+    tile.template rows<T, 0, SIDE>(
+        lds,
+        [&](int i, int j, int r) {
+            Pack<float, 4> g = tile.sums(i, j, r);
+            const Pack<float, 4> u = tile.sums(i + SIDE, j, r);
 #pragma unroll
-    for (int j = 0; j < TILE::FM; ++j)
-#pragma unroll
-        for (int i = 0; i < TILE::FN / 2; ++i)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                Pack<float, 4> g, u;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    g.v[e] = tile.acc[i][j][4 * r + e];
-                    u.v[e] = tile.acc[i + TILE::FN / 2][j][4 * r + e];
-                }
-                gate_store<T>(o, m0 + tile.wm * TILE::WM + 32 * j + tile.lane % 32, f0 + tile.n_first(i) + 8 * r + 4 * (tile.lane / 32), g, u);
-            }
+            for (int e = 0; e < 4; ++e) g.v[e] = gate_act(o.act, g.v[e]) * u.v[e];
+            return g;
+        },
+        [&](int m, int n, const auto &v) {
+            constexpr int PER = 16 / sizeof(T);
+            const int f = f0 + n, have = min(PER, o.F - f);
+            if (m0 + m >= o.M || have <= 0) return;
+            T *at = (T *)o.y + (m0 + m) * o.y_m + f;
+            if (have == PER) loose_store<T, PER>(at, v);
+            else store_pack<false, T, PER>(at, v, have);
+        });
 }
 
 template <class T>
@@ -281,22 +288,24 @@ struct MatrixOut {
     bool add;
 };
 
-template <class T>
-__device__ __forceinline__ void matrix_store(const MatrixOut &o, long m, int n, const Pack<float, 4> &v)
+template <class T, int N>
+__device__ __forceinline__ void matrix_store(const MatrixOut &o, long m, int n, const Pack<float, N> &v)
 {
-    const int second = m >= o.half, have = min(4, o.cols - n);
+    const int second = m >= o.half, have = min(N, o.cols - n);
     m -= second ? o.half : 0;
     if (m >= o.rows || have <= 0) return;
     T *at = (T *)o.p[second] + m * o.stride + n;
-    Pack<T, 4> r;
-    if (have == 4) {
-        Pack<T, 4> old{};
-        if (o.add) old = loose_load<T, 4>(at);
+    Pack<T, N> r;
+    if (have == N) {
+        Pack<T, N> old{};
+        if (o.add) old = loose_load<T, N>(at);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) r.v[e] = from_f<T>(o.add ? to_f(old.v[e]) + v.v[e] : v.v[e]);
-        loose_store<T, 4>(at, r);
+        for (int e = 0; e < N; ++e) r.v[e] = from_f<T>(o.add ? to_f(old.v[e]) + v.v[e] : v.v[e]);
+        loose_store<T, N>(at, r);
     } else {
-        for (int e = 0; e < have; ++e) at[e] = from_f<T>(o.add ? to_f(at[e]) + v.v[e] : v.v[e]);
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+            if (e < have) at[e] = from_f<T>(o.add ? to_f(at[e]) + v.v[e] : v.v[e]);
     }
 }
 
@@ -310,21 +319,35 @@ __global__ __launch_bounds__(TILE::THREADS) void product_kernel(Problem p, Matri
     split_range(p, blockIdx.y, t0, t1);
     TILE tile;
     tile.run(p, m0, n0, t0, t1, lds);
+    auto sums = [&](int i, int j, int r) { return tile.sums(i, j, r); };
     if (part) {
         float *at = part + (long)blockIdx.y * part_rows * part_cols;
-        tile.each([&](int m, int n, const Pack<float, 4> &v) {
+        tile.template rows<float, 0, TILE::FN>(lds, sums, [&](int m, int n, const Pack<float, 4> &v) {
             if (m0 + m < part_rows && n0 + n < part_cols) *reinterpret_cast<Pack<float, 4> *>(at + (long)(m0 + m) * part_cols + n0 + n) = v;
         });
         return;
     }
-    tile.each([&](int m, int n, const Pack<float, 4> &v) { matrix_store<T>(o, (long)m0 + m, n0 + n, v); });
+    if (o.add) {       // added to in fp32: old values and sums are rounded together
+        tile.template rows<float, 0, TILE::FN>(lds, sums, [&](int m, int n, const Pack<float, 4> &v) { matrix_store<T, 4>(o, (long)m0 + m, n0 + n, v); });
+        return;
+    }
+    tile.template rows<T, 0, TILE::FN>(lds, sums, [&](int m, int n, const auto &v) {
+        constexpr int PER = 16 / sizeof(T);
+        long row = (long)m0 + m;
+        const int second = row >= o.half, col = n0 + n, have = min(PER, o.cols - col);
+        row -= second ? o.half : 0;
+        if (row >= o.rows || have <= 0) return;
+        T *at = (T *)o.p[second] + row * o.stride + col;
+        if (have == PER) loose_store<T, PER>(at, v);
+        else store_pack<false, T, PER>(at, v, have);
+    });
 }
 
 // dx's and the weights' products
 template <class T> using LargeAlong = Tile<T, 256, 256, 2, 4, 2, true, false, true>;
-template <class T> using SmallAlong = Tile<T, 128, 128, 2, 2, 4, true, false, true>;
+template <class T> using SmallAlong = Tile<T, 128, 128, 2, 2, 2, true, false, true>;
 template <class T> using LargeAcross = Tile<T, 256, 256, 2, 4, 2, false, false, false>;
-template <class T> using SmallAcross = Tile<T, 128, 128, 2, 2, 4, false, false, false>;
+template <class T> using SmallAcross = Tile<T, 128, 128, 2, 2, 2, false, false, false>;
 
 template <class T>
 __global__ __launch_bounds__(256) void product_join_kernel(const float *part, int splits, MatrixOut o, long rows, int cols)
@@ -339,7 +362,7 @@ __global__ __launch_bounds__(256) void product_join_kernel(const float *part, in
 #pragma unroll
             for (int e = 0; e < 4; ++e) v.v[e] += a.v[e];
         }
-        matrix_store<T>(o, m, n, v);
+        matrix_store<T, 4>(o, m, n, v);
     }
 }
 
@@ -354,8 +377,8 @@ unsigned grid_for(long n) { return (unsigned)std::min((n + 255) / 256, 1l << 16)
 
 constexpr int kUnits = 256;      // compute units
 
-// Tiles of 256 by 256 or of 128 by 128, whichever take less time in whole rounds of a workgroup to a unit (a small one has a quarter of the work at about
-// 0.7 of the rate); the reduction in parts of 8 steps at least where small ones are too few.
+// Tiles of 256 by 256, one to a unit, or of 128 by 128, two to a unit, whichever take less time in whole rounds (a round of small ones has half the work of
+// one of large ones, at about 0.7 of the rate); the reduction in parts of 8 steps at least where small ones are too few.
 struct Shape {
     bool large;
     int tiles_m, tiles_n, splits;
@@ -364,14 +387,14 @@ struct Shape {
 Shape shape_of(long m, long n, long steps)
 {
     auto tiles = [&](long side) { return ((m + side - 1) / side) * ((n + side - 1) / side); };
-    auto rounds = [](long t) { return (double)((t + kUnits - 1) / kUnits); };
+    auto rounds = [](long t, long each) { return (double)((t + each - 1) / each); };
     Shape s;
-    const double large = rounds(tiles(256)), small = rounds(tiles(128)) * 0.25 / 0.7;
+    const double large = rounds(tiles(256), kUnits), small = rounds(tiles(128), 2 * kUnits) * 0.5 / 0.7;
     s.large = large <= small;
     const int side = s.large ? 256 : 128;
     s.tiles_m = (int)((m + side - 1) / side);
     s.tiles_n = (int)((n + side - 1) / side);
-    s.splits = s.large ? 1 : (int)std::max(1l, std::min(kUnits / tiles(128), steps / 8));
+    s.splits = s.large ? 1 : (int)std::max(1l, std::min(2 * kUnits / tiles(128), steps / 8));
     return s;
 }
 
@@ -534,7 +557,7 @@ hipError_t fwd(const ucd_gated_projection_t &d, const void *x, const void *wg, c
     shape_into(p, l.fwd);
     float *part = p.splits > 1 ? (float *)(ws + l.part) : nullptr;
     if (l.fwd.large) return forward<T, Tile<T, 256, 256, 2, 4, 2, true, true, true>>(p, o, part, s);
-    return forward<T, Tile<T, 128, 128, 2, 2, 4, true, true, true>>(p, o, part, s);
+    return forward<T, Tile<T, 128, 128, 2, 2, 2, true, true, true>>(p, o, part, s);
 }
 
 template <class T>

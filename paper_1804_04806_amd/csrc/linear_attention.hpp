@@ -57,7 +57,7 @@ template <> struct Mma<bf16_t> {
     __device__ static __forceinline__ Frag along(const char *tile, int first, int k0)
     {
         const int lane = threadIdx.x % 64;
-        return *reinterpret_cast<const Frag *>(tile + TileLds<bf16_t, COLS>::cell(lane % 32, lane / 32) + first * TileLds<bf16_t, COLS>::ROW + k0 * 2);
+        return lds_get<Frag>(tile + TileLds<bf16_t, COLS>::cell(lane % 32, lane / 32) + first * TileLds<bf16_t, COLS>::ROW + k0 * 2);
     }
     // sums i, i + 1, ... of a tile of them as an operand: lanes 0-31 have rows 0 .. 3 and 8 .. 11 of 16, lanes 32-63 rows 4 .. 7 and 12 .. 15.  What is
     // multiplied with them is stored in that order (SUMS_ORDER): 8, 8, 8 and 8 bytes of 32 as 0, 2, 1, 3
@@ -95,7 +95,7 @@ template <> struct Mma<bf16_t> {
     __device__ static __forceinline__ Frag along16(const char *tile, int first, int k0)
     {
         const int lane = threadIdx.x % 64;
-        return *reinterpret_cast<const Frag *>(tile + TileLds<bf16_t, COLS>::cell(lane % 16, lane / 16) + first * TileLds<bf16_t, COLS>::ROW + k0 * 2);
+        return lds_get<Frag>(tile + TileLds<bf16_t, COLS>::cell(lane % 16, lane / 16) + first * TileLds<bf16_t, COLS>::ROW + k0 * 2);
     }
     // those steps of a tile in its own order that along16 gives of one in the sums'
     template <int COLS>
@@ -106,8 +106,8 @@ template <> struct Mma<bf16_t> {
         struct Both {
             s16x4 lo, hi;
         } v;
-        v.lo = *reinterpret_cast<const s16x4 *>(p);
-        v.hi = *reinterpret_cast<const s16x4 *>(p + 16);
+        v.lo = lds_get<s16x4>(p);
+        v.hi = lds_get<s16x4>(p + 16);
         return __builtin_bit_cast(Frag, v);
     }
     __device__ static __forceinline__ f32x4 product16(const Frag &a, const Frag &b, f32x4 c)
@@ -148,7 +148,7 @@ template <> struct Mma<float> {
     __device__ static __forceinline__ Frag along(const char *tile, int first, int k0)
     {
         const int lane = threadIdx.x % 64;
-        return *reinterpret_cast<const Frag *>(tile + TileLds<float, COLS>::cell(lane % 32, lane / 32) + first * TileLds<float, COLS>::ROW + k0 * 4);
+        return lds_get<Frag>(tile + TileLds<float, COLS>::cell(lane % 32, lane / 32) + first * TileLds<float, COLS>::ROW + k0 * 4);
     }
     template <int COLS>
     __device__ static __forceinline__ Frag along16_other(const char *tile, int first, int k0) { return along16<COLS>(tile, first, k0); }
@@ -162,8 +162,7 @@ template <> struct Mma<float> {
         Frag v;
 #pragma unroll
         for (int i = 0; i < 4; ++i)      // row 4 (lane / 32) + i of 8, from k0, of which there may be an odd number in 16
-            v.v[i] = *reinterpret_cast<const float *>(tile + TileLds<float, COLS>::at(k0 % 16 + lane / 32 * 4 + i, lane % 32) + k0 / 16 * 16 * TileLds<float, COLS>::ROW +
-                                                      first * 4);
+            v.v[i] = lds_get<float>(tile + TileLds<float, COLS>::at(k0 % 16 + lane / 32 * 4 + i, lane % 32) + k0 / 16 * 16 * TileLds<float, COLS>::ROW + first * 4);
         return v;
     }
     __device__ static __forceinline__ f32x16 product(const Frag &a, const Frag &b, f32x16 c)
@@ -177,7 +176,7 @@ template <> struct Mma<float> {
     __device__ static __forceinline__ Frag along16(const char *tile, int first, int k0)
     {
         const int lane = threadIdx.x % 64;
-        return *reinterpret_cast<const Frag *>(tile + TileLds<float, COLS>::cell(lane % 16, lane / 16) + first * TileLds<float, COLS>::ROW + k0 * 4);
+        return lds_get<Frag>(tile + TileLds<float, COLS>::cell(lane % 16, lane / 16) + first * TileLds<float, COLS>::ROW + k0 * 4);
     }
     __device__ static __forceinline__ f32x4 product16(const Frag &a, const Frag &b, f32x4 c)
     {
@@ -283,10 +282,10 @@ struct Fetch {
             char *to = tile + TileLds<T, COLS>::cell(ROWS % 16 == 0 ? r : r + i * ROWS, SUMS_ORDER ? c & ~1 : c) + (ROWS % 16 == 0 ? i * ROWS * TileLds<T, COLS>::ROW : 0);
             if (SUMS_ORDER) {
                 to += c % 2 * 8;
-                *reinterpret_cast<u32x2 *>(to) = u32x2{x[0], x[1]};
-                *reinterpret_cast<u32x2 *>(to + 16) = u32x2{x[2], x[3]};
+                lds_put(to, u32x2{x[0], x[1]});
+                lds_put(to + 16, u32x2{x[2], x[3]});
             } else {
-                *reinterpret_cast<u32x4 *>(to) = x;
+                lds_put(to, x);
             }
         }
     }

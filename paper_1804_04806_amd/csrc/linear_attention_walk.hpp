@@ -224,7 +224,7 @@ __global__ __launch_bounds__(2 * COLS, sizeof(T) == 2 ? 256 / COLS : 128 / COLS)
                             const float w = ChunkDecays::pair<T>(hi, lo, shi[i].v[e], sizeof(T) == 4 ? slo[i].v[e] : 0.f) * p.p_scale;
                             v[e] = s + e <= t ? acc[i][e] * w : 0.f;
                         }
-                        *reinterpret_cast<Pack<T, 4> *>(lds_p + TP::at(t, s)) = pack_four<T>(v[0], v[1], v[2], v[3]);
+                        lds_put(lds_p + TP::at(t, s), pack_four<T>(v[0], v[1], v[2], v[3]));
                     }
                 }
             }
@@ -276,12 +276,12 @@ __global__ __launch_bounds__(2 * COLS, sizeof(T) == 2 ? 256 / COLS : 128 / COLS)
                     for (int pass = 0; pass < DOT_PASSES; ++pass) {
 #pragma unroll
                         for (int i = 0; i < 2; ++i)
-                            *reinterpret_cast<u32x4 *>(turn + (16 * i + turn_row) * TURN_ROW + turn_at) = dots[DG ? tb : 0][DG ? pass : 0][DG ? i : 0];
+                            lds_put(turn + (16 * i + turn_row) * TURN_ROW + turn_at, dots[DG ? tb : 0][DG ? pass : 0][DG ? i : 0]);
                         wave_lds_order();
                         constexpr int QUADS = 4 / DOT_PASSES;
 #pragma unroll
                         for (int r = 0; r < QUADS; ++r) {
-                            const auto v = *reinterpret_cast<const Pack<T, 4> *>(turn + row * TURN_ROW + (8 * r + 4 * half) * (int)sizeof(T));
+                            const auto v = lds_get<Pack<T, 4>>(turn + row * TURN_ROW + (8 * r + 4 * half) * (int)sizeof(T));
 #pragma unroll
                             for (int e = 0; e < 4; ++e) sum = fmaf(to_f(v.v[e]), y[tb][4 * (pass * QUADS + r) + e], sum);
                         }
@@ -358,13 +358,13 @@ __global__ __launch_bounds__(2 * COLS, sizeof(T) == 2 ? 256 / COLS : 128 / COLS)
                     for (int r = 0; r < QUADS; ++r) {
                         const int q = 4 * (pass * QUADS + r);
                         char *to = turn + row * TURN_ROW + (8 * r + 4 * half) * osize;
-                        if constexpr (osize == 4) *reinterpret_cast<Pack<float, 4> *>(to) = pack_four<float>(y[tb][q], y[tb][q + 1], y[tb][q + 2], y[tb][q + 3]);
-                        else *reinterpret_cast<Pack<T, 4> *>(to) = pack_four<T>(y[tb][q], y[tb][q + 1], y[tb][q + 2], y[tb][q + 3]);
+                        if constexpr (osize == 4) lds_put(to, pack_four<float>(y[tb][q], y[tb][q + 1], y[tb][q + 2], y[tb][q + 3]));
+                        else lds_put(to, pack_four<T>(y[tb][q], y[tb][q + 1], y[tb][q + 2], y[tb][q + 3]));
                     }
                     wave_lds_order();
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
-                        const u32x4 v = *reinterpret_cast<const u32x4 *>(turn + (16 * i + turn_row) * TURN_ROW + turn_at);
+                        const u32x4 v = lds_get<u32x4>(turn + (16 * i + turn_row) * TURN_ROW + turn_at);
                         const int tr = 32 * tb + 16 * i + turn_row, tr_at = REV ? kChunk - 1 - tr : tr;
                         const int x = x0 + pass * (64 / osize) + lane % 4 * PER, have = cols - x;
                         const uint32_t o = (uint32_t)(tr_at * o_l) + x * osize;

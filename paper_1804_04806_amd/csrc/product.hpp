@@ -102,7 +102,7 @@ struct Stage {
         const int lane = threadIdx.x % 64;
         if (ALONG) {
             const int r = lane % 32, c = (lane / 32) ^ (r / 2 % 8) ^ (2 * kk);
-            return *reinterpret_cast<const bf16x8 *>(lds + r * (BK * 2) + c * 16 + first * (BK * 2));
+            return lds_get<bf16x8>(lds + r * (BK * 2) + c * 16 + first * (BK * 2));
         }
         // 16 lanes fetch 4 rows of 16 columns each, 4 columns a lane, and get a column each
         const int at = first + lane / 16 % 2 * 16 + lane % 4 * 4, k = lane / 32 * 8 + lane % 16 / 4;
@@ -197,7 +197,7 @@ struct Tile {
         for (int i = 0; i < FN; ++i)
 #pragma unroll
             for (int j = 0; j < FM; ++j) acc[i][j] = f32x16{};
-        if (t0 >= t1) return;
+        if (t0 >= t1) return;      // of all waves
         // the first step's "last products of the step before" are of zeros
 #pragma unroll
         for (int i = 0; i < FN; ++i) n[1][i] = bf16x8{};
@@ -233,21 +233,45 @@ struct Tile {
             into = into + STEP == LDS ? 0 : into + STEP;
         }
         multiply(3);
-        __builtin_amdgcn_s_waitcnt(0x0F70);      // vmcnt(0): nothing is on its way to this LDS any more
+        __builtin_amdgcn_s_waitcnt(0x0070);      // vmcnt(0) lgkmcnt(0): nothing is on its way to this LDS any more, and nobody reads it
+        lds_barrier();
     }
 
-    // f(m, n, values): four neighbours in n, places within the tile; each fragment of the n side by itself
-    template <class F>
-    __device__ __forceinline__ void each(F f) const
+    // Outputs in rows: a lane's sums are 16 bytes of a row at most, so that they go through LDS, 32 rows of a wave's COUNT fragments from FIRST on at a time.
+    // value(i, j, r): four neighbours of fragment (i, j), from 8 r + 4 (lane / 32) on; sink(m, n, pack): 16 bytes of O at places within the tile.
+    // Stored from the sums as they lie, tiles' ends took 18 us of each round of forward (8192 x 2048 x 8192).
+    template <class O, int FIRST, int COUNT, class V, class S>
+    __device__ __forceinline__ void rows(char *lds, V value, S sink) const
     {
+        constexpr int WIDTH = COUNT * 32 * (int)sizeof(O), ROW = WIDTH + 16, PER = 16 / (int)sizeof(O), LANES = WIDTH / 16, EACH = 64 / LANES;
+        constexpr int REGION = 32 * (FN * 32 * 4 + 16);      // a wave's, the same for all widths: the waves go from one to the next each in its own time
+        static_assert(32 * ROW <= REGION && WAVES_M * WAVES_N * REGION <= LDS, "");
+        char *own = lds + (wn * WAVES_M + wm) * REGION;
 #pragma unroll
-        for (int j = 0; j < FM; ++j)
+        for (int j = 0; j < FM; ++j) {
 #pragma unroll
-            for (int i = 0; i < FN; ++i)
+            for (int i = 0; i < COUNT; ++i)
 #pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    f(wm * WM + 32 * j + lane % 32, n_first(i) + 8 * r + 4 * (lane / 32),
-                      Pack<float, 4>{{acc[i][j][4 * r], acc[i][j][4 * r + 1], acc[i][j][4 * r + 2], acc[i][j][4 * r + 3]}});
+                for (int r = 0; r < 4; ++r) {
+                    const Pack<float, 4> v = value(FIRST + i, j, r);
+                    Pack<O, 4> o;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) o.v[e] = from_f<O>(v.v[e]);
+                    lds_put(own + lane % 32 * ROW + (32 * i + 8 * r + 4 * (lane / 32)) * (int)sizeof(O), o);
+                }
+            wave_lds_order();
+#pragma unroll
+            for (int i = 0; i < 32 / EACH; ++i) {
+                const int row = i * EACH + lane / LANES, col = lane % LANES * PER;
+                const Pack<O, PER> v = lds_get<Pack<O, PER>>(own + row * ROW + col * (int)sizeof(O));
+                sink(wm * WM + 32 * j + row, n_first(FIRST) + col, v);
+            }
+            wave_lds_order();
+        }
+    }
+    __device__ __forceinline__ Pack<float, 4> sums(int i, int j, int r) const
+    {
+        return Pack<float, 4>{{acc[i][j][4 * r], acc[i][j][4 * r + 1], acc[i][j][4 * r + 2], acc[i][j][4 * r + 3]}};
     }
 };
 

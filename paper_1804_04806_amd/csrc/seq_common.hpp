@@ -267,6 +267,23 @@ __device__ __forceinline__ void join_columns(const float *part, long rows, long 
     }
 }
 
+// LDS that is written as one type and read as another, as tiles and turned rows are: without these the compiler may take the two for different memory and
+// move a read behind a write.
+template <class V>
+struct __attribute__((may_alias)) AnyType {
+    V v;
+};
+template <class V>
+__device__ __forceinline__ V lds_get(const char *p)
+{
+    return reinterpret_cast<const AnyType<V> *>(p)->v;
+}
+template <class V>
+__device__ __forceinline__ void lds_put(char *p, const V &v)
+{
+    reinterpret_cast<AnyType<V> *>(p)->v = v;
+}
+
 // Orders a wave's own LDS accesses: the hardware runs them in program order, the compiler has to keep them so.
 __device__ __forceinline__ void wave_lds_order()
 {
