@@ -181,63 +181,118 @@ __global__ __launch_bounds__(256) void gated_join_kernel(const float *part, int 
 
 // ---- few tokens ----------------------------------------------------------------------------------------------------
 //
-// Up to 64 tokens: the weights are read once, straight into the matrix instructions' operands, 16 bytes a lane.  A workgroup has 16 columns of both
-// sides and all tokens; its eight waves share the reduction out, a step of 32 (16 for fp32) each by turns, and join their sums in LDS.
+// Up to 64 tokens: the weights are read once, straight into the matrix instructions' operands, 16 bytes a lane.  A workgroup has 16 CT columns of both
+// sides and all tokens; its eight waves share the reduction out, two steps of 32 (16 for fp32), 128 bytes of a row, each by turns, and join their sums
+// in LDS.  Loads are without branches, AHEAD turns before their use.
 
 constexpr int kFewWaves = 8, kFewTokens = 64;
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
-// 16 bytes of a row; elements from `have` on are 0
-template <class T>
-__device__ __forceinline__ Pack<T, 16 / sizeof(T)> load_piece(const T *p, int have)
-{
-    constexpr int N = 16 / sizeof(T);
-    if (have >= N) return loose_load<T, N>(p);
-    return load_pack<false, T, N>(p, have);
-}
+// Rows from `base` on, read in pieces of 16 bytes.  WHOLE: rows of whole pieces at multiples of 4 bytes, through a buffer: what is not there is 0.
+// Otherwise element by element at a row's end.
+template <class T, bool WHOLE>
+struct FewRows {
+    static constexpr int N = 16 / sizeof(T);
+    __amdgpu_buffer_rsrc_t rsrc;
+    const T *base;
+    long stride;
 
-__device__ __forceinline__ f32x4 few_product(const Pack<bf16_t, 8> &w, const Pack<bf16_t, 8> &x, f32x4 acc)
+    __device__ __forceinline__ FewRows(const T *p, long stride_) : base(p), stride(stride_)
+    {
+        if (WHOLE) rsrc = __builtin_amdgcn_make_buffer_rsrc((void *)uniform(p), 0, (int)0x80000000u, 0x00020000);
+    }
+    // the piece at k of a row, of which `have` elements are there
+    __device__ __forceinline__ u32x4 load(int row, bool real, int k, int have) const
+    {
+        if constexpr (WHOLE) {
+            const uint32_t at = (uint32_t)(row * stride + k) * (uint32_t)sizeof(T);
+            const auto v = __builtin_amdgcn_raw_buffer_load_b128(rsrc, real && have > 0 ? (int)at : (int)0x80000000u, 0, 0);
+            return __builtin_bit_cast(u32x4, v);
+        } else {
+            const int n = real ? have : 0;
+            const T *p = base + row * stride + k;
+            return __builtin_bit_cast(u32x4, n >= N ? loose_load<T, N>(p) : load_pack<false, T, N>(p, n));
+        }
+    }
+};
+
+__device__ __forceinline__ f32x4 few_product(bf16_t, const u32x4 &w, const u32x4 &x, f32x4 acc)
 {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w), __builtin_bit_cast(bf16x8, x), acc, 0, 0, 0);
 }
-__device__ __forceinline__ f32x4 few_product(const Pack<float, 4> &w, const Pack<float, 4> &x, f32x4 acc)
+__device__ __forceinline__ f32x4 few_product(float, const u32x4 &w, const u32x4 &x, f32x4 acc)
 {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(w.v[i], x.v[i], acc, 0, 0, 0);
+    for (int i = 0; i < 4; ++i) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(w[i]), __uint_as_float(x[i]), acc, 0, 0, 0);
     return acc;
 }
 
-template <class T, int MT>
+template <class T, int MT, int CT, int AHEAD, bool WHOLE>
 __global__ __launch_bounds__(64 * kFewWaves) void gated_few_kernel(const T *x, long x_m, const T *wg, const T *wu, int D, GateOut o)
 {
-    constexpr int N = 16 / sizeof(T), STEP = 4 * N;
-    __shared__ f32x4 sums[kFewWaves][2 * MT][64];
+    constexpr int N = 16 / sizeof(T), STEP = 4 * N, TURN = 2 * STEP;
+    __shared__ f32x4 sums[kFewWaves][2 * CT * MT][64];
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, row = lane % 16;
-    const long f0 = blockIdx.x * 16l, f = f0 + row;
-    const bool real = f < o.F;
-    f32x4 g[MT] = {}, u[MT] = {};
-#pragma unroll 4
-    for (int k0 = wave * STEP; k0 < D; k0 += kFewWaves * STEP) {
-        const int k = k0 + lane / 16 * N, have = D - k;
-        const auto a = load_piece<T>(wg + f * D + k, real ? have : 0), b = load_piece<T>(wu + f * D + k, real ? have : 0);
+    const long f0 = blockIdx.x * (16l * CT);
+    const int left = (int)min(16l * CT, o.F - f0);
+    const FewRows<T, WHOLE> rg(wg + f0 * D, D), ru(wu + f0 * D, D), rx(x, x_m);
+    f32x4 acc[2][CT][MT] = {};
+    struct Turn {
+        u32x4 w[2][2][CT], x[2][MT];
+    } turn[AHEAD];
+    const auto load = [&](Turn &r, int k0) {
 #pragma unroll
-        for (int t = 0; t < MT; ++t) {
-            const int m = 16 * t + row;
-            const auto v = load_piece<T>(x + m * x_m + k, m < o.M ? have : 0);
-            g[t] = few_product(a, v, g[t]);
-            u[t] = few_product(b, v, u[t]);
+        for (int h = 0; h < 2; ++h) {
+            const int k = k0 + h * STEP + lane / 16 * N, have = D - k;
+#pragma unroll
+            for (int c = 0; c < CT; ++c) {
+                r.w[h][0][c] = rg.load(16 * c + row, 16 * c + row < left, k, have);
+                r.w[h][1][c] = ru.load(16 * c + row, 16 * c + row < left, k, have);
+            }
+#pragma unroll
+            for (int t = 0; t < MT; ++t) r.x[h][t] = rx.load(16 * t + row, 16 * t + row < o.M, k, have);
+        }
+    };
+    // Workgroups begin at turns of their own: x's lines are then not asked for by all of them at once.
+    const int turns = (D + kFewWaves * TURN - 1) / (kFewWaves * TURN);
+    int at = blockIdx.x / 8 % turns, next = 0;
+    const auto load_next = [&](Turn &r) {
+        load(r, next < turns ? (at * kFewWaves + (wave + blockIdx.x / 8) % kFewWaves) * TURN : D);
+        ++next;
+        at = at + 1 < turns ? at + 1 : 0;
+    };
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) load_next(turn[i]);
+    for (int done = 0; done < turns; done += AHEAD) {
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            Turn &r = turn[i];
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int t = 0; t < MT; ++t)
+#pragma unroll
+                    for (int c = 0; c < CT; ++c)
+#pragma unroll
+                        for (int side = 0; side < 2; ++side) acc[side][c][t] = few_product(T(), r.w[h][side][c], r.x[h][t], acc[side][c][t]);
+            load_next(r);
         }
     }
 #pragma unroll
-    for (int t = 0; t < MT; ++t) sums[wave][2 * t][lane] = g[t], sums[wave][2 * t + 1][lane] = u[t];
+    for (int c = 0; c < CT; ++c)
+#pragma unroll
+        for (int t = 0; t < MT; ++t)
+#pragma unroll
+            for (int side = 0; side < 2; ++side) sums[wave][2 * (c * MT + t) + side][lane] = acc[side][c][t];
     __syncthreads();
     // a lane's sums: column 4 (lane / 16) + 0 .. 3, token lane % 16
-    for (int t = wave; t < MT; t += kFewWaves) {
+    for (int i = wave; i < CT * MT; i += kFewWaves) {
         Pack<float, 4> gate{}, up{};
         for (int w = 0; w < kFewWaves; ++w)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) gate.v[e] += sums[w][2 * t][lane][e], up.v[e] += sums[w][2 * t + 1][lane][e];
-        gate_store<T>(o, 16 * t + row, (int)f0 + 4 * (lane / 16), gate, up);
+            for (int e = 0; e < 4; ++e) gate.v[e] += sums[w][2 * i][lane][e], up.v[e] += sums[w][2 * i + 1][lane][e];
+        gate_store<T>(o, 16 * (i % MT) + row, (int)f0 + 16 * (i / MT) + 4 * (lane / 16), gate, up);
     }
 }
 
@@ -501,15 +556,25 @@ hipError_t operands(const ucd_gated_projection_t &d, const Layout &l, const void
     return e;
 }
 
+template <class T, int MT, int CT, int AHEAD>
+void few_of(const ucd_gated_projection_t &d, const T *x, const T *wg, const T *wu, const GateOut &o, bool whole, hipStream_t s)
+{
+    const unsigned grid = (unsigned)((d.F + 16 * CT - 1) / (16 * CT));
+    if (whole) gated_few_kernel<T, MT, CT, AHEAD, true><<<grid, 64 * kFewWaves, 0, s>>>(x, d.x_m, wg, wu, d.D, o);
+    else gated_few_kernel<T, MT, CT, 1, false><<<grid, 64 * kFewWaves, 0, s>>>(x, d.x_m, wg, wu, d.D, o);
+}
+
 template <class T>
 hipError_t few(const ucd_gated_projection_t &d, const void *x, const void *wg, const void *wu, const GateOut &o, hipStream_t s)
 {
-    const unsigned grid = (unsigned)((d.F + 15) / 16);
-    const int mt = (d.M + 15) / 16;
     const T *px = (const T *)x, *pg = (const T *)wg, *pu = (const T *)wu;
-    if (mt == 1) gated_few_kernel<T, 1><<<grid, 64 * kFewWaves, 0, s>>>(px, d.x_m, pg, pu, d.D, o);
-    else if (mt == 2) gated_few_kernel<T, 2><<<grid, 64 * kFewWaves, 0, s>>>(px, d.x_m, pg, pu, d.D, o);
-    else gated_few_kernel<T, 4><<<grid, 64 * kFewWaves, 0, s>>>(px, d.x_m, pg, pu, d.D, o);
+    const bool whole = d.D * sizeof(T) % 16 == 0 && (d.M == 1 || d.x_m * sizeof(T) % 4 == 0) && (((uintptr_t)x | (uintptr_t)wg | (uintptr_t)wu) & 3u) == 0;
+    const bool two = d.F >= 32 * 256;
+    if (d.M <= 16) few_of<T, 1, 1, 4>(d, px, pg, pu, o, whole, s);
+    else if (d.M <= 32 && two) few_of<T, 2, 2, 2>(d, px, pg, pu, o, whole, s);
+    else if (d.M <= 32) few_of<T, 2, 1, 2>(d, px, pg, pu, o, whole, s);
+    else if (two) few_of<T, 4, 2, 2>(d, px, pg, pu, o, whole, s);
+    else few_of<T, 4, 1, 2>(d, px, pg, pu, o, whole, s);
     return hipGetLastError();
 }
 
