@@ -1,7 +1,6 @@
 /*
- * ucd -- sequence operators: group norm with an activation, short causal convolution, selective
- * state space scan, linear attention and gated projection, with their gradients and, for decoding,
- * their single-token forms.
+ * ucd -- sequence operators: group norm with an activation, short causal convolution and
+ * selective state space scan, with their gradients and, for decoding, their single-token forms.
  *
  * Conventions beside those of ucd.h (device pointers, caller-owned buffers and stream, status
  * codes, no allocation, no synchronisation, nothing launched by a call that fails)
@@ -13,10 +12,7 @@
  *     Calls that would be 2^31 workgroups (the scan's 2^30) are UCD_E_UNSUPPORTED.
  *   - dtype 0: activations (and their gradients, filters and convolution states) fp32; dtype 1:
  *     bfloat16, rounded to nearest-even once.  Everything else is fp32: norm weights, biases, A,
- *     skip, states of the scan and the attention, statistics, gradients of all weights but the gated
- *     projection's; and so is all arithmetic but the products of linear attention and gated
- *     projection, whose operands are bfloat16 (what is computed on the way is rounded to it once; what
- *     is added to a state is not) and whose sums are fp32.
+ *     skip, scan states, statistics, gradients of all weights; and so is all arithmetic.
  *   - Any alignment of an element's own size is accepted, of workspaces and saved states 16 bytes.
  *   - Outputs overlap no input and no other output, but for state_out == state_in.
  *   - Gradients of weights are beta * old + sum, beta in {0, 1}, as in ucd_conv_bwd_filter: a
@@ -40,9 +36,8 @@
 extern "C" {
 #endif
 
-/* Activations; SiLU(v) = v / (1 + exp(-v)); of the gated projection alone, GELU in its tanh form,
- * v (1 + tanh(sqrt(2/pi) (v + 0.044715 v^3))) / 2. */
-enum { UCD_ACT_NONE = 0, UCD_ACT_SILU = 1, UCD_ACT_GELU = 2 };
+/* Activations; SiLU(v) = v / (1 + exp(-v)). */
+enum { UCD_ACT_NONE = 0, UCD_ACT_SILU = 1 };
 
 /* The directions of an operator, for workspace queries. */
 enum { UCD_SEQ_FWD = 0, UCD_SEQ_BWD = 1 };
@@ -156,88 +151,6 @@ int ucd_scan_bwd(const ucd_scan_t *scan, const ucd_scan_in_t *in, const void *dy
 
 /* One token of each sequence (L = 1; lengths is not read): as Forward with state_in = state_out = state. */
 int ucd_scan_step(const ucd_scan_t *scan, const ucd_scan_in_t *in, float *state, void *y, void *stream);
-
-/* ---- linear attention with a decay for each head -------------------------------------------------
- * q, k (B, L, Hk, Dk), v, y (B, L, H, Dv), g (B, L, H): each of the Hk heads of q and k serves H/Hk
- * neighbouring heads of v.  Every head has a state of Dk by Dv, rows of Dv:
- *   l_t = decay + g_t,   S_t = exp(l_t) S_{t-1} + k_t^T v_t,   S_{-1} = state_in or 0,
- *   y_t = scale q_t S_t.
- * decay (H) are constants of the heads, g the decays' own part for every token, both logarithms and
- * at most 0 together; without either (NULL) its term is left out.  What is below -80 counts as -80,
- * exp of which is as good as 0: -infinity forgets what was before the token.  Tokens are taken 64 at a
- * time, from a sequence's first on: a value that is not finite may reach all 64 outputs and gradients
- * around it, beside those of the formulas.  1 <= Dk, Dv <= 128 (wider heads of v are more heads of v to
- * one of q and k); Hk divides H; B, L >= 0.  Rows of q, k, v, g and y, and a token's stride of
- * theirs, are at most 2^23 elements. */
-typedef struct {
-    int32_t B, L, H, Hk, Dk, Dv, dtype;
-    int32_t n_slots;
-    float scale;
-    int64_t q_b, q_l, k_b, k_l, v_b, v_l, g_b, g_l, y_b, y_l;
-} ucd_linear_attention_t;
-
-typedef struct {
-    const void *q, *k, *v;
-    const void *g;            /* may be NULL */
-    const float *decay;       /* may be NULL */
-    const int32_t *lengths;   /* may be NULL */
-    const int32_t *slots;     /* may be NULL */
-} ucd_linear_attention_in_t;
-
-/* Receivers of the gradients: g (where the input has it) and state (the gradient of state_in,
- * (B, H, Dk, Dv)) may be NULL. */
-typedef struct {
-    void *q, *k, *v, *g;
-    float *state;
-} ucd_linear_attention_grad_t;
-
-/* Bytes of workspace of a direction, and of what Forward keeps for Backward.  Host only. */
-size_t ucd_linear_attention_workspace_size(const ucd_linear_attention_t *attention, int dir);
-size_t ucd_linear_attention_saved_size(const ucd_linear_attention_t *attention);
-
-/* state_in (NULL: zeros), state_out (NULL: not wanted): (n_slots or B, H, Dk, Dv) floats.  saved (NULL:
- * no Backward will follow): ucd_linear_attention_saved_size bytes. */
-int ucd_linear_attention_fwd(const ucd_linear_attention_t *attention, const ucd_linear_attention_in_t *in,
-                             const float *state_in, float *state_out, void *y, void *saved, size_t saved_bytes,
-                             void *ws, size_t ws_bytes, void *stream);
-
-/* Backward, without slots; saved is what Forward wrote for the same inputs.  dstate_out (NULL: zeros):
- * gradient of state_out, (B, H, Dk, Dv) floats. */
-int ucd_linear_attention_bwd(const ucd_linear_attention_t *attention, const ucd_linear_attention_in_t *in,
-                             const void *dy, const float *dstate_out, const void *saved, size_t saved_bytes,
-                             const ucd_linear_attention_grad_t *grad, void *ws, size_t ws_bytes, void *stream);
-
-/* One token of each sequence (L = 1; lengths is not read): as Forward with state_in = state_out = state. */
-int ucd_linear_attention_step(const ucd_linear_attention_t *attention, const ucd_linear_attention_in_t *in,
-                              float *state, void *y, void *stream);
-
-/* ---- gated projection ---------------------------------------------------------------------------
- * Both projections of a gated feed-forward block, its activation and its product: x (M, D), one row a
- * token, w_gate, w_up (F, D) with dense rows of x's type, y (M, F):
- *   y = act(x w_gate^T) * (x w_up^T).
- * The weights' gradients are of the weights' type: in bfloat16 they are rounded once, and parts of a
- * mini-batch (beta = 1) once each.  dgate and dup, the gradients of both projections, are rounded once
- * to bfloat16 before they are multiplied where dtype is 1.  fp32 operands are multiplied as three
- * bfloat16 parts each, to about 2^-22 of a product; sums of one that is not finite are not finite.
- * 1 <= D, F <= 2^20, a row's stride 2^21 at most; M >= 0. */
-typedef struct {
-    int32_t M, D, F, act, dtype;
-    int64_t x_m, y_m;             /* strides of x, dx and of y, dy */
-} ucd_gated_projection_t;
-
-/* Bytes of workspace of a direction, and of what Forward keeps for Backward (both projections, fp32).
- * Host only. */
-size_t ucd_gated_projection_workspace_size(const ucd_gated_projection_t *gated, int dir);
-size_t ucd_gated_projection_saved_size(const ucd_gated_projection_t *gated);
-
-/* saved (NULL: no Backward will follow): ucd_gated_projection_saved_size bytes. */
-int ucd_gated_projection_fwd(const ucd_gated_projection_t *gated, const void *x, const void *w_gate, const void *w_up,
-                             void *y, void *saved, size_t saved_bytes, void *ws, size_t ws_bytes, void *stream);
-
-/* dx, dw_gate, dw_up (weights' type) from dy and what Forward kept for the same inputs. */
-int ucd_gated_projection_bwd(const ucd_gated_projection_t *gated, const void *x, const void *w_gate, const void *w_up,
-                             const void *dy, const void *saved, size_t saved_bytes, void *dx, void *dw_gate,
-                             void *dw_up, float beta, void *ws, size_t ws_bytes, void *stream);
 
 #ifdef __cplusplus
 }

@@ -1,6 +1,6 @@
 """TEST INFRASTRUCTURE ONLY: the sequence operators (group norm with an activation, short causal
 convolution, selective state space scan, linear attention, gated projection) and their gradients in numpy, 64 bits, written from the
-formulas in include/ucd_seq.h token by token.  Shares no code with the library.
+formulas in include/ucd_seq.h and include/ucd_mix.h token by token.  Shares no code with the library.
 """
 import numpy as np
 

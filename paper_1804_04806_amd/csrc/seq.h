@@ -1,4 +1,4 @@
-// Host-side launchers of the sequence operators' kernels (include/ucd_seq.h has the formulas).  Descriptors have been
+// Host-side launchers of the sequence operators' kernels (include/ucd_seq.h and include/ucd_mix.h have the formulas).  Descriptors have been
 // checked and their strides filled in; every launcher only enqueues on `s` and returns the launch status.
 #pragma once
 #include <hip/hip_runtime.h>
@@ -6,7 +6,7 @@
 #include <cstddef>
 #include <cstdint>
 
-#include "ucd_seq.h"
+#include "ucd_mix.h"
 
 namespace ucd {
 

@@ -1,5 +1,5 @@
-// C-ABI of the sequence operators: validation and the calls of their launchers.  See include/ucd_seq.h for the contract.
-#include "ucd_seq.h"
+// C-ABI of the sequence operators: validation and the calls of their launchers.  See include/ucd_seq.h and include/ucd_mix.h for the contract.
+#include "ucd_mix.h"
 
 #include <algorithm>
 #include <cmath>

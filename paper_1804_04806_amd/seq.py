@@ -1,5 +1,5 @@
-"""ctypes binding of the sequence operators: the same entry points as include/ucd_seq.h, argument
-marshalling only.  Device buffers are torch tensors (their ``data_ptr()``), raw integer addresses or
+"""ctypes binding of the sequence operators: the same entry points as include/ucd_seq.h and
+include/ucd_mix.h, argument marshalling only.  Device buffers are torch tensors (their ``data_ptr()``), raw integer addresses or
 None; the library is the one ``ucd.lib()`` loads.  Kernels are launched on the current device, which has to be the
 buffers', and by default on its current stream.
 """
@@ -15,6 +15,8 @@ EXPORTS = [
     "ucd_group_norm_workspace_size", "ucd_group_norm_fwd", "ucd_group_norm_bwd",
     "ucd_causal_conv_workspace_size", "ucd_causal_conv_fwd", "ucd_causal_conv_bwd", "ucd_causal_conv_step",
     "ucd_scan_workspace_size", "ucd_scan_saved_size", "ucd_scan_fwd", "ucd_scan_bwd", "ucd_scan_step",
+]
+MIX_EXPORTS = [
     "ucd_linear_attention_workspace_size", "ucd_linear_attention_saved_size", "ucd_linear_attention_fwd",
     "ucd_linear_attention_bwd", "ucd_linear_attention_step",
     "ucd_gated_projection_workspace_size", "ucd_gated_projection_saved_size", "ucd_gated_projection_fwd",

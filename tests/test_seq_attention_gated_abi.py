@@ -1,5 +1,9 @@
 """Linear attention and gated projection without a GPU: what the entry points refuse (on the host, before anything is launched; the
 addresses below are never read), the sizes that they ask for, and the oracle's gradients against differences."""
+import ctypes
+import os
+import re
+
 import numpy as np
 import pytest
 
@@ -10,6 +14,15 @@ P = 1 << 20   # an aligned address
 ATTENTION = dict(B=2, L=3, H=4, Hk=2, Dk=8, Dv=16)
 GATED = dict(M=100, D=16, F=24)
 BIG = dict(saved_bytes=1 << 40, ws=P, ws_bytes=1 << 40)
+
+
+def test_every_declared_symbol_is_exported():
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    text = re.sub(r"/\*.*?\*/", "", open(os.path.join(root, "include", "ucd_mix.h")).read(), flags=re.S)
+    names = sorted(set(re.findall(r"\b(ucd_[a-z_0-9]+)\s*\(", text)))
+    assert names == sorted(seq.MIX_EXPORTS)
+    lib = ctypes.CDLL(ucd.LIB_PATH)
+    assert all(hasattr(lib, n) and hasattr(seq, n) for n in names)
 
 
 def refused(status, call, *args, **kw):
