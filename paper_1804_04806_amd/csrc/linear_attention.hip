@@ -13,10 +13,14 @@
 // few heads are cut into segments: their own states first, then the states at their starts, then all segments at once.
 //
 // The gradient of a decay is that of all paths that cross it: pairs of tokens within the chunk, tokens with the states before and behind it, and the
-// state that passes through:  dl_u = sum_{s < u <= t} W[t, s] + sum_{t >= u} a_t + sum_{s < u} b_s + c,
-//   W = scale (q k^T) o (dy v^T) o D,  a_t = q_t . (dq_t's part of S_in),  b_s = k_s . (dk_s's part of dS_out),  c = e^{G_C} <S_in, dS_out>.
-// Sums over whole sequences of q_t . dq_t - k_t . dk_t would be the same in exact arithmetic, but lose in their differences what the paths that do not
-// cross the token leave of rounding.
+// state that passes through.  With W[t, s] = scale (q_t . k_s) (dy_t . v_s) D,
+//   dl_u = sum_{s < u <= t} W[t, s] + sum_{t >= u} a_t + sum_{s < u} b_s + c,
+//   a_t = q_t . (dq_t's part of S_in),  b_s = k_s . (dk_s's part of dS_out),  c = e^{G_C} <S_in, dS_out>.
+// A_t = q_t . dq_t is a_t and W's row, B_s = k_s . dk_s is b_s and W's column, so that
+//   dl_u = sum_{t >= u} (A_t - (B_t - b_t)) + sum_{s < u} b_s + c.
+// A pair that does not cross u is in a row and in a column, of the same product rounded to the same 16 bits: what is left of it is rounding of 32 bits.
+// Sums of A - B over whole sequences would be the same as this in exact arithmetic, but the states' roundings are not the same on both sides.  (Pairs
+// in a kernel of their own read all inputs again, 59 us of 526 for 8 x 2048 tokens of 16 heads of 128.)
 #include <algorithm>
 
 #include "linear_attention.hpp"
@@ -56,81 +60,10 @@ hipError_t join_states(const Mix &p, hipStream_t s)
 namespace {
 using namespace attention;
 
-// sum_{s < t} W[t, s] - sum_{t > s} W[t, s] of the same token, for every token of a chunk: to pairs (B, H, L).
-struct Pairs {
-    Rows q, k, v, dy;
-    float scale;
-    Decays decays;
-    const int32_t *lengths;
-    int B, L, H;
-    float *out;
-};
-
-template <class T, int DK, int DV, bool WHOLE>
-__global__ __launch_bounds__(256) void pairs_kernel(Pairs p)
-{
-    typedef Mma<T> M;
-    constexpr int WIDE = DK > DV ? DK : DV;
-    __shared__ __attribute__((aligned(16))) char lds_a[TileLds<T, WIDE>::BYTES], lds_b[TileLds<T, WIDE>::BYTES];
-    __shared__ float w[kChunk][kChunk + 1];
-    __shared__ ChunkDecays dec;
-    __shared__ float parts[256];
-    const int chunks = (p.L + kChunk - 1) / kChunk;
-    const unsigned place = xcd_place();
-    const int head = place % p.H, chunk = place / p.H % chunks, seq = place / p.H / chunks;
-    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), row = lane % 32, half = lane / 32;
-    const int n = p.lengths ? max(0, min(p.L, p.lengths[seq])) : p.L, first = chunk * kChunk;
-    float *out = p.out + ((long)seq * p.H + head) * p.L + first;
-    Fetch<T, DK, WHOLE, 256> fq, fk;
-    Fetch<T, DV, WHOLE, 256> fv, fo;
-    auto load = [&](auto &f, const Rows &r) {
-        f.init(r.width, r.l * sizeof(T), false);
-        f.load(r.template at<T>(seq, head) + first * r.l, r.l * sizeof(T), n - first);
-    };
-    auto store = [&](const auto &f, const Rows &r, char *to) { f.store(to, r.template at<T>(seq, head) + first * r.l); };
-    load(fq, p.q);
-    load(fk, p.k);
-    load(fo, p.dy);
-    load(fv, p.v);
-    const int t0 = wave % 2 * 32, s0 = wave / 2 * 32, t = t0 + row;
-    f32x16 acc{}, acc2{};
-    if (wave == 0) dec.set(first + lane < n ? p.decays.get<T>(seq, head, first + lane) : 0.f, 1.f, 1.f);
-    store(fq, p.q, lds_a);
-    store(fk, p.k, lds_b);
-    lds_barrier();
-    if (s0 <= t0)
-#pragma unroll
-        for (int k = 0; k < DK; k += M::K) acc = M::product(M::template along<DK>(lds_b, s0, k), M::template along<DK>(lds_a, t0, k), acc);
-    lds_barrier();
-    store(fo, p.dy, lds_a);
-    store(fv, p.v, lds_b);
-    lds_barrier();
-    if (s0 <= t0)
-#pragma unroll
-        for (int k = 0; k < DV; k += M::K) acc2 = M::product(M::template along<DV>(lds_b, s0, k), M::template along<DV>(lds_a, t0, k), acc2);
-#pragma unroll
-    for (int r = 0; r < 16; ++r) {
-        const int s = s0 + 8 * (r / 4) + 4 * half + r % 4;
-        const float d = ChunkDecays::pair<float>(dec.hi[t], dec.lo[t], dec.hi[s], dec.lo[s]);
-        w[t][s] = s < t ? p.scale * acc[r] * acc2[r] * d : 0.f;
-    }
-    lds_barrier();
-    // four threads to a token: half of its row, half of its column
-    const int token = threadIdx.x % 64, part = threadIdx.x / 64;
-    float sum = 0.f;
-    for (int i = 0; i < 32; ++i) {
-        const int o = part % 2 * 32 + i;
-        sum += part < 2 ? w[token][o] : -w[o][token];
-    }
-    parts[threadIdx.x] = sum;
-    lds_barrier();
-    if (threadIdx.x < 64 && first + token < p.L) out[token] = (parts[token] + parts[64 + token]) + (parts[128 + token] + parts[192 + token]);
-}
-
-// dg of a chunk's tokens, one lane each: sums of pairs and a from the token to the chunk's end, of b before it, and c
+// dg of a chunk's tokens, one lane each: sums of A - (B - b) from the token to the chunk's end, of b before it, and c.  A, B and b are `planes` sums each
 template <class T>
-__global__ __launch_bounds__(64) void decay_gradient_kernel(const float *pairs, const float *a, const float *b, const float *c, int tiles_a, int B, int L,
-                                                            int H, const int32_t *lengths, T *dg, long g_b, long g_l)
+__global__ __launch_bounds__(64) void decay_gradient_kernel(const float *A, const float *B_, const float *b, const float *c, int planes, int tiles, int B,
+                                                            int L, int H, const int32_t *lengths, T *dg, long g_b, long g_l)
 {
     const int chunks = (L + kChunk - 1) / kChunk;
     const long tasks = (long)B * H * chunks, plane = (long)B * H * L;
@@ -141,13 +74,16 @@ __global__ __launch_bounds__(64) void decay_gradient_kernel(const float *pairs, 
         const int n = lengths ? max(0, min(L, lengths[seq])) : L;
         float ahead = 0.f, behind = 0.f, through = 0.f;
         if (t < n) {
-            ahead = pairs[sh * L + t];
-            for (int j = 0; j < tiles_a; ++j) {
-                ahead += a[j * plane + sh * L + t];
-                behind += b[j * plane + sh * L + t];
+            float crossing = 0.f;
+            for (int j = 0; j < planes; ++j) {
+                const long at = j * plane + sh * L + t;
+                ahead += A[at];
+                crossing += B_[at] - b[at];
+                behind += b[at];
             }
+            ahead -= crossing;
         }
-        for (int j = 0; j < tiles_a; ++j) through += c[((long)j * B * H + sh) * chunks + chunk];
+        for (int j = 0; j < tiles; ++j) through += c[((long)j * B * H + sh) * chunks + chunk];
 #pragma unroll
         for (int d = 1; d < 64; d *= 2) {
             const float up = __shfl_down(ahead, d), down = __shfl_up(behind, d);
@@ -233,11 +169,11 @@ __global__ __launch_bounds__(256) void attention_step_kernel(StepParams p)
 // ---- plans ---------------------------------------------------------------------------------------------------------
 
 // Segments of a walk: as many as fill the card where there are few heads, of one chunk at least.  A segment more is a walk over its keys for its own state.
-void segments_of(int B, int L, int H, int &segments, int &per)
+void segments_of(int B, int L, int H, bool f32, int &segments, int &per)
 {
-    constexpr long kFit = 512;       // workgroups that the card has at once
+    const long fit = f32 ? 256 : 512;       // workgroups that the card has at once, one or two on a compute unit
     const long have = (long)B * H, chunks = std::max(1, chunks_of(L));
-    const long want = std::max(1l, std::min(kFit / std::max(1l, have), chunks));
+    const long want = std::max(1l, std::min(fit / std::max(1l, have), chunks));
     per = (int)((chunks + want - 1) / want);
     segments = (int)((chunks + per - 1) / per);
 }
@@ -245,7 +181,7 @@ void segments_of(int B, int L, int H, int &segments, int &per)
 struct Layout {
     int segments, per;
     size_t starts, decay;
-    size_t pairs, a, b, c, keep, heads, bytes;
+    size_t a, b, all_b, c, keep, heads, bytes;
 };
 
 size_t state_size(const ucd_linear_attention_t &d) { return (size_t)d.B * d.H * d.Dk * d.Dv; }
@@ -260,7 +196,7 @@ Layout layout_of(const ucd_linear_attention_t &d, int dir)
         return here;
     };
     const size_t esize = d.dtype == 1 ? 2 : 4;
-    segments_of(d.B, d.L, d.H, l.segments, l.per);
+    segments_of(d.B, d.L, d.H, d.dtype == 0, l.segments, l.per);
     const size_t bh = (size_t)d.B * d.H;
     if (l.segments > 1) {
         l.starts = take(l.segments * state_size(d) * 4);
@@ -269,25 +205,16 @@ Layout layout_of(const ucd_linear_attention_t &d, int dir)
     if (dir == UCD_SEQ_BWD) {
         const int cols = cols_of(d.Dv, d.Dk, d.dtype == 0);      // of dq's and dk's walks
         const size_t tiles = tiles_of(d.Dk, cols);
-        l.pairs = take(bh * d.L * 4);
-        l.a = take(tiles * bh * d.L * 4);
-        l.b = take(tiles * bh * d.L * 4);
+        const size_t planes = tiles * (cols / 32);
+        l.a = take(planes * bh * d.L * 4);
+        l.b = take(planes * bh * d.L * 4);
+        l.all_b = take(planes * bh * d.L * 4);
         l.c = take(tiles * bh * chunks_of(d.L) * 4);
         l.keep = take(tiles * bh * chunks_of(d.L) * cols * (d.Dv > 64 ? 128 : 64) * esize);
         if (d.H != d.Hk) l.heads = take(bh * d.L * d.Dk * 4);
     }
     l.bytes = at;
     return l;
-}
-
-template <class T, bool WHOLE>
-hipError_t run_pairs(const Pairs &r, unsigned grid, hipStream_t s)
-{
-    if (r.k.width > 64 && r.v.width > 64) pairs_kernel<T, 128, 128, WHOLE><<<grid, 256, 0, s>>>(r);
-    else if (r.k.width > 64) pairs_kernel<T, 128, 64, WHOLE><<<grid, 256, 0, s>>>(r);
-    else if (r.v.width > 64) pairs_kernel<T, 64, 128, WHOLE><<<grid, 256, 0, s>>>(r);
-    else pairs_kernel<T, 64, 64, WHOLE><<<grid, 256, 0, s>>>(r);
-    return hipGetLastError();
 }
 
 Mix mix_base(const ucd_linear_attention_t &d, const ucd_linear_attention_in_t &in)
@@ -405,14 +332,14 @@ hipError_t bwd(const ucd_linear_attention_t &d, const ucd_linear_attention_in_t 
     // dk: dv's states, transposed
     b.state_in = dstate_out;
     b.starts = p.starts;
-    b.dots = decays ? (float *)(ws + l.b) : nullptr;
+    b.dots = decays ? (float *)(ws + l.all_b) : nullptr;
+    b.state_dots = (float *)(ws + l.b);
     if ((e = heads(b, grad.k, d.k_b, d.k_l, true)) != hipSuccess) return e;
     if (!decays || d.L == 0) return hipSuccess;
-    Pairs r{q, k, v, o, d.scale, a.decays, in.lengths, d.B, d.L, d.H, (float *)(ws + l.pairs)};
-    const unsigned grid = (unsigned)((long)d.B * d.H * chunks_of(d.L));
-    if ((e = whole ? run_pairs<T, true>(r, grid, s) : run_pairs<T, false>(r, grid, s)) != hipSuccess) return e;
-    decay_gradient_kernel<T><<<std::min(grid, 1u << 20), 64, 0, s>>>(r.out, a.dots, b.dots, a.passes, b.tiles, d.B, d.L, d.H, in.lengths, (T *)grad.g,
-                                                                    d.g_b, d.g_l);
+    const unsigned grid = (unsigned)std::min((long)d.B * d.H * chunks_of(d.L), 1l << 20);
+    const int planes = b.tiles * (cols_of(d.Dv, d.Dk, d.dtype == 0) / 32);
+    decay_gradient_kernel<T><<<grid, 64, 0, s>>>(a.dots, b.dots, b.state_dots, a.passes, planes, b.tiles, d.B, d.L, d.H, in.lengths, (T *)grad.g, d.g_b,
+                                                 d.g_l);
     return hipGetLastError();
 }
 

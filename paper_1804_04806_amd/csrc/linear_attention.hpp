@@ -389,7 +389,7 @@ struct Mix {
     float *starts;               // (segments, B, H, rows, columns) with the strides of state_in, or null
     bool started;                // starts are there already, from a walk over the same states
     float *segment_decay;        // (segments, B, H)
-    float *dots;                 // (column tiles, B, H, L), or null
+    float *dots, *state_dots;    // (column tiles' waves, B, H, L): rows of `dot` with the outputs and, backward, with the state's part of them; or null
     void *chunk_states;          // states at the chunks' starts, by workgroup, chunk and thread
     float *passes;               // (column tiles, B, H, chunks): c
     int tiles;

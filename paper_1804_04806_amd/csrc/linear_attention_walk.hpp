@@ -35,7 +35,7 @@ enum { OUTPUTS, DECAYS, STATES };
 // weighted for the state's update, each wave its own columns, which stay in registers for the pairs' products.  Two barriers a chunk: behind the tiles,
 // and behind the pairs, which the waves share out.
 template <class T, int DK, int COLS, bool REV, int FOR, bool WHOLE, bool OUT32, bool EXACT>
-__global__ __launch_bounds__(2 * COLS, sizeof(T) == 2 ? 256 / COLS : 128 / COLS) void mix_kernel(Mix p)
+__global__ __launch_bounds__(2 * COLS, sizeof(T) == 2 && (COLS == 128 || DK == 64) ? 2 : 1) void mix_kernel(Mix p)
 {
     constexpr int THREADS = 2 * COLS, WAVES = COLS / 32;
     constexpr bool OUT = FOR != STATES, DG = FOR == DECAYS;
@@ -48,7 +48,7 @@ __global__ __launch_bounds__(2 * COLS, sizeof(T) == 2 ? 256 / COLS : 128 / COLS)
     constexpr int ST = DK / 32, KS = kChunk / M::K;      // tiles of a wave's state, 32 by 32; reduction steps over a chunk's tokens
     __shared__ __attribute__((aligned(16))) char lds_q[OUT ? TQ::BYTES : 16], lds_k[TQ::BYTES], lds_v[TV::BYTES], lds_p[OUT ? TP::BYTES : 16];
     __shared__ ChunkDecays decays[2];
-    __shared__ float lds_dot[WAVES][kChunk], lds_pass[WAVES];
+    __shared__ float lds_pass[WAVES];
     // a wave's outputs on their way to rows: 32 rows of 64 bytes (and what they are multiplied with from rows).  Stored from the sums as they lie, 16 bytes
     // each of 32 rows, they took 2900 cycles of a chunk's 13000
     constexpr int TURN_ROW = 80;
@@ -139,6 +139,57 @@ __global__ __launch_bounds__(2 * COLS, sizeof(T) == 2 ? 256 / COLS : 128 / COLS)
     };
     const long d_l = DG ? p.dot.l * (long)sizeof(T) : 0;
     const T *dp = DG ? p.dot.template at<T>(at.seq, at.head) + col0 : nullptr;
+    // Dots of the outputs with rows of `dot` (what the output is the gradient of), for the decays' gradient: rows' pieces of 16 bytes, and the sums over a
+    // wave's columns, one plane for each.  A second read of the pieces, from the cache, costs less than their registers.
+    constexpr int DOT_PASSES = (int)sizeof(T) / 2, DOT_COLS = 64 / (int)sizeof(T), DOT_PER = 16 / (int)sizeof(T);
+    u32x4 dots[DG ? 2 : 1][DG ? DOT_PASSES : 1][DG ? 2 : 1];
+    auto load_dots = [&](long tok0) {
+        const auto rsrc = buffer_of((const char *)dp + tok0 * d_l, chunk_bytes(d_l, n - (int)tok0));
+#pragma unroll
+        for (int tb = 0; tb < 2; ++tb)
+#pragma unroll
+            for (int pass = 0; pass < DOT_PASSES; ++pass)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const int t = 32 * tb + 16 * i + turn_row, t_at = REV ? kChunk - 1 - t : t;
+                    const int x = x0 + pass * DOT_COLS + lane % 4 * DOT_PER, have = cols - x;
+                    const uint32_t o = (uint32_t)(t_at * d_l) + x * (uint32_t)sizeof(T);
+                    u32x4 &d = dots[DG ? tb : 0][DG ? pass : 0][DG ? i : 0];
+                    if (WHOLE) {
+                        d = __builtin_amdgcn_raw_buffer_load_b128(rsrc, have > 0 ? o : kOut, 0, 0);
+                    } else {
+                        Pack<T, DOT_PER> v;
+#pragma unroll
+                        for (int e = 0; e < DOT_PER; ++e) {
+                            if constexpr (sizeof(T) == 4) v.v[e] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rsrc, e < have ? o + 4 * e : kOut, 0, 0));
+                            else v.v[e] = __builtin_bit_cast(T, (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(rsrc, e < have ? o + 2 * e : kOut, 0, 0));
+                        }
+                        d = __builtin_bit_cast(u32x4, v);
+                    }
+                }
+    };
+    auto put_dot = [&](float *to, int c, int tb, const f32x16 &y) {
+        float sum = 0.f;
+#pragma unroll
+        for (int pass = 0; pass < DOT_PASSES; ++pass) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) lds_put(turn + (16 * i + turn_row) * TURN_ROW + turn_at, dots[DG ? tb : 0][DG ? pass : 0][DG ? i : 0]);
+            wave_lds_order();
+            constexpr int QUADS = 4 / DOT_PASSES;
+#pragma unroll
+            for (int r = 0; r < QUADS; ++r) {
+                const auto v = lds_get<Pack<T, 4>>(turn + row * TURN_ROW + (8 * r + 4 * half) * (int)sizeof(T));
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sum = fmaf(to_f(v.v[e]), y[4 * (pass * QUADS + r) + e], sum);
+            }
+            wave_lds_order();
+        }
+        float other = sum;
+        swap_halves(sum, other);
+        sum += other;
+        const int t = token(c, 32 * tb + row);
+        if (half == 0 && t < p.L) to[(((long)(at.tile * WAVES + wave) * p.B + at.seq) * p.H + at.head) * p.L + t] = sum;
+    };
     if (c0 < c1) {
         fetch_decay(c0);
         set_decays(c0);
@@ -157,34 +208,7 @@ __global__ __launch_bounds__(2 * COLS, sizeof(T) == 2 ? 256 / COLS : 128 / COLS)
 #pragma unroll
             for (int i = 0; i < PIECES; ++i) before[DG && REV ? i : 0] = from[i * THREADS];
         }
-        // what the part of the first state is multiplied with: its rows' pieces of 16 bytes
-        constexpr int DOT_PASSES = (int)sizeof(T) / 2, DOT_COLS = 64 / (int)sizeof(T), DOT_PER = 16 / (int)sizeof(T);
-        u32x4 dots[DG ? 2 : 1][DG ? DOT_PASSES : 1][DG ? 2 : 1];
-        if (DG) {
-            const auto rsrc = buffer_of((const char *)dp + tok0 * d_l, chunk_bytes(d_l, n - (int)tok0));
-#pragma unroll
-            for (int tb = 0; tb < 2; ++tb)
-#pragma unroll
-                for (int pass = 0; pass < DOT_PASSES; ++pass)
-#pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        const int t = 32 * tb + 16 * i + turn_row, t_at = REV ? kChunk - 1 - t : t;
-                        const int x = x0 + pass * DOT_COLS + lane % 4 * DOT_PER, have = cols - x;
-                        const uint32_t o = (uint32_t)(t_at * d_l) + x * (uint32_t)sizeof(T);
-                        u32x4 &d = dots[DG ? tb : 0][DG ? pass : 0][DG ? i : 0];
-                        if (WHOLE) {
-                            d = __builtin_amdgcn_raw_buffer_load_b128(rsrc, have > 0 ? o : kOut, 0, 0);
-                        } else {
-                            Pack<T, DOT_PER> v;
-#pragma unroll
-                            for (int e = 0; e < DOT_PER; ++e) {
-                                if constexpr (sizeof(T) == 4) v.v[e] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rsrc, e < have ? o + 4 * e : kOut, 0, 0));
-                                else v.v[e] = __builtin_bit_cast(T, (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(rsrc, e < have ? o + 2 * e : kOut, 0, 0));
-                            }
-                            d = __builtin_bit_cast(u32x4, v);
-                        }
-                    }
-        }
+        if (DG && REV) load_dots(tok0);
         set_decays(c + 1);
         // Operands are read in batches ahead of their products: one by one each product would wait for its own.
         if (OUT) {
@@ -270,30 +294,10 @@ __global__ __launch_bounds__(2 * COLS, sizeof(T) == 2 ? 256 / COLS : 128 / COLS)
                 const float first = dec.first[32 * tb + row];
 #pragma unroll
                 for (int r = 0; r < 16; ++r) y[tb][r] *= first;
-                if (DG) {
-                    float sum = 0.f;
-#pragma unroll
-                    for (int pass = 0; pass < DOT_PASSES; ++pass) {
-#pragma unroll
-                        for (int i = 0; i < 2; ++i)
-                            lds_put(turn + (16 * i + turn_row) * TURN_ROW + turn_at, dots[DG ? tb : 0][DG ? pass : 0][DG ? i : 0]);
-                        wave_lds_order();
-                        constexpr int QUADS = 4 / DOT_PASSES;
-#pragma unroll
-                        for (int r = 0; r < QUADS; ++r) {
-                            const auto v = lds_get<Pack<T, 4>>(turn + row * TURN_ROW + (8 * r + 4 * half) * (int)sizeof(T));
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) sum = fmaf(to_f(v.v[e]), y[tb][4 * (pass * QUADS + r) + e], sum);
-                        }
-                        wave_lds_order();
-                    }
-                    float other = sum;
-                    swap_halves(sum, other);
-                    sum += other;
-                    if (half == 0) lds_dot[wave][32 * tb + row] = sum;
-                }
+                if (DG && REV) put_dot(p.state_dots, c, tb, y[tb]);
             }
         }
+        if (DG) load_dots(tok0);
         // the state behind the chunk
         const float whole = dec.whole;
 #pragma unroll
@@ -344,6 +348,10 @@ __global__ __launch_bounds__(2 * COLS, sizeof(T) == 2 ? 256 / COLS : 128 / COLS)
                 y[1] = M::product(own[k], pairs[k], y[1]);
                 if (k < KS / 2) y[0] = M::product(own[k], pairs[KS + k], y[0]);
             }
+            if (DG) {
+#pragma unroll
+                for (int tb = 0; tb < 2; ++tb) put_dot(p.dots, c, tb, y[tb]);
+            }
 #pragma unroll
             for (int tb = 0; tb < 2; ++tb) {
                 const auto rsrc = buffer_of(out + tok0 * o_l, chunk_bytes(o_l, p.L - (int)tok0));
@@ -381,13 +389,6 @@ __global__ __launch_bounds__(2 * COLS, sizeof(T) == 2 ? 256 / COLS : 128 / COLS)
                     }
                     wave_lds_order();
                 }
-            }
-            if (DG && threadIdx.x < kChunk) {
-                const int t = token(c, threadIdx.x);
-                float all = lds_dot[0][threadIdx.x];
-#pragma unroll
-                for (int i = 1; i < WAVES; ++i) all += lds_dot[i][threadIdx.x];
-                if (t < p.L) p.dots[(((long)at.tile * p.B + at.seq) * p.H + at.head) * p.L + t] = all;
             }
             if (DG && REV && threadIdx.x == 64) {
                 const int chunk = chunks - 1 - c;
