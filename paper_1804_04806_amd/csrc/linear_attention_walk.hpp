@@ -202,6 +202,7 @@ __global__ __launch_bounds__(2 * COLS, sizeof(T) == 2 && (COLS == 128 || DK == 6
         fk.store(lds_k, (const char *)kp + tok0 * k_l);
         fv.store(lds_v, (const char *)vp + tok0 * v_l);
         lds_barrier();
+        if (!OUT) fetch(c + 1);
         Frag before[DG && REV ? PIECES : 1];
         if (DG && REV) {
             const Frag *from = kept(c);
@@ -333,7 +334,7 @@ __global__ __launch_bounds__(2 * COLS, sizeof(T) == 2 && (COLS == 128 || DK == 6
             }
         }
         __builtin_amdgcn_sched_barrier(0);
-        fetch(c + 1);      // not before: its registers would be missing above
+        if (OUT) fetch(c + 1);      // not before: its registers would be missing above
         if (!OUT && threadIdx.x < 64) segment_decay += (double)dec.hi[63] + (double)dec.lo[63];
         lds_barrier();
         if (OUT) {
