@@ -400,6 +400,7 @@ __global__ __launch_bounds__(TILE::THREADS) void product_kernel(Problem p, Matri
 
 // dx's and the weights' products
 template <class T> using LargeAlong = Tile<T, 256, 256, 2, 4, 2, true, false, true>;
+template <class T> using MiddleAlong = Tile<T, 192, 256, 2, 4, 2, true, false, true>;
 template <class T> using SmallAlong = Tile<T, 128, 128, 2, 2, 2, true, false, true>;
 template <class T> using LargeAcross = Tile<T, 256, 256, 2, 4, 2, false, false, false>;
 template <class T> using SmallAcross = Tile<T, 128, 128, 2, 2, 2, false, false, false>;
@@ -432,24 +433,26 @@ unsigned grid_for(long n) { return (unsigned)std::min((n + 255) / 256, 1l << 16)
 
 constexpr int kUnits = 256;      // compute units
 
-// Tiles of 256 by 256, one to a unit, or of 128 by 128, two to a unit, whichever take less time in whole rounds (a round of small ones has half the work of
-// one of large ones, at about 0.7 of the rate); the reduction in parts of 8 steps at least where small ones are too few.
+// Tiles of 256 by 256 or 192 by 256, one to a unit, or of 128 by 128, two to a unit, whichever take least time in whole rounds; the reduction in parts of 8
+// steps at least where small ones are too few.  A round of the second has 3/4 of the first one's work, a round of small ones half of it at about 0.7 of the
+// rate (forward of 4096 x 1024 x 2816: two rounds of 256 by 256 65 us, two of 192 by 256 56 us).  Tiles of 192 are of operands along their rows alone.
 struct Shape {
-    bool large;
+    int side;      // rows of a tile
     int tiles_m, tiles_n, splits;
 };
 
-Shape shape_of(long m, long n, long steps)
+Shape shape_of(long m, long n, long steps, bool along)
 {
-    auto tiles = [&](long side) { return ((m + side - 1) / side) * ((n + side - 1) / side); };
+    auto tiles = [&](long rows, long cols) { return ((m + rows - 1) / rows) * ((n + cols - 1) / cols); };
     auto rounds = [](long t, long each) { return (double)((t + each - 1) / each); };
+    const double large = rounds(tiles(256, 256), kUnits), mid = rounds(tiles(192, 256), kUnits) * 0.75 / 0.95,
+                 small = rounds(tiles(128, 128), 2 * kUnits) * 0.5 / 0.7;
     Shape s;
-    const double large = rounds(tiles(256), kUnits), small = rounds(tiles(128), 2 * kUnits) * 0.5 / 0.7;
-    s.large = large <= small;
-    const int side = s.large ? 256 : 128;
-    s.tiles_m = (int)((m + side - 1) / side);
-    s.tiles_n = (int)((n + side - 1) / side);
-    s.splits = s.large ? 1 : (int)std::max(1l, std::min(2 * kUnits / tiles(128), steps / 8));
+    s.side = along && mid < large && mid <= small ? 192 : large <= small ? 256 : 128;
+    s.tiles_m = (int)((m + s.side - 1) / s.side);
+    const int cols = s.side == 128 ? 128 : 256;
+    s.tiles_n = (int)((n + cols - 1) / cols);
+    s.splits = s.side != 128 ? 1 : (int)std::max(1l, std::min(2 * kUnits / tiles(128, 128), steps / 8));
     return s;
 }
 
@@ -490,14 +493,14 @@ Layout layout_of(const ucd_gated_projection_t &d, int dir, bool x_aligned, bool 
     l.w_plane = round_up((long)d.F * l.width, 128);
     const long d_steps = (l.width + BK - 1) / BK * l.phases;
     if (dir == UCD_SEQ_FWD) {
-        l.fwd = shape_of(d.M, 2l * d.F, d_steps);
+        l.fwd = shape_of(d.M, 2l * d.F, d_steps, true);
         if (l.few) {
             l.bytes = 0;
             return l;
         }
     } else {
-        l.dx = shape_of(d.M, d.D, 2l * l.half / BK * l.phases);
-        l.dw = shape_of(2l * l.half, d.D, ((long)d.M + BK - 1) / BK * l.phases);
+        l.dx = shape_of(d.M, d.D, 2l * l.half / BK * l.phases, true);
+        l.dw = shape_of(2l * l.half, d.D, ((long)d.M + BK - 1) / BK * l.phases, false);
         l.dg_plane = (long)d.M * l.dg_row;
         l.dg = take((size_t)l.planes * l.dg_plane * 2);
     }
@@ -621,7 +624,8 @@ hipError_t fwd(const ucd_gated_projection_t &d, const void *x, const void *wg, c
     p.phases = l.phases;
     shape_into(p, l.fwd);
     float *part = p.splits > 1 ? (float *)(ws + l.part) : nullptr;
-    if (l.fwd.large) return forward<T, Tile<T, 256, 256, 2, 4, 2, true, true, true>>(p, o, part, s);
+    if (l.fwd.side == 256) return forward<T, Tile<T, 256, 256, 2, 4, 2, true, true, true>>(p, o, part, s);
+    if (l.fwd.side == 192) return forward<T, Tile<T, 192, 256, 2, 4, 2, true, true, true>>(p, o, part, s);
     return forward<T, Tile<T, 128, 128, 2, 2, 2, true, true, true>>(p, o, part, s);
 }
 
@@ -657,8 +661,9 @@ hipError_t bwd(const ucd_gated_projection_t &d, const void *x, const void *wg, c
     out.half = 1l << 40;
     out.cols = d.D;
     float *part = p.splits > 1 ? (float *)(ws + l.part) : nullptr;
-    e = l.dx.large ? multiply<T, LargeAlong<T>>(p, out, part, d.M, s)
-                   : multiply<T, SmallAlong<T>>(p, out, part, d.M, s);
+    e = l.dx.side == 256   ? multiply<T, LargeAlong<T>>(p, out, part, d.M, s)
+        : l.dx.side == 192 ? multiply<T, MiddleAlong<T>>(p, out, part, d.M, s)
+                           : multiply<T, SmallAlong<T>>(p, out, part, d.M, s);
     if (e != hipSuccess) return e;
     // [dWg; dWu] = dG^T x: both across
     p.m = og;
@@ -676,8 +681,8 @@ hipError_t bwd(const ucd_gated_projection_t &d, const void *x, const void *wg, c
     out.half = l.half;
     out.add = add;
     part = p.splits > 1 ? (float *)(ws + l.part) : nullptr;
-    return l.dw.large ? multiply<T, LargeAcross<T>>(p, out, part, 2l * l.half, s)
-                      : multiply<T, SmallAcross<T>>(p, out, part, 2l * l.half, s);
+    return l.dw.side == 256 ? multiply<T, LargeAcross<T>>(p, out, part, 2l * l.half, s)
+                            : multiply<T, SmallAcross<T>>(p, out, part, 2l * l.half, s);
 }
 
 GateOut gate_out(const ucd_gated_projection_t &d, void *y, float *saved)
