@@ -28,7 +28,7 @@ enum { UCD_ACT_GELU = 2 };
  *   y_t = scale q_t S_t.
  * decay (H) are constants of the heads, g the decays' own part for every token, both logarithms and
  * at most 0 together; without either (NULL) its term is left out.  What is below -80 counts as -80,
- * exp of which is as good as 0: -infinity forgets what was before the token.  Tokens are taken 64 at a
+ * exp of which is as good as 0: -infinity forgets what was before the token, and has no gradient.  Tokens are taken 64 at a
  * time, from a sequence's first on: a value that is not finite may reach all 64 outputs and gradients
  * around it, beside those of the formulas.  1 <= Dk, Dv <= 128 (wider heads of v are more heads of v to
  * one of q and k); Hk divides H; B, L >= 0.  Rows of q, k, v, g and y, and a token's stride of

@@ -16,7 +16,7 @@
 // state that passes through.  With W[t, s] = scale (q_t . k_s) (dy_t . v_s) D,
 //   dl_u = sum_{s < u <= t} W[t, s] + sum_{t >= u} a_t + sum_{s < u} b_s + c,
 //   a_t = q_t . (dq_t's part of S_in),  b_s = k_s . (dk_s's part of dS_out),  c = e^{G_C} <S_in, dS_out>.
-// A_t = q_t . dq_t is a_t and W's row, B_s = k_s . dk_s is b_s and W's column, so that
+// A_t = q_t . dq_t without W[t, t] is a_t and W's row, B_s = k_s . dk_s without W[s, s] is b_s and W's column, so that
 //   dl_u = sum_{t >= u} (A_t - (B_t - b_t)) + sum_{s < u} b_s + c.
 // A pair that does not cross u is in a row and in a column, of the same product rounded to the same 16 bits: what is left of it is rounding of 32 bits.
 // Sums of A - B over whole sequences would be the same as this in exact arithmetic, but the states' roundings are not the same on both sides.  (Pairs
@@ -63,7 +63,7 @@ using namespace attention;
 // dg of a chunk's tokens, one lane each: sums of A - (B - b) from the token to the chunk's end, of b before it, and c.  A, B and b are `planes` sums each
 template <class T>
 __global__ __launch_bounds__(64) void decay_gradient_kernel(const float *A, const float *B_, const float *b, const float *c, int planes, int tiles, int B,
-                                                            int L, int H, const int32_t *lengths, T *dg, long g_b, long g_l)
+                                                            int L, int H, const int32_t *lengths, Decays decays, T *dg, long g_b, long g_l)
 {
     const int chunks = (L + kChunk - 1) / kChunk;
     const long tasks = (long)B * H * chunks, plane = (long)B * H * L;
@@ -91,7 +91,9 @@ __global__ __launch_bounds__(64) void decay_gradient_kernel(const float *A, cons
             if (lane >= d) behind += down;
         }
         const float before = __shfl_up(behind, 1);
-        if (t < L) dg[seq * g_b + t * g_l + head] = from_f<T>(t < n ? ahead + (lane ? before : 0.f) + through : 0.f);
+        // a decay that forgets everything has none: what is left of sums around it is rounding
+        const bool real = t < n && !(decays.get<T>(seq, head, t) <= kLeast);
+        if (t < L) dg[seq * g_b + t * g_l + head] = from_f<T>(real ? ahead + (lane ? before : 0.f) + through : 0.f);
     }
 }
 
@@ -338,8 +340,8 @@ hipError_t bwd(const ucd_linear_attention_t &d, const ucd_linear_attention_in_t 
     if (!decays || d.L == 0) return hipSuccess;
     const unsigned grid = (unsigned)std::min((long)d.B * d.H * chunks_of(d.L), 1l << 20);
     const int planes = b.tiles * (cols_of(d.Dv, d.Dk, d.dtype == 0) / 32);
-    decay_gradient_kernel<T><<<grid, 64, 0, s>>>(a.dots, b.dots, b.state_dots, a.passes, planes, b.tiles, d.B, d.L, d.H, in.lengths, (T *)grad.g, d.g_b,
-                                                 d.g_l);
+    decay_gradient_kernel<T><<<grid, 64, 0, s>>>(a.dots, b.dots, b.state_dots, a.passes, planes, b.tiles, d.B, d.L, d.H, in.lengths, a.decays,
+                                                 (T *)grad.g, d.g_b, d.g_l);
     return hipGetLastError();
 }
 

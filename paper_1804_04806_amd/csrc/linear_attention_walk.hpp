@@ -107,12 +107,16 @@ __global__ __launch_bounds__(2 * COLS, sizeof(T) == 2 && (COLS == 128 || DK == 6
     fv.init(cols, v_l, REV);
     // of a chunk that is none nothing is read: loads and stores are the same ones for every chunk, so that a load's data is waited for without the stores
     // behind it
-    auto fetch = [&](int chunk) {
+    auto fetch_q = [&](int chunk) {
+        const long t = token0(chunk);
+        fq.load((const char *)qp + t * q_l, q_l, chunk < c1 ? n - (int)t : 0);
+    };
+    auto fetch = [&](int chunk, bool all) {
         const long t = token0(chunk);
         const int there = chunk < c1 ? n - (int)t : 0;
-        if (OUT) fq.load((const char *)qp + t * q_l, q_l, there);
         fk.load((const char *)kp + t * k_l, k_l, there);
         fv.load((const char *)vp + t * v_l, v_l, there);
+        if (OUT && all) fetch_q(chunk);
     };
     // the first wave sets the decays of the chunk that comes; those of the one behind it are on their way
     uint32_t raw_decay = 0;
@@ -143,38 +147,40 @@ __global__ __launch_bounds__(2 * COLS, sizeof(T) == 2 && (COLS == 128 || DK == 6
     // wave's columns, one plane for each.  A second read of the pieces, from the cache, costs less than their registers.
     constexpr int DOT_PASSES = (int)sizeof(T) / 2, DOT_COLS = 64 / (int)sizeof(T), DOT_PER = 16 / (int)sizeof(T);
     u32x4 dots[DG ? 2 : 1][DG ? DOT_PASSES : 1][DG ? 2 : 1];
-    auto load_dots = [&](long tok0) {
+    auto load_dots = [&](long tok0, int tb) {
         const auto rsrc = buffer_of((const char *)dp + tok0 * d_l, chunk_bytes(d_l, n - (int)tok0));
 #pragma unroll
-        for (int tb = 0; tb < 2; ++tb)
+        for (int pass = 0; pass < DOT_PASSES; ++pass)
 #pragma unroll
-            for (int pass = 0; pass < DOT_PASSES; ++pass)
+            for (int i = 0; i < 2; ++i) {
+                const int t = 32 * tb + 16 * i + turn_row, t_at = REV ? kChunk - 1 - t : t;
+                const int x = x0 + pass * DOT_COLS + lane % 4 * DOT_PER, have = cols - x;
+                const uint32_t o = (uint32_t)(t_at * d_l) + x * (uint32_t)sizeof(T);
+                u32x4 &d = dots[DG ? tb : 0][DG ? pass : 0][DG ? i : 0];
+                if (WHOLE) {
+                    d = __builtin_amdgcn_raw_buffer_load_b128(rsrc, have > 0 ? o : kOut, 0, 0);
+                } else {
+                    Pack<T, DOT_PER> v;
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const int t = 32 * tb + 16 * i + turn_row, t_at = REV ? kChunk - 1 - t : t;
-                    const int x = x0 + pass * DOT_COLS + lane % 4 * DOT_PER, have = cols - x;
-                    const uint32_t o = (uint32_t)(t_at * d_l) + x * (uint32_t)sizeof(T);
-                    u32x4 &d = dots[DG ? tb : 0][DG ? pass : 0][DG ? i : 0];
-                    if (WHOLE) {
-                        d = __builtin_amdgcn_raw_buffer_load_b128(rsrc, have > 0 ? o : kOut, 0, 0);
-                    } else {
-                        Pack<T, DOT_PER> v;
-#pragma unroll
-                        for (int e = 0; e < DOT_PER; ++e) {
-                            if constexpr (sizeof(T) == 4) v.v[e] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rsrc, e < have ? o + 4 * e : kOut, 0, 0));
-                            else v.v[e] = __builtin_bit_cast(T, (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(rsrc, e < have ? o + 2 * e : kOut, 0, 0));
-                        }
-                        d = __builtin_bit_cast(u32x4, v);
+                    for (int e = 0; e < DOT_PER; ++e) {
+                        if constexpr (sizeof(T) == 4) v.v[e] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rsrc, e < have ? o + 4 * e : kOut, 0, 0));
+                        else v.v[e] = __builtin_bit_cast(T, (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(rsrc, e < have ? o + 2 * e : kOut, 0, 0));
                     }
+                    d = __builtin_bit_cast(u32x4, v);
                 }
+            }
     };
-    auto put_dot = [&](float *to, int c, int tb, const f32x16 &y) {
+    auto put_dots = [&](int tb, int pass) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) lds_put(turn + (16 * i + turn_row) * TURN_ROW + turn_at, dots[DG ? tb : 0][DG ? pass : 0][DG ? i : 0]);
+        wave_lds_order();
+    };
+    // of rows 32 tb + 0 .. 31; `there`: their first pass is in `turn` already
+    auto dot = [&](float *to, int c, int tb, const f32x16 &y, bool there) {
         float sum = 0.f;
 #pragma unroll
         for (int pass = 0; pass < DOT_PASSES; ++pass) {
-#pragma unroll
-            for (int i = 0; i < 2; ++i) lds_put(turn + (16 * i + turn_row) * TURN_ROW + turn_at, dots[DG ? tb : 0][DG ? pass : 0][DG ? i : 0]);
-            wave_lds_order();
+            if (!there || pass) put_dots(tb, pass);
             constexpr int QUADS = 4 / DOT_PASSES;
 #pragma unroll
             for (int r = 0; r < QUADS; ++r) {
@@ -190,26 +196,43 @@ __global__ __launch_bounds__(2 * COLS, sizeof(T) == 2 && (COLS == 128 || DK == 6
         const int t = token(c, 32 * tb + row);
         if (half == 0 && t < p.L) to[(((long)(at.tile * WAVES + wave) * p.B + at.seq) * p.H + at.head) * p.L + t] = sum;
     };
+    // A token's pair with itself crosses no decay and may be all there is beside the rest: outputs get it behind the dots.  Elements of step k of it, or
+    // all others.
+    auto diagonal = [&](const Frag &f, int k, bool its) {
+        constexpr int WORDS = sizeof(Frag) / 4, PER = 4 / (int)sizeof(T), E = M::K / 2;
+        struct Words {
+            uint32_t w[WORDS];
+        };
+        Words v = __builtin_bit_cast(Words, f);
+        const int d = row - k * M::K % 32 - half * E;
+#pragma unroll
+        for (int i = 0; i < WORDS; ++i) {
+            const uint32_t of = PER == 2 ? 0xffffu << (d & 1) * 16 : 0xffffffffu, mask = (PER == 2 ? d >> 1 : d) == i ? of : 0u;
+            v.w[i] &= its ? mask : ~mask;
+        }
+        return __builtin_bit_cast(Frag, v);
+    };
     if (c0 < c1) {
         fetch_decay(c0);
         set_decays(c0);
-        fetch(c0);
+        fetch(c0, true);
     }
     for (int c = c0; c < c1; ++c) {
         const ChunkDecays &dec = decays[c & 1];
         const long tok0 = token0(c);
-        if (OUT) fq.template store<M::SUMS_ORDER>(lds_q, (const char *)qp + tok0 * q_l);
         fk.store(lds_k, (const char *)kp + tok0 * k_l);
         fv.store(lds_v, (const char *)vp + tok0 * v_l);
+        if (OUT) fq.template store<M::SUMS_ORDER>(lds_q, (const char *)qp + tok0 * q_l);
         lds_barrier();
-        if (!OUT) fetch(c + 1);
+        if (!OUT) fetch(c + 1, true);
         Frag before[DG && REV ? PIECES : 1];
         if (DG && REV) {
             const Frag *from = kept(c);
 #pragma unroll
             for (int i = 0; i < PIECES; ++i) before[DG && REV ? i : 0] = from[i * THREADS];
         }
-        if (DG && REV) load_dots(tok0);
+        if (DG) load_dots(tok0, 1);
+        if (DG && REV) load_dots(tok0, 0);
         set_decays(c + 1);
         // Operands are read in batches ahead of their products: one by one each product would wait for its own.
         if (OUT) {
@@ -258,7 +281,7 @@ __global__ __launch_bounds__(2 * COLS, sizeof(T) == 2 && (COLS == 128 || DK == 6
         f32x16 y[2] = {};
         if (OUT) {
             float pass = 0.f;
-            constexpr int BATCH = 4;      // steps at a time
+            constexpr int BATCH = DG && REV ? 2 : 4;      // steps at a time; registers are missing for more where the states before are there, too
             Frag fragq[2][BATCH][2];
             auto read = [&](int k) {
 #pragma unroll
@@ -295,10 +318,13 @@ __global__ __launch_bounds__(2 * COLS, sizeof(T) == 2 && (COLS == 128 || DK == 6
                 const float first = dec.first[32 * tb + row];
 #pragma unroll
                 for (int r = 0; r < 16; ++r) y[tb][r] *= first;
-                if (DG && REV) put_dot(p.state_dots, c, tb, y[tb]);
+                if (DG && REV) dot(p.state_dots, c, tb, y[tb], false);
             }
         }
-        if (DG) load_dots(tok0);
+        if (DG) {      // for what comes behind the pairs: rows 32 .. 63 wait in LDS (16 bits: there they are, if those behind the state were just multiplied)
+            if (!REV || DOT_PASSES > 1) put_dots(1, 0);
+            load_dots(tok0, 0);
+        }
         // the state behind the chunk
         const float whole = dec.whole;
 #pragma unroll
@@ -334,7 +360,7 @@ __global__ __launch_bounds__(2 * COLS, sizeof(T) == 2 && (COLS == 128 || DK == 6
             }
         }
         __builtin_amdgcn_sched_barrier(0);
-        if (OUT) fetch(c + 1);      // not before: its registers would be missing above
+        if (OUT) fetch(c + 1, !DG);      // not before: its registers would be missing above
         if (!OUT && threadIdx.x < 64) segment_decay += (double)dec.hi[63] + (double)dec.lo[63];
         lds_barrier();
         if (OUT) {
@@ -346,12 +372,18 @@ __global__ __launch_bounds__(2 * COLS, sizeof(T) == 2 && (COLS == 128 || DK == 6
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int k = 0; k < KS; ++k) {
-                y[1] = M::product(own[k], pairs[k], y[1]);
-                if (k < KS / 2) y[0] = M::product(own[k], pairs[KS + k], y[0]);
+                y[1] = M::product(own[k], DG && k >= KS / 2 ? diagonal(pairs[k], k, false) : pairs[k], y[1]);
+                if (k < KS / 2) y[0] = M::product(own[k], DG ? diagonal(pairs[KS + k], k, false) : pairs[KS + k], y[0]);
             }
             if (DG) {
 #pragma unroll
-                for (int tb = 0; tb < 2; ++tb) put_dot(p.dots, c, tb, y[tb]);
+                for (int tb = 2; tb-- > 0;) dot(p.dots, c, tb, y[tb], tb == 1);
+                fetch_q(c + 1);
+#pragma unroll
+                for (int k = 0; k < KS; ++k) {      // read again: registers are missing
+                    const int tb = k / (KS / 2);
+                    y[tb] = M::product(own[k], diagonal(M::template along<kChunk>(lds_p, 32 * tb, k * M::K), k, true), y[tb]);
+                }
             }
 #pragma unroll
             for (int tb = 0; tb < 2; ++tb) {

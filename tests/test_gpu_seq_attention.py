@@ -37,8 +37,8 @@ def inputs(shape, dtype, seed, decays="both", resets=False):
     v = {"q": values(rng, B, L, Hk, Dk, dtype=dtype), "k": values(rng, B, L, Hk, Dk, std=Dk ** -0.25, dtype=dtype),
          "v": values(rng, B, L, H, Dv, dtype=dtype), "dy": values(rng, B, L, H, Dv, std=0.3, dtype=dtype),
          "state": values(rng, B, H, Dk, Dv), "dstate": values(rng, B, H, Dk, Dv, std=0.3), "g": None, "decay": None}
-    if decays in ("token", "both"):
-        g = -np.exp(rng.uniform(np.log(1e-3), 0, (B, L, H)))
+    if decays in ("token", "both", "strong"):
+        g = -np.exp(rng.uniform(np.log(1e-3), 0, (B, L, H))) if decays != "strong" else -rng.uniform(6, 9, (B, L, H))
         if resets:
             g[rng.uniform(size=g.shape) < 0.02] = -np.inf
         v["g"] = np.asarray(values(rng, 1), np.float32) * 0 + g.astype(np.float32)
@@ -100,6 +100,9 @@ def run(shape, dtype, seed=0, decays="both", resets=False, lengths=False, state=
     ws_check()
     for name in grads:
         off(grads[name].get(), want[name], dtype, name, n)
+    if resets:      # what forgets everything has no gradient, exactly
+        forgotten = np.isneginf(v["g"])
+        assert forgotten.any() and not grads["g"].get()[forgotten].any()
     check(dfirst.cpu().numpy(), want["state"], 0, "dstate")
 
 
@@ -113,6 +116,13 @@ def test_against_oracle(shape, dtype):
 @pytest.mark.parametrize("decays", ["none", "head", "token"])
 def test_decays(decays, dtype):
     run((2, 140, 3, 3, 40, 64), dtype, 1, decays)
+
+
+@pytest.mark.parametrize("dtype", [0, 1])
+@pytest.mark.parametrize("shape", [(2, 140, 3, 3, 40, 64), (1, 70, 2, 1, 128, 128)], ids=str)
+def test_strong_decays(shape, dtype):
+    """Each token forgets all but a thousandth of those before it: what the decays' gradient is of is that much smaller than a token's own part."""
+    run(shape, dtype, 5, "strong")
 
 
 @pytest.mark.parametrize("dtype", [0, 1])
