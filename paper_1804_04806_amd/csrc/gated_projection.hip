@@ -69,25 +69,39 @@ __device__ __forceinline__ void store_planes(bf16_t *to, long plane, const float
     for (int i = 0; i < Planes<T>::N; ++i) *reinterpret_cast<Pack<bf16_t, 8> *>(to + i * plane) = p[i];
 }
 
-// rows x cols elements, rows `stride` apart -> planes of rows of `width`, a multiple of 8 from cols on, filled up with 0
+// rows x cols elements, rows `stride` apart -> planes of rows of `width`, a multiple of 8 from cols on, filled up with 0.  Up to three matrices in a launch,
+// grid.y: of small ones most of a copy's 5 us is its launch.
+struct Copy {
+    const void *from;
+    long stride, rows, plane;
+    bf16_t *to;
+};
+struct Copies {
+    Copy c[3];
+    int count, cols, width;
+};
+
 template <class T>
-__global__ __launch_bounds__(256) void copy_rows_kernel(const T *from, long stride, long rows, int cols, bf16_t *to, int width, long plane)
+__global__ __launch_bounds__(256) void copy_rows_kernel(Copies all)
 {
-    const int packs = width / 8;
-    for (long i = blockIdx.x * 256l + threadIdx.x; i < rows * packs; i += gridDim.x * 256l) {
-        const long row = i / packs;
-        const int c = (int)(i % packs) * 8, have = min(8, cols - c);
-        const T *src = from + row * stride + c;
+    const Copy &p = all.c[blockIdx.y];
+    const int packs = all.width / 8;
+    const long size = p.rows * packs;
+    const bool small = size <= 0x7fffffffl;
+    for (long i = blockIdx.x * 256l + threadIdx.x; i < size; i += gridDim.x * 256l) {
+        const long row = small ? (long)((uint32_t)i / (uint32_t)packs) : i / packs;
+        const int c = (int)(i - row * packs) * 8, have = min(8, all.cols - c);
+        const T *src = (const T *)p.from + row * p.stride + c;
         float v[8];
         if (have == 8) {
-            const Pack<T, 8> p = loose_load<T, 8>(src);
+            const Pack<T, 8> r = loose_load<T, 8>(src);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = to_f(p.v[j]);
+            for (int j = 0; j < 8; ++j) v[j] = to_f(r.v[j]);
         } else {
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[j] = j < have ? to_f(src[j]) : 0.f;
         }
-        store_planes<T>(to + row * width + c, plane, v);
+        store_planes<T>(p.to + row * all.width + c, p.plane, v);
     }
 }
 
@@ -524,19 +538,11 @@ Layout layout_of(const ucd_gated_projection_t &d, int dir, bool x_aligned, bool 
 
 bool aligned16(const void *p) { return ((uintptr_t)p & 15u) == 0; }
 
-template <class T>
-hipError_t copy_rows(const void *from, long stride, long rows, int cols, bf16_t *to, int width, long plane, hipStream_t s)
-{
-    copy_rows_kernel<T><<<grid_for(rows * (width / 8)), 256, 0, s>>>((const T *)from, stride, rows, cols, to, width, plane);
-    return hipGetLastError();
-}
-
 // x and the weights as operands, copied where they have to be
 template <class T>
 hipError_t operands(const ucd_gated_projection_t &d, const Layout &l, const void *x, const void *wg, const void *wu, char *ws, Operand &ox, Operand &ow,
                     hipStream_t s)
 {
-    hipError_t e = hipSuccess;
     ox.p[0] = ox.p[1] = (const bf16_t *)x;
     ox.stride = d.x_m;
     ow.p[0] = (const bf16_t *)wg;
@@ -544,19 +550,27 @@ hipError_t operands(const ucd_gated_projection_t &d, const Layout &l, const void
     ow.stride = d.D;
     ox.plane = l.x_plane;
     ow.plane = l.w_plane;
+    Copies all{};
+    all.cols = d.D;
+    all.width = l.width;
     if (l.copy_x) {
-        ox.p[0] = ox.p[1] = (bf16_t *)(ws + l.x);
+        bf16_t *to = (bf16_t *)(ws + l.x);
+        ox.p[0] = ox.p[1] = to;
         ox.stride = l.width;
-        if ((e = copy_rows<T>(x, d.x_m, d.M, d.D, (bf16_t *)(ws + l.x), l.width, l.x_plane, s)) != hipSuccess) return e;
+        all.c[all.count++] = Copy{x, (long)d.x_m, d.M, l.x_plane, to};
     }
     if (l.copy_w) {
-        ow.p[0] = (bf16_t *)(ws + l.wg);
-        ow.p[1] = (bf16_t *)(ws + l.wu);
+        bf16_t *gate = (bf16_t *)(ws + l.wg), *up = (bf16_t *)(ws + l.wu);
+        ow.p[0] = gate;
+        ow.p[1] = up;
         ow.stride = l.width;
-        if ((e = copy_rows<T>(wg, d.D, d.F, d.D, (bf16_t *)(ws + l.wg), l.width, l.w_plane, s)) != hipSuccess) return e;
-        if ((e = copy_rows<T>(wu, d.D, d.F, d.D, (bf16_t *)(ws + l.wu), l.width, l.w_plane, s)) != hipSuccess) return e;
+        all.c[all.count++] = Copy{wg, d.D, d.F, l.w_plane, gate};
+        all.c[all.count++] = Copy{wu, d.D, d.F, l.w_plane, up};
     }
-    return e;
+    if (all.count == 0) return hipSuccess;
+    const long rows = std::max(l.copy_x ? (long)d.M : 0l, l.copy_w ? (long)d.F : 0l);
+    copy_rows_kernel<T><<<dim3(grid_for(rows * (l.width / 8)), (unsigned)all.count), 256, 0, s>>>(all);
+    return hipGetLastError();
 }
 
 template <class T, int MT, int CT, int AHEAD>
