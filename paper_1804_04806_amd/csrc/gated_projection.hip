@@ -470,6 +470,22 @@ Shape shape_of(long m, long n, long steps, bool along)
     return s;
 }
 
+// Up to 64 tokens: straight from memory (gated_few_kernel), whose work on the tokens grows with them, or tiles, which have a join.  bf16, 2048 -> 8192, 16, 32 and
+// 64 tokens: 16.9, 17.2 and 22.9 us against 16.9, 17.6 and 20.6; 4096 -> 16384: 58, 69 and 86 against 57, 59 and 63; 1024 -> 2816: 7.5, 7.4 and 9.5 against
+// 10.6, 10.7 and 11.3.  fp32 and what has to be copied first would be read and written before tiles.
+bool few_tokens(const ucd_gated_projection_t &d)
+{
+    const long weights = (long)d.D * d.F;
+    return d.M <= 16 || (d.M <= kFewTokens && (d.dtype == 0 || weights < (d.M <= 32 ? 1l << 25 : 1l << 24)));
+}
+
+// One row of tiles of 64 by 128, three to a unit.
+Shape low_shape(long n, long steps)
+{
+    const long tiles = (n + 127) / 128;
+    return Shape{64, 1, (int)tiles, (int)std::max(1l, std::min(3 * kUnits / tiles, steps / 8))};
+}
+
 // What a call has in its workspace, in bytes from its begin; a part of no bytes is not needed.
 struct Layout {
     int planes, phases;
@@ -494,9 +510,9 @@ Layout layout_of(const ucd_gated_projection_t &d, int dir, bool x_aligned, bool 
     l.width = (int)round_up(d.D, 8);
     l.half = (int)round_up(d.F, BK);
     l.dg_row = 2l * l.half + BK;      // rows that are a power of two apart meet in few of the caches' channels (dx of 8192 x 2048 x 8192: 870 TFLOP/s against 979)
-    l.few = d.M <= kFewTokens;
     l.copy_w = f32 || d.D % 8 != 0 || !w_aligned;
     l.copy_x = f32 || d.D % 8 != 0 || !x_aligned || (d.M > 1 && d.x_m % 8 != 0);
+    l.few = few_tokens(d) || (d.M <= kFewTokens && (l.copy_x || l.copy_w));
     size_t at = 0;
     auto take = [&](size_t n) {
         const size_t here = at;
@@ -507,7 +523,7 @@ Layout layout_of(const ucd_gated_projection_t &d, int dir, bool x_aligned, bool 
     l.w_plane = round_up((long)d.F * l.width, 128);
     const long d_steps = (l.width + BK - 1) / BK * l.phases;
     if (dir == UCD_SEQ_FWD) {
-        l.fwd = shape_of(d.M, 2l * d.F, d_steps, true);
+        l.fwd = d.M <= kFewTokens ? low_shape(2l * d.F, d_steps) : shape_of(d.M, 2l * d.F, d_steps, true);
         if (l.few) {
             l.bytes = 0;
             return l;
@@ -586,7 +602,9 @@ hipError_t few(const ucd_gated_projection_t &d, const void *x, const void *wg, c
 {
     const T *px = (const T *)x, *pg = (const T *)wg, *pu = (const T *)wu;
     const bool whole = d.D * sizeof(T) % 16 == 0 && (d.M == 1 || d.x_m * sizeof(T) % 4 == 0) && (((uintptr_t)x | (uintptr_t)wg | (uintptr_t)wu) & 3u) == 0;
-    const bool two = d.F >= 32 * 256;
+    // 32 columns to a workgroup read the tokens half as often as 16, but need enough of them: 2048 -> 8192, 32 and 64 tokens, 17.2 and 23.0 us against 19.7 and
+    // 28.9 (one token: 15.0, 4.5 TB/s)
+    const bool two = d.F >= 32 * kUnits;
     if (d.M <= 16) few_of<T, 1, 1, 4>(d, px, pg, pu, o, whole, s);
     else if (d.M <= 32 && two) few_of<T, 2, 2, 2>(d, px, pg, pu, o, whole, s);
     else if (d.M <= 32) few_of<T, 2, 1, 2>(d, px, pg, pu, o, whole, s);
@@ -640,6 +658,7 @@ hipError_t fwd(const ucd_gated_projection_t &d, const void *x, const void *wg, c
     float *part = p.splits > 1 ? (float *)(ws + l.part) : nullptr;
     if (l.fwd.side == 256) return forward<T, Tile<T, 256, 256, 2, 4, 2, true, true, true>>(p, o, part, s);
     if (l.fwd.side == 192) return forward<T, Tile<T, 192, 256, 2, 4, 2, true, true, true>>(p, o, part, s);
+    if (l.fwd.side == 64) return forward<T, Tile<T, 64, 128, 2, 2, 2, true, true, true>>(p, o, part, s);
     return forward<T, Tile<T, 128, 128, 2, 2, 2, true, true, true>>(p, o, part, s);
 }
 
@@ -711,7 +730,7 @@ using namespace gated;
 size_t gated_projection_ws_bytes(const ucd_gated_projection_t &d, int dir)
 {
     if (d.M == 0) return 0;
-    return layout_of(d, dir, false, false).bytes;
+    return std::max(layout_of(d, dir, false, false).bytes, layout_of(d, dir, true, true).bytes);      // few tokens that lie askew need none
 }
 
 size_t gated_projection_saved_bytes(const ucd_gated_projection_t &d) { return (size_t)d.M * 2 * wide_of(d) * 4; }
