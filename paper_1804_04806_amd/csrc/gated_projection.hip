@@ -197,7 +197,7 @@ __global__ __launch_bounds__(256) void gated_join_kernel(const float *part, int 
 //
 // Up to 64 tokens: the weights are read once, straight into the matrix instructions' operands, 16 bytes a lane.  A workgroup has 16 CT columns of both
 // sides and all tokens; its eight waves share the reduction out, two steps of 32 (16 for fp32), 128 bytes of a row, each by turns, and join their sums
-// in LDS.  Loads are without branches, AHEAD turns before their use.
+// in LDS.  Loads are without branches, AHEAD turns before their use.  Memory bounds it for few tokens, what is read of the tokens for many.
 
 constexpr int kFewWaves = 8, kFewTokens = 64;
 typedef float f32x4 __attribute__((ext_vector_type(4)));
@@ -470,13 +470,12 @@ Shape shape_of(long m, long n, long steps, bool along)
     return s;
 }
 
-// Up to 64 tokens: straight from memory (gated_few_kernel), whose work on the tokens grows with them, or tiles, which have a join.  bf16, 2048 -> 8192, 16, 32 and
-// 64 tokens: 16.9, 17.2 and 22.9 us against 16.9, 17.6 and 20.6; 4096 -> 16384: 58, 69 and 86 against 57, 59 and 63; 1024 -> 2816: 7.5, 7.4 and 9.5 against
-// 10.6, 10.7 and 11.3.  fp32 and what has to be copied first would be read and written before tiles.
+// Up to 64 tokens: straight from memory (gated_few_kernel), whose work on the tokens grows with them, or tiles, which have a join.  bf16, 17, 32 and 64 tokens,
+// us: 1024 -> 2816 6.1, 6.8 and 8.9 against 10.5, 10.8 and 11.5; 2048 -> 4096 8.9, 10.2 and 14.2 against 12.3, 12.5 and 13.1; 2048 -> 6144 15.5, 17.8 and 25.5
+// against 14.1, 14.7 and 16.0; 4096 -> 16384 57, 64 and 86 against 57, 59 and 63.  fp32 and what has to be copied first would be read and written before tiles.
 bool few_tokens(const ucd_gated_projection_t &d)
 {
-    const long weights = (long)d.D * d.F;
-    return d.M <= 16 || (d.M <= kFewTokens && (d.dtype == 0 || weights < (d.M <= 32 ? 1l << 25 : 1l << 24)));
+    return d.M <= 16 || (d.M <= kFewTokens && (d.dtype == 0 || (long)d.D * d.F <= 1l << 23));
 }
 
 // One row of tiles of 64 by 128, three to a unit.
@@ -603,13 +602,15 @@ hipError_t few(const ucd_gated_projection_t &d, const void *x, const void *wg, c
     const T *px = (const T *)x, *pg = (const T *)wg, *pu = (const T *)wu;
     const bool whole = d.D * sizeof(T) % 16 == 0 && (d.M == 1 || d.x_m * sizeof(T) % 4 == 0) && (((uintptr_t)x | (uintptr_t)wg | (uintptr_t)wu) & 3u) == 0;
     // 32 columns to a workgroup read the tokens half as often as 16, but need enough of them: 2048 -> 8192, 32 and 64 tokens, 17.2 and 23.0 us against 19.7 and
-    // 28.9 (one token: 15.0, 4.5 TB/s)
+    // 28.9 (two turns ahead)
     const bool two = d.F >= 32 * kUnits;
-    if (d.M <= 16) few_of<T, 1, 1, 4>(d, px, pg, pu, o, whole, s);
-    else if (d.M <= 32 && two) few_of<T, 2, 2, 2>(d, px, pg, pu, o, whole, s);
-    else if (d.M <= 32) few_of<T, 2, 1, 2>(d, px, pg, pu, o, whole, s);
-    else if (two) few_of<T, 4, 2, 2>(d, px, pg, pu, o, whole, s);
-    else few_of<T, 4, 1, 2>(d, px, pg, pu, o, whole, s);
+    // two turns ahead pay where there are many: one token, 8192 -> 8192, 49.5 us (5.4 TB/s) against 52.2; 2048 -> 8192, 13.4 against 12.6 (5.3)
+    if (d.M <= 16 && d.D * sizeof(T) <= 4096) few_of<T, 1, 1, 1>(d, px, pg, pu, o, whole, s);
+    else if (d.M <= 16) few_of<T, 1, 1, 2>(d, px, pg, pu, o, whole, s);
+    else if (d.M <= 32 && two) few_of<T, 2, 2, 1>(d, px, pg, pu, o, whole, s);
+    else if (d.M <= 32) few_of<T, 2, 1, 1>(d, px, pg, pu, o, whole, s);
+    else if (two) few_of<T, 4, 2, 1>(d, px, pg, pu, o, whole, s);
+    else few_of<T, 4, 1, 1>(d, px, pg, pu, o, whole, s);
     return hipGetLastError();
 }
 
