@@ -114,7 +114,8 @@ __global__ __launch_bounds__(256) void sum_heads_kernel(const float *part, int L
 
 // ---- single tokens -------------------------------------------------------------------------------------------------
 //
-// The state is read and written once, 4 bytes an element: memory bounds it.  A workgroup has 32 columns of a head's state, 8 lanes of 4 columns to a row.
+// The state is read and written once, 4 bytes an element: memory bounds it (128 sequences of 16 heads of 128 by 128: 57 us, 4.7 TB/s).  A workgroup has 32
+// columns of a head's state, 8 lanes of 4 columns to a row.
 
 struct StepParams {
     ucd_linear_attention_t d;
@@ -125,7 +126,8 @@ struct StepParams {
     int tiles;
 };
 
-template <class T>
+// WIDE: rows of whole packs of 4, read through a buffer, all of a thread's at once and none under a condition.
+template <class T, bool WIDE>
 __global__ __launch_bounds__(256) void attention_step_kernel(StepParams p)
 {
     __shared__ float sums[32][33];
@@ -139,22 +141,46 @@ __global__ __launch_bounds__(256) void attention_step_kernel(StepParams p)
     }
     const int shared = d.H / d.Hk;
     const T *q = (const T *)p.in.q + seq * d.q_b + (long)(head / shared) * d.Dk, *k = (const T *)p.in.k + seq * d.k_b + (long)(head / shared) * d.Dk;
-    float *s = p.state + ((long)slot * d.H + head) * d.Dk * d.Dv + x;
-    const Pack<T, 4> v = load_pack<false, T, 4>((const T *)p.in.v + seq * d.v_b + (long)head * d.Dv + x, have);
+    float *s = p.state + ((long)slot * d.H + head) * d.Dk * d.Dv;
+    const auto rsrc = buffer_of(s, (uint32_t)(d.Dk * d.Dv) * 4u);
+    constexpr int ROWS = 4;      // 128 of them at most
+    u32x4 held[WIDE ? ROWS : 1];
+    auto place = [&](int j) { return group + 32 * j < d.Dk && have > 0 ? ((group + 32 * j) * d.Dv + x) * 4u : kOut; };
+    if (WIDE)
+#pragma unroll
+        for (int j = 0; j < ROWS; ++j) held[WIDE ? j : 0] = __builtin_amdgcn_raw_buffer_load_b128(rsrc, place(j), 0, 0);
+    const Pack<T, 4> v = load_pack<WIDE, T, 4>((const T *)p.in.v + seq * d.v_b + (long)head * d.Dv + x, have);
     const float a = exp_full(p.decays.get<T>(seq, head, 0));
     Pack<float, 4> sum{};
-#pragma unroll 4
-    for (int i = group; i < d.Dk; i += 32) {
-        float *at = s + (long)i * d.Dv;
-        Pack<float, 4> h = have == 4 ? loose_load<float, 4>(at) : load_pack<false, float, 4>(at, have);
-        const float ki = to_f(k[i]), qi = to_f(q[i]);
+    auto move = [&](Pack<float, 4> &h, float ki, float qi) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             h.v[e] = fmaf(a, h.v[e], ki * to_f(v.v[e]));
             sum.v[e] = fmaf(qi, h.v[e], sum.v[e]);
         }
-        if (have == 4) loose_store<float, 4>(at, h);
-        else store_pack<false, float, 4>(at, h, have);
+    };
+    if constexpr (WIDE) {
+        float ks[ROWS], qs[ROWS];
+#pragma unroll
+        for (int j = 0; j < ROWS; ++j) {
+            const int i = group + 32 * j, there = min(i, d.Dk - 1);
+            ks[j] = to_f(k[there]);
+            qs[j] = i < d.Dk ? to_f(q[there]) : 0.f;
+        }
+#pragma unroll
+        for (int j = 0; j < ROWS; ++j) {
+            auto h = __builtin_bit_cast(Pack<float, 4>, held[j]);
+            if (group + 32 * j < d.Dk) move(h, ks[j], qs[j]);      // what is not there may be multiplied to a NaN
+            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, h), rsrc, place(j), 0, 0);
+        }
+    } else {
+        for (int i = group; i < d.Dk; i += 32) {
+            float *at = s + (long)i * d.Dv + x;
+            Pack<float, 4> h = have == 4 ? loose_load<float, 4>(at) : load_pack<false, float, 4>(at, have);
+            move(h, to_f(k[i]), to_f(q[i]));
+            if (have == 4) loose_store<float, 4>(at, h);
+            else store_pack<false, float, 4>(at, h, have);
+        }
     }
 #pragma unroll
     for (int e = 0; e < 4; ++e) sums[group][threadIdx.x % 8 * 4 + e] = sum.v[e];
@@ -381,8 +407,9 @@ hipError_t linear_attention_step(const ucd_linear_attention_t &d, const ucd_line
 {
     StepParams p{d, in, Decays{in.g, d.g_b, d.g_l, in.decay}, state, y, (d.Dv + 31) / 32};
     const unsigned grid = (unsigned)((long)d.B * d.H * p.tiles);
-    if (d.dtype == 1) attention_step_kernel<bf16_t><<<grid, 256, 0, s>>>(p);
-    else attention_step_kernel<float><<<grid, 256, 0, s>>>(p);
+    const bool wide = d.Dv % 4 == 0;
+    if (d.dtype == 1) wide ? attention_step_kernel<bf16_t, true><<<grid, 256, 0, s>>>(p) : attention_step_kernel<bf16_t, false><<<grid, 256, 0, s>>>(p);
+    else wide ? attention_step_kernel<float, true><<<grid, 256, 0, s>>>(p) : attention_step_kernel<float, false><<<grid, 256, 0, s>>>(p);
     return hipGetLastError();
 }
 
