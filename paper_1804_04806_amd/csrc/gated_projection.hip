@@ -478,7 +478,7 @@ bool few_tokens(const ucd_gated_projection_t &d)
     return d.M <= 16 || (d.M <= kFewTokens && (d.dtype == 0 || (long)d.D * d.F <= 1l << 23));
 }
 
-// One row of tiles of 64 by 128, three to a unit.
+// One row of tiles of 64 by 128, three to a unit, and parts of 8 steps at least: 2048 -> 8192, 64 tokens, four parts 20.3 us, two 21.1, six 24.2.
 Shape low_shape(long n, long steps)
 {
     const long tiles = (n + 127) / 128;
