@@ -1,5 +1,6 @@
 // What the linear attention's kernels share: tiles of 64 tokens in LDS, their products, decays.
 #pragma once
+#include "piece_words.hpp"
 #include "seq.h"
 #include "seq_common.hpp"
 
@@ -200,8 +201,6 @@ __device__ __forceinline__ unsigned xcd_place()
     return xcd * (n / 8) + min(xcd, n % 8) + blockIdx.x / 8;
 }
 
-// Reads behind a buffer's end give 0.
-constexpr uint32_t kOut = 0x80000000u;
 constexpr long kMostStride = 1l << 23;          // of a token: 64 tokens in 32-bit offsets of bytes
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
@@ -219,8 +218,8 @@ __device__ __forceinline__ uint32_t chunk_bytes(long stride, int tokens) { retur
 
 // A tile's pieces of 16 bytes on their way from memory: thread i has cells i, i + THREADS, ...  They are words that nothing looks at before they are stored
 // (elements of 16 bits would be taken apart, and waited for, right behind the load), and are read through a buffer that ends behind the last token that
-// there is: no branches.  WHOLE: rows of whole pieces at multiples of 4 bytes.  Otherwise word by word: those that begin before the row's end, from the
-// multiple of 4 bytes at or below the piece's begin; what does not belong to the piece goes when it is stored.
+// there is: no branches.  WHOLE: rows of whole pieces at multiples of 4 bytes.  Otherwise word by word (piece_word), those that hold something of the piece;
+// what does not belong to it goes when it is stored.
 template <class T, int COLS, bool WHOLE, int THREADS>
 struct Fetch {
     static constexpr int PER = 16 / sizeof(T), CELLS = COLS / PER, N = kChunk * CELLS / THREADS, ROWS = THREADS / CELLS;
@@ -254,10 +253,9 @@ struct Fetch {
             const auto rsrc = buffer_of((const char *)base - odd, 0x80000000u);
 #pragma unroll
             for (int i = 0; i < N; ++i) {
-                const uint32_t at = first + i * step, from = (at + odd) & ~3u, end = at + odd + have * (uint32_t)sizeof(T);
 #pragma unroll
                 for (int w = 0; w < WORDS; ++w)
-                    v[i][w] = __builtin_amdgcn_raw_buffer_load_b32(rsrc, at < bytes && from + 4 * w < end ? from + 4 * w : kOut, 0, 0);
+                    v[i][w] = __builtin_amdgcn_raw_buffer_load_b32(rsrc, piece_word(first + i * step, odd, have * (uint32_t)sizeof(T), bytes, w), 0, 0);
             }
         }
     }
