@@ -117,7 +117,7 @@ __global__ __launch_bounds__(64) void decay_gradient_kernel(const float *A, cons
     }
 }
 
-// out (B, L, Hk, D) = sums over neighbouring heads of part (B, L, H, D)
+// out (B, L, Hk, D) = sums over neighbouring heads of part (B, H, L, D), head by head so that a token's stride stays small whatever there are of heads
 template <class T>
 __global__ __launch_bounds__(256) void sum_heads_kernel(const float *part, int L, int H, int Hk, int D, long tokens, T *out, long o_b, long o_l)
 {
@@ -125,10 +125,11 @@ __global__ __launch_bounds__(256) void sum_heads_kernel(const float *part, int L
     for (long i = blockIdx.x * 256l + threadIdx.x; i < tokens * width; i += gridDim.x * 256l) {
         const long tok = i / width;
         const int c = (int)(i % width), hk = c / D, x = c % D;
-        const float *at = part + (tok * H + (long)hk * shared) * D + x;
+        const long seq = tok / L, t = tok % L;
+        const float *at = part + ((seq * H + (long)hk * shared) * L + t) * D + x;
         float v = at[0];
-        for (int j = 1; j < shared; ++j) v += at[(long)j * D];
-        out[tok / L * o_b + tok % L * o_l + c] = from_f<T>(v);
+        for (int j = 1; j < shared; ++j) v += at[(long)j * L * D];
+        out[seq * o_b + t * o_l + c] = from_f<T>(v);
     }
 }
 
@@ -291,6 +292,7 @@ hipError_t fwd(const ucd_linear_attention_t &d, const ucd_linear_attention_in_t 
     p.v = Rows{in.v, (long)d.v_b, (long)d.v_l, 1, d.Dv};
     p.out = y;
     p.out_b = d.y_b;
+    p.out_h = d.Dv;
     p.out_l = d.y_l;
     p.p_scale = p.first_scale = d.scale;
     p.last_scale = 1.f;
@@ -327,6 +329,7 @@ hipError_t bwd(const ucd_linear_attention_t &d, const ucd_linear_attention_in_t 
     p.v = o;
     p.out = grad.v;
     p.out_b = d.v_b;
+    p.out_h = d.Dv;
     p.out_l = d.v_l;
     p.p_scale = p.last_scale = d.scale;
     p.first_scale = 1.f;
@@ -359,8 +362,9 @@ hipError_t bwd(const ucd_linear_attention_t &d, const ucd_linear_attention_in_t 
     auto heads = [&](Mix &m, void *out, long o_b, long o_l, bool rev) {
         m.out_f32 = shared > 1;
         m.out = shared > 1 ? ws + l.heads : out;
-        m.out_l = shared > 1 ? (long)d.H * d.Dk : o_l;
-        m.out_b = shared > 1 ? m.out_l * d.L : o_b;
+        m.out_l = shared > 1 ? d.Dk : o_l;
+        m.out_h = shared > 1 ? (long)d.L * d.Dk : d.Dk;
+        m.out_b = shared > 1 ? d.H * m.out_h : o_b;
         const hipError_t e = rev ? run_mix<T, true>(m, whole, s) : run_mix<T, false>(m, whole, s);
         if (shared == 1) return e;
         const long tokens = (long)d.B * d.L;

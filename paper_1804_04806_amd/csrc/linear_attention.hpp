@@ -374,7 +374,7 @@ struct Rows {
 struct Mix {
     Rows q, k, v, dot;           // dot: rows like the output's, multiplied with the part of the state at the chunk's start; may be none
     void *out;
-    long out_b, out_l;
+    long out_b, out_h, out_l;    // of sequence, head and token; a token's is kMostStride at most
     bool out_f32;                // parts of T = bfloat16, for the heads that share a row of it
     float p_scale, first_scale, last_scale;
     Decays decays;

@@ -68,7 +68,7 @@ __global__ __launch_bounds__(2 * COLS, sizeof(T) == 2 && (COLS == 128 || DK == 6
     constexpr int osize = OUT32 ? 4 : (int)sizeof(T);      // fp32 outputs are parts that are summed up over the heads that share a row
     static_assert(!OUT32 || sizeof(T) == 2, "");
     const long o_l = p.out_l * osize;
-    char *out = (char *)p.out + (at.seq * p.out_b + (long)at.head * p.v.width + col0) * osize;
+    char *out = (char *)p.out + (at.seq * p.out_b + at.head * p.out_h + col0) * osize;
 
     if (idle) {
         for (int c = c0; c < c1 && OUT; ++c)
