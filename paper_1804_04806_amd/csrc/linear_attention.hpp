@@ -1,5 +1,7 @@
 // What the linear attention's kernels share: tiles of 64 tokens in LDS, their products, decays.
 #pragma once
+#include <cstddef>
+
 #include "piece_words.hpp"
 #include "seq.h"
 #include "seq_common.hpp"
@@ -319,8 +321,9 @@ struct Decays {
 };
 
 // A chunk's decays from its rows' own: `hi` + `lo` sums over the rows up to each, in units of 2 (two floats: their differences are exact to 32 bits
-// whatever the sums), `first` 2^sum, `last` 2^(what is decayed behind a row).  A wave computes them, a row per lane, in 64 bits.
-struct ChunkDecays {
+// whatever the sums), `first` 2^sum, `last` 2^(what is decayed behind a row).  A wave computes them, a row per lane, in 64 bits.  They are read in packs of
+// four, which begin at multiples of 16 bytes, also those of the second of two chunks side by side.
+struct alignas(16) ChunkDecays {
     float hi[kChunk], lo[kChunk], first[kChunk], last[kChunk], whole;
 
     // v + v of another lane, 0 where there is none: the steps of a sum over all lanes up to each
@@ -358,7 +361,9 @@ struct ChunkDecays {
     {
         return exp2_fast(sizeof(T) == 2 ? t_hi - s_hi : (t_hi - s_hi) + (t_lo - s_lo));
     }
+    __device__ static __forceinline__ Pack<float, 4> four(const float *p) { return lds_get<Pack<float, 4>>((const char *)p); }
 };
+static_assert(sizeof(ChunkDecays) % 16 == 0 && offsetof(ChunkDecays, lo) % 16 == 0 && offsetof(ChunkDecays, last) % 16 == 0, "whole packs");
 
 // ---- a walk --------------------------------------------------------------------------------------------------------
 

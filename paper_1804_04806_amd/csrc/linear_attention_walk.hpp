@@ -255,8 +255,8 @@ __global__ __launch_bounds__(2 * COLS, sizeof(T) == 2 && (COLS == 128 || DK == 6
 #pragma unroll
                         for (int k = 0; k < NK; ++k) fragk[i][k] = M::template along16_other<DK>(lds_k, sb + 16 * i, k * M::K16);
                         const int s = sb + 16 * i + 4 * (lane / 16);
-                        shi[i] = *reinterpret_cast<const Pack<float, 4> *>(&dec.hi[s]);
-                        if (sizeof(T) == 4) slo[i] = *reinterpret_cast<const Pack<float, 4> *>(&dec.lo[s]);
+                        shi[i] = ChunkDecays::four(dec.hi + s);
+                        if (sizeof(T) == 4) slo[i] = ChunkDecays::four(dec.lo + s);
                     }
                     __builtin_amdgcn_sched_barrier(0);
                     f32x4 acc[BATCH] = {};
@@ -340,7 +340,7 @@ __global__ __launch_bounds__(2 * COLS, sizeof(T) == 2 && (COLS == 128 || DK == 6
             auto read = [&](int k) {
                 own[k] = M::template across<COLS>(lds_v, x0, k * M::K);
 #pragma unroll
-                for (int e = 0; e < E / 4; ++e) w[k % 2][e] = *reinterpret_cast<const Pack<float, 4> *>(&dec.last[k * M::K + half * E + 4 * e]);
+                for (int e = 0; e < E / 4; ++e) w[k % 2][e] = ChunkDecays::four(dec.last + k * M::K + half * E + 4 * e);
 #pragma unroll
                 for (int i = 0; i < ST; ++i) a[k % 2][i] = M::template across<DK>(lds_k, 32 * i, k * M::K);
             };
