@@ -18,7 +18,8 @@
 //   a_t = q_t . (dq_t's part of S_in),  b_s = k_s . (dk_s's part of dS_out),  c = e^{G_C} <S_in, dS_out>.
 // A_t = q_t . dq_t without W[t, t] is a_t and W's row, B_s = k_s . dk_s without W[s, s] is b_s and W's column, so that
 //   dl_u = sum_{t >= u} (A_t - (B_t - b_t)) + sum_{s < u} b_s + c.
-// A pair that does not cross u is in a row and in a column, of the same product rounded to the same 16 bits: what is left of it is rounding of 32 bits.
+// A pair that does not cross u is in a row and in a column, of the same product rounded to the same 16 bits (both walks take its decay from sums that are the
+// same to far below 32 bits, and round it once): what is left of it is rounding of 32 bits.
 // Sums of A - B over whole sequences would be the same as this in exact arithmetic, but the states' roundings are not the same on both sides.  (Pairs
 // in a kernel of their own read all inputs again, 59 us of 526 for 8 x 2048 tokens of 16 heads of 128.)
 #include <algorithm>

@@ -355,11 +355,17 @@ struct alignas(16) ChunkDecays {
         last[lane] = last_scale * exp2_fast((float)(all - sum));
         if (lane == 63) whole = exp2_fast((float)all);
     }
-    // 2^(sums of row t less those of row s); 16-bit operands need no more than one float of each: sums are 64 * 80 / ln 2 at most, 2^-11 of a unit exact
-    template <class T>
+    // 2^(sums of row t less those of row s); 16-bit operands need no more than one float of each: sums are 64 * 80 / ln 2 at most, 2^-11 of a unit exact.
+    // SAME: the same float whichever end the sums begin at, so that a walk forward and one backward round the same products to the same 16 bits.  The
+    // difference is then rounded once: what the floats' own loses is put back with the second ones' difference.
+    template <class T, bool SAME>
     __device__ static __forceinline__ float pair(float t_hi, float t_lo, float s_hi, float s_lo)
     {
-        return exp2_fast(sizeof(T) == 2 ? t_hi - s_hi : (t_hi - s_hi) + (t_lo - s_lo));
+        const float d = t_hi - s_hi;
+        if (sizeof(T) == 4) return exp2_fast(d + (t_lo - s_lo));
+        if (!SAME) return exp2_fast(d);
+        const float of_s = d - t_hi, lost = (t_hi - (d - of_s)) - (s_hi + of_s);
+        return exp2_fast(d + (lost + (t_lo - s_lo)));
     }
     __device__ static __forceinline__ Pack<float, 4> four(const float *p) { return lds_get<Pack<float, 4>>((const char *)p); }
 };

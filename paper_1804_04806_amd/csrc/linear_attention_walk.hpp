@@ -239,6 +239,7 @@ __global__ __launch_bounds__(2 * COLS, sizeof(T) == 2 && (COLS == 128 || DK == 6
         if (OUT) {
             // P[t, s] in tiles of 16 by 16: a lane has row t and 4 s.  A wave has a row of tiles of four, or two of them
             constexpr int NK = DK / M::K16, BATCH = sizeof(T) == 2 ? 2 : 1;      // tiles at a time
+            constexpr bool BOTH = DG || sizeof(T) == 4;                          // floats of the sums of decays
 #pragma unroll
             for (int part = 0; part < 4 / WAVES; ++part) {
                 const int tb = (part ? 3 - wave : wave) * 16, t = tb + lane % 16;
@@ -249,14 +250,14 @@ __global__ __launch_bounds__(2 * COLS, sizeof(T) == 2 && (COLS == 128 || DK == 6
 #pragma unroll
                 for (int sb = 0; sb < kChunk; sb += 16 * BATCH) {
                     Frag fragk[BATCH][NK];
-                    Pack<float, 4> shi[BATCH], slo[BATCH];
+                    Pack<float, 4> shi[BATCH], slo[BOTH ? BATCH : 1];
 #pragma unroll
                     for (int i = 0; i < BATCH; ++i) {
 #pragma unroll
                         for (int k = 0; k < NK; ++k) fragk[i][k] = M::template along16_other<DK>(lds_k, sb + 16 * i, k * M::K16);
                         const int s = sb + 16 * i + 4 * (lane / 16);
                         shi[i] = ChunkDecays::four(dec.hi + s);
-                        if (sizeof(T) == 4) slo[i] = ChunkDecays::four(dec.lo + s);
+                        if (BOTH) slo[BOTH ? i : 0] = ChunkDecays::four(dec.lo + s);
                     }
                     __builtin_amdgcn_sched_barrier(0);
                     f32x4 acc[BATCH] = {};
@@ -270,7 +271,7 @@ __global__ __launch_bounds__(2 * COLS, sizeof(T) == 2 && (COLS == 128 || DK == 6
                         float v[4];
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
-                            const float w = ChunkDecays::pair<T>(hi, lo, shi[i].v[e], sizeof(T) == 4 ? slo[i].v[e] : 0.f) * p.p_scale;
+                            const float w = ChunkDecays::pair<T, DG>(hi, lo, shi[i].v[e], BOTH ? slo[BOTH ? i : 0].v[e] : 0.f) * p.p_scale;
                             v[e] = s + e <= t ? acc[i][e] * w : 0.f;
                         }
                         lds_put(lds_p + TP::at(t, s), pack_four<T>(v[0], v[1], v[2], v[3]));
