@@ -66,7 +66,8 @@ int ucd_linear_attention_fwd(const ucd_linear_attention_t *attention, const ucd_
                              void *ws, size_t ws_bytes, void *stream);
 
 /* Backward, without slots; saved is what Forward wrote for the same inputs.  dstate_out (NULL: zeros):
- * gradient of state_out, (B, H, Dk, Dv) floats. */
+ * gradient of state_out, (B, H, Dk, Dv) floats.  Sums for g's gradient run in another order: q's and k's may
+ * round to another last bit than without it.  Nothing else that is left out changes what is written. */
 int ucd_linear_attention_bwd(const ucd_linear_attention_t *attention, const ucd_linear_attention_in_t *in,
                              const void *dy, const float *dstate_out, const void *saved, size_t saved_bytes,
                              const ucd_linear_attention_grad_t *grad, void *ws, size_t ws_bytes, void *stream);

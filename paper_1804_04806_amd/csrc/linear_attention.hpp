@@ -117,7 +117,7 @@ template <> struct Mma<bf16_t> {
     {
         return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
     }
-    // w a in PARTS bfloat16 parts, the largest first: three are as exact as the sums' 32 bits, two leave 2^-17
+    // w a in PARTS bfloat16 parts, the largest first: three are as exact as the sums' 32 bits
     template <int PARTS>
     __device__ static __forceinline__ void weighted(const Frag &a, const float *w, Frag (&out)[PARTS])
     {

@@ -35,13 +35,12 @@ enum { OUTPUTS, DECAYS, STATES };
 // weighted for the state's update, each wave its own columns, which stay in registers for the pairs' products.  Two barriers a chunk: behind the tiles,
 // and behind the pairs, which the waves share out.  Memory bounds it, 16 bits, at two workgroups to a compute unit: 8 x 2048 tokens of 16 heads of 128, Forward
 // 81 us for 270 MB, dv 72, dq and dk, with the decays' gradient, 110 and 126 for 470 MB each.  fp32 is bound by its matrix instructions.
-template <class T, int DK, int COLS, bool REV, int FOR, bool WHOLE, bool OUT32, bool EXACT>
+template <class T, int DK, int COLS, bool REV, int FOR, bool WHOLE, bool OUT32>
 __global__ __launch_bounds__(2 * COLS, sizeof(T) == 2 && (COLS == 128 || DK == 64) ? 2 : 1) void mix_kernel(Mix p)
 {
     constexpr int THREADS = 2 * COLS, WAVES = COLS / 32;
     constexpr bool OUT = FOR != STATES, DG = FOR == DECAYS;
-    // EXACT: what is added to a state that a caller gets is as exact as the state's 32 bits; one that goes into 16-bit operands alone has 16 to 17 bits of it
-    constexpr int PARTS = sizeof(T) == 4 ? 1 : EXACT ? 3 : 2;
+    constexpr int PARTS = sizeof(T) == 4 ? 1 : 3;        // of what is added to a state: as exact as its 32 bits, whoever reads it
     typedef Mma<T> M;
     typedef TileLds<T, DK> TQ;
     typedef TileLds<T, COLS> TV;
@@ -461,10 +460,8 @@ template <class T, int DK, int COLS, bool REV, bool WHOLE>
 hipError_t run_mix_of(const Mix &p, hipStream_t s)
 {
     const unsigned groups = (unsigned)((long)p.B * p.H * p.tiles);
-    const bool exact = p.state_out != nullptr;
     if (p.segments > 1 && !p.started) {
-        if (exact) mix_kernel<T, DK, COLS, REV, STATES, WHOLE, false, true><<<groups * (p.segments - 1), 2 * COLS, 0, s>>>(p);
-        else mix_kernel<T, DK, COLS, REV, STATES, WHOLE, false, false><<<groups * (p.segments - 1), 2 * COLS, 0, s>>>(p);
+        mix_kernel<T, DK, COLS, REV, STATES, WHOLE, false><<<groups * (p.segments - 1), 2 * COLS, 0, s>>>(p);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
@@ -475,12 +472,11 @@ hipError_t run_mix_of(const Mix &p, hipStream_t s)
     const unsigned grid = groups * p.segments;
     if (sizeof(T) == 2 && p.out_f32) {
         if constexpr (sizeof(T) == 2) {
-            if (p.dots) mix_kernel<T, DK, COLS, REV, DECAYS, WHOLE, true, false><<<grid, 2 * COLS, 0, s>>>(p);
-            else mix_kernel<T, DK, COLS, REV, OUTPUTS, WHOLE, true, false><<<grid, 2 * COLS, 0, s>>>(p);
+            if (p.dots) mix_kernel<T, DK, COLS, REV, DECAYS, WHOLE, true><<<grid, 2 * COLS, 0, s>>>(p);
+            else mix_kernel<T, DK, COLS, REV, OUTPUTS, WHOLE, true><<<grid, 2 * COLS, 0, s>>>(p);
         }
-    } else if (p.dots) mix_kernel<T, DK, COLS, REV, DECAYS, WHOLE, false, false><<<grid, 2 * COLS, 0, s>>>(p);
-    else if (exact) mix_kernel<T, DK, COLS, REV, OUTPUTS, WHOLE, false, true><<<grid, 2 * COLS, 0, s>>>(p);
-    else mix_kernel<T, DK, COLS, REV, OUTPUTS, WHOLE, false, false><<<grid, 2 * COLS, 0, s>>>(p);
+    } else if (p.dots) mix_kernel<T, DK, COLS, REV, DECAYS, WHOLE, false><<<grid, 2 * COLS, 0, s>>>(p);
+    else mix_kernel<T, DK, COLS, REV, OUTPUTS, WHOLE, false><<<grid, 2 * COLS, 0, s>>>(p);
     return hipGetLastError();
 }
 
