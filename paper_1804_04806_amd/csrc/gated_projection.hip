@@ -6,6 +6,7 @@
 // one product.  Operands that the products cannot read as they lie (fp32, rows of no whole 16 bytes) are copied first.
 #include <algorithm>
 
+#include "gated_plan.hpp"
 #include "product.hpp"
 #include "seq.h"
 
@@ -13,6 +14,7 @@ namespace ucd {
 namespace gated {
 using namespace seq;
 using namespace product;
+static_assert(kStep == BK, "plans count the products' steps");
 
 constexpr float kGelu = 1.59576912160573071176f, kCube = 0.044715f;    // 2 sqrt(2 / pi)
 
@@ -36,8 +38,6 @@ __device__ __forceinline__ float gate_slope(int act, float v, float &value)
     const float rest = s * (1.f - s);
     return rest == 0.f ? s : fmaf(v * inner, rest, s);
 }
-
-inline long round_up(long n, long to) { return (n + to - 1) / to * to; }
 
 // ---- copies --------------------------------------------------------------------------------------------------------
 
@@ -200,7 +200,7 @@ __global__ __launch_bounds__(256) void gated_join_kernel(const float *part, int 
 // sides and all tokens; its eight waves share the reduction out, two steps of 32 (16 for fp32), 128 bytes of a row, each by turns, and join their sums
 // in LDS.  Loads are without branches, AHEAD turns before their use.  Memory bounds it for few tokens, what is read of the tokens for many.
 
-constexpr int kFewWaves = 8, kFewTokens = 64;
+constexpr int kFewWaves = 8;
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
@@ -447,44 +447,12 @@ __global__ __launch_bounds__(256) void clear_kernel(char *p, long row_bytes, lon
 
 unsigned grid_for(long n) { return (unsigned)std::min((n + 255) / 256, 1l << 16); }
 
-constexpr int kUnits = 256;      // compute units
-
-// Tiles of 256 by 256 or 192 by 256, one to a unit, or of 128 by 128, two to a unit, whichever take least time in whole rounds; the reduction in parts of 8
-// steps at least where small ones are too few.  A round of the second has 3/4 of the first one's work, a round of small ones half of it at about 0.7 of the
-// rate (forward of 4096 x 1024 x 2816: two rounds of 256 by 256 65 us, two of 192 by 256 56 us).  Tiles of 192 are of operands along their rows alone.
-struct Shape {
-    int side;      // rows of a tile
-    int tiles_m, tiles_n, splits;
-};
-
-Shape shape_of(long m, long n, long steps, bool along)
-{
-    auto tiles = [&](long rows, long cols) { return ((m + rows - 1) / rows) * ((n + cols - 1) / cols); };
-    auto rounds = [](long t, long each) { return (double)((t + each - 1) / each); };
-    const double large = rounds(tiles(256, 256), kUnits), mid = rounds(tiles(192, 256), kUnits) * 0.75 / 0.95,
-                 small = rounds(tiles(128, 128), 2 * kUnits) * 0.5 / 0.7;
-    Shape s;
-    s.side = along && mid < large && mid <= small ? 192 : large <= small ? 256 : 128;
-    s.tiles_m = (int)((m + s.side - 1) / s.side);
-    const int cols = s.side == 128 ? 128 : 256;
-    s.tiles_n = (int)((n + cols - 1) / cols);
-    s.splits = s.side != 128 ? 1 : (int)std::max(1l, std::min(2 * kUnits / tiles(128, 128), steps / 8));
-    return s;
-}
-
 // Up to 64 tokens: straight from memory (gated_few_kernel), whose work on the tokens grows with them, or tiles, which have a join.  bf16, 17, 32 and 64 tokens,
 // us: 1024 -> 2816 6.1, 6.8 and 8.9 against 10.5, 10.8 and 11.5; 2048 -> 4096 8.9, 10.2 and 14.2 against 12.3, 12.5 and 13.1; 2048 -> 6144 15.5, 17.8 and 25.5
 // against 14.1, 14.7 and 16.0; 4096 -> 16384 57, 64 and 86 against 57, 59 and 63.  fp32 and what has to be copied first would be read and written before tiles.
 bool few_tokens(const ucd_gated_projection_t &d)
 {
     return d.M <= 16 || (d.M <= kFewTokens && (d.dtype == 0 || (long)d.D * d.F <= 1l << 23));
-}
-
-// One row of tiles of 64 by 128, three to a unit, and parts of 8 steps at least: 2048 -> 8192, 64 tokens, four parts 20.3 us, two 21.1, six 24.2.
-Shape low_shape(long n, long steps)
-{
-    const long tiles = (n + 127) / 128;
-    return Shape{64, 1, (int)tiles, (int)std::max(1l, std::min(3 * kUnits / tiles, steps / 8))};
 }
 
 // What a call has in its workspace, in bytes from its begin; a part of no bytes is not needed.
@@ -522,16 +490,15 @@ Layout layout_of(const ucd_gated_projection_t &d, int dir, bool x_aligned, bool 
     };
     l.x_plane = round_up((long)d.M * l.width, 128);
     l.w_plane = round_up((long)d.F * l.width, 128);
-    const long d_steps = (l.width + BK - 1) / BK * l.phases;
     if (dir == UCD_SEQ_FWD) {
-        l.fwd = d.M <= kFewTokens ? low_shape(2l * d.F, d_steps) : shape_of(d.M, 2l * d.F, d_steps, true);
+        l.fwd = forward_shape(d.M, d.D, d.F, l.phases);
         if (l.few) {
             l.bytes = 0;
             return l;
         }
     } else {
-        l.dx = shape_of(d.M, d.D, 2l * l.half / BK * l.phases, true);
-        l.dw = shape_of(2l * l.half, d.D, ((long)d.M + BK - 1) / BK * l.phases, false);
+        l.dx = dx_shape(d.M, d.D, d.F, l.phases);
+        l.dw = dw_shape(d.M, d.D, d.F, l.phases);
         l.dg_plane = (long)d.M * l.dg_row;
         l.dg = take((size_t)l.planes * l.dg_plane * 2);
     }
