@@ -2,7 +2,8 @@
 //
 // Products bound it from some hundred tokens on, the weights' bytes below.  Forward is one product whose tiles hold the same columns of both
 // projections, so that a lane has both sides of a gate in registers and writes y alone (for Backward, both sides in fp32 too).  Backward first turns
-// dy and what was kept into dG = [dgate | dup], bfloat16 (rounded once: the products' operand), then dx = dG [Wg; Wu] and [dWg; dWu] = dG^T x, each
+// dy and what was kept into dG = [dgate | dup], bfloat16 (rounded once, the products' operand: gradients are 2.3e-3 off instead of their own rounding's
+// 1.7e-3), then dx = dG [Wg; Wu] and [dWg; dWu] = dG^T x, each
 // one product.  Operands that the products cannot read as they lie (fp32, rows of no whole 16 bytes) are copied first.
 #include <algorithm>
 
@@ -450,6 +451,8 @@ unsigned grid_for(long n) { return (unsigned)std::min((n + 255) / 256, 1l << 16)
 // Up to 64 tokens: straight from memory (gated_few_kernel), whose work on the tokens grows with them, or tiles, which have a join.  bf16, 17, 32 and 64 tokens,
 // us: 1024 -> 2816 6.1, 6.8 and 8.9 against 10.5, 10.8 and 11.5; 2048 -> 4096 8.9, 10.2 and 14.2 against 12.3, 12.5 and 13.1; 2048 -> 6144 15.5, 17.8 and 25.5
 // against 14.1, 14.7 and 16.0; 4096 -> 16384 57, 64 and 86 against 57, 59 and 63.  fp32 and what has to be copied first would be read and written before tiles.
+// The border of 2^23 is the middle of these: just below it 64 tokens lose some 5 %, and more where F is small and with it the number of workgroups
+// (4096 -> 2048 15.1, 18.3 and 27.1 against 15.8, 16.2 and 16.9).
 bool few_tokens(const ucd_gated_projection_t &d)
 {
     return d.M <= 16 || (d.M <= kFewTokens && (d.dtype == 0 || (long)d.D * d.F <= 1l << 23));
@@ -573,7 +576,9 @@ hipError_t few(const ucd_gated_projection_t &d, const void *x, const void *wg, c
     // 32 columns to a workgroup read the tokens half as often as 16, but need enough of them: 2048 -> 8192, 32 and 64 tokens, 17.2 and 23.0 us against 19.7 and
     // 28.9 (two turns ahead)
     const bool two = d.F >= 32 * kUnits;
-    // two turns ahead pay where there are many: one token, 8192 -> 8192, 49.5 us (5.4 TB/s) against 52.2; 2048 -> 8192, 13.4 against 12.6 (5.3)
+    // two turns ahead pay for one token where there are many: rows of 4096, 6144 and 8192 -> 8192, bf16, 25.9, 36.2 and 53.1 us against 28.0, 37.6 and 56.0 (fp32 of
+    // half as many the same), and make no difference to 16 tokens.  Of fewer or an odd number the last is empty: 1024, 1536 and 2560 10.0, 13.1 and 18.8 against
+    // 9.0, 11.9 and 17.5; at the border, 2048, 14.8 against 15.7 from memory, 13.4 against 12.6 where the card's cache has part of it.
     if (d.M <= 16 && d.D * sizeof(T) <= 4096) few_of<T, 1, 1, 1>(d, px, pg, pu, o, whole, s);
     else if (d.M <= 16) few_of<T, 1, 1, 2>(d, px, pg, pu, o, whole, s);
     else if (d.M <= 32 && two) few_of<T, 2, 2, 1>(d, px, pg, pu, o, whole, s);

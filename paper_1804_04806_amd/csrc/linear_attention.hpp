@@ -415,7 +415,7 @@ inline int chunks_of(int L) { return (L + kChunk - 1) / kChunk; }
 inline int tiles_of(int width, int cols) { return (width + cols - 1) / cols; }
 
 // Columns of a state to a workgroup, 32 to a wave: all of them, so that pairs of tokens are computed once.  fp32 states of many rows have four waves also for
-// few columns (two are out of registers: 5 x 677 tokens of 6 heads of 72 by 41, Forward 87 us against 38).
+// few columns, two of them without any (two waves are out of registers: 5 x 677 tokens of 6 heads of 72 by 41, Forward's walk 71 us against 45).
 inline int cols_of(int rows, int cols, bool f32) { return cols > 64 || (f32 && rows > 64) ? 128 : 64; }
 
 // Rows that Fetch can read by whole pieces

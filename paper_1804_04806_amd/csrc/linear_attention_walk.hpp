@@ -33,8 +33,10 @@ enum { OUTPUTS, DECAYS, STATES };
 // A wave has its columns of the state as sums of the matrix instructions, DK rows of them, and uses those sums as they lie as an operand of q S: the
 // reduction runs over the state's rows in the order in which the sums hold them, for q too, so that the state never goes through LDS.  v is
 // weighted for the state's update, each wave its own columns, which stay in registers for the pairs' products.  Two barriers a chunk: behind the tiles,
-// and behind the pairs, which the waves share out.  Memory bounds it, 16 bits, at two workgroups to a compute unit: 8 x 2048 tokens of 16 heads of 128, Forward
-// 81 us for 270 MB, dv 72, dq and dk, with the decays' gradient, 110 and 126 for 470 MB each.  fp32 is bound by its matrix instructions.
+// and behind the pairs, which the waves share out.  16-bit tensors have their pairs' weights, and the state where it is an operand, rounded to 16 bits: that
+// is what their matrix instructions take, and errors grow from the output's own 1.7e-3 to 2.4e-3 in the 2-norm.  Memory bounds it, 16 bits, at two workgroups
+// to a compute unit: 8 x 2048 tokens of 16 heads of 128, Forward 78 us for 270 MB, dv 73, dq and dk, with the decays' gradient, 113 and 128 for 470 MB each.
+// fp32 is bound by its matrix instructions.
 template <class T, int DK, int COLS, bool REV, int FOR, bool WHOLE, bool OUT32>
 __global__ __launch_bounds__(2 * COLS, sizeof(T) == 2 && (COLS == 128 || DK == 64) ? 2 : 1) void mix_kernel(Mix p)
 {
